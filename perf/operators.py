@@ -142,18 +142,18 @@ def _placement(case, idx):
 
 
 def _to_8_bits(v):
-    """(codes e4m3, scales as powers of two) of v [rows, columns] fp32, a scale for each row and 32 columns."""
+    """(codes e4m3 [rows, blocks * 32], scale bytes [blocks, rows]) of v [rows, columns] fp32: 32 columns of a row share one."""
     rows, cols = v.shape
     blocks = torch.nn.functional.pad(v, (0, -cols % _BLOCK)).view(rows, -1, _BLOCK)
     m, e = torch.frexp(blocks.abs().amax(-1))           # amax = m 2^e, 0.5 <= m < 1; 448 = 0.875 2^9
     k = torch.where(m == 0, torch.full_like(e, -127), (e - 9 + (m > 0.875).int()).clamp(-127, 127))
     codes = torch.ldexp(blocks, -k[..., None]).to(torch.float8_e4m3fn).view(rows, -1)
-    return codes, (k + 127).to(torch.uint8)
+    return codes, (k + 127).to(torch.uint8).T
 
 
 def _from_8_bits(codes, scale, cols, dtype):
     v = codes.view(torch.float8_e4m3fn).to(dtype).view(codes.shape[0], -1, _BLOCK)
-    return torch.ldexp(v, scale.to(torch.int32)[..., None] - 127).reshape(codes.shape[0], -1)[:, :cols]
+    return torch.ldexp(v, scale.T.to(torch.int32)[..., None] - 127).reshape(codes.shape[0], -1)[:, :cols]
 
 
 def _rows_by_expert(case, g, p, width, std):
@@ -183,12 +183,12 @@ def _inputs(case, seed):
         for name in ("gate", "up"):
             wide = -(-F // _BLOCK) * _BLOCK
             codes = torch.empty(s["xp"].shape[0], wide, dtype=torch.uint8, device="cuda")
-            scale = torch.empty(s["xp"].shape[0], wide // _BLOCK, dtype=torch.uint8, device="cuda")
+            scale = torch.empty(wide // _BLOCK, s["xp"].shape[0], dtype=torch.uint8, device="cuda")
             for lo in range(0, codes.shape[0], 4096):
                 hi = min(lo + 4096, codes.shape[0])
                 v = torch.randn(hi - lo, F, generator=g, device="cuda").mul_(std).mul_((s["row_pair"][lo:hi] >= 0)[:, None])
                 c, k = _to_8_bits(v)
-                codes[lo:hi], scale[lo:hi] = c.view(torch.uint8), k
+                codes[lo:hi], scale[:, lo:hi] = c.view(torch.uint8), k
             s[name + "8"], s[name + "_scale"] = codes, scale
     if case["op"] == "combine":
         s["dout"], s["yp"] = _normal(g, (T, D), 0.01), _rows_by_expert(case, g, s, D, 0.5)
@@ -217,7 +217,7 @@ def prepare(case, seed):
             s["h"] = torch.zeros(rows, F, **bf)
             for name in ("gate", "up"):
                 s[name + "8"] = torch.zeros(rows, wide, **u8)
-                s[name + "_scale"] = torch.zeros(rows, wide // _BLOCK, **u8)
+                s[name + "_scale"] = torch.zeros(wide // _BLOCK, rows, **u8)
         if case["op"] == "backward":
             s["dgate"], s["dup"], s["h"] = (torch.empty(rows, F, **bf) for _ in range(3))
             s["dxp"] = torch.zeros(rows, D, **bf)
@@ -272,14 +272,14 @@ def _plain_save(s):
     rows, wide = xp.shape[0], -(-F // _BLOCK) * _BLOCK
     h = torch.zeros(rows, F, dtype=torch.bfloat16, device="cuda")
     codes = torch.zeros(2, rows, wide, dtype=torch.float8_e4m3fn, device="cuda")
-    scale = torch.zeros(2, rows, wide // _BLOCK, dtype=torch.uint8, device="cuda")
+    scale = torch.zeros(2, wide // _BLOCK, rows, dtype=torch.uint8, device="cuda")
     for e, (lo, hi) in enumerate(s["extents"]):          # the experts hold different numbers of rows
         if hi > lo:
             x = xp[lo:hi].float()
             g, u = x @ s["w_gate"][e].float().T, x @ s["w_up"][e].float().T
             h[lo:hi] = g * torch.sigmoid(g) * u
-            codes[0, lo:hi], scale[0, lo:hi] = _to_8_bits(g)
-            codes[1, lo:hi], scale[1, lo:hi] = _to_8_bits(u)
+            codes[0, lo:hi], scale[0, :, lo:hi] = _to_8_bits(g)
+            codes[1, lo:hi], scale[1, :, lo:hi] = _to_8_bits(u)
     return h, codes[0], codes[1], scale[0].view(torch.float8_e8m0fnu), scale[1].view(torch.float8_e8m0fnu)
 
 
@@ -289,8 +289,8 @@ def _plain_backward(s):
     dw_gate, dw_up, dw_down = (torch.empty_like(s[k]) for k in ("w_gate", "w_up", "w_down"))
     for e, (lo, hi) in enumerate(s["extents"]):
         x, dy = s["xp"][lo:hi].float(), s["dyp"][lo:hi].float()
-        g = _from_8_bits(s["gate8"][lo:hi], s["gate_scale"][lo:hi], F, torch.float32)
-        u = _from_8_bits(s["up8"][lo:hi], s["up_scale"][lo:hi], F, torch.float32)
+        g = _from_8_bits(s["gate8"][lo:hi], s["gate_scale"][:, lo:hi], F, torch.float32)
+        u = _from_8_bits(s["up8"][lo:hi], s["up_scale"][:, lo:hi], F, torch.float32)
         sig = torch.sigmoid(g)
         act = g * sig
         dh = dy @ s["w_down"][e].float()
@@ -359,7 +359,7 @@ def exact(case, seed):
             return h, kept[0], kept[1], None, None
         dxp, grads = zeros(rows, D), [zeros(E, F, D), zeros(E, F, D), zeros(E, D, F)]
         for e, (lo, hi) in enumerate(s["extents"]):
-            g, u = (_from_8_bits(s[k + "8"][lo:hi], s[k + "_scale"][lo:hi], F, d) for k in ("gate", "up"))
+            g, u = (_from_8_bits(s[k + "8"][lo:hi], s[k + "_scale"][:, lo:hi], F, d) for k in ("gate", "up"))
             x, dy = s["xp"][lo:hi].to(d), s["dyp"][lo:hi].to(d)
             ex = torch.exp(-g)
             slope = (1 + ex + g * ex) / (1 + ex) ** 2     # derivative of g / (1 + exp(-g))
