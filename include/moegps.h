@@ -275,6 +275,87 @@ MOEGPS_API int moegps_expert_ffn_down(moegps_ctx_t* ctx, const void* h_ws, const
 MOEGPS_API int moegps_combine(moegps_ctx_t* ctx, const void* yp, const int32_t* pair_row, const float* topk_w,
                    void* out, void* stream);
 
+/* ---- the training step: gradients of the calls above, on the same tables and buffers ----
+ * Padding rows of a slot (row_pair < 0) hold no token: whatever their memory holds, they enter no sum over rows.
+ *
+ * expert_ffn_gate_up_save - moegps_expert_ffn_gate_up (h_ws bit for bit), which also keeps the two products
+ * g = xp w_gate^T and u = xp w_up^T of every row in 8 bits for the backward pass.  32 consecutive columns of a row form
+ * a block with one power-of-two scale 2^k, k the smallest integer with max|v| <= 448 * 2^k; a code is v * 2^-k in e4m3
+ * (nearest even), the scale byte is k + 127 (0 for a block of zeros).  A block that holds an infinity or a NaN has scale
+ * byte 255 and decodes to NaN.
+ * gate8, up8: uint8 [Rcap, P], P = F rounded up to a multiple of 32 (the last block of a row is filled up with zeros);
+ * gate_scale, up_scale: uint8 [P/32, Rcap].  Rows as in moegps_expert_ffn: rows outside every slot are not written. */
+MOEGPS_API int moegps_expert_ffn_gate_up_save(moegps_ctx_t* ctx, const void* xp, const int32_t* slot_row_off,
+                                              const int32_t* slot_expert, const void* w_gate, const void* w_up,
+                                              void* h_ws, void* gate8, void* up8, void* gate_scale, void* up_scale,
+                                              void* stream);
+
+/* expert_ffn_backward - gradient of moegps_expert_ffn.  With g, u decoded from what gate_up_save kept, s = sigmoid(g),
+ * e the row's expert, and dyp the gradient of yp:
+ *   dh = dyp w_down[e];  dgate = dh u s (1 + g (1 - s));  dup = dh g s;  h = g s u
+ *   dxp = dgate w_gate[e] + dup w_up[e]
+ *   dw_gate[e] = sum dgate^T xp;  dw_up[e] = sum dup^T xp;  dw_down[e] = sum dyp^T h    over the tokens' rows of all
+ *   copies of e; zero for an expert without rows.
+ * bf16 operands, fp32 accumulation; dgate, dup and h are rounded to bf16 between the steps, results once at the end.
+ * dyp, xp: bf16 [Rcap,D]; slot_row_off, slot_expert, row_pair as dispatch left them; slot_off: int32 [E+1] from the plan;
+ * gate8 ... up_scale as moegps_expert_ffn_gate_up_save wrote them; dgate, dup, h_ws: bf16 [Rcap,F] scratch (h_ws may be
+ * the forward pass's); dxp: bf16 [Rcap,D], padding rows unspecified; dw_gate, dw_up: bf16 [E,F,D]; dw_down: bf16
+ * [E,D,F], fully overwritten.  With T = 0 only the weight gradients are written (zeros).
+ * A slot with an extent outside [0, Rcap] is skipped and MOEGPS_ERR_BAD_INDEX recorded, as in moegps_expert_ffn. */
+MOEGPS_API int moegps_expert_ffn_backward(moegps_ctx_t* ctx, const void* dyp, const void* xp, const int32_t* slot_row_off,
+                                          const int32_t* slot_off, const int32_t* slot_expert, const int32_t* row_pair,
+                                          const void* w_gate, const void* w_up, const void* w_down, const void* gate8,
+                                          const void* up8, const void* gate_scale, const void* up_scale, void* dgate,
+                                          void* dup, void* h_ws, void* dxp, void* dw_gate, void* dw_up, void* dw_down,
+                                          void* stream);
+
+/* Its three steps as separate calls (same kernels), in this order: act writes dgate, dup and h_ws, input writes dxp,
+ * weights writes the weight gradients.  A caller with frozen experts leaves out weights; the first layer of a model
+ * leaves out input. */
+MOEGPS_API int moegps_expert_ffn_backward_act(moegps_ctx_t* ctx, const void* dyp, const int32_t* slot_row_off,
+                                              const int32_t* slot_expert, const void* w_down, const void* gate8,
+                                              const void* up8, const void* gate_scale, const void* up_scale, void* dgate,
+                                              void* dup, void* h_ws, void* stream);
+MOEGPS_API int moegps_expert_ffn_backward_input(moegps_ctx_t* ctx, const void* dgate, const void* dup,
+                                                const int32_t* slot_row_off, const int32_t* slot_expert,
+                                                const void* w_gate, const void* w_up, void* dxp, void* stream);
+MOEGPS_API int moegps_expert_ffn_backward_weights(moegps_ctx_t* ctx, const void* dyp, const void* xp, const void* dgate,
+                                                  const void* dup, const void* h_ws, const int32_t* slot_row_off,
+                                                  const int32_t* slot_off, const int32_t* row_pair, void* dw_gate,
+                                                  void* dw_up, void* dw_down, void* stream);
+
+/* combine_backward - gradient of moegps_combine: dyp[pair_row[t,j]] = topk_w[t,j] * dout[t] (bf16, nearest even),
+ * dtopk_w[t,j] = <dout[t], yp[pair_row[t,j]]> (fp32).
+ * dout: bf16 [T,D]; yp: bf16 [Rcap,D]; dyp: bf16 [Rcap,D], padding rows not written; dtopk_w: fp32 [T,K].
+ * A row outside [0, Rcap) is skipped (dtopk_w 0) and MOEGPS_ERR_BAD_INDEX recorded. */
+MOEGPS_API int moegps_combine_backward(moegps_ctx_t* ctx, const void* dout, const void* yp, const int32_t* pair_row,
+                                       const float* topk_w, void* dyp, float* dtopk_w, void* stream);
+
+/* dispatch_backward - gradient of the layer's input: dx[t] = sum_j dxp[pair_row[t,j]], and with dlogit (else pass NULL
+ * for it, topk_idx and w_router) + sum_j dlogit[t,j] w_router[topk_idx[t,j]], the router's part.  fp32 sums in
+ * ascending j, one rounding to bf16.
+ * dxp: bf16 [Rcap,D]; dlogit: fp32 [T,K] from moegps_route_backward; w_router: bf16 [E,D]; dx: bf16 [T,D]. */
+MOEGPS_API int moegps_dispatch_backward(moegps_ctx_t* ctx, const void* dxp, const int32_t* pair_row,
+                                        const int32_t* topk_idx, const float* dlogit, const void* w_router, void* dx,
+                                        void* stream);
+
+/* route_backward - gradient of moegps_route's gate weights.  With m[t] = sum_i topk_w[t,i] dtopk_w[t,i]:
+ *   gate_mode 0: dlogit[t,j] = topk_w (dtopk_w - m);  gate_mode 1: times 1 - sigmoid(logit), the K selected logits being
+ *   computed again from x, w_router and bias.  Logits that were not selected have no gradient.
+ *   dw_router[e] = sum dlogit x[t], dbias[e] = sum dlogit over the pairs of e (zero for an expert without pairs).
+ * x: bf16 [T,D]; w_router: bf16 [E,D], bias: fp32 [E] or NULL and topk_idx: int32 [T,K] are read in gate_mode 1 only
+ * (w_router and topk_idx may be NULL otherwise); topk_w, dtopk_w: fp32 [T,K]; slot_row_off, row_pair from dispatch,
+ * slot_off from the plan (they list the pairs by expert); dlogit: fp32 [T,K]; dw_router: fp32 [E,D]; dbias: fp32 [E].
+ * fp32 throughout, fixed summation order.  workspace: moegps_route_backward_workspace_bytes(shape) bytes, contents
+ * irrelevant; its size cannot be checked here. */
+MOEGPS_API int moegps_route_backward(moegps_ctx_t* ctx, const void* x, const void* w_router, const float* bias,
+                                     const int32_t* topk_idx, const float* topk_w, const float* dtopk_w,
+                                     const int32_t* slot_row_off, const int32_t* slot_off, const int32_t* row_pair,
+                                     float* dlogit, float* dw_router, float* dbias, void* workspace, void* stream);
+
+/* Bytes of `workspace` for moegps_route_backward (0 for an invalid shape). */
+MOEGPS_API size_t moegps_route_backward_workspace_bytes(const moegps_shape_t* shape);
+
 /* predictor_update - state of Distribution-Only Prediction across batches (paper, Section 3.2.1:
  * the maximum-likelihood estimate p_e = n_e / N of Eq. 1, averaged over the batches seen).  state[e] += hist[e]; state / sum(state) is then Eq. 1 over all tokens
  * seen.  predicted_hist = state divided by the smallest power of two that makes its largest entry fit

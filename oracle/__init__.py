@@ -25,3 +25,13 @@ from .moe_oracle import (  # noqa: F401
     combine,
     moe_layer,
 )
+from .moe_gradients import (  # noqa: F401
+    act8_decode,
+    act8_encode,
+    combine_backward,
+    dispatch_backward,
+    e4m3_round,
+    expert_ffn_backward,
+    gate_up,
+    route_backward,
+)

@@ -42,6 +42,11 @@ class Shape:
     def Rcap(self) -> int:
         return self.T * self.K + self.S * (self.row_align - 1)
 
+    @property
+    def P(self) -> int:
+        """Columns of a row of 8-bit activations: F rounded up to whole blocks of 32."""
+        return (self.F + 31) // 32 * 32
+
     def c_struct(self) -> moegps_shape_t:
         return moegps_shape_t(*(getattr(self, f[0]) for f in moegps_shape_t._fields_))
 
@@ -57,6 +62,9 @@ EXPORTS = (
     "moegps_expert_ffn", "moegps_expert_ffn_gate_up", "moegps_expert_ffn_down", "moegps_combine",
     "moegps_status", "moegps_launch_count", "moegps_last_cuda_error", "moegps_error_string",
     "moegps_selftest_bounded_wait", "moegps_predictor_update", "moegps_predictor_update_ema", "moegps_error_rate",
+    "moegps_expert_ffn_gate_up_save", "moegps_expert_ffn_backward", "moegps_expert_ffn_backward_act",
+    "moegps_expert_ffn_backward_input", "moegps_expert_ffn_backward_weights", "moegps_combine_backward",
+    "moegps_dispatch_backward", "moegps_route_backward", "moegps_route_backward_workspace_bytes",
 )
 
 
@@ -109,6 +117,15 @@ def _lib():
         "moegps_expert_ffn_gate_up": (ctypes.c_int, [vp] * 8),
         "moegps_expert_ffn_down": (ctypes.c_int, [vp] * 7),
         "moegps_combine": (ctypes.c_int, [vp] * 6),
+        "moegps_expert_ffn_gate_up_save": (ctypes.c_int, [vp] * 12),
+        "moegps_expert_ffn_backward": (ctypes.c_int, [vp] * 22),
+        "moegps_expert_ffn_backward_act": (ctypes.c_int, [vp] * 13),
+        "moegps_expert_ffn_backward_input": (ctypes.c_int, [vp] * 9),
+        "moegps_expert_ffn_backward_weights": (ctypes.c_int, [vp] * 13),
+        "moegps_combine_backward": (ctypes.c_int, [vp] * 8),
+        "moegps_dispatch_backward": (ctypes.c_int, [vp] * 8),
+        "moegps_route_backward": (ctypes.c_int, [vp] * 15),
+        "moegps_route_backward_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(moegps_shape_t)]),
         "moegps_selftest_bounded_wait": (ctypes.c_int, [vp, i64, vp]),
         "moegps_predictor_update": (ctypes.c_int, [vp] * 5),
         "moegps_predictor_update_ema": (ctypes.c_int, [vp, vp, vp, i32, vp, vp]),
@@ -364,6 +381,115 @@ class Context:
             _ptr(topk_w, torch.float32, (s.T, s.K), "topk_w"),
             _ptr(out, torch.bfloat16, (s.T, s.D), "out"), _stream(stream)), "moegps_combine")
 
+    # -- the training step --------------------------------------------------------------------
+    def expert_ffn_gate_up_save(self, xp, slot_row_off, slot_expert, w_gate, w_up, h_ws, gate8, up8, gate_scale, up_scale,
+                                stream=None):
+        s = self.shape
+        codes, scales = (s.Rcap, s.P), (s.P // 32, s.Rcap)
+        self._check(_lib().moegps_expert_ffn_gate_up_save(
+            self._h, _ptr(xp, torch.bfloat16, (s.Rcap, s.D), "xp"),
+            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
+            _ptr(slot_expert, torch.int32, (s.S,), "slot_expert"),
+            _ptr(w_gate, torch.bfloat16, (s.E, s.F, s.D), "w_gate"),
+            _ptr(w_up, torch.bfloat16, (s.E, s.F, s.D), "w_up"),
+            _ptr(h_ws, torch.bfloat16, (s.Rcap, s.F), "h_ws"),
+            _ptr(gate8, torch.uint8, codes, "gate8"), _ptr(up8, torch.uint8, codes, "up8"),
+            _ptr(gate_scale, torch.uint8, scales, "gate_scale"), _ptr(up_scale, torch.uint8, scales, "up_scale"),
+            _stream(stream)), "moegps_expert_ffn_gate_up_save")
+
+    def expert_ffn_backward(self, dyp, xp, slot_row_off, slot_off, slot_expert, row_pair, w_gate, w_up, w_down, gate8, up8,
+                            gate_scale, up_scale, dgate, dup, h_ws, dxp, dw_gate, dw_up, dw_down, stream=None):
+        s = self.shape
+        rows_d, rows_f = (s.Rcap, s.D), (s.Rcap, s.F)
+        codes, scales = (s.Rcap, s.P), (s.P // 32, s.Rcap)
+        up, down = (s.E, s.F, s.D), (s.E, s.D, s.F)
+        self._check(_lib().moegps_expert_ffn_backward(
+            self._h, _ptr(dyp, torch.bfloat16, rows_d, "dyp"), _ptr(xp, torch.bfloat16, rows_d, "xp"),
+            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
+            _ptr(slot_off, torch.int32, (s.E + 1,), "slot_off"),
+            _ptr(slot_expert, torch.int32, (s.S,), "slot_expert"),
+            _ptr(row_pair, torch.int32, (s.Rcap,), "row_pair"),
+            _ptr(w_gate, torch.bfloat16, up, "w_gate"), _ptr(w_up, torch.bfloat16, up, "w_up"),
+            _ptr(w_down, torch.bfloat16, down, "w_down"),
+            _ptr(gate8, torch.uint8, codes, "gate8"), _ptr(up8, torch.uint8, codes, "up8"),
+            _ptr(gate_scale, torch.uint8, scales, "gate_scale"), _ptr(up_scale, torch.uint8, scales, "up_scale"),
+            _ptr(dgate, torch.bfloat16, rows_f, "dgate"), _ptr(dup, torch.bfloat16, rows_f, "dup"),
+            _ptr(h_ws, torch.bfloat16, rows_f, "h_ws"), _ptr(dxp, torch.bfloat16, rows_d, "dxp"),
+            _ptr(dw_gate, torch.bfloat16, up, "dw_gate"), _ptr(dw_up, torch.bfloat16, up, "dw_up"),
+            _ptr(dw_down, torch.bfloat16, down, "dw_down"), _stream(stream)), "moegps_expert_ffn_backward")
+
+    def expert_ffn_backward_act(self, dyp, slot_row_off, slot_expert, w_down, gate8, up8, gate_scale, up_scale, dgate, dup,
+                                h_ws, stream=None):
+        s = self.shape
+        codes, scales = (s.Rcap, s.P), (s.P // 32, s.Rcap)
+        self._check(_lib().moegps_expert_ffn_backward_act(
+            self._h, _ptr(dyp, torch.bfloat16, (s.Rcap, s.D), "dyp"),
+            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
+            _ptr(slot_expert, torch.int32, (s.S,), "slot_expert"),
+            _ptr(w_down, torch.bfloat16, (s.E, s.D, s.F), "w_down"),
+            _ptr(gate8, torch.uint8, codes, "gate8"), _ptr(up8, torch.uint8, codes, "up8"),
+            _ptr(gate_scale, torch.uint8, scales, "gate_scale"), _ptr(up_scale, torch.uint8, scales, "up_scale"),
+            _ptr(dgate, torch.bfloat16, (s.Rcap, s.F), "dgate"), _ptr(dup, torch.bfloat16, (s.Rcap, s.F), "dup"),
+            _ptr(h_ws, torch.bfloat16, (s.Rcap, s.F), "h_ws"), _stream(stream)), "moegps_expert_ffn_backward_act")
+
+    def expert_ffn_backward_input(self, dgate, dup, slot_row_off, slot_expert, w_gate, w_up, dxp, stream=None):
+        s = self.shape
+        self._check(_lib().moegps_expert_ffn_backward_input(
+            self._h, _ptr(dgate, torch.bfloat16, (s.Rcap, s.F), "dgate"), _ptr(dup, torch.bfloat16, (s.Rcap, s.F), "dup"),
+            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
+            _ptr(slot_expert, torch.int32, (s.S,), "slot_expert"),
+            _ptr(w_gate, torch.bfloat16, (s.E, s.F, s.D), "w_gate"), _ptr(w_up, torch.bfloat16, (s.E, s.F, s.D), "w_up"),
+            _ptr(dxp, torch.bfloat16, (s.Rcap, s.D), "dxp"), _stream(stream)), "moegps_expert_ffn_backward_input")
+
+    def expert_ffn_backward_weights(self, dyp, xp, dgate, dup, h_ws, slot_row_off, slot_off, row_pair, dw_gate, dw_up, dw_down,
+                                    stream=None):
+        s = self.shape
+        self._check(_lib().moegps_expert_ffn_backward_weights(
+            self._h, _ptr(dyp, torch.bfloat16, (s.Rcap, s.D), "dyp"), _ptr(xp, torch.bfloat16, (s.Rcap, s.D), "xp"),
+            _ptr(dgate, torch.bfloat16, (s.Rcap, s.F), "dgate"), _ptr(dup, torch.bfloat16, (s.Rcap, s.F), "dup"),
+            _ptr(h_ws, torch.bfloat16, (s.Rcap, s.F), "h_ws"),
+            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
+            _ptr(slot_off, torch.int32, (s.E + 1,), "slot_off"), _ptr(row_pair, torch.int32, (s.Rcap,), "row_pair"),
+            _ptr(dw_gate, torch.bfloat16, (s.E, s.F, s.D), "dw_gate"), _ptr(dw_up, torch.bfloat16, (s.E, s.F, s.D), "dw_up"),
+            _ptr(dw_down, torch.bfloat16, (s.E, s.D, s.F), "dw_down"), _stream(stream)), "moegps_expert_ffn_backward_weights")
+
+    def combine_backward(self, dout, yp, pair_row, topk_w, dyp, dtopk_w, stream=None):
+        s = self.shape
+        self._check(_lib().moegps_combine_backward(
+            self._h, _ptr(dout, torch.bfloat16, (s.T, s.D), "dout"), _ptr(yp, torch.bfloat16, (s.Rcap, s.D), "yp"),
+            _ptr(pair_row, torch.int32, (s.T, s.K), "pair_row"), _ptr(topk_w, torch.float32, (s.T, s.K), "topk_w"),
+            _ptr(dyp, torch.bfloat16, (s.Rcap, s.D), "dyp"), _ptr(dtopk_w, torch.float32, (s.T, s.K), "dtopk_w"),
+            _stream(stream)), "moegps_combine_backward")
+
+    def dispatch_backward(self, dxp, pair_row, topk_idx, dlogit, w_router, dx, stream=None):
+        """dlogit None: without the router's part (topk_idx and w_router are not read)."""
+        s = self.shape
+        part = dlogit is not None
+        self._check(_lib().moegps_dispatch_backward(
+            self._h, _ptr(dxp, torch.bfloat16, (s.Rcap, s.D), "dxp"), _ptr(pair_row, torch.int32, (s.T, s.K), "pair_row"),
+            _ptr(topk_idx, torch.int32, (s.T, s.K), "topk_idx") if part else None,
+            _ptr(dlogit, torch.float32, (s.T, s.K), "dlogit") if part else None,
+            _ptr(w_router, torch.bfloat16, (s.E, s.D), "w_router") if part else None,
+            _ptr(dx, torch.bfloat16, (s.T, s.D), "dx"), _stream(stream)), "moegps_dispatch_backward")
+
+    def route_backward(self, x, w_router, bias, topk_idx, topk_w, dtopk_w, slot_row_off, slot_off, row_pair, dlogit,
+                       dw_router, dbias, workspace, stream=None):
+        s = self.shape
+        if workspace is None or workspace.numel() * workspace.element_size() < route_backward_workspace_bytes(s):
+            raise MoegpsError(ERR_WORKSPACE_TOO_SMALL, "moegps_route_backward")
+        softmax = s.gate_mode == 0                       # then w_router, bias and topk_idx are not read
+        self._check(_lib().moegps_route_backward(
+            self._h, _ptr(x, torch.bfloat16, (s.T, s.D), "x"),
+            _ptr(w_router, torch.bfloat16, (s.E, s.D), "w_router", allow_none=softmax),
+            _ptr(bias, torch.float32, (s.E,), "bias", allow_none=True),
+            _ptr(topk_idx, torch.int32, (s.T, s.K), "topk_idx", allow_none=softmax),
+            _ptr(topk_w, torch.float32, (s.T, s.K), "topk_w"), _ptr(dtopk_w, torch.float32, (s.T, s.K), "dtopk_w"),
+            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
+            _ptr(slot_off, torch.int32, (s.E + 1,), "slot_off"), _ptr(row_pair, torch.int32, (s.Rcap,), "row_pair"),
+            _ptr(dlogit, torch.float32, (s.T, s.K), "dlogit"), _ptr(dw_router, torch.float32, (s.E, s.D), "dw_router"),
+            _ptr(dbias, torch.float32, (s.E,), "dbias"), _ptr(workspace, workspace.dtype, None, "workspace"),
+            _stream(stream)), "moegps_route_backward")
+
     def predictor_update(self, hist, state, predicted_hist, stream=None):
         s = self.shape
         self._check(_lib().moegps_predictor_update(
@@ -414,6 +540,11 @@ def rcap(shape: Shape) -> int:
 def workspace_bytes(shape: Shape) -> int:
     cs = shape.c_struct()
     return int(_lib().moegps_workspace_bytes(ctypes.byref(cs)))
+
+
+def route_backward_workspace_bytes(shape: Shape) -> int:
+    cs = shape.c_struct()
+    return int(_lib().moegps_route_backward_workspace_bytes(ctypes.byref(cs)))
 
 
 def error_string(code: int) -> str:

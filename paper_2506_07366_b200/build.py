@@ -11,8 +11,9 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libmoegps.so")
 SOURCES = ["api.cu", "route.cu", "histogram.cu", "plan.cu", "pack.cu", "dispatch.cu", "expert_ffn.cu", "combine.cu",
-           "predictor.cu", "selftest.cu"]
-HEADERS = ["common.cuh", "sm100.cuh", "route_epilogue.cuh", "slot_offsets.cuh"]
+           "predictor.cu", "selftest.cu", "expert_ffn_backward.cu", "shuffle_backward.cu", "route_backward.cu"]
+HEADERS = ["common.cuh", "sm100.cuh", "route_epilogue.cuh", "slot_offsets.cuh", "grouped_gemm.cuh", "act8.cuh", "bf16x8.cuh",
+           "route_backward.cuh"]
 
 
 def _nvcc() -> str:

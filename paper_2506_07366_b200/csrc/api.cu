@@ -5,6 +5,7 @@
 #include <stdlib.h>
 
 #include "common.cuh"
+#include "route_backward.cuh"
 
 namespace {
 
@@ -49,6 +50,7 @@ int moegps_create(moegps_ctx_t** out, const moegps_shape_t* shape, int device) {
   ctx->tm1_valid = false;
   ctx->tm2_valid = false;
   for (bool& b : ctx->ffn_attr_done) b = false;
+  for (bool& b : ctx->ffn_backward_attr_done) b = false;
   ctx->rt_valid = false;
   ctx->route_attr_done = false;
   ctx->dispatch_attr_done = false;
@@ -239,6 +241,119 @@ int moegps_combine(moegps_ctx_t* ctx, const void* yp, const int32_t* pair_row, c
   if (ctx->shape.T == 0) return MOEGPS_OK;
   if (!all_ok(yp, pair_row, topk_w, out)) return MOEGPS_ERR_INVALID_ARG;
   return moegps_launch_combine(ctx, yp, pair_row, topk_w, out, (cudaStream_t)stream);
+}
+
+int moegps_expert_ffn_gate_up_save(moegps_ctx_t* ctx, const void* xp, const int32_t* slot_row_off,
+                                   const int32_t* slot_expert, const void* w_gate, const void* w_up, void* h_ws,
+                                   void* gate8, void* up8, void* gate_scale, void* up_scale, void* stream) {
+  if (!ctx) return MOEGPS_ERR_INVALID_ARG;
+  if (int rc = moegps_check_device(ctx)) return rc;
+  if (ctx->shape.T == 0) return MOEGPS_OK;
+  if (!all_ok(xp, slot_row_off, slot_expert, w_gate, w_up, h_ws, gate8, up8, gate_scale, up_scale)) return MOEGPS_ERR_INVALID_ARG;
+  return moegps_launch_ffn_gate_up_save(ctx, xp, slot_row_off, slot_expert, w_gate, w_up, h_ws, gate8, up8, gate_scale,
+                                        up_scale, (cudaStream_t)stream);
+}
+
+int moegps_expert_ffn_backward_act(moegps_ctx_t* ctx, const void* dyp, const int32_t* slot_row_off,
+                                   const int32_t* slot_expert, const void* w_down, const void* gate8, const void* up8,
+                                   const void* gate_scale, const void* up_scale, void* dgate, void* dup, void* h_ws,
+                                   void* stream) {
+  if (!ctx) return MOEGPS_ERR_INVALID_ARG;
+  if (int rc = moegps_check_device(ctx)) return rc;
+  if (ctx->shape.T == 0) return MOEGPS_OK;
+  if (!all_ok(dyp, slot_row_off, slot_expert, w_down, gate8, up8, gate_scale, up_scale, dgate, dup, h_ws))
+    return MOEGPS_ERR_INVALID_ARG;
+  return moegps_launch_ffn_backward_act(ctx, dyp, slot_row_off, slot_expert, w_down, gate8, up8, gate_scale, up_scale, dgate,
+                                        dup, h_ws, (cudaStream_t)stream);
+}
+
+int moegps_expert_ffn_backward_input(moegps_ctx_t* ctx, const void* dgate, const void* dup, const int32_t* slot_row_off,
+                                     const int32_t* slot_expert, const void* w_gate, const void* w_up, void* dxp,
+                                     void* stream) {
+  if (!ctx) return MOEGPS_ERR_INVALID_ARG;
+  if (int rc = moegps_check_device(ctx)) return rc;
+  if (ctx->shape.T == 0) return MOEGPS_OK;
+  if (!all_ok(dgate, dup, slot_row_off, slot_expert, w_gate, w_up, dxp)) return MOEGPS_ERR_INVALID_ARG;
+  return moegps_launch_ffn_backward_input(ctx, dgate, dup, slot_row_off, slot_expert, w_gate, w_up, dxp,
+                                          (cudaStream_t)stream);
+}
+
+int moegps_expert_ffn_backward_weights(moegps_ctx_t* ctx, const void* dyp, const void* xp, const void* dgate, const void* dup,
+                                       const void* h_ws, const int32_t* slot_row_off, const int32_t* slot_off,
+                                       const int32_t* row_pair, void* dw_gate, void* dw_up, void* dw_down, void* stream) {
+  if (!ctx || !all_ok(dw_gate, dw_up, dw_down)) return MOEGPS_ERR_INVALID_ARG;
+  if (int rc = moegps_check_device(ctx)) return rc;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (ctx->shape.T == 0) {                          // no tokens: every gradient is zero
+    const size_t bytes = (size_t)ctx->shape.E * ctx->shape.F * ctx->shape.D * 2;
+    for (void* p : {dw_gate, dw_up, dw_down}) MOEGPS_CUDA_TRY(ctx, cudaMemsetAsync(p, 0, bytes, st));
+    return MOEGPS_OK;
+  }
+  if (!all_ok(dyp, xp, dgate, dup, h_ws, slot_row_off, slot_off, row_pair)) return MOEGPS_ERR_INVALID_ARG;
+  return moegps_launch_ffn_backward_weights(ctx, dyp, xp, dgate, dup, h_ws, slot_row_off, slot_off, row_pair, dw_gate, dw_up,
+                                            dw_down, st);
+}
+
+int moegps_expert_ffn_backward(moegps_ctx_t* ctx, const void* dyp, const void* xp, const int32_t* slot_row_off,
+                               const int32_t* slot_off, const int32_t* slot_expert, const int32_t* row_pair,
+                               const void* w_gate, const void* w_up, const void* w_down, const void* gate8, const void* up8,
+                               const void* gate_scale, const void* up_scale, void* dgate, void* dup, void* h_ws, void* dxp,
+                               void* dw_gate, void* dw_up, void* dw_down, void* stream) {
+  if (!ctx || !all_ok(dw_gate, dw_up, dw_down)) return MOEGPS_ERR_INVALID_ARG;
+  // everything is checked before the first launch
+  if (ctx->shape.T > 0 && !all_ok(dyp, xp, slot_row_off, slot_off, slot_expert, row_pair, w_gate, w_up, w_down, gate8, up8,
+                                  gate_scale, up_scale, dgate, dup, h_ws, dxp))
+    return MOEGPS_ERR_INVALID_ARG;
+  int rc = moegps_expert_ffn_backward_act(ctx, dyp, slot_row_off, slot_expert, w_down, gate8, up8, gate_scale, up_scale, dgate,
+                                          dup, h_ws, stream);
+  if (rc != MOEGPS_OK) return rc;
+  rc = moegps_expert_ffn_backward_input(ctx, dgate, dup, slot_row_off, slot_expert, w_gate, w_up, dxp, stream);
+  if (rc != MOEGPS_OK) return rc;
+  return moegps_expert_ffn_backward_weights(ctx, dyp, xp, dgate, dup, h_ws, slot_row_off, slot_off, row_pair, dw_gate, dw_up,
+                                            dw_down, stream);
+}
+
+int moegps_combine_backward(moegps_ctx_t* ctx, const void* dout, const void* yp, const int32_t* pair_row,
+                            const float* topk_w, void* dyp, float* dtopk_w, void* stream) {
+  if (!ctx) return MOEGPS_ERR_INVALID_ARG;
+  if (int rc = moegps_check_device(ctx)) return rc;
+  if (ctx->shape.T == 0) return MOEGPS_OK;
+  if (!all_ok(dout, yp, pair_row, topk_w, dyp, dtopk_w)) return MOEGPS_ERR_INVALID_ARG;
+  return moegps_launch_combine_backward(ctx, dout, yp, pair_row, topk_w, dyp, dtopk_w, (cudaStream_t)stream);
+}
+
+int moegps_dispatch_backward(moegps_ctx_t* ctx, const void* dxp, const int32_t* pair_row, const int32_t* topk_idx,
+                             const float* dlogit, const void* w_router, void* dx, void* stream) {
+  if (!ctx) return MOEGPS_ERR_INVALID_ARG;
+  if (int rc = moegps_check_device(ctx)) return rc;
+  if (ctx->shape.T == 0) return MOEGPS_OK;
+  if (!all_ok(dxp, pair_row, dx)) return MOEGPS_ERR_INVALID_ARG;
+  if (dlogit && !all_ok(topk_idx, dlogit, w_router)) return MOEGPS_ERR_INVALID_ARG;
+  return moegps_launch_dispatch_backward(ctx, dxp, pair_row, topk_idx, dlogit, w_router, dx, (cudaStream_t)stream);
+}
+
+size_t moegps_route_backward_workspace_bytes(const moegps_shape_t* shape) {
+  return check_shape(shape) == MOEGPS_OK ? route_backward::bytes(*shape) : 0;
+}
+
+int moegps_route_backward(moegps_ctx_t* ctx, const void* x, const void* w_router, const float* bias,
+                          const int32_t* topk_idx, const float* topk_w, const float* dtopk_w, const int32_t* slot_row_off,
+                          const int32_t* slot_off, const int32_t* row_pair, float* dlogit, float* dw_router, float* dbias,
+                          void* workspace, void* stream) {
+  if (!ctx || !all_ok(dw_router, dbias)) return MOEGPS_ERR_INVALID_ARG;
+  if (int rc = moegps_check_device(ctx)) return rc;
+  const moegps_shape_t& s = ctx->shape;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (s.T == 0) {                                   // no tokens: every gradient is zero
+    MOEGPS_CUDA_TRY(ctx, cudaMemsetAsync(dw_router, 0, sizeof(float) * s.E * s.D, st));
+    MOEGPS_CUDA_TRY(ctx, cudaMemsetAsync(dbias, 0, sizeof(float) * s.E, st));
+    return MOEGPS_OK;
+  }
+  if (!all_ok(x, topk_w, dtopk_w, slot_row_off, slot_off, row_pair, dlogit, workspace)) return MOEGPS_ERR_INVALID_ARG;
+  if (s.gate_mode == 1 && !all_ok(w_router, topk_idx)) return MOEGPS_ERR_INVALID_ARG;
+  if (bias && (reinterpret_cast<uintptr_t>(bias) & 3u)) return MOEGPS_ERR_INVALID_ARG;
+  return moegps_launch_route_backward(ctx, x, w_router, bias, topk_idx, topk_w, dtopk_w, slot_row_off, slot_off, row_pair,
+                                      dlogit, dw_router, dbias, workspace, st);
 }
 
 int moegps_status(moegps_ctx_t* ctx, void* stream, int32_t* host_status) {

@@ -2,32 +2,13 @@
 //   out[t,:] = sum_{j<K} topk_w[t,j] * yp[pair_row[t,j],:]
 // One warp per token, 128-bit loads of the K expert rows, fp32 accumulation in ascending j,
 // bf16 round-to-nearest-even on store.  No atomics => deterministic.
+#include "bf16x8.cuh"
 #include "common.cuh"
 
 namespace {
 
 constexpr int kWarpsPerBlock = 8;
 constexpr int kThreads = kWarpsPerBlock * 32;
-
-__device__ __forceinline__ void fma8(float (&acc)[8], float w, const uint4& v) {
-  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    // a bf16 is the upper half of an fp32
-    acc[2 * i] = fmaf(w, __uint_as_float(u[i] << 16), acc[2 * i]);
-    acc[2 * i + 1] = fmaf(w, __uint_as_float(u[i] & 0xffff0000u), acc[2 * i + 1]);
-  }
-}
-
-__device__ __forceinline__ uint4 pack8(const float (&acc)[8]) {
-  uint32_t u[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(acc[2 * i], acc[2 * i + 1]);
-    u[i] = *reinterpret_cast<const uint32_t*>(&h);
-  }
-  return make_uint4(u[0], u[1], u[2], u[3]);
-}
 
 template <int KT>   // KT = compile-time K (1..8)
 __global__ void __launch_bounds__(kThreads)

@@ -25,7 +25,8 @@ struct moegps_ctx {
   const void* tm_key2[2];   // h_ws, w_down
   CUtensorMap tm_h, tm_w2;
   bool tm2_valid;
-  bool ffn_attr_done[2]; // dynamic shared-memory limit raised: gate+up and down instantiations of the GEMM kernel
+  bool ffn_attr_done[3]; // dynamic shared-memory limit raised: gate+up, down, gate+up with kept activations
+  bool ffn_backward_attr_done[3];   // the same for the gradient's kernels: act, input, weights
   // cached TMA descriptors of the router
   const void* rt_key[2];
   CUtensorMap tm_rx, tm_rw;
@@ -112,3 +113,23 @@ int moegps_launch_ffn_down(moegps_ctx* ctx, const void* h_ws, const int32_t* slo
                            const int32_t* slot_expert, const void* w_down, void* yp, cudaStream_t st);
 int moegps_launch_combine(moegps_ctx* ctx, const void* yp, const int32_t* pair_row, const float* topk_w,
                           void* out, cudaStream_t st);
+int moegps_launch_ffn_gate_up_save(moegps_ctx* ctx, const void* xp, const int32_t* slot_row_off,
+                                   const int32_t* slot_expert, const void* w_gate, const void* w_up, void* h_ws,
+                                   void* gate8, void* up8, void* gate_scale, void* up_scale, cudaStream_t st);
+int moegps_launch_ffn_backward_act(moegps_ctx* ctx, const void* dyp, const int32_t* slot_row_off, const int32_t* slot_expert,
+                                   const void* w_down, const void* gate8, const void* up8, const void* gate_scale,
+                                   const void* up_scale, void* dgate, void* dup, void* h_ws, cudaStream_t st);
+int moegps_launch_ffn_backward_input(moegps_ctx* ctx, const void* dgate, const void* dup, const int32_t* slot_row_off,
+                                     const int32_t* slot_expert, const void* w_gate, const void* w_up, void* dxp,
+                                     cudaStream_t st);
+int moegps_launch_ffn_backward_weights(moegps_ctx* ctx, const void* dyp, const void* xp, const void* dgate, const void* dup,
+                                       const void* h_ws, const int32_t* slot_row_off, const int32_t* slot_off,
+                                       const int32_t* row_pair, void* dw_gate, void* dw_up, void* dw_down, cudaStream_t st);
+int moegps_launch_combine_backward(moegps_ctx* ctx, const void* dout, const void* yp, const int32_t* pair_row,
+                                   const float* topk_w, void* dyp, float* dtopk_w, cudaStream_t st);
+int moegps_launch_dispatch_backward(moegps_ctx* ctx, const void* dxp, const int32_t* pair_row, const int32_t* topk_idx,
+                                    const float* dlogit, const void* w_router, void* dx, cudaStream_t st);
+int moegps_launch_route_backward(moegps_ctx* ctx, const void* x, const void* w_router, const float* bias,
+                                 const int32_t* topk_idx, const float* topk_w, const float* dtopk_w,
+                                 const int32_t* slot_row_off, const int32_t* slot_off, const int32_t* row_pair,
+                                 float* dlogit, float* dw_router, float* dbias, void* workspace, cudaStream_t st);

@@ -23,85 +23,13 @@
 // And: cutting the tiles of a last round that is at most half full into two 128-column halves (down
 // GEMM; 7.35 rounds of tiles on the Mixtral-shaped layer) gained 1 % there and nothing elsewhere, so
 // the partial last round is not what separates the down GEMM from the gate+up GEMM.
-#include "common.cuh"
-#include "sm100.cuh"
+#include "act8.cuh"
+#include "grouped_gemm.cuh"
 
 namespace {
 
 using namespace sm100;
-
-constexpr int BM = 128;            // rows per tile
-constexpr int BNACC = 256;         // accumulator columns per tile
-#ifndef MOEGPS_FFN_BK
-#define MOEGPS_FFN_BK 64
-#endif
-// K elements per stage = one swizzle row of BK*2 bytes.  Measured on B200: 64 (128-byte rows, 4
-// stages of 48 KiB) beats 32 (64-byte rows, 8 stages of 24 KiB) by about 25 %: TMA moves 128-byte
-// rows far more efficiently, which outweighs the deeper ring.
-constexpr int BK = MOEGPS_FFN_BK;
-constexpr int kRowBytes = BK * 2;
-constexpr int kABytes = BM * BK * 2;
-constexpr int kBHalfBytes = 128 * BK * 2;
-constexpr int kStageBytes = kABytes + 2 * kBHalfBytes;       // 48 KiB
-constexpr int kMaxS = 1024;
-
-template <int kStages_, int kAccs_, int kEpiWarps_, int kCtasPerSm_>
-struct GemmCfg {
-  static constexpr int kStages = kStages_;        // ring depth (48 KiB per stage)
-  static constexpr int kAccs = kAccs_;            // 256-column TMEM accumulators
-  static constexpr int kEpiWarps = kEpiWarps_;    // 4: one per TMEM lane quarter; 8: two per quarter, half the columns each
-  static constexpr int kCtasPerSm = kCtasPerSm_;
-  static constexpr int kThreads = 64 + 32 * kEpiWarps_;   // producer warp, MMA warp, epilogue warps
-  static constexpr int kTmemCols = 256 * kAccs_;
-};
-using WideCfg = GemmCfg<256 / BK, 2, 8, 1>;       // 192 KiB of ring
-
-// Per-CTA copy of what decoding a tile needs.  tile_base[s] = first tile index of slot s.
-struct __align__(16) Tables {
-  int32_t tile_base[kMaxS + 1];
-};
-
-constexpr int kStageRowBytes = 80;                 // epilogue staging: 64 payload bytes per row, conflict-free pitch
-constexpr int kStagingBytesPerWarp = 32 * kStageRowBytes;
-
-template <class Cfg>
-constexpr size_t smem_bytes_of() {
-  return 1024 /* alignment slack */ + (size_t)Cfg::kStages * kStageBytes + sizeof(Tables) + 256 +
-         (size_t)Cfg::kEpiWarps * kStagingBytesPerWarp;
-}
-static_assert(smem_bytes_of<WideCfg>() <= 227 * 1024, "one CTA per SM");
-
-struct TileCoord {
-  int m0;        // first row of the tile in the permuted buffer
-  int row_end;   // one past the last row of the slot's extent
-  int n_tile;
-  int expert;
-};
-
-__device__ __forceinline__ TileCoord decode_tile(const Tables& tb, const int32_t* __restrict__ slot_row_off,
-                                               const int32_t* __restrict__ slot_expert, int S, int tile, int n_tiles) {
-  int lo = 0, hi = S;                 // find s with tile_base[s] <= tile < tile_base[s+1]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (tb.tile_base[mid] <= tile) lo = mid; else hi = mid;
-  }
-  const int s = lo;
-  const int local = tile - tb.tile_base[s];
-  const int mt = (tb.tile_base[s + 1] - tb.tile_base[s]) / n_tiles;   // row tiles of this slot
-  TileCoord c;
-  c.n_tile = local / mt;
-  // (the slot tables are a few KiB that every CTA reads: they stay in L1/L2; only slots that passed
-  // the checks of the table build own tiles, so these values are in range)
-  c.m0 = __ldg(slot_row_off + s) + (local % mt) * BM;
-  c.row_end = __ldg(slot_row_off + s + 1);
-  c.expert = __ldg(slot_expert + s);
-  return c;
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
+using namespace grouped_gemm;
 
 // silu(g) = g / (1 + exp(-g)) = g * (0.5 + 0.5 tanh(g / 2)), with the hardware tanh approximation
 // (relative error about 2^-11; the product is rounded to bf16, 2^-9, right after).
@@ -110,6 +38,12 @@ __device__ __forceinline__ float silu_fast(float g) {
   asm("tanh.approx.f32 %0, %1;" : "=f"(t) : "f"(0.5f * g));
   return g * fmaf(0.5f, t, 0.5f);
 }
+
+// Where moegps_expert_ffn_gate_up_save keeps the activations (see act8.cuh): codes [rcap][pitch], scales [blocks][rcap].
+struct SavedActs {
+  uint8_t *gate8, *up8, *gate_scale, *up_scale;
+  int rcap;
+};
 
 // Epilogue of one tile for one warp: 32 accumulator rows (one per lane) x half of the tile's output
 // columns, TMEM -> registers -> bf16 -> shared-memory staging -> global.
@@ -120,12 +54,16 @@ __device__ __forceinline__ float silu_fast(float g) {
 // L2/HBM throughput.  Instead each 32-column chunk (64 bytes per row) goes through a per-warp
 // staging buffer (rows 80 bytes apart: conflict-free) and is written out with four lanes per row,
 // i.e. whole 64-byte segments.  `row0` is the first of the warp's 32 rows, `row_end` the slot's end.
-template <bool kSwiGLU>
+// kSave: the chunk's 32 gate and 32 up columns of each row are one block each of the 8-bit activations (act8.cuh):
+// a lane has its row's block in registers, so the block maximum needs no exchange between lanes.
+template <bool kSwiGLU, bool kSave>
 __device__ __forceinline__ void drain_tile(uint32_t taddr, uint8_t* staging, int lane, __nv_bfloat16* out,
-                                           int row0, int row_end, int col0, int n_dim, int c_begin, int c_end) {
+                                           int row0, int row_end, int col0, int n_dim, int c_begin, int c_end,
+                                           const SavedActs& save) {
 #pragma unroll 1
   for (int c0 = c_begin; c0 < c_end; c0 += 32) {
     uint32_t o[16];
+    [[maybe_unused]] uint32_t codes[2][8], scale[2];
     if constexpr (kSwiGLU) {
       uint32_t g[32], u[32];
       tmem_ld32(taddr + c0, g);
@@ -136,6 +74,10 @@ __device__ __forceinline__ void drain_tile(uint32_t taddr, uint8_t* staging, int
         const float g0 = __uint_as_float(g[2 * i]), g1 = __uint_as_float(g[2 * i + 1]);
         o[i] = pack_bf16(silu_fast(g0) * __uint_as_float(u[2 * i]), silu_fast(g1) * __uint_as_float(u[2 * i + 1]));
       }
+      if constexpr (kSave) {
+        scale[0] = act8::encode(g, codes[0]);
+        scale[1] = act8::encode(u, codes[1]);
+      }
     } else {
       uint32_t a[32];
       tmem_ld32(taddr + c0, a);
@@ -143,31 +85,42 @@ __device__ __forceinline__ void drain_tile(uint32_t taddr, uint8_t* staging, int
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[i] = pack_bf16(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1]));
     }
-    uint4* mine = reinterpret_cast<uint4*>(staging + lane * kStageRowBytes);
+    store_chunk(o, staging, lane, out, row0, row_end, col0 + c0, n_dim);
+    if constexpr (kSave) {
+      // 32 bytes of gate codes and 32 of up codes for each row, again four lanes per row
+      const int piece = lane & 3;
+      uint4* mine = reinterpret_cast<uint4*>(staging + lane * kStageRowBytes);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) mine[v] = make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
-    __syncwarp();
-    const int piece = lane & 3;                       // which 16 bytes of the row's 64
-    const int col = col0 + c0 + 8 * piece;
+      for (int v = 0; v < 4; ++v)
+        mine[v] = make_uint4(codes[v >> 1][4 * (v & 1)], codes[v >> 1][4 * (v & 1) + 1], codes[v >> 1][4 * (v & 1) + 2],
+                             codes[v >> 1][4 * (v & 1) + 3]);
+      __syncwarp();
+      const int block = (col0 + c0) / act8::kBlock;
+      const bool in = col0 + c0 < n_dim;
+      uint8_t* plane = (piece < 2 ? save.gate8 : save.up8) + block * act8::kBlock + 16 * (piece & 1);
 #pragma unroll
-    for (int it = 0; it < 4; ++it) {
-      const int r = it * 8 + (lane >> 2);
-      const uint4 val = *reinterpret_cast<const uint4*>(staging + r * kStageRowBytes + piece * 16);
-      const int row = row0 + r;
-      if (row < row_end && col + 8 <= n_dim) *reinterpret_cast<uint4*>(out + (size_t)row * n_dim + col) = val;
+      for (int it = 0; it < 4; ++it) {
+        const int r = it * 8 + (lane >> 2);
+        const uint4 val = *reinterpret_cast<const uint4*>(staging + r * kStageRowBytes + piece * 16);
+        if (in && row0 + r < row_end) *reinterpret_cast<uint4*>(plane + (size_t)(row0 + r) * act8::pitch_of(n_dim)) = val;
+      }
+      if (in && row0 + lane < row_end) {              // scales are stored block-major: consecutive rows, consecutive bytes
+        save.gate_scale[(size_t)block * save.rcap + row0 + lane] = (uint8_t)scale[0];
+        save.up_scale[(size_t)block * save.rcap + row0 + lane] = (uint8_t)scale[1];
+      }
+      __syncwarp();
     }
-    __syncwarp();
   }
 }
 
 // kSwiGLU = true : out[row, n_tile*128 + c] = silu(acc[c]) * acc[128 + c],  c < 128
 // kSwiGLU = false: out[row, n_tile*256 + c] = acc[c],                        c < 256
-template <bool kSwiGLU, class Cfg>
+template <bool kSwiGLU, bool kSave, class Cfg>
 __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kCtasPerSm)
 grouped_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0,
                     const __grid_constant__ CUtensorMap tm_b1, const int32_t* __restrict__ slot_row_off,
                     const int32_t* __restrict__ slot_expert, int S, int E, int n_dim, int k_dim, int rcap,
-                    __nv_bfloat16* __restrict__ out, int32_t* __restrict__ status) {
+                    __nv_bfloat16* __restrict__ out, const SavedActs save, int32_t* __restrict__ status) {
   constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs, kThreads = Cfg::kThreads;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -180,7 +133,6 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
   uint64_t* acc_empty = bars + 2 * kStages + kAccs;  // [kAccs]  epilogue -> MMA
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 2 * kAccs);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int* warp_tiles = const_cast<int*>(reinterpret_cast<volatile int*>(tmem_slot + 2));   // [32] scan scratch
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cols_per_tile = kSwiGLU ? 128 : 256;
@@ -201,54 +153,12 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
     tmem_alloc(tmem_slot, Cfg::kTmemCols);
     tmem_relinquish();
   }
-  // tiles per slot.  A slot whose extent is not inside [0, rcap] (offsets negative, decreasing or
-  // past the buffers) gets no tiles: nothing is read or written for it, and the caller is told.
-  for (int s = threadIdx.x; s <= kMaxS; s += kThreads) {
-    int cnt = 0;
-    if (s < S) {
-      const int lo = slot_row_off[s], hi = slot_row_off[s + 1];
-      const int e = slot_expert[s];
-      if (lo < 0 || hi < lo || hi > rcap) {
-        if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
-      } else if (hi > lo && e >= 0 && e < E) {
-        cnt = ((hi - lo + BM - 1) / BM) * n_tiles;
-      } else if (hi > lo && e >= E) {
-        if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
-      }
-    }
-    tb.tile_base[s] = cnt;
-  }
+  build_tables<kThreads>(tb, slot_row_off, slot_expert, S, E, n_tiles, rcap, status);
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  // exclusive prefix sum of the counts (warp 0: lane l owns entries 33 l .. 33 l + 32; 32 * 33 > kMaxS)
-  if (warp == 0) {
-    constexpr int kPer = (kMaxS + 1 + 31) / 32;
-    int v[kPer], sum = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int s = lane * kPer + i;
-      v[i] = s <= kMaxS ? tb.tile_base[s] : 0;
-      sum += v[i];
-    }
-    int incl = sum;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane >= d) incl += o;
-    }
-    int run = incl - sum;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int s = lane * kPer + i;
-      if (s <= kMaxS) tb.tile_base[s] = run;
-      run += v[i];
-    }
-    if (lane == 31) warp_tiles[0] = incl;
-  }
-  __syncthreads();
   const uint32_t tmem_base = *tmem_slot;
-  const int total_tiles = warp_tiles[0];
+  const int total_tiles = tb.tile_base[kMaxS];
 
   // ---------------------------------------------------------------- roles
   if (warp == 0) {
@@ -322,8 +232,8 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
       tc_fence_after_sync();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * BNACC;
       const int col0 = tc.n_tile * cols_per_tile;
-      drain_tile<kSwiGLU>(taddr, staging, lane, out, tc.m0 + quarter * 32, tc.row_end, col0, n_dim, c_begin,
-                          c_begin + kShare);
+      drain_tile<kSwiGLU, kSave>(taddr, staging, lane, out, tc.m0 + quarter * 32, tc.row_end, col0, n_dim, c_begin,
+                                 c_begin + kShare, save);
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&acc_empty[acc]);
@@ -404,29 +314,27 @@ int tmap_failed(moegps_ctx* ctx) {
   return MOEGPS_ERR_CUDA;
 }
 
-template <bool kSwiGLU, class Cfg>
+template <bool kSwiGLU, bool kSave, class Cfg>
 int launch_gemm(moegps_ctx* ctx, bool* attr_done, const CUtensorMap& ta, const CUtensorMap& tb0, const CUtensorMap& tb1,
                 const int32_t* slot_row_off, const int32_t* slot_expert, int n_dim, int k_dim, void* out,
-                cudaStream_t st) {
+                const SavedActs& save, cudaStream_t st) {
   const moegps_shape_t& s = ctx->shape;
   constexpr size_t smem = smem_bytes_of<Cfg>();
   if (!*attr_done) {
-    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(grouped_gemm_kernel<kSwiGLU, Cfg>,
+    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(grouped_gemm_kernel<kSwiGLU, kSave, Cfg>,
                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     *attr_done = true;
   }
-  grouped_gemm_kernel<kSwiGLU, Cfg><<<ctx->sm_count * Cfg::kCtasPerSm, Cfg::kThreads, smem, st>>>(
+  grouped_gemm_kernel<kSwiGLU, kSave, Cfg><<<ctx->sm_count * Cfg::kCtasPerSm, Cfg::kThreads, smem, st>>>(
       ta, tb0, tb1, slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim, (int)moegps_rcap_of(s),
-      static_cast<__nv_bfloat16*>(out), ctx->d_status);
+      static_cast<__nv_bfloat16*>(out), save, ctx->d_status);
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }
 
 }  // namespace
 
-int moegps_launch_ffn_gate_up(moegps_ctx* ctx, const void* xp, const int32_t* slot_row_off,
-                              const int32_t* slot_expert, const void* w_gate, const void* w_up, void* h_ws,
-                              cudaStream_t st) {
+static int gate_up_tmaps(moegps_ctx* ctx, const void* xp, const void* w_gate, const void* w_up) {
   const moegps_shape_t& s = ctx->shape;
   const uint64_t rcap = (uint64_t)moegps_rcap_of(s);
   if (!(ctx->tm1_valid && ctx->tm_key1[0] == xp && ctx->tm_key1[1] == w_gate && ctx->tm_key1[2] == w_up)) {
@@ -438,8 +346,27 @@ int moegps_launch_ffn_gate_up(moegps_ctx* ctx, const void* xp, const int32_t* sl
     ctx->tm_key1[0] = xp; ctx->tm_key1[1] = w_gate; ctx->tm_key1[2] = w_up;
     ctx->tm1_valid = true;
   }
-  return launch_gemm<true, WideCfg>(ctx, &ctx->ffn_attr_done[0], ctx->tm_xp, ctx->tm_w1, ctx->tm_w3, slot_row_off,
-                                    slot_expert, s.F, s.D, h_ws, st);
+  return MOEGPS_OK;
+}
+
+int moegps_launch_ffn_gate_up(moegps_ctx* ctx, const void* xp, const int32_t* slot_row_off,
+                              const int32_t* slot_expert, const void* w_gate, const void* w_up, void* h_ws,
+                              cudaStream_t st) {
+  const moegps_shape_t& s = ctx->shape;
+  if (int rc = gate_up_tmaps(ctx, xp, w_gate, w_up)) return rc;
+  return launch_gemm<true, false, WideCfg>(ctx, &ctx->ffn_attr_done[0], ctx->tm_xp, ctx->tm_w1, ctx->tm_w3, slot_row_off,
+                                           slot_expert, s.F, s.D, h_ws, SavedActs{}, st);
+}
+
+int moegps_launch_ffn_gate_up_save(moegps_ctx* ctx, const void* xp, const int32_t* slot_row_off,
+                                   const int32_t* slot_expert, const void* w_gate, const void* w_up, void* h_ws,
+                                   void* gate8, void* up8, void* gate_scale, void* up_scale, cudaStream_t st) {
+  const moegps_shape_t& s = ctx->shape;
+  if (int rc = gate_up_tmaps(ctx, xp, w_gate, w_up)) return rc;
+  const SavedActs save = {static_cast<uint8_t*>(gate8), static_cast<uint8_t*>(up8), static_cast<uint8_t*>(gate_scale),
+                          static_cast<uint8_t*>(up_scale), (int)moegps_rcap_of(s)};
+  return launch_gemm<true, true, WideCfg>(ctx, &ctx->ffn_attr_done[2], ctx->tm_xp, ctx->tm_w1, ctx->tm_w3, slot_row_off,
+                                          slot_expert, s.F, s.D, h_ws, save, st);
 }
 
 int moegps_launch_ffn_down(moegps_ctx* ctx, const void* h_ws, const int32_t* slot_row_off,
@@ -454,6 +381,6 @@ int moegps_launch_ffn_down(moegps_ctx* ctx, const void* h_ws, const int32_t* slo
     ctx->tm_key2[0] = h_ws; ctx->tm_key2[1] = w_down;
     ctx->tm2_valid = true;
   }
-  return launch_gemm<false, WideCfg>(ctx, &ctx->ffn_attr_done[1], ctx->tm_h, ctx->tm_w2, ctx->tm_w2, slot_row_off,
-                                     slot_expert, s.D, s.F, yp, st);
+  return launch_gemm<false, false, WideCfg>(ctx, &ctx->ffn_attr_done[1], ctx->tm_h, ctx->tm_w2, ctx->tm_w2, slot_row_off,
+                                     slot_expert, s.D, s.F, yp, SavedActs{}, st);
 }

@@ -1,0 +1,591 @@
+// Gradient of the expert-parallel SwiGLU FFN over ragged slots.  With g = xp W1^T, u = xp W3^T kept in 8 bits by
+// moegps_expert_ffn_gate_up_save (act8.cuh), s = sigmoid(g), h = g s u and yp = h W2^T:
+//   1. act     : dh = dyp W2;  dgate = dh u s (1 + g (1 - s)),  dup = dh g s,  and h again      [rows x F, over D]
+//   2. input   : dxp = dgate W1 + dup W3                                                        [rows x D, over 2 F]
+//   3. weights : dW1[e] = dgate^T xp, dW3[e] = dup^T xp, dW2[e] = dyp^T h                       [F x D and D x F, over rows]
+// Three persistent kernels on the tensor cores, with the ring, the TMEM accumulators and the warp roles of the
+// forward GEMMs (expert_ffn.cu).  What differs is the operands' orientation: the weights are stored for the forward
+// product, so in (1) and (2) the contraction runs along their row index, and in (3) along the row index of both
+// operands.  Nothing is transposed in memory: TMA brings boxes of 64 contiguous elements x 64 rows, and the MMA reads
+// them as MN-major operands.
+// dgate, dup and h are rounded to bf16 between the kernels (they are operands of bf16 MMAs); dh never leaves the
+// accumulator.  All sums are fp32 in tensor memory, rounded to bf16 once at the store.
+#include "act8.cuh"
+#include "grouped_gemm.cuh"
+
+namespace {
+
+using namespace sm100;
+using namespace grouped_gemm;
+
+constexpr int kBoxBytes = 64 * BK * 2;             // a box of an MN-major operand: 64 elements x BK rows
+static_assert(BK == 64, "boxes are one 128-byte swizzle span wide and BK rows high");
+static_assert(kABytes == 2 * kBoxBytes && 2 * kBHalfBytes == 4 * kBoxBytes, "a stage holds 2 + 4 boxes");
+
+// The 8-bit activations that (1) reads: codes [rcap][pitch], scales [blocks][rcap].
+struct KeptActs {
+  const uint8_t *gate8, *up8, *gate_scale, *up_scale;
+};
+struct ActOutputs {
+  __nv_bfloat16 *dgate, *dup, *h;
+};
+
+// A lane's 32 + 32 codes of one block, with their scales; zero where there is no such row or block.
+struct KeptBlock {
+  uint4 g[2], u[2];
+  uint32_t gs, us;
+};
+__device__ __forceinline__ void load_block(KeptBlock& b, const KeptActs& kept, int row, int row_end, int col, int n_dim,
+                                           int rcap) {
+  if (row < row_end && col < n_dim) {
+    const size_t at = (size_t)row * act8::pitch_of(n_dim) + col;
+    const uint4* g = reinterpret_cast<const uint4*>(kept.gate8 + at);
+    const uint4* u = reinterpret_cast<const uint4*>(kept.up8 + at);
+    b.g[0] = __ldg(g);
+    b.g[1] = __ldg(g + 1);
+    b.u[0] = __ldg(u);
+    b.u[1] = __ldg(u + 1);
+    const size_t sc = (size_t)(col / act8::kBlock) * rcap + row;
+    b.gs = __ldg(kept.gate_scale + sc);
+    b.us = __ldg(kept.up_scale + sc);
+  } else {
+    b.g[0] = b.g[1] = b.u[0] = b.u[1] = make_uint4(0, 0, 0, 0);
+    b.gs = b.us = 0;
+  }
+}
+
+// The four values of one code word each, with their part of dh -> packed dgate, dup, h.
+__device__ __forceinline__ void act_gradient(uint32_t gw, uint32_t uw, float gs, float us, const uint32_t* dh, uint32_t* dgate,
+                                             uint32_t* dup, uint32_t* h) {
+  float g[4], u[4];
+  act8::decode4(gw, gs, g);
+  act8::decode4(uw, us, u);
+  float dg[4], du[4], hh[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float d = __uint_as_float(dh[i]);
+    const float s = __fdividef(1.f, 1.f + __expf(-g[i]));
+    const float a = g[i] * s;                       // silu
+    dg[i] = d * u[i] * fmaf(a, 1.f - s, s);         // s (1 + g (1 - s)) = s + a (1 - s)
+    du[i] = d * a;
+    hh[i] = a * u[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    dgate[i] = pack_bf16(dg[2 * i], dg[2 * i + 1]);
+    dup[i] = pack_bf16(du[2 * i], du[2 * i + 1]);
+    h[i] = pack_bf16(hh[2 * i], hh[2 * i + 1]);
+  }
+}
+
+// Epilogue of (1) for one warp: 32 rows x [c_begin, c_end) columns of dh.  The codes of a chunk are loaded while the
+// chunk before it is worked on (the first one before the accumulator is complete).
+__device__ __forceinline__ void drain_act(uint32_t taddr, uint8_t* staging, int lane, const KeptActs& kept, KeptBlock& next,
+                                          const ActOutputs& out, int row0, int row_end, int col0, int n_dim, int c_begin,
+                                          int c_end, int rcap) {
+#pragma unroll 1
+  for (int c0 = c_begin; c0 < c_end; c0 += 32) {
+    const KeptBlock cur = next;
+    if (c0 + 32 < c_end) load_block(next, kept, row0 + lane, row_end, col0 + c0 + 32, n_dim, rcap);
+    uint32_t acc[32];
+    tmem_ld32(taddr + c0, acc);
+    tmem_ld_wait();
+    const float gs = act8::scale_of(cur.gs), us = act8::scale_of(cur.us);
+    const uint32_t gw[8] = {cur.g[0].x, cur.g[0].y, cur.g[0].z, cur.g[0].w, cur.g[1].x, cur.g[1].y, cur.g[1].z, cur.g[1].w};
+    const uint32_t uw[8] = {cur.u[0].x, cur.u[0].y, cur.u[0].z, cur.u[0].w, cur.u[1].x, cur.u[1].y, cur.u[1].z, cur.u[1].w};
+    uint32_t dgate[16], dup[16], h[16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) act_gradient(gw[i], uw[i], gs, us, acc + 4 * i, dgate + 2 * i, dup + 2 * i, h + 2 * i);
+    store_chunk(dgate, staging, lane, out.dgate, row0, row_end, col0 + c0, n_dim);
+    store_chunk(dup, staging, lane, out.dup, row0, row_end, col0 + c0, n_dim);
+    store_chunk(h, staging, lane, out.h, row0, row_end, col0 + c0, n_dim);
+  }
+}
+
+// Epilogue of (2) and (3): accumulator -> bf16 -> global.  kZero: the sum has no terms.
+template <bool kZero>
+__device__ __forceinline__ void drain_plain(uint32_t taddr, uint8_t* staging, int lane, __nv_bfloat16* out, int row0,
+                                            int row_end, int col0, int n_dim, int c_begin, int c_end) {
+#pragma unroll 1
+  for (int c0 = c_begin; c0 < c_end; c0 += 32) {
+    uint32_t o[16];
+    if constexpr (kZero) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[i] = 0;
+    } else {
+      uint32_t a[32];
+      tmem_ld32(taddr + c0, a);
+      tmem_ld_wait();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[i] = pack_bf16(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1]));
+    }
+    store_chunk(o, staging, lane, out, row0, row_end, col0 + c0, n_dim);
+  }
+}
+
+// The barriers behind the ring, and what else the roles share.
+template <class Cfg>
+struct Bars {
+  uint64_t *full, *empty, *acc_full, *acc_empty;
+  uint32_t* tmem_slot;
+  volatile int* abort_flag;
+  __device__ explicit Bars(uint8_t* at) {
+    full = reinterpret_cast<uint64_t*>(at);         // [kStages] TMA -> MMA
+    empty = full + Cfg::kStages;                    // [kStages] MMA -> TMA
+    acc_full = empty + Cfg::kStages;                // [kAccs]   MMA -> epilogue
+    acc_empty = acc_full + Cfg::kAccs;              // [kAccs]   epilogue -> MMA
+    tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + Cfg::kAccs);
+    abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  }
+  __device__ void init() const {
+    for (int i = 0; i < Cfg::kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < Cfg::kAccs; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], Cfg::kEpiWarps); }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+};
+
+// let copies and MMAs that are still in flight end before the CTA retires
+__device__ __forceinline__ void linger() {
+  for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+}
+
+// ------------------------------------------------------------------------------------------------ (1) and (2)
+// C[rows, n_dim] = sum over `pairs` of A_p[rows, k_dim] B_p[e][k_dim, n_dim]; A K-major, B MN-major.
+// kAct: one pair (dyp, W2) and the activation's gradient as epilogue; else two pairs (dgate, W1), (dup, W3).
+template <bool kAct, class Cfg>
+__global__ void __launch_bounds__(Cfg::kThreads, Cfg::kCtasPerSm)
+data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_constant__ CUtensorMap tm_b0,
+                     const __grid_constant__ CUtensorMap tm_a1, const __grid_constant__ CUtensorMap tm_b1,
+                     const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert, int S, int E, int n_dim,
+                     int k_dim, int rcap, const KeptActs kept, const ActOutputs act_out, __nv_bfloat16* __restrict__ out,
+                     int32_t* __restrict__ status) {
+  constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs, kThreads = Cfg::kThreads;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* stage_mem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  Tables& tb = *reinterpret_cast<Tables*>(stage_mem + (size_t)kStages * kStageBytes);
+  const Bars<Cfg> bar(stage_mem + (size_t)kStages * kStageBytes + sizeof(Tables));
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_tiles = (n_dim + BNACC - 1) / BNACC;
+  const int kb_per_pair = (k_dim + BK - 1) / BK;
+  const int num_kb = kAct ? kb_per_pair : 2 * kb_per_pair;
+
+  if (threadIdx.x == 0) {
+    bar.init();
+    prefetch_tensormap(&tm_a0);
+    prefetch_tensormap(&tm_b0);
+    if (!kAct) { prefetch_tensormap(&tm_a1); prefetch_tensormap(&tm_b1); }
+  }
+  if (warp == 1) {
+    tmem_alloc(bar.tmem_slot, Cfg::kTmemCols);
+    tmem_relinquish();
+  }
+  build_tables<kThreads>(tb, slot_row_off, slot_expert, S, E, n_tiles, rcap, status);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *bar.tmem_slot;
+  const int total_tiles = tb.tile_base[kMaxS];
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
+        const TileCoord tc = decode_tile(tb, slot_row_off, slot_expert, S, tile, n_tiles);
+        const int nb0 = tc.n_tile * BNACC;
+        for (int kb = 0; kb < num_kb; ++kb) {
+          if (!mbar_wait(&bar.empty[stage], phase ^ 1u, bar.abort_flag)) { ok = false; break; }
+          uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
+          mbar_arrive_expect_tx(&bar.full[stage], kStageBytes);
+          const bool second = !kAct && kb >= kb_per_pair;
+          const int k0 = (second ? kb - kb_per_pair : kb) * BK;
+          const CUtensorMap* ta = second ? &tm_a1 : &tm_a0;
+          const CUtensorMap* tbm = second ? &tm_b1 : &tm_b0;
+          tma_load_2d(sa, ta, &bar.full[stage], k0, tc.m0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            tma_load_3d(sa + kABytes + i * kBoxBytes, tbm, &bar.full[stage], nb0 + 64 * i, k0, tc.expert);
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (!ok) linger();
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t idesc = idesc_bf16_f32(BM, BNACC, false, true);
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = true;
+      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
+        if (!mbar_wait(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag)) { ok = false; break; }
+        tc_fence_after_sync();
+        const uint32_t d_tmem = tmem_base + (uint32_t)acc * BNACC;
+        for (int kb = 0; kb < num_kb; ++kb) {
+          if (!mbar_wait(&bar.full[stage], phase, bar.abort_flag)) { ok = false; break; }
+          tc_fence_after_sync();
+          const uint32_t sa = smem_u32(stage_mem + (size_t)stage * kStageBytes);
+          const uint64_t da = smem_desc_k<kRowBytes>(sa);
+          const uint64_t db = smem_desc_mn(sa + kABytes, kBoxBytes);
+#pragma unroll
+          for (int k = 0; k < BK / 16; ++k)      // A advances 32 bytes along its rows, B 16 rows of 128 bytes
+            mma_bf16(d_tmem, da + (uint64_t)(k * 2), db + (uint64_t)(k * 128), idesc, (kb | k) != 0);
+          mma_commit(&bar.empty[stage]);
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        mma_commit(&bar.acc_full[acc]);
+        if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+      }
+      if (!ok) linger();
+    }
+  } else {
+    const int quarter = warp & 3;                 // TMEM lanes this warp may read
+    constexpr int kShare = BNACC / (Cfg::kEpiWarps / 4);
+    const int c_begin = ((warp - 2) >> 2) * kShare;
+    uint8_t* staging = stage_mem + (size_t)kStages * kStageBytes + sizeof(Tables) + 256 + (warp - 2) * kStagingBytesPerWarp;
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    bool ok = true;
+    for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
+      const TileCoord tc = decode_tile(tb, slot_row_off, slot_expert, S, tile, n_tiles);
+      const int row0 = tc.m0 + quarter * 32, col0 = tc.n_tile * BNACC;
+      [[maybe_unused]] KeptBlock block;
+      if constexpr (kAct) load_block(block, kept, row0 + lane, tc.row_end, col0 + c_begin, n_dim, rcap);
+      if (!mbar_wait(&bar.acc_full[acc], acc_phase, bar.abort_flag, 256)) { ok = false; break; }
+      tc_fence_after_sync();
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * BNACC;
+      if constexpr (kAct)
+        drain_act(taddr, staging, lane, kept, block, act_out, row0, tc.row_end, col0, n_dim, c_begin, c_begin + kShare, rcap);
+      else
+        drain_plain<false>(taddr, staging, lane, out, row0, tc.row_end, col0, n_dim, c_begin, c_begin + kShare);
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bar.acc_empty[acc]);
+      if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+    }
+  }
+
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (threadIdx.x == 0 && *bar.abort_flag) moegps_report(status, MOEGPS_ERR_TIMEOUT, (int)blockIdx.x);
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, Cfg::kTmemCols);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ (3)
+// Occupied rows of every slot: first row and count.  The padding that dispatch leaves at a slot's end (row_pair < 0)
+// holds no token and must not enter the sums, whatever its memory holds.
+struct SlotRows {
+  int2 ext[kMaxS];
+};
+
+// Tiles are blocks of BM x BNACC elements of one weight gradient.  Per expert: dW1, dW3 (F x D each), then dW2 (D x F).
+// Inside one gradient the order runs over bands of kBand row tiles, column by column: tiles in flight at the same time
+// form a near-square patch of the gradient, so the operand columns they read are shared in L2.
+constexpr int kBand = 12;
+struct WTile {
+  int expert, which, m0, n0, m_dim, n_dim;
+};
+struct WGeom {
+  int F, D, per1, per2;              // tiles of dW1 (and dW3), of dW2
+  __host__ __device__ WGeom(int F_, int D_) : F(F_), D(D_) {
+    per1 = ((F + BM - 1) / BM) * ((D + BNACC - 1) / BNACC);
+    per2 = ((D + BM - 1) / BM) * ((F + BNACC - 1) / BNACC);
+  }
+  __host__ __device__ int per_expert() const { return 2 * per1 + per2; }
+};
+__device__ __forceinline__ WTile decode_wtile(const WGeom& g, int tile) {
+  WTile t;
+  t.expert = tile / g.per_expert();
+  int q = tile - t.expert * g.per_expert();
+  t.which = q < g.per1 ? 0 : q < 2 * g.per1 ? 1 : 2;
+  q -= t.which * g.per1;
+  t.m_dim = t.which == 2 ? g.D : g.F;
+  t.n_dim = t.which == 2 ? g.F : g.D;
+  const int mt = (t.m_dim + BM - 1) / BM, nt = (t.n_dim + BNACC - 1) / BNACC;
+  const int band = q / (kBand * nt);
+  q -= band * kBand * nt;
+  const int high = min(kBand, mt - band * kBand);
+  t.n0 = q / high * BNACC;
+  t.m0 = (band * kBand + q % high) * BM;
+  return t;
+}
+
+// occupied rows of expert e's slots [first, last)
+__device__ __forceinline__ int rows_of(const SlotRows& sr, int first, int last) {
+  int n = 0;
+  for (int s = first; s < last; ++s) n += sr.ext[s].y;
+  return n;
+}
+
+template <class Cfg>
+__global__ void __launch_bounds__(Cfg::kThreads, Cfg::kCtasPerSm)
+weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __grid_constant__ CUtensorMap tm_dup,
+                       const __grid_constant__ CUtensorMap tm_dyp, const __grid_constant__ CUtensorMap tm_xp,
+                       const __grid_constant__ CUtensorMap tm_h, const int32_t* __restrict__ slot_row_off,
+                       const int32_t* __restrict__ slot_off, const int32_t* __restrict__ row_pair, int S, int E, int F, int D,
+                       int rcap, __nv_bfloat16* __restrict__ dw_gate, __nv_bfloat16* __restrict__ dw_up,
+                       __nv_bfloat16* __restrict__ dw_down, int32_t* __restrict__ status) {
+  constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs, kThreads = Cfg::kThreads;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ int32_t s_slot_off[256 + 1];
+  uint8_t* stage_mem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  SlotRows& sr = *reinterpret_cast<SlotRows*>(stage_mem + (size_t)kStages * kStageBytes);
+  const Bars<Cfg> bar(stage_mem + (size_t)kStages * kStageBytes + sizeof(SlotRows));
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const WGeom geom(F, D);
+  const int total_tiles = E * geom.per_expert();
+
+  if (threadIdx.x == 0) {
+    bar.init();
+    prefetch_tensormap(&tm_dgate);
+    prefetch_tensormap(&tm_dup);
+    prefetch_tensormap(&tm_dyp);
+    prefetch_tensormap(&tm_xp);
+    prefetch_tensormap(&tm_h);
+  }
+  if (warp == 1) {
+    tmem_alloc(bar.tmem_slot, Cfg::kTmemCols);
+    tmem_relinquish();
+  }
+  for (int s = threadIdx.x; s < S; s += kThreads) {
+    const int lo = slot_row_off[s], hi = slot_row_off[s + 1];
+    int n = 0;
+    if (lo < 0 || hi < lo || hi > rcap) {
+      if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
+    } else {
+      int a = lo, b = hi;                          // first padding row: occupied rows come first
+      while (a < b) {
+        const int mid = (a + b) >> 1;
+        if (row_pair[mid] >= 0) a = mid + 1; else b = mid;
+      }
+      n = a - lo;
+    }
+    sr.ext[s] = make_int2(lo, n);
+  }
+  for (int e = threadIdx.x; e <= E; e += kThreads) {
+    int v = slot_off[e];
+    if (v < 0 || v > S) {
+      if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, e);
+      v = 0;
+    }
+    s_slot_off[e] = v;
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *bar.tmem_slot;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
+        const WTile t = decode_wtile(geom, tile);
+        const CUtensorMap* ta = t.which == 0 ? &tm_dgate : t.which == 1 ? &tm_dup : &tm_dyp;
+        const CUtensorMap* tbm = t.which == 2 ? &tm_h : &tm_xp;
+        const int last = s_slot_off[t.expert + 1];
+        for (int s = s_slot_off[t.expert]; ok && s < last; ++s) {
+          const int2 ext = sr.ext[s];
+          for (int r = 0; r < ext.y; r += BK) {
+            if (!mbar_wait(&bar.empty[stage], phase ^ 1u, bar.abort_flag)) { ok = false; break; }
+            uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
+            mbar_arrive_expect_tx(&bar.full[stage], kStageBytes);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) tma_load_2d(sa + i * kBoxBytes, ta, &bar.full[stage], t.m0 + 64 * i, ext.x + r);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              tma_load_2d(sa + kABytes + i * kBoxBytes, tbm, &bar.full[stage], t.n0 + 64 * i, ext.x + r);
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+      if (!ok) linger();
+    }
+  } else if (warp == 1) {
+    // The whole warp walks the K blocks: lane 0 waits and issues; at the last block of a slot the other lanes join it
+    // to blank the rows behind the slot's end that the last MMA would read (at most 15, of both operands, since
+    // 0 * NaN is NaN).  A failed wait leaves the loops at the next tile, for all lanes together.
+    constexpr uint32_t idesc = idesc_bf16_f32(BM, BNACC, true, true);
+    int stage = 0, acc = 0;
+    uint32_t phase = 0, acc_phase = 0;
+    bool ok = true;
+    for (int tile = blockIdx.x; tile < total_tiles; tile += gridDim.x) {
+      const WTile t = decode_wtile(geom, tile);
+      const int first = s_slot_off[t.expert], last = s_slot_off[t.expert + 1];
+      if (rows_of(sr, first, last) == 0) continue;
+      if (lane == 0) ok = mbar_wait(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag);
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      if (!ok) break;
+      tc_fence_after_sync();
+      const uint32_t d_tmem = tmem_base + (uint32_t)acc * BNACC;
+      uint32_t accumulate = 0;
+      for (int s = first; s < last; ++s) {
+        const int n = sr.ext[s].y;
+        for (int r = 0; r < n; r += BK) {
+          const int valid = min(BK, n - r), steps = (valid + 15) >> 4;
+          if (valid & 15) {
+            __syncwarp();                          // lane 0 has consumed the stages before: the phase is unambiguous
+            const bool here = ok && mbar_wait(&bar.full[stage], phase, bar.abort_flag);
+            ok = __all_sync(0xffffffffu, here);
+            if (ok) {
+              uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
+              const int blank = 16 * steps - valid;         // rows valid .. 16 steps - 1, eight 16-byte words each
+              for (int i = lane; i < 6 * 8 * blank; i += 32) {
+                const int word = i & 7, row = valid + (i >> 3) % blank, box = (i >> 3) / blank;
+                *reinterpret_cast<uint4*>(sa + box * kBoxBytes + row * kRowBytes + word * 16) = make_uint4(0, 0, 0, 0);
+              }
+              fence_proxy_async();
+            }
+            __syncwarp();
+          }
+          if (lane == 0 && ok) {
+            ok = mbar_wait(&bar.full[stage], phase, bar.abort_flag);
+            if (ok) {
+              tc_fence_after_sync();
+              const uint32_t sa = smem_u32(stage_mem + (size_t)stage * kStageBytes);
+              const uint64_t da = smem_desc_mn(sa, kBoxBytes);
+              const uint64_t db = smem_desc_mn(sa + kABytes, kBoxBytes);
+              for (int k = 0; k < steps; ++k) {
+                mma_bf16(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
+                accumulate = 1;
+              }
+              mma_commit(&bar.empty[stage]);
+            }
+          }
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      if (!ok) break;
+      if (lane == 0) mma_commit(&bar.acc_full[acc]);
+      if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+    }
+    if (!ok && lane == 0) linger();
+  } else {
+    const int quarter = warp & 3;
+    constexpr int kShare = BNACC / (Cfg::kEpiWarps / 4);
+    const int c_begin = ((warp - 2) >> 2) * kShare;
+    uint8_t* staging = stage_mem + (size_t)kStages * kStageBytes + sizeof(SlotRows) + 256 + (warp - 2) * kStagingBytesPerWarp;
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    for (int tile = blockIdx.x; tile < total_tiles; tile += gridDim.x) {
+      const WTile t = decode_wtile(geom, tile);
+      __nv_bfloat16* out = (t.which == 0 ? dw_gate : t.which == 1 ? dw_up : dw_down) + (size_t)t.expert * t.m_dim * t.n_dim;
+      const int row0 = t.m0 + quarter * 32;
+      if (rows_of(sr, s_slot_off[t.expert], s_slot_off[t.expert + 1]) == 0) {      // no token chose this expert
+        drain_plain<true>(0, staging, lane, out, row0, t.m_dim, t.n0, t.n_dim, c_begin, c_begin + kShare);
+        continue;
+      }
+      if (!mbar_wait(&bar.acc_full[acc], acc_phase, bar.abort_flag, 256)) break;
+      tc_fence_after_sync();
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * BNACC;
+      drain_plain<false>(taddr, staging, lane, out, row0, t.m_dim, t.n0, t.n_dim, c_begin, c_begin + kShare);
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bar.acc_empty[acc]);
+      if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+    }
+  }
+
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (threadIdx.x == 0 && *bar.abort_flag) moegps_report(status, MOEGPS_ERR_TIMEOUT, (int)blockIdx.x);
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, Cfg::kTmemCols);
+  }
+}
+
+template <class Cfg>
+constexpr size_t weight_smem_bytes() {
+  return 1024 + (size_t)Cfg::kStages * kStageBytes + sizeof(SlotRows) + 256 + (size_t)Cfg::kEpiWarps * kStagingBytesPerWarp;
+}
+static_assert(weight_smem_bytes<WideCfg>() + 257 * 4 <= 227 * 1024, "one CTA per SM");
+
+int tmap_failed(moegps_ctx* ctx) {
+  ctx->last_cuda_error = (int)cudaErrorInvalidValue;
+  return MOEGPS_ERR_CUDA;
+}
+
+template <bool kAct>
+int launch_data_gradient(moegps_ctx* ctx, const CUtensorMap& a0, const CUtensorMap& b0, const CUtensorMap& a1,
+                         const CUtensorMap& b1, const int32_t* slot_row_off, const int32_t* slot_expert, int n_dim, int k_dim,
+                         const KeptActs& kept, const ActOutputs& act_out, void* out, cudaStream_t st) {
+  const moegps_shape_t& s = ctx->shape;
+  constexpr size_t smem = smem_bytes_of<WideCfg>();
+  bool& done = ctx->ffn_backward_attr_done[kAct ? 0 : 1];
+  if (!done) {
+    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(data_gradient_kernel<kAct, WideCfg>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                              (int)smem));
+    done = true;
+  }
+  data_gradient_kernel<kAct, WideCfg><<<ctx->sm_count, WideCfg::kThreads, smem, st>>>(
+      a0, b0, a1, b1, slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim, (int)moegps_rcap_of(s), kept, act_out,
+      static_cast<__nv_bfloat16*>(out), ctx->d_status);
+  MOEGPS_AFTER_LAUNCH(ctx);
+  return MOEGPS_OK;
+}
+
+}  // namespace
+
+int moegps_launch_ffn_backward_act(moegps_ctx* ctx, const void* dyp, const int32_t* slot_row_off, const int32_t* slot_expert,
+                                   const void* w_down, const void* gate8, const void* up8, const void* gate_scale,
+                                   const void* up_scale, void* dgate, void* dup, void* h_ws, cudaStream_t st) {
+  const moegps_shape_t& s = ctx->shape;
+  CUtensorMap a, b;
+  if (!(moegps_make_tmap_2d(&a, dyp, (uint64_t)moegps_rcap_of(s), s.D, BM, BK) &&
+        moegps_make_tmap_3d(&b, w_down, s.E, s.D, s.F, BK, 64)))
+    return tmap_failed(ctx);
+  const KeptActs kept = {static_cast<const uint8_t*>(gate8), static_cast<const uint8_t*>(up8),
+                         static_cast<const uint8_t*>(gate_scale), static_cast<const uint8_t*>(up_scale)};
+  const ActOutputs out = {static_cast<__nv_bfloat16*>(dgate), static_cast<__nv_bfloat16*>(dup),
+                          static_cast<__nv_bfloat16*>(h_ws)};
+  return launch_data_gradient<true>(ctx, a, b, a, b, slot_row_off, slot_expert, s.F, s.D, kept, out, nullptr, st);
+}
+
+int moegps_launch_ffn_backward_input(moegps_ctx* ctx, const void* dgate, const void* dup, const int32_t* slot_row_off,
+                                     const int32_t* slot_expert, const void* w_gate, const void* w_up, void* dxp,
+                                     cudaStream_t st) {
+  const moegps_shape_t& s = ctx->shape;
+  const uint64_t rcap = (uint64_t)moegps_rcap_of(s);
+  CUtensorMap a0, b0, a1, b1;
+  if (!(moegps_make_tmap_2d(&a0, dgate, rcap, s.F, BM, BK) && moegps_make_tmap_2d(&a1, dup, rcap, s.F, BM, BK) &&
+        moegps_make_tmap_3d(&b0, w_gate, s.E, s.F, s.D, BK, 64) && moegps_make_tmap_3d(&b1, w_up, s.E, s.F, s.D, BK, 64)))
+    return tmap_failed(ctx);
+  return launch_data_gradient<false>(ctx, a0, b0, a1, b1, slot_row_off, slot_expert, s.D, s.F, KeptActs{}, ActOutputs{}, dxp,
+                                     st);
+}
+
+int moegps_launch_ffn_backward_weights(moegps_ctx* ctx, const void* dyp, const void* xp, const void* dgate, const void* dup,
+                                       const void* h_ws, const int32_t* slot_row_off, const int32_t* slot_off,
+                                       const int32_t* row_pair, void* dw_gate, void* dw_up, void* dw_down, cudaStream_t st) {
+  const moegps_shape_t& s = ctx->shape;
+  const uint64_t rcap = (uint64_t)moegps_rcap_of(s);
+  CUtensorMap t_dgate, t_dup, t_dyp, t_xp, t_h;
+  if (!(moegps_make_tmap_2d(&t_dgate, dgate, rcap, s.F, BK, 64) && moegps_make_tmap_2d(&t_dup, dup, rcap, s.F, BK, 64) &&
+        moegps_make_tmap_2d(&t_dyp, dyp, rcap, s.D, BK, 64) && moegps_make_tmap_2d(&t_xp, xp, rcap, s.D, BK, 64) &&
+        moegps_make_tmap_2d(&t_h, h_ws, rcap, s.F, BK, 64)))
+    return tmap_failed(ctx);
+  constexpr size_t smem = weight_smem_bytes<WideCfg>();
+  if (!ctx->ffn_backward_attr_done[2]) {
+    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(weight_gradient_kernel<WideCfg>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                              (int)smem));
+    ctx->ffn_backward_attr_done[2] = true;
+  }
+  weight_gradient_kernel<WideCfg><<<ctx->sm_count, WideCfg::kThreads, smem, st>>>(
+      t_dgate, t_dup, t_dyp, t_xp, t_h, slot_row_off, slot_off, row_pair, s.S, s.E, s.F, s.D, (int)rcap,
+      static_cast<__nv_bfloat16*>(dw_gate), static_cast<__nv_bfloat16*>(dw_up), static_cast<__nv_bfloat16*>(dw_down),
+      ctx->d_status);
+  MOEGPS_AFTER_LAUNCH(ctx);
+  return MOEGPS_OK;
+}

@@ -66,6 +66,9 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
   }
 }
 
+// Makes this thread's shared-memory writes visible to the asynchronous units (TMA, tensor core).
+__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // ----------------------------------------------------------------------------------- TMA
 __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap* tm) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory");
@@ -128,11 +131,27 @@ __device__ __forceinline__ uint64_t smem_desc_k(uint32_t smem_addr) {
 }
 __device__ __forceinline__ uint64_t smem_desc_k_sw128(uint32_t smem_addr) { return smem_desc_k<128>(smem_addr); }
 
-// Instruction descriptor: bf16 x bf16 -> fp32, both operands K-major, tile M x N.
-__host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N) {
+// The same for an operand whose M (or N) index is the contiguous one ("MN-major"): blocks of 64 MN elements
+// (128 bytes, one swizzle span) x BK rows of K, as a TMA box of 64 columns x BK rows leaves them.  Eight K rows are
+// 1024 bytes apart (stride offset), the next 64 MN elements `block_bytes` further (leading offset).  An MMA's 16 K
+// rows are 2048 bytes, so advancing along K adds 128 to the start-address field.
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t smem_addr, uint32_t block_bytes) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr & 0x3ffffu) >> 4);
+  d |= (uint64_t)(block_bytes >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+// Instruction descriptor: bf16 x bf16 -> fp32, tile M x N; operands K-major unless said otherwise.
+__host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N, bool a_mn_major = false, bool b_mn_major = false) {
   return (1u << 4)                       // D format: fp32
          | (1u << 7)                     // A format: bf16
          | (1u << 10)                    // B format: bf16
+         | ((a_mn_major ? 1u : 0u) << 15)
+         | ((b_mn_major ? 1u : 0u) << 16)
          | ((uint32_t)(N >> 3) << 17)    // N / 8
          | ((uint32_t)(M >> 4) << 24);   // M / 16
 }
