@@ -144,6 +144,13 @@ def _lib():
 
 
 def _ptr(t, dtype, shape, name, allow_none=False):
+    """Device address of a tensor that is what the call needs, else an exception that says what is wrong.  A call's
+    tensors are checked one by one in front of a launch of a few microseconds, so the usual case is one expression."""
+    try:
+        if t.is_cuda and t.dtype is dtype and (shape is None or t.shape == shape) and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
     if t is None:
         if allow_none:
             return None
@@ -154,17 +161,16 @@ def _ptr(t, dtype, shape, name, allow_none=False):
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    return ctypes.c_void_p(t.data_ptr())
+    raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
 def _stream(stream):
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the handle alone: torch.cuda.current_stream() builds an object around it
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, torch.cuda.Stream):
-        return ctypes.c_void_p(stream.cuda_stream)
-    return ctypes.c_void_p(int(stream))
+        return stream.cuda_stream
+    return int(stream)
 
 
 class Context:
@@ -175,6 +181,14 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("moegps needs a CUDA device (sm_100a); there is no CPU path")
         self.shape = shape
+        # shapes of the training step's tensors
+        rows = shape.Rcap
+        self._td, self._tk, self._ed = (shape.T, shape.D), (shape.T, shape.K), (shape.E, shape.D)
+        self._rows, self._rows_d, self._rows_f = (rows,), (rows, shape.D), (rows, shape.F)
+        self._codes, self._scales = (rows, shape.P), (shape.P // 32, rows)
+        self._efd, self._edf = (shape.E, shape.F, shape.D), (shape.E, shape.D, shape.F)
+        self._s, self._s1, self._e, self._e1 = (shape.S,), (shape.S + 1,), (shape.E,), (shape.E + 1,)
+        self._route_backward_bytes = route_backward_workspace_bytes(shape)
         self.device = torch.cuda.current_device() if device is None else int(device)
         self._h = ctypes.c_void_p()
         cs = shape.c_struct()
@@ -384,110 +398,94 @@ class Context:
     # -- the training step --------------------------------------------------------------------
     def expert_ffn_gate_up_save(self, xp, slot_row_off, slot_expert, w_gate, w_up, h_ws, gate8, up8, gate_scale, up_scale,
                                 stream=None):
-        s = self.shape
-        codes, scales = (s.Rcap, s.P), (s.P // 32, s.Rcap)
+        bf16, i32, u8 = torch.bfloat16, torch.int32, torch.uint8
         self._check(_lib().moegps_expert_ffn_gate_up_save(
-            self._h, _ptr(xp, torch.bfloat16, (s.Rcap, s.D), "xp"),
-            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
-            _ptr(slot_expert, torch.int32, (s.S,), "slot_expert"),
-            _ptr(w_gate, torch.bfloat16, (s.E, s.F, s.D), "w_gate"),
-            _ptr(w_up, torch.bfloat16, (s.E, s.F, s.D), "w_up"),
-            _ptr(h_ws, torch.bfloat16, (s.Rcap, s.F), "h_ws"),
-            _ptr(gate8, torch.uint8, codes, "gate8"), _ptr(up8, torch.uint8, codes, "up8"),
-            _ptr(gate_scale, torch.uint8, scales, "gate_scale"), _ptr(up_scale, torch.uint8, scales, "up_scale"),
+            self._h, _ptr(xp, bf16, self._rows_d, "xp"), _ptr(slot_row_off, i32, self._s1, "slot_row_off"),
+            _ptr(slot_expert, i32, self._s, "slot_expert"), _ptr(w_gate, bf16, self._efd, "w_gate"),
+            _ptr(w_up, bf16, self._efd, "w_up"), _ptr(h_ws, bf16, self._rows_f, "h_ws"),
+            _ptr(gate8, u8, self._codes, "gate8"), _ptr(up8, u8, self._codes, "up8"),
+            _ptr(gate_scale, u8, self._scales, "gate_scale"), _ptr(up_scale, u8, self._scales, "up_scale"),
             _stream(stream)), "moegps_expert_ffn_gate_up_save")
 
     def expert_ffn_backward(self, dyp, xp, slot_row_off, slot_off, slot_expert, row_pair, w_gate, w_up, w_down, gate8, up8,
                             gate_scale, up_scale, dgate, dup, h_ws, dxp, dw_gate, dw_up, dw_down, stream=None):
-        s = self.shape
-        rows_d, rows_f = (s.Rcap, s.D), (s.Rcap, s.F)
-        codes, scales = (s.Rcap, s.P), (s.P // 32, s.Rcap)
-        up, down = (s.E, s.F, s.D), (s.E, s.D, s.F)
+        bf16, i32, u8 = torch.bfloat16, torch.int32, torch.uint8
         self._check(_lib().moegps_expert_ffn_backward(
-            self._h, _ptr(dyp, torch.bfloat16, rows_d, "dyp"), _ptr(xp, torch.bfloat16, rows_d, "xp"),
-            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
-            _ptr(slot_off, torch.int32, (s.E + 1,), "slot_off"),
-            _ptr(slot_expert, torch.int32, (s.S,), "slot_expert"),
-            _ptr(row_pair, torch.int32, (s.Rcap,), "row_pair"),
-            _ptr(w_gate, torch.bfloat16, up, "w_gate"), _ptr(w_up, torch.bfloat16, up, "w_up"),
-            _ptr(w_down, torch.bfloat16, down, "w_down"),
-            _ptr(gate8, torch.uint8, codes, "gate8"), _ptr(up8, torch.uint8, codes, "up8"),
-            _ptr(gate_scale, torch.uint8, scales, "gate_scale"), _ptr(up_scale, torch.uint8, scales, "up_scale"),
-            _ptr(dgate, torch.bfloat16, rows_f, "dgate"), _ptr(dup, torch.bfloat16, rows_f, "dup"),
-            _ptr(h_ws, torch.bfloat16, rows_f, "h_ws"), _ptr(dxp, torch.bfloat16, rows_d, "dxp"),
-            _ptr(dw_gate, torch.bfloat16, up, "dw_gate"), _ptr(dw_up, torch.bfloat16, up, "dw_up"),
-            _ptr(dw_down, torch.bfloat16, down, "dw_down"), _stream(stream)), "moegps_expert_ffn_backward")
+            self._h, _ptr(dyp, bf16, self._rows_d, "dyp"), _ptr(xp, bf16, self._rows_d, "xp"),
+            _ptr(slot_row_off, i32, self._s1, "slot_row_off"), _ptr(slot_off, i32, self._e1, "slot_off"),
+            _ptr(slot_expert, i32, self._s, "slot_expert"), _ptr(row_pair, i32, self._rows, "row_pair"),
+            _ptr(w_gate, bf16, self._efd, "w_gate"), _ptr(w_up, bf16, self._efd, "w_up"),
+            _ptr(w_down, bf16, self._edf, "w_down"), _ptr(gate8, u8, self._codes, "gate8"),
+            _ptr(up8, u8, self._codes, "up8"), _ptr(gate_scale, u8, self._scales, "gate_scale"),
+            _ptr(up_scale, u8, self._scales, "up_scale"), _ptr(dgate, bf16, self._rows_f, "dgate"),
+            _ptr(dup, bf16, self._rows_f, "dup"), _ptr(h_ws, bf16, self._rows_f, "h_ws"),
+            _ptr(dxp, bf16, self._rows_d, "dxp"), _ptr(dw_gate, bf16, self._efd, "dw_gate"),
+            _ptr(dw_up, bf16, self._efd, "dw_up"), _ptr(dw_down, bf16, self._edf, "dw_down"),
+            _stream(stream)), "moegps_expert_ffn_backward")
 
     def expert_ffn_backward_act(self, dyp, slot_row_off, slot_expert, w_down, gate8, up8, gate_scale, up_scale, dgate, dup,
                                 h_ws, stream=None):
-        s = self.shape
-        codes, scales = (s.Rcap, s.P), (s.P // 32, s.Rcap)
+        bf16, i32, u8 = torch.bfloat16, torch.int32, torch.uint8
         self._check(_lib().moegps_expert_ffn_backward_act(
-            self._h, _ptr(dyp, torch.bfloat16, (s.Rcap, s.D), "dyp"),
-            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
-            _ptr(slot_expert, torch.int32, (s.S,), "slot_expert"),
-            _ptr(w_down, torch.bfloat16, (s.E, s.D, s.F), "w_down"),
-            _ptr(gate8, torch.uint8, codes, "gate8"), _ptr(up8, torch.uint8, codes, "up8"),
-            _ptr(gate_scale, torch.uint8, scales, "gate_scale"), _ptr(up_scale, torch.uint8, scales, "up_scale"),
-            _ptr(dgate, torch.bfloat16, (s.Rcap, s.F), "dgate"), _ptr(dup, torch.bfloat16, (s.Rcap, s.F), "dup"),
-            _ptr(h_ws, torch.bfloat16, (s.Rcap, s.F), "h_ws"), _stream(stream)), "moegps_expert_ffn_backward_act")
+            self._h, _ptr(dyp, bf16, self._rows_d, "dyp"), _ptr(slot_row_off, i32, self._s1, "slot_row_off"),
+            _ptr(slot_expert, i32, self._s, "slot_expert"), _ptr(w_down, bf16, self._edf, "w_down"),
+            _ptr(gate8, u8, self._codes, "gate8"), _ptr(up8, u8, self._codes, "up8"),
+            _ptr(gate_scale, u8, self._scales, "gate_scale"), _ptr(up_scale, u8, self._scales, "up_scale"),
+            _ptr(dgate, bf16, self._rows_f, "dgate"), _ptr(dup, bf16, self._rows_f, "dup"),
+            _ptr(h_ws, bf16, self._rows_f, "h_ws"), _stream(stream)), "moegps_expert_ffn_backward_act")
 
     def expert_ffn_backward_input(self, dgate, dup, slot_row_off, slot_expert, w_gate, w_up, dxp, stream=None):
-        s = self.shape
+        bf16, i32 = torch.bfloat16, torch.int32
         self._check(_lib().moegps_expert_ffn_backward_input(
-            self._h, _ptr(dgate, torch.bfloat16, (s.Rcap, s.F), "dgate"), _ptr(dup, torch.bfloat16, (s.Rcap, s.F), "dup"),
-            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
-            _ptr(slot_expert, torch.int32, (s.S,), "slot_expert"),
-            _ptr(w_gate, torch.bfloat16, (s.E, s.F, s.D), "w_gate"), _ptr(w_up, torch.bfloat16, (s.E, s.F, s.D), "w_up"),
-            _ptr(dxp, torch.bfloat16, (s.Rcap, s.D), "dxp"), _stream(stream)), "moegps_expert_ffn_backward_input")
+            self._h, _ptr(dgate, bf16, self._rows_f, "dgate"), _ptr(dup, bf16, self._rows_f, "dup"),
+            _ptr(slot_row_off, i32, self._s1, "slot_row_off"), _ptr(slot_expert, i32, self._s, "slot_expert"),
+            _ptr(w_gate, bf16, self._efd, "w_gate"), _ptr(w_up, bf16, self._efd, "w_up"),
+            _ptr(dxp, bf16, self._rows_d, "dxp"), _stream(stream)), "moegps_expert_ffn_backward_input")
 
     def expert_ffn_backward_weights(self, dyp, xp, dgate, dup, h_ws, slot_row_off, slot_off, row_pair, dw_gate, dw_up, dw_down,
                                     stream=None):
-        s = self.shape
+        bf16, i32 = torch.bfloat16, torch.int32
         self._check(_lib().moegps_expert_ffn_backward_weights(
-            self._h, _ptr(dyp, torch.bfloat16, (s.Rcap, s.D), "dyp"), _ptr(xp, torch.bfloat16, (s.Rcap, s.D), "xp"),
-            _ptr(dgate, torch.bfloat16, (s.Rcap, s.F), "dgate"), _ptr(dup, torch.bfloat16, (s.Rcap, s.F), "dup"),
-            _ptr(h_ws, torch.bfloat16, (s.Rcap, s.F), "h_ws"),
-            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
-            _ptr(slot_off, torch.int32, (s.E + 1,), "slot_off"), _ptr(row_pair, torch.int32, (s.Rcap,), "row_pair"),
-            _ptr(dw_gate, torch.bfloat16, (s.E, s.F, s.D), "dw_gate"), _ptr(dw_up, torch.bfloat16, (s.E, s.F, s.D), "dw_up"),
-            _ptr(dw_down, torch.bfloat16, (s.E, s.D, s.F), "dw_down"), _stream(stream)), "moegps_expert_ffn_backward_weights")
+            self._h, _ptr(dyp, bf16, self._rows_d, "dyp"), _ptr(xp, bf16, self._rows_d, "xp"),
+            _ptr(dgate, bf16, self._rows_f, "dgate"), _ptr(dup, bf16, self._rows_f, "dup"),
+            _ptr(h_ws, bf16, self._rows_f, "h_ws"), _ptr(slot_row_off, i32, self._s1, "slot_row_off"),
+            _ptr(slot_off, i32, self._e1, "slot_off"), _ptr(row_pair, i32, self._rows, "row_pair"),
+            _ptr(dw_gate, bf16, self._efd, "dw_gate"), _ptr(dw_up, bf16, self._efd, "dw_up"),
+            _ptr(dw_down, bf16, self._edf, "dw_down"), _stream(stream)), "moegps_expert_ffn_backward_weights")
 
     def combine_backward(self, dout, yp, pair_row, topk_w, dyp, dtopk_w, stream=None):
-        s = self.shape
+        bf16, f32 = torch.bfloat16, torch.float32
         self._check(_lib().moegps_combine_backward(
-            self._h, _ptr(dout, torch.bfloat16, (s.T, s.D), "dout"), _ptr(yp, torch.bfloat16, (s.Rcap, s.D), "yp"),
-            _ptr(pair_row, torch.int32, (s.T, s.K), "pair_row"), _ptr(topk_w, torch.float32, (s.T, s.K), "topk_w"),
-            _ptr(dyp, torch.bfloat16, (s.Rcap, s.D), "dyp"), _ptr(dtopk_w, torch.float32, (s.T, s.K), "dtopk_w"),
-            _stream(stream)), "moegps_combine_backward")
+            self._h, _ptr(dout, bf16, self._td, "dout"), _ptr(yp, bf16, self._rows_d, "yp"),
+            _ptr(pair_row, torch.int32, self._tk, "pair_row"), _ptr(topk_w, f32, self._tk, "topk_w"),
+            _ptr(dyp, bf16, self._rows_d, "dyp"), _ptr(dtopk_w, f32, self._tk, "dtopk_w"), _stream(stream)),
+            "moegps_combine_backward")
 
     def dispatch_backward(self, dxp, pair_row, topk_idx, dlogit, w_router, dx, stream=None):
         """dlogit None: without the router's part (topk_idx and w_router are not read)."""
-        s = self.shape
+        bf16, i32 = torch.bfloat16, torch.int32
         part = dlogit is not None
         self._check(_lib().moegps_dispatch_backward(
-            self._h, _ptr(dxp, torch.bfloat16, (s.Rcap, s.D), "dxp"), _ptr(pair_row, torch.int32, (s.T, s.K), "pair_row"),
-            _ptr(topk_idx, torch.int32, (s.T, s.K), "topk_idx") if part else None,
-            _ptr(dlogit, torch.float32, (s.T, s.K), "dlogit") if part else None,
-            _ptr(w_router, torch.bfloat16, (s.E, s.D), "w_router") if part else None,
-            _ptr(dx, torch.bfloat16, (s.T, s.D), "dx"), _stream(stream)), "moegps_dispatch_backward")
+            self._h, _ptr(dxp, bf16, self._rows_d, "dxp"), _ptr(pair_row, i32, self._tk, "pair_row"),
+            _ptr(topk_idx, i32, self._tk, "topk_idx") if part else None,
+            _ptr(dlogit, torch.float32, self._tk, "dlogit") if part else None,
+            _ptr(w_router, bf16, self._ed, "w_router") if part else None,
+            _ptr(dx, bf16, self._td, "dx"), _stream(stream)), "moegps_dispatch_backward")
 
     def route_backward(self, x, w_router, bias, topk_idx, topk_w, dtopk_w, slot_row_off, slot_off, row_pair, dlogit,
                        dw_router, dbias, workspace, stream=None):
-        s = self.shape
-        if workspace is None or workspace.numel() * workspace.element_size() < route_backward_workspace_bytes(s):
+        if workspace is None or workspace.numel() * workspace.element_size() < self._route_backward_bytes:
             raise MoegpsError(ERR_WORKSPACE_TOO_SMALL, "moegps_route_backward")
-        softmax = s.gate_mode == 0                       # then w_router, bias and topk_idx are not read
+        bf16, i32, f32 = torch.bfloat16, torch.int32, torch.float32
+        softmax = self.shape.gate_mode == 0              # then w_router, bias and topk_idx are not read
         self._check(_lib().moegps_route_backward(
-            self._h, _ptr(x, torch.bfloat16, (s.T, s.D), "x"),
-            _ptr(w_router, torch.bfloat16, (s.E, s.D), "w_router", allow_none=softmax),
-            _ptr(bias, torch.float32, (s.E,), "bias", allow_none=True),
-            _ptr(topk_idx, torch.int32, (s.T, s.K), "topk_idx", allow_none=softmax),
-            _ptr(topk_w, torch.float32, (s.T, s.K), "topk_w"), _ptr(dtopk_w, torch.float32, (s.T, s.K), "dtopk_w"),
-            _ptr(slot_row_off, torch.int32, (s.S + 1,), "slot_row_off"),
-            _ptr(slot_off, torch.int32, (s.E + 1,), "slot_off"), _ptr(row_pair, torch.int32, (s.Rcap,), "row_pair"),
-            _ptr(dlogit, torch.float32, (s.T, s.K), "dlogit"), _ptr(dw_router, torch.float32, (s.E, s.D), "dw_router"),
-            _ptr(dbias, torch.float32, (s.E,), "dbias"), _ptr(workspace, workspace.dtype, None, "workspace"),
+            self._h, _ptr(x, bf16, self._td, "x"), _ptr(w_router, bf16, self._ed, "w_router", allow_none=softmax),
+            _ptr(bias, f32, self._e, "bias", allow_none=True),
+            _ptr(topk_idx, i32, self._tk, "topk_idx", allow_none=softmax), _ptr(topk_w, f32, self._tk, "topk_w"),
+            _ptr(dtopk_w, f32, self._tk, "dtopk_w"), _ptr(slot_row_off, i32, self._s1, "slot_row_off"),
+            _ptr(slot_off, i32, self._e1, "slot_off"), _ptr(row_pair, i32, self._rows, "row_pair"),
+            _ptr(dlogit, f32, self._tk, "dlogit"), _ptr(dw_router, f32, self._ed, "dw_router"),
+            _ptr(dbias, f32, self._e, "dbias"), _ptr(workspace, workspace.dtype, None, "workspace"),
             _stream(stream)), "moegps_route_backward")
 
     def predictor_update(self, hist, state, predicted_hist, stream=None):

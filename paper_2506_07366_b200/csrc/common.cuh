@@ -26,7 +26,9 @@ struct moegps_ctx {
   CUtensorMap tm_h, tm_w2;
   bool tm2_valid;
   bool ffn_attr_done[3]; // dynamic shared-memory limit raised: gate+up, down, gate+up with kept activations
-  bool ffn_backward_attr_done[3];   // the same for the gradient's kernels: act, input, weights
+  bool data_gradient_attr_done[2][3];   // the same for the gradient's kernels: (act, input) x tile widths
+  bool weight_gradient_attr_done;
+  bool route_backward_attr_done;
   // cached TMA descriptors of the router
   const void* rt_key[2];
   CUtensorMap tm_rx, tm_rw;

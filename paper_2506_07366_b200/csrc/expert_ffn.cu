@@ -158,7 +158,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  const int total_tiles = tb.tile_base[kMaxS];
+  const int total_tiles = tb.tile_base[S];
 
   // ---------------------------------------------------------------- roles
   if (warp == 0) {

@@ -22,6 +22,18 @@ constexpr int kBoxBytes = 64 * BK * 2;             // a box of an MN-major opera
 static_assert(BK == 64, "boxes are one 128-byte swizzle span wide and BK rows high");
 static_assert(kABytes == 2 * kBoxBytes && 2 * kBHalfBytes == 4 * kBoxBytes, "a stage holds 2 + 4 boxes");
 
+// Launch shape of (1) and (2): BM x BN tiles, a ring of 192 KiB whatever the stage's size.  256 columns feed the tensor
+// core best (a stage's bytes against its products); 128 or 64 are for layers with fewer tiles than SMs, where one CTA
+// would otherwise stream a whole column of the weights by itself while others idle.
+template <int BN_>
+struct DataCfg {
+  static constexpr int BN = BN_, kStageBytes = kABytes + BN * kRowBytes, kStages = 192 * 1024 / kStageBytes;
+  static constexpr int kAccs = 2, kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps, kTmemCols = kAccs * BN;
+  static constexpr size_t kSmem = 1024 + 192 * 1024 + sizeof(Tables) + 256 + (size_t)kEpiWarps * kStagingBytesPerWarp;
+};
+static_assert(DataCfg<256>::kStages == 4 && DataCfg<128>::kStages == 6 && DataCfg<64>::kStages == 8, "whole stages");
+static_assert(DataCfg<256>::kSmem <= 227 * 1024, "one CTA per SM");
+
 // The 8-bit activations that (1) reads: codes [rcap][pitch], scales [blocks][rcap].
 struct KeptActs {
   const uint8_t *gate8, *up8, *gate_scale, *up_scale;
@@ -154,20 +166,21 @@ __device__ __forceinline__ void linger() {
 // C[rows, n_dim] = sum over `pairs` of A_p[rows, k_dim] B_p[e][k_dim, n_dim]; A K-major, B MN-major.
 // kAct: one pair (dyp, W2) and the activation's gradient as epilogue; else two pairs (dgate, W1), (dup, W3).
 template <bool kAct, class Cfg>
-__global__ void __launch_bounds__(Cfg::kThreads, Cfg::kCtasPerSm)
+__global__ void __launch_bounds__(Cfg::kThreads, 1)
 data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_constant__ CUtensorMap tm_b0,
                      const __grid_constant__ CUtensorMap tm_a1, const __grid_constant__ CUtensorMap tm_b1,
                      const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert, int S, int E, int n_dim,
                      int k_dim, int rcap, const KeptActs kept, const ActOutputs act_out, __nv_bfloat16* __restrict__ out,
                      int32_t* __restrict__ status) {
-  constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs, kThreads = Cfg::kThreads;
+  constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs, kThreads = Cfg::kThreads, BN = Cfg::BN;
+  constexpr int kStageBytes = Cfg::kStageBytes;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* stage_mem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   Tables& tb = *reinterpret_cast<Tables*>(stage_mem + (size_t)kStages * kStageBytes);
   const Bars<Cfg> bar(stage_mem + (size_t)kStages * kStageBytes + sizeof(Tables));
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n_tiles = (n_dim + BNACC - 1) / BNACC;
+  const int n_tiles = (n_dim + BN - 1) / BN;
   const int kb_per_pair = (k_dim + BK - 1) / BK;
   const int num_kb = kAct ? kb_per_pair : 2 * kb_per_pair;
 
@@ -186,7 +199,7 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = *bar.tmem_slot;
-  const int total_tiles = tb.tile_base[kMaxS];
+  const int total_tiles = tb.tile_base[S];
 
   if (warp == 0) {
     if (lane == 0) {
@@ -195,7 +208,7 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
       bool ok = true;
       for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
         const TileCoord tc = decode_tile(tb, slot_row_off, slot_expert, S, tile, n_tiles);
-        const int nb0 = tc.n_tile * BNACC;
+        const int nb0 = tc.n_tile * BN;
         for (int kb = 0; kb < num_kb; ++kb) {
           if (!mbar_wait(&bar.empty[stage], phase ^ 1u, bar.abort_flag)) { ok = false; break; }
           uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
@@ -206,7 +219,7 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
           const CUtensorMap* tbm = second ? &tm_b1 : &tm_b0;
           tma_load_2d(sa, ta, &bar.full[stage], k0, tc.m0);
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < BN / 64; ++i)
             tma_load_3d(sa + kABytes + i * kBoxBytes, tbm, &bar.full[stage], nb0 + 64 * i, k0, tc.expert);
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
@@ -215,14 +228,14 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
     }
   } else if (warp == 1) {
     if (lane == 0) {
-      constexpr uint32_t idesc = idesc_bf16_f32(BM, BNACC, false, true);
+      constexpr uint32_t idesc = idesc_bf16_f32(BM, BN, false, true);
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
       for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
         if (!mbar_wait(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
-        const uint32_t d_tmem = tmem_base + (uint32_t)acc * BNACC;
+        const uint32_t d_tmem = tmem_base + (uint32_t)acc * BN;
         for (int kb = 0; kb < num_kb; ++kb) {
           if (!mbar_wait(&bar.full[stage], phase, bar.abort_flag)) { ok = false; break; }
           tc_fence_after_sync();
@@ -243,7 +256,7 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
     }
   } else {
     const int quarter = warp & 3;                 // TMEM lanes this warp may read
-    constexpr int kShare = BNACC / (Cfg::kEpiWarps / 4);
+    constexpr int kShare = BN / (Cfg::kEpiWarps / 4);
     const int c_begin = ((warp - 2) >> 2) * kShare;
     uint8_t* staging = stage_mem + (size_t)kStages * kStageBytes + sizeof(Tables) + 256 + (warp - 2) * kStagingBytesPerWarp;
     int acc = 0;
@@ -251,12 +264,12 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
     bool ok = true;
     for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
       const TileCoord tc = decode_tile(tb, slot_row_off, slot_expert, S, tile, n_tiles);
-      const int row0 = tc.m0 + quarter * 32, col0 = tc.n_tile * BNACC;
+      const int row0 = tc.m0 + quarter * 32, col0 = tc.n_tile * BN;
       [[maybe_unused]] KeptBlock block;
       if constexpr (kAct) load_block(block, kept, row0 + lane, tc.row_end, col0 + c_begin, n_dim, rcap);
       if (!mbar_wait(&bar.acc_full[acc], acc_phase, bar.abort_flag, 256)) { ok = false; break; }
       tc_fence_after_sync();
-      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * BNACC;
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * BN;
       if constexpr (kAct)
         drain_act(taddr, staging, lane, kept, block, act_out, row0, tc.row_end, col0, n_dim, c_begin, c_begin + kShare, rcap);
       else
@@ -330,7 +343,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
                        const __grid_constant__ CUtensorMap tm_dyp, const __grid_constant__ CUtensorMap tm_xp,
                        const __grid_constant__ CUtensorMap tm_h, const int32_t* __restrict__ slot_row_off,
                        const int32_t* __restrict__ slot_off, const int32_t* __restrict__ row_pair, int S, int E, int F, int D,
-                       int rcap, __nv_bfloat16* __restrict__ dw_gate, __nv_bfloat16* __restrict__ dw_up,
+                       int row_align, int rcap, __nv_bfloat16* __restrict__ dw_gate, __nv_bfloat16* __restrict__ dw_up,
                        __nv_bfloat16* __restrict__ dw_down, int32_t* __restrict__ status) {
   constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs, kThreads = Cfg::kThreads;
   extern __shared__ uint8_t smem_raw[];
@@ -361,12 +374,23 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
     if (lo < 0 || hi < lo || hi > rcap) {
       if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
     } else {
-      int a = lo, b = hi;                          // first padding row: occupied rows come first
-      while (a < b) {
-        const int mid = (a + b) >> 1;
-        if (row_pair[mid] >= 0) a = mid + 1; else b = mid;
+      // padding is at the slot's end, fewer than row_align rows: looked at 16 rows at a time (loads that do not wait for
+      // one another; a binary search is a chain of memory round trips)
+      n = hi - lo;
+      const int least = max(0, n - (row_align - 1));
+      bool more = n > least;
+      while (more) {
+        int tail = 0;
+        bool pad = true;
+#pragma unroll
+        for (int i = 1; i <= 16; ++i) {
+          const int p = n - i >= least ? row_pair[lo + n - i] : 0;
+          pad = pad && p < 0;
+          tail += pad ? 1 : 0;
+        }
+        n -= tail;
+        more = tail == 16 && n > least;
       }
-      n = a - lo;
     }
     sr.ext[s] = make_int2(lo, n);
   }
@@ -517,23 +541,43 @@ int tmap_failed(moegps_ctx* ctx) {
   return MOEGPS_ERR_CUDA;
 }
 
-template <bool kAct>
+template <bool kAct, int BN>
 int launch_data_gradient(moegps_ctx* ctx, const CUtensorMap& a0, const CUtensorMap& b0, const CUtensorMap& a1,
                          const CUtensorMap& b1, const int32_t* slot_row_off, const int32_t* slot_expert, int n_dim, int k_dim,
                          const KeptActs& kept, const ActOutputs& act_out, void* out, cudaStream_t st) {
+  using Cfg = DataCfg<BN>;
   const moegps_shape_t& s = ctx->shape;
-  constexpr size_t smem = smem_bytes_of<WideCfg>();
-  bool& done = ctx->ffn_backward_attr_done[kAct ? 0 : 1];
+  bool& done = ctx->data_gradient_attr_done[kAct ? 0 : 1][BN == 256 ? 2 : BN == 128 ? 1 : 0];
   if (!done) {
-    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(data_gradient_kernel<kAct, WideCfg>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                              (int)smem));
+    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(data_gradient_kernel<kAct, Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                              (int)Cfg::kSmem));
     done = true;
   }
-  data_gradient_kernel<kAct, WideCfg><<<ctx->sm_count, WideCfg::kThreads, smem, st>>>(
+  data_gradient_kernel<kAct, Cfg><<<ctx->sm_count, Cfg::kThreads, Cfg::kSmem, st>>>(
       a0, b0, a1, b1, slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim, (int)moegps_rcap_of(s), kept, act_out,
       static_cast<__nv_bfloat16*>(out), ctx->d_status);
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
+}
+
+// Tile width for n_dim output columns: the widest with a tile for every SM.  The slots' loads are on the device; a layer
+// has at least R / BM row tiles, and about one for each slot.
+int tile_width(const moegps_ctx* ctx, int n_dim) {
+  const moegps_shape_t& s = ctx->shape;
+  const int64_t R = (int64_t)s.T * s.K, spread = s.S < R ? s.S : R, full = (R + BM - 1) / BM;
+  const int64_t row_tiles = full > spread ? full : spread;
+  for (int bn : {256, 128})
+    if (row_tiles * ((n_dim + bn - 1) / bn) >= ctx->sm_count) return bn;
+  return 64;
+}
+
+template <bool kAct, typename... Args>
+int launch_data_gradient_any(moegps_ctx* ctx, int n_dim, Args... args) {
+  switch (tile_width(ctx, n_dim)) {
+    case 256: return launch_data_gradient<kAct, 256>(ctx, args...);
+    case 128: return launch_data_gradient<kAct, 128>(ctx, args...);
+    default: return launch_data_gradient<kAct, 64>(ctx, args...);
+  }
 }
 
 }  // namespace
@@ -550,7 +594,7 @@ int moegps_launch_ffn_backward_act(moegps_ctx* ctx, const void* dyp, const int32
                          static_cast<const uint8_t*>(gate_scale), static_cast<const uint8_t*>(up_scale)};
   const ActOutputs out = {static_cast<__nv_bfloat16*>(dgate), static_cast<__nv_bfloat16*>(dup),
                           static_cast<__nv_bfloat16*>(h_ws)};
-  return launch_data_gradient<true>(ctx, a, b, a, b, slot_row_off, slot_expert, s.F, s.D, kept, out, nullptr, st);
+  return launch_data_gradient_any<true>(ctx, s.F, a, b, a, b, slot_row_off, slot_expert, s.F, s.D, kept, out, nullptr, st);
 }
 
 int moegps_launch_ffn_backward_input(moegps_ctx* ctx, const void* dgate, const void* dup, const int32_t* slot_row_off,
@@ -562,8 +606,8 @@ int moegps_launch_ffn_backward_input(moegps_ctx* ctx, const void* dgate, const v
   if (!(moegps_make_tmap_2d(&a0, dgate, rcap, s.F, BM, BK) && moegps_make_tmap_2d(&a1, dup, rcap, s.F, BM, BK) &&
         moegps_make_tmap_3d(&b0, w_gate, s.E, s.F, s.D, BK, 64) && moegps_make_tmap_3d(&b1, w_up, s.E, s.F, s.D, BK, 64)))
     return tmap_failed(ctx);
-  return launch_data_gradient<false>(ctx, a0, b0, a1, b1, slot_row_off, slot_expert, s.D, s.F, KeptActs{}, ActOutputs{}, dxp,
-                                     st);
+  return launch_data_gradient_any<false>(ctx, s.D, a0, b0, a1, b1, slot_row_off, slot_expert, s.D, s.F, KeptActs{},
+                                         ActOutputs{}, dxp, st);
 }
 
 int moegps_launch_ffn_backward_weights(moegps_ctx* ctx, const void* dyp, const void* xp, const void* dgate, const void* dup,
@@ -577,13 +621,14 @@ int moegps_launch_ffn_backward_weights(moegps_ctx* ctx, const void* dyp, const v
         moegps_make_tmap_2d(&t_h, h_ws, rcap, s.F, BK, 64)))
     return tmap_failed(ctx);
   constexpr size_t smem = weight_smem_bytes<WideCfg>();
-  if (!ctx->ffn_backward_attr_done[2]) {
+  if (!ctx->weight_gradient_attr_done) {
     MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(weight_gradient_kernel<WideCfg>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                               (int)smem));
-    ctx->ffn_backward_attr_done[2] = true;
+    ctx->weight_gradient_attr_done = true;
   }
   weight_gradient_kernel<WideCfg><<<ctx->sm_count, WideCfg::kThreads, smem, st>>>(
-      t_dgate, t_dup, t_dyp, t_xp, t_h, slot_row_off, slot_off, row_pair, s.S, s.E, s.F, s.D, (int)rcap,
+      t_dgate, t_dup, t_dyp, t_xp, t_h, slot_row_off, slot_off, row_pair, s.S, s.E, s.F, s.D,
+      s.row_align, (int)rcap,
       static_cast<__nv_bfloat16*>(dw_gate), static_cast<__nv_bfloat16*>(dw_up), static_cast<__nv_bfloat16*>(dw_down),
       ctx->d_status);
   MOEGPS_AFTER_LAUNCH(ctx);

@@ -4,15 +4,17 @@
 // (the logits that were not selected get no gradient), and
 //   dWr[e] = sum over the pairs of e of dl x[t],   db[e] = sum over the pairs of e of dl.
 //
-// Three kernels:
-//   1. dlogit  : one warp per token.  The forward pass keeps the weights, not the scores, so the sigmoid
-//                form recomputes the K selected logits (Wr stays in L2); softmax needs only w and dw.
-//                One more block lists the units of the next step.
-//   2. partial : dlogit is sparse (K of E), so dWr is a weighted sum of rows rather than a matrix
+// Kernels:
+//   1. logits  : (sigmoid form only) the forward pass keeps the weights, not the scores, so the K selected logits are
+//                computed again.  A token needs K rows of Wr, together K times x: from L2 that alone took 83 us on 4096
+//                tokens x 7168, 8 of 256 experts.  So a block owns 128 columns: that slice of Wr (all experts) fits in its
+//                shared memory, x is read once, and the slices' partial sums are added by the next kernel.
+//   2. dlogit  : one thread per pair.  One more block lists the units of the next step.
+//   3. partial : dlogit is sparse (K of E), so dWr is a weighted sum of rows rather than a matrix
 //                product: the pairs of one expert are consecutive in the permuted order, and a unit is
 //                up to kUnitRows of them.  Its rows of x are gathered through row_pair (x is read K
 //                times, but from L2: it is the unpermuted tensor) and summed in fp32.
-//   3. reduce  : the units of an expert are added in order.
+//   4. reduce  : the units of an expert are added in order.
 // No atomics: the sums have a fixed order.
 #include "bf16x8.cuh"
 #include "common.cuh"
@@ -65,138 +67,197 @@ __device__ void list_units(int E, int S, int64_t Rcap, int max_units, const int3
     units[first + i] = make_int4(e, lo + i * kUnitRows, min(hi, lo + (i + 1) * kUnitRows), 0);
 }
 
-template <int KT, bool kSigmoid>
+constexpr int kSliceCols = route_backward::kSliceCols;
+constexpr int kSliceWords = kSliceCols / 8;          // 16-byte words of a row's slice
+
+// Adds the eight values of every lane over groups of eight lanes; lane i of a group returns the sum of the v[i].
+__device__ __forceinline__ float transpose_add8(const float (&v)[8], int i) {
+  float a[4], b[2];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float keep = (i & 4) ? v[j + 4] : v[j], give = (i & 4) ? v[j] : v[j + 4];
+    a[j] = keep + __shfl_xor_sync(0xffffffffu, give, 4);
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float keep = (i & 2) ? a[j + 2] : a[j], give = (i & 2) ? a[j] : a[j + 2];
+    b[j] = keep + __shfl_xor_sync(0xffffffffu, give, 2);
+  }
+  const float keep = (i & 1) ? b[1] : b[0], give = (i & 1) ? b[0] : b[1];
+  return keep + __shfl_xor_sync(0xffffffffu, give, 1);
+}
+
+// block (s, c): columns [128 s, 128 s + 128) of tokens [c per, c per + per) -> part[s][pair].  Eight lanes take one token:
+// a group reads 128 contiguous bytes of a row of the slice at a time, so the shared-memory reads have no conflicts
+// whatever experts the four tokens of a warp chose.
+template <int KT>
 __global__ void __launch_bounds__(kThreads)
-dlogit_kernel(const uint4* __restrict__ x, const uint4* __restrict__ w_router, const float* __restrict__ bias,
+logits_kernel(const uint4* __restrict__ x, const uint4* __restrict__ w_router, const int32_t* __restrict__ topk_idx, int T,
+              int E, int chunks, int per, float* __restrict__ part, int32_t* __restrict__ status) {
+  extern __shared__ uint4 slice[];                   // [E][kSliceWords]
+  const int tid = threadIdx.x, first = blockIdx.x * kSliceWords;
+  for (int i = tid; i < E * kSliceWords; i += kThreads) {
+    const int e = i / kSliceWords, c = first + i % kSliceWords;
+    slice[i] = c < chunks ? w_router[(int64_t)e * chunks + c] : make_uint4(0, 0, 0, 0);
+  }
+  __syncthreads();
+  const int i = tid & 7, group = (tid & 31) & ~7;
+  const int begin = blockIdx.y * per, end = min(begin + per, T);
+  float* out = part + (int64_t)blockIdx.x * T * KT;
+  // the next token's words and (lane j of the group) its j-th expert, loaded while the present one is worked on
+  const bool have0 = first + i < chunks, have1 = first + 8 + i < chunks;
+  uint4 next0, next1;
+  int next_e;
+  auto fetch = [&](int t) {
+    const uint4* row = x + (int64_t)t * chunks + first + i;
+    next0 = t < end && have0 ? row[0] : make_uint4(0, 0, 0, 0);
+    next1 = t < end && have1 ? row[8] : make_uint4(0, 0, 0, 0);
+    next_e = t < end && i < KT ? topk_idx[(int64_t)t * KT + i] : 0;
+  };
+  int t = begin + (tid >> 3);
+  fetch(t);
+  for (int t0 = begin; t0 < end; t0 += kThreads / 8, t += kThreads / 8) {
+    float x0[8], x1[8], dot[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    unpack8(x0, next0);
+    unpack8(x1, next1);
+    int my_e = next_e;
+    if (my_e < 0 || my_e >= E) {
+      moegps_report(status, MOEGPS_ERR_BAD_INDEX, t);
+      my_e = 0;
+    }
+    fetch(t + kThreads / 8);
+#pragma unroll
+    for (int j = 0; j < KT; ++j) {
+      const uint4* row = slice + __shfl_sync(0xffffffffu, my_e, group + j) * kSliceWords + i;
+      float wf[8];
+      unpack8(wf, row[0]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) dot[j] = fmaf(x0[k], wf[k], dot[j]);
+      unpack8(wf, row[8]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) dot[j] = fmaf(x1[k], wf[k], dot[j]);
+    }
+    const float sum = transpose_add8(dot, i);
+    if (t < end && i < KT) out[(int64_t)t * KT + i] = sum;
+  }
+}
+
+template <bool kSigmoid>
+__global__ void __launch_bounds__(kThreads)
+dlogit_kernel(const float* __restrict__ part, int slices, const float* __restrict__ bias,
               const int32_t* __restrict__ topk_idx, const float* __restrict__ topk_w, const float* __restrict__ dtopk_w,
-              int T, int E, int S, int chunks, int64_t Rcap, int max_units, const int32_t* __restrict__ slot_row_off,
+              int64_t R, int K, int E, int S, int64_t Rcap, int max_units, const int32_t* __restrict__ slot_row_off,
               const int32_t* __restrict__ slot_off, float* __restrict__ dlogit, int32_t* __restrict__ unit_first,
               int4* __restrict__ units, int32_t* __restrict__ status) {
   if (blockIdx.x == 0) {
     list_units(E, S, Rcap, max_units, slot_row_off, slot_off, unit_first, units, status);
     return;
   }
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t t = ((int64_t)blockIdx.x - 1) * kWarps + warp;
-  if (t >= T) return;
-  float w[KT], dw[KT], m = 0.f;
-#pragma unroll
-  for (int j = 0; j < KT; ++j) {
-    w[j] = topk_w[t * KT + j];
-    dw[j] = dtopk_w[t * KT + j];
-  }
-#pragma unroll
-  for (int j = 0; j < KT; ++j) m = fmaf(w[j], dw[j], m);
-  float logit[KT];
-#pragma unroll
-  for (int j = 0; j < KT; ++j) logit[j] = 0.f;
+  const int64_t p = ((int64_t)blockIdx.x - 1) * kThreads + threadIdx.x;
+  if (p >= R) return;
+  const int64_t p0 = p / K * K;
+  float m = 0.f;
+  for (int j = 0; j < K; ++j) m = fmaf(topk_w[p0 + j], dtopk_w[p0 + j], m);
+  float d = topk_w[p] * (dtopk_w[p] - m);
   if constexpr (kSigmoid) {
-    int expert[KT];
-#pragma unroll
-    for (int j = 0; j < KT; ++j) {
-      expert[j] = topk_idx[t * KT + j];
-      if (expert[j] < 0 || expert[j] >= E) {
-        if (lane == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, (int)t);
-        expert[j] = 0;
-        w[j] = 0.f;
-      }
-    }
-    for (int c = lane; c < chunks; c += 32) {
-      float xf[8];
-      unpack8(xf, x[t * chunks + c]);
-#pragma unroll
-      for (int j = 0; j < KT; ++j) {
-        float rf[8];
-        unpack8(rf, w_router[(int64_t)expert[j] * chunks + c]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) logit[j] = fmaf(xf[i], rf[i], logit[j]);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < KT; ++j) {
-#pragma unroll
-      for (int s = 16; s > 0; s >>= 1) logit[j] += __shfl_xor_sync(0xffffffffu, logit[j], s);
-      if (bias) logit[j] += bias[expert[j]];
-    }
+    const int e = topk_idx[p];
+    float logit = 0.f;
+#pragma unroll 16
+    for (int s = 0; s < slices; ++s) logit += part[(int64_t)s * R + p];
+    if (e < 0 || e >= E) d = 0.f;                     // reported by logits_kernel
+    else if (bias) logit += bias[e];
+    d *= 1.f / (1.f + expf(logit));                   // 1 - sigmoid
   }
-  if (lane == 0) {
-#pragma unroll
-    for (int j = 0; j < KT; ++j) {
-      float d = w[j] * (dw[j] - m);
-      if constexpr (kSigmoid) d *= 1.f / (1.f + expf(logit[j]));      // 1 - sigmoid
-      dlogit[t * KT + j] = d;
-    }
-  }
+  dlogit[p] = d;
 }
 
-// block (u, c): columns [2048 c, 2048 c + 2048) of unit u; a thread sums eight columns over the unit's rows
-__global__ void __launch_bounds__(kThreads)
+// block (u, c): columns [1024 c, 1024 c + 1024) of unit u; a thread sums eight columns over the unit's rows, eight rows
+// in flight at a time.  An expert with one unit needs no second pass: its sums are the result.
+constexpr int kPartThreads = 128;
+
+__global__ void __launch_bounds__(kPartThreads)
 partial_kernel(const uint4* __restrict__ x, const int32_t* __restrict__ row_pair, const float* __restrict__ dlogit, int64_t R,
                int K, int E, int D, const int32_t* __restrict__ unit_first, const int4* __restrict__ units,
-               float* __restrict__ part, float* __restrict__ part_b, int32_t* __restrict__ status) {
+               float* __restrict__ part, float* __restrict__ part_b, float* __restrict__ dw_router,
+               int32_t* __restrict__ status) {
+  static_assert(kUnitRows == 64, "two warps list the unit's rows");
   __shared__ float s_dl[kUnitRows];
   __shared__ int s_t[kUnitRows];
+  __shared__ int s_n[2];
   const int u = blockIdx.x;
   if (u >= unit_first[E]) return;
   const int4 unit = units[u];
-  const int rows = unit.z - unit.y;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31;
+  // the unit's tokens in order, without its padding rows
+  int p = -1;
+  unsigned have = 0;
   if (tid < kUnitRows) {
-    float dl = 0.f;
-    int t = -1;
-    if (tid < rows) {
-      const int p = row_pair[unit.y + tid];
-      if (p >= 0 && p < R) {
-        dl = dlogit[p];
-        t = p / K;
-      } else if (p >= R) {
-        moegps_report(status, MOEGPS_ERR_BAD_INDEX, unit.y + tid);
-      }
+    if (unit.y + tid < unit.z) p = row_pair[unit.y + tid];
+    if (p >= R) {
+      moegps_report(status, MOEGPS_ERR_BAD_INDEX, unit.y + tid);
+      p = -1;
     }
-    s_dl[tid] = dl;
-    s_t[tid] = t;
+    have = __ballot_sync(0xffffffffu, p >= 0);
+    if (lane == 0) s_n[tid >> 5] = __popc(have);
   }
   __syncthreads();
-  const int chunks = D / 8, c = blockIdx.y * kThreads + tid;
+  const int n = s_n[0] + s_n[1];
+  if (p >= 0) {
+    const int at = (tid >= 32 ? s_n[0] : 0) + __popc(have & ((1u << lane) - 1));
+    s_dl[at] = dlogit[p];
+    s_t[at] = p / K;
+  }
+  __syncthreads();
+  const int chunks = D / 8, c = blockIdx.y * kPartThreads + tid;
   if (blockIdx.y == 0 && tid == 0) {
     float b = 0.f;
-    for (int r = 0; r < rows; ++r) b += s_dl[r];
+    for (int r = 0; r < n; ++r) b += s_dl[r];
     part_b[u] = b;
   }
   if (c >= chunks) return;
   float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll 8
-  for (int r = 0; r < rows; ++r) {
-    const int t = s_t[r];
-    if (t >= 0) fma8(acc, s_dl[r], x[(int64_t)t * chunks + c]);
+  const uint4* xc = x + c;
+  int r = 0;
+  for (; r + 8 <= n; r += 8) {
+    uint4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = xc[(int64_t)s_t[r + i] * chunks];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) fma8(acc, s_dl[r + i], v[i]);
   }
-  float4* o = reinterpret_cast<float4*>(part + (int64_t)u * D + 8 * c);
+  for (; r < n; ++r) fma8(acc, s_dl[r], xc[(int64_t)s_t[r] * chunks]);
+  const bool only = unit_first[unit.x + 1] - unit_first[unit.x] == 1;
+  float4* o = reinterpret_cast<float4*>((only ? dw_router + (int64_t)unit.x * D : part + (int64_t)u * D) + 8 * c);
   o[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
   o[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
 }
 
-// block (e, c): columns [128 c, 128 c + 128) of expert e; warp v adds units v, v + 8, ..., then the warps are added
+// The units of expert e are shared by W warps (each takes every W-th one, their sums are added in order), W growing with
+// their number, and a block's other warps take further groups of 128 columns: block (e, y) adds columns
+// [128 G y, 128 G y + 128 G), G = 8 / W.  The grid has room for G = 1; blocks beyond an expert's columns end at once.
 __global__ void __launch_bounds__(kThreads)
 reduce_kernel(const float* __restrict__ part, const float* __restrict__ part_b, int D,
               const int32_t* __restrict__ unit_first, float* __restrict__ dw_router, float* __restrict__ dbias) {
   __shared__ float4 s_acc[kWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int e = blockIdx.x, col = (blockIdx.y * 32 + lane) * 4;
-  const int first = unit_first[e], last = unit_first[e + 1];
+  const int e = blockIdx.x;
+  const int first = unit_first[e], last = unit_first[e + 1], n = last - first;
+  const int W = n <= 4 ? 1 : n <= 8 ? 2 : n <= 16 ? 4 : 8;
+  const int group = blockIdx.y * (kWarps / W) + warp / W, col = 128 * group + 4 * lane;
+  if (blockIdx.y * (kWarps / W) * 128 >= D || (n == 1 && blockIdx.y > 0)) return;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (col < D) {
-#pragma unroll 4
-    for (int u = first + warp; u < last; u += kWarps) {
+  if (col < D && n != 1) {
+#pragma unroll 8
+    for (int u = first + warp % W; u < last; u += W) {
       const float4 v = *reinterpret_cast<const float4*>(part + (int64_t)u * D + col);
       a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
     }
   }
   s_acc[warp][lane] = a;
   __syncthreads();
-  if (warp == 0 && col < D) {
-#pragma unroll
-    for (int v = 1; v < kWarps; ++v) {
-      const float4 b = s_acc[v][lane];
+  if (warp % W == 0 && col < D && n != 1) {        // (one unit: partial_kernel has stored the result)
+    for (int v = 1; v < W; ++v) {
+      const float4 b = s_acc[warp + v][lane];
       a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
     }
     *reinterpret_cast<float4*>(dw_router + (int64_t)e * D + col) = a;
@@ -222,25 +283,42 @@ int moegps_launch_route_backward(moegps_ctx* ctx, const void* x, const void* w_r
   const int max_units = (int)route_backward::max_units(s);
   const route_backward::Workspace ws = route_backward::carve(s, workspace);
   const uint4 *xv = static_cast<const uint4*>(x), *rv = static_cast<const uint4*>(w_router);
-  const int blocks = 1 + (s.T + kWarps - 1) / kWarps;
-#define MOEGPS_LAUNCH(KT, G)                                                                                             \
-  dlogit_kernel<KT, G><<<blocks, kThreads, 0, st>>>(xv, rv, bias, topk_idx, topk_w, dtopk_w, s.T, s.E, s.S, chunks, Rcap, \
-                                                    max_units, slot_row_off, slot_off, dlogit, ws.unit_first, ws.units,  \
-                                                    ctx->d_status)
-#define MOEGPS_CASE(KT)                                                     \
-  case KT:                                                                  \
-    if (s.gate_mode == 1) MOEGPS_LAUNCH(KT, true); else MOEGPS_LAUNCH(KT, false); \
+  const int slices = route_backward::slices(s);
+  if (s.gate_mode == 1) {
+    const size_t smem = (size_t)s.E * kSliceWords * sizeof(uint4);
+    // at most three blocks for every SM, the number that the slices of 256 experts leave room for: one more would wait
+    // for the others to end.  No block without 32 tokens of its own.
+    int pieces = 3 * ctx->sm_count / slices;
+    if (pieces < 1) pieces = 1;
+    if (pieces > (s.T + 31) / 32) pieces = (s.T + 31) / 32;
+    const int per = (s.T + pieces - 1) / pieces;
+    const dim3 grid(slices, (s.T + per - 1) / per);
+#define MOEGPS_CASE(KT)                                                                                                \
+  case KT:                                                                                                             \
+    if (!ctx->route_backward_attr_done)                                                                                \
+      MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(logits_kernel<KT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)); \
+    logits_kernel<KT><<<grid, kThreads, smem, st>>>(xv, rv, topk_idx, s.T, s.E, chunks, per, ws.part, ctx->d_status);   \
     break;
-  switch (s.K) {
-    MOEGPS_CASE(1) MOEGPS_CASE(2) MOEGPS_CASE(3) MOEGPS_CASE(4)
-    MOEGPS_CASE(5) MOEGPS_CASE(6) MOEGPS_CASE(7) MOEGPS_CASE(8)
-    default: return MOEGPS_ERR_UNSUPPORTED_SHAPE;
-  }
+    switch (s.K) {
+      MOEGPS_CASE(1) MOEGPS_CASE(2) MOEGPS_CASE(3) MOEGPS_CASE(4)
+      MOEGPS_CASE(5) MOEGPS_CASE(6) MOEGPS_CASE(7) MOEGPS_CASE(8)
+      default: return MOEGPS_ERR_UNSUPPORTED_SHAPE;
+    }
 #undef MOEGPS_CASE
+    ctx->route_backward_attr_done = true;
+    MOEGPS_AFTER_LAUNCH(ctx);
+  }
+  const int blocks = 1 + (int)((R + kThreads - 1) / kThreads);
+#define MOEGPS_LAUNCH(G)                                                                                             \
+  dlogit_kernel<G><<<blocks, kThreads, 0, st>>>(ws.part, slices, bias, topk_idx, topk_w, dtopk_w, R, s.K, s.E, s.S, Rcap, \
+                                                max_units, slot_row_off, slot_off, dlogit, ws.unit_first, ws.units,  \
+                                                ctx->d_status)
+  if (s.gate_mode == 1) MOEGPS_LAUNCH(true); else MOEGPS_LAUNCH(false);
 #undef MOEGPS_LAUNCH
   MOEGPS_AFTER_LAUNCH(ctx);
-  partial_kernel<<<dim3(max_units, (chunks + kThreads - 1) / kThreads), kThreads, 0, st>>>(
-      xv, row_pair, dlogit, R, s.K, s.E, s.D, ws.unit_first, ws.units, ws.part, ws.part_b, ctx->d_status);
+  partial_kernel<<<dim3(max_units, (chunks + kPartThreads - 1) / kPartThreads), kPartThreads, 0, st>>>(
+      xv, row_pair, dlogit, R, s.K, s.E, s.D, ws.unit_first, ws.units, ws.part, ws.part_b, dw_router,
+      ctx->d_status);
   MOEGPS_AFTER_LAUNCH(ctx);
   reduce_kernel<<<dim3(s.E, (s.D + 127) / 128), kThreads, 0, st>>>(ws.part, ws.part_b, s.D, ws.unit_first, dw_router, dbias);
   MOEGPS_AFTER_LAUNCH(ctx);
