@@ -53,7 +53,6 @@ int moegps_create(moegps_ctx_t** out, const moegps_shape_t* shape, int device) {
   for (auto& v : ctx->data_gradient_attr_done)
     for (bool& b : v) b = false;
   ctx->weight_gradient_attr_done = false;
-  ctx->route_backward_attr_done = false;
   ctx->rt_valid = false;
   ctx->route_attr_done = false;
   ctx->dispatch_attr_done = false;

@@ -28,7 +28,6 @@ struct moegps_ctx {
   bool ffn_attr_done[3]; // dynamic shared-memory limit raised: gate+up, down, gate+up with kept activations
   bool data_gradient_attr_done[2][3];   // the same for the gradient's kernels: (act, input) x tile widths
   bool weight_gradient_attr_done;
-  bool route_backward_attr_done;
   // cached TMA descriptors of the router
   const void* rt_key[2];
   CUtensorMap tm_rx, tm_rw;
@@ -68,6 +67,24 @@ inline void moegps_trace_launch(const moegps_ctx* ctx, const char* where) {
     }                                                                \
   } while (0)
 
+// Launches a kernel that may start while the stream's previous kernel still runs, as far as its own
+// wait_for_predecessor(): the launch and the set-up in front of that call overlap the predecessor's end.
+template <typename... KArgs, typename... Args>
+static inline cudaError_t launch_after(void (*kernel)(KArgs...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st,
+                                       Args... args) {
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
 static inline bool moegps_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 static inline int64_t moegps_rcap_of(const moegps_shape_t& s) {
@@ -81,6 +98,12 @@ static inline int moegps_check_device(const moegps_ctx* ctx) {
   if (cudaGetDevice(&dev) != cudaSuccess) return MOEGPS_ERR_CUDA;
   return dev == ctx->device ? MOEGPS_OK : MOEGPS_ERR_INVALID_ARG;
 }
+
+// Device side of launch_after.  The wait returns when the predecessor grid has ended and its writes are visible (at once
+// for a kernel that was launched without one); nothing that an earlier kernel of the stream may write, or still reads,
+// is touched before it.
+__device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // First error wins; later ones are dropped.
 __device__ __forceinline__ void moegps_report(int32_t* status, int code, int detail) {

@@ -190,6 +190,8 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
     prefetch_tensormap(&tm_b0);
     if (!kAct) { prefetch_tensormap(&tm_a1); prefetch_tensormap(&tm_b1); }
   }
+  launch_dependents();
+  wait_for_predecessor();
   if (warp == 1) {
     tmem_alloc(bar.tmem_slot, Cfg::kTmemCols);
     tmem_relinquish();
@@ -364,6 +366,8 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
     prefetch_tensormap(&tm_xp);
     prefetch_tensormap(&tm_h);
   }
+  launch_dependents();
+  wait_for_predecessor();
   if (warp == 1) {
     tmem_alloc(bar.tmem_slot, Cfg::kTmemCols);
     tmem_relinquish();
@@ -553,9 +557,9 @@ int launch_data_gradient(moegps_ctx* ctx, const CUtensorMap& a0, const CUtensorM
                                               (int)Cfg::kSmem));
     done = true;
   }
-  data_gradient_kernel<kAct, Cfg><<<ctx->sm_count, Cfg::kThreads, Cfg::kSmem, st>>>(
-      a0, b0, a1, b1, slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim, (int)moegps_rcap_of(s), kept, act_out,
-      static_cast<__nv_bfloat16*>(out), ctx->d_status);
+  MOEGPS_CUDA_TRY(ctx, launch_after(data_gradient_kernel<kAct, Cfg>, dim3(ctx->sm_count), Cfg::kThreads, Cfg::kSmem, st, a0, b0,
+                                    a1, b1, slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim, (int)moegps_rcap_of(s), kept,
+                                    act_out, static_cast<__nv_bfloat16*>(out), ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }
@@ -626,11 +630,10 @@ int moegps_launch_ffn_backward_weights(moegps_ctx* ctx, const void* dyp, const v
                                               (int)smem));
     ctx->weight_gradient_attr_done = true;
   }
-  weight_gradient_kernel<WideCfg><<<ctx->sm_count, WideCfg::kThreads, smem, st>>>(
-      t_dgate, t_dup, t_dyp, t_xp, t_h, slot_row_off, slot_off, row_pair, s.S, s.E, s.F, s.D,
-      s.row_align, (int)rcap,
-      static_cast<__nv_bfloat16*>(dw_gate), static_cast<__nv_bfloat16*>(dw_up), static_cast<__nv_bfloat16*>(dw_down),
-      ctx->d_status);
+  MOEGPS_CUDA_TRY(ctx, launch_after(weight_gradient_kernel<WideCfg>, dim3(ctx->sm_count), WideCfg::kThreads, smem, st, t_dgate,
+                                    t_dup, t_dyp, t_xp, t_h, slot_row_off, slot_off, row_pair, s.S, s.E, s.F, s.D, s.row_align,
+                                    (int)rcap, static_cast<__nv_bfloat16*>(dw_gate), static_cast<__nv_bfloat16*>(dw_up),
+                                    static_cast<__nv_bfloat16*>(dw_down), ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }

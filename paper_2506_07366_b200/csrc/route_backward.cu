@@ -5,17 +5,17 @@
 //   dWr[e] = sum over the pairs of e of dl x[t],   db[e] = sum over the pairs of e of dl.
 //
 // Kernels:
-//   1. logits  : (sigmoid form only) the forward pass keeps the weights, not the scores, so the K selected logits are
-//                computed again.  A token needs K rows of Wr, together K times x: from L2 that alone took 83 us on 4096
-//                tokens x 7168, 8 of 256 experts.  So a block owns 128 columns: that slice of Wr (all experts) fits in its
-//                shared memory, x is read once, and the slices' partial sums are added by the next kernel.
+//   1. logits  : (sigmoid form only) the forward pass keeps the weights, not the scores, so the router's own GEMM gives the
+//                logits again (route.cu), bit for bit those that the selection was made on.  Its tensor-core sums cost
+//                26 us on 4096 tokens x 7168 and 256 experts; 8 dot products for each token on the CUDA cores took 83 us
+//                with Wr from L2, and 40 + 6 us with slices of it in shared memory.
 //   2. dlogit  : one thread per pair.  One more block lists the units of the next step.
 //   3. partial : dlogit is sparse (K of E), so dWr is a weighted sum of rows rather than a matrix
 //                product: the pairs of one expert are consecutive in the permuted order, and a unit is
 //                up to kUnitRows of them.  Its rows of x are gathered through row_pair (x is read K
 //                times, but from L2: it is the unpermuted tensor) and summed in fp32.
 //   4. reduce  : the units of an expert are added in order.
-// No atomics: the sums have a fixed order.
+// No atomics: the sums have a fixed order.  Each kernel is launched while the one before it drains (launch_after).
 #include "bf16x8.cuh"
 #include "common.cuh"
 #include "route_backward.cuh"
@@ -25,7 +25,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kUnitRows = route_backward::kUnitRows;
-constexpr int kMaxE = 256;
 
 // Lists the units: expert e owns rows slot_row_off[slot_off[e]] .. slot_row_off[slot_off[e+1]], cut into
 // pieces of kUnitRows.  One block; thread e takes expert e (E <= 256).
@@ -67,88 +66,14 @@ __device__ void list_units(int E, int S, int64_t Rcap, int max_units, const int3
     units[first + i] = make_int4(e, lo + i * kUnitRows, min(hi, lo + (i + 1) * kUnitRows), 0);
 }
 
-constexpr int kSliceCols = route_backward::kSliceCols;
-constexpr int kSliceWords = kSliceCols / 8;          // 16-byte words of a row's slice
-
-// Adds the eight values of every lane over groups of eight lanes; lane i of a group returns the sum of the v[i].
-__device__ __forceinline__ float transpose_add8(const float (&v)[8], int i) {
-  float a[4], b[2];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float keep = (i & 4) ? v[j + 4] : v[j], give = (i & 4) ? v[j] : v[j + 4];
-    a[j] = keep + __shfl_xor_sync(0xffffffffu, give, 4);
-  }
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const float keep = (i & 2) ? a[j + 2] : a[j], give = (i & 2) ? a[j] : a[j + 2];
-    b[j] = keep + __shfl_xor_sync(0xffffffffu, give, 2);
-  }
-  const float keep = (i & 1) ? b[1] : b[0], give = (i & 1) ? b[0] : b[1];
-  return keep + __shfl_xor_sync(0xffffffffu, give, 1);
-}
-
-// block (s, c): columns [128 s, 128 s + 128) of tokens [c per, c per + per) -> part[s][pair].  Eight lanes take one token:
-// a group reads 128 contiguous bytes of a row of the slice at a time, so the shared-memory reads have no conflicts
-// whatever experts the four tokens of a warp chose.
-template <int KT>
-__global__ void __launch_bounds__(kThreads)
-logits_kernel(const uint4* __restrict__ x, const uint4* __restrict__ w_router, const int32_t* __restrict__ topk_idx, int T,
-              int E, int chunks, int per, float* __restrict__ part, int32_t* __restrict__ status) {
-  extern __shared__ uint4 slice[];                   // [E][kSliceWords]
-  const int tid = threadIdx.x, first = blockIdx.x * kSliceWords;
-  for (int i = tid; i < E * kSliceWords; i += kThreads) {
-    const int e = i / kSliceWords, c = first + i % kSliceWords;
-    slice[i] = c < chunks ? w_router[(int64_t)e * chunks + c] : make_uint4(0, 0, 0, 0);
-  }
-  __syncthreads();
-  const int i = tid & 7, group = (tid & 31) & ~7;
-  const int begin = blockIdx.y * per, end = min(begin + per, T);
-  float* out = part + (int64_t)blockIdx.x * T * KT;
-  // the next token's words and (lane j of the group) its j-th expert, loaded while the present one is worked on
-  const bool have0 = first + i < chunks, have1 = first + 8 + i < chunks;
-  uint4 next0, next1;
-  int next_e;
-  auto fetch = [&](int t) {
-    const uint4* row = x + (int64_t)t * chunks + first + i;
-    next0 = t < end && have0 ? row[0] : make_uint4(0, 0, 0, 0);
-    next1 = t < end && have1 ? row[8] : make_uint4(0, 0, 0, 0);
-    next_e = t < end && i < KT ? topk_idx[(int64_t)t * KT + i] : 0;
-  };
-  int t = begin + (tid >> 3);
-  fetch(t);
-  for (int t0 = begin; t0 < end; t0 += kThreads / 8, t += kThreads / 8) {
-    float x0[8], x1[8], dot[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    unpack8(x0, next0);
-    unpack8(x1, next1);
-    int my_e = next_e;
-    if (my_e < 0 || my_e >= E) {
-      moegps_report(status, MOEGPS_ERR_BAD_INDEX, t);
-      my_e = 0;
-    }
-    fetch(t + kThreads / 8);
-#pragma unroll
-    for (int j = 0; j < KT; ++j) {
-      const uint4* row = slice + __shfl_sync(0xffffffffu, my_e, group + j) * kSliceWords + i;
-      float wf[8];
-      unpack8(wf, row[0]);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) dot[j] = fmaf(x0[k], wf[k], dot[j]);
-      unpack8(wf, row[8]);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) dot[j] = fmaf(x1[k], wf[k], dot[j]);
-    }
-    const float sum = transpose_add8(dot, i);
-    if (t < end && i < KT) out[(int64_t)t * KT + i] = sum;
-  }
-}
-
 template <bool kSigmoid>
 __global__ void __launch_bounds__(kThreads)
-dlogit_kernel(const float* __restrict__ part, int slices, const float* __restrict__ bias,
-              const int32_t* __restrict__ topk_idx, const float* __restrict__ topk_w, const float* __restrict__ dtopk_w,
+dlogit_kernel(const float* __restrict__ logits, const int32_t* __restrict__ topk_idx, const float* __restrict__ topk_w, const float* __restrict__ dtopk_w,
               int64_t R, int K, int E, int S, int64_t Rcap, int max_units, const int32_t* __restrict__ slot_row_off,
               const int32_t* __restrict__ slot_off, float* __restrict__ dlogit, int32_t* __restrict__ unit_first,
               int4* __restrict__ units, int32_t* __restrict__ status) {
+  launch_dependents();
+  wait_for_predecessor();
   if (blockIdx.x == 0) {
     list_units(E, S, Rcap, max_units, slot_row_off, slot_off, unit_first, units, status);
     return;
@@ -161,11 +86,10 @@ dlogit_kernel(const float* __restrict__ part, int slices, const float* __restric
   float d = topk_w[p] * (dtopk_w[p] - m);
   if constexpr (kSigmoid) {
     const int e = topk_idx[p];
-    float logit = 0.f;
-#pragma unroll 16
-    for (int s = 0; s < slices; ++s) logit += part[(int64_t)s * R + p];
-    if (e < 0 || e >= E) d = 0.f;                     // reported by logits_kernel
-    else if (bias) logit += bias[e];
+    const bool valid = e >= 0 && e < E;
+    if (!valid) moegps_report(status, MOEGPS_ERR_BAD_INDEX, (int)(p / K));
+    const float logit = valid ? logits[p / K * E + e] : 0.f;
+    if (!valid) d = 0.f;
     d *= 1.f / (1.f + expf(logit));                   // 1 - sigmoid
   }
   dlogit[p] = d;
@@ -184,6 +108,8 @@ partial_kernel(const uint4* __restrict__ x, const int32_t* __restrict__ row_pair
   __shared__ float s_dl[kUnitRows];
   __shared__ int s_t[kUnitRows];
   __shared__ int s_n[2];
+  launch_dependents();
+  wait_for_predecessor();
   const int u = blockIdx.x;
   if (u >= unit_first[E]) return;
   const int4 unit = units[u];
@@ -240,6 +166,8 @@ reduce_kernel(const float* __restrict__ part, const float* __restrict__ part_b, 
               const int32_t* __restrict__ unit_first, float* __restrict__ dw_router, float* __restrict__ dbias) {
   __shared__ float4 s_acc[kWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  launch_dependents();
+  wait_for_predecessor();
   const int e = blockIdx.x;
   const int first = unit_first[e], last = unit_first[e + 1], n = last - first;
   const int W = n <= 4 ? 1 : n <= 8 ? 2 : n <= 16 ? 4 : 8;
@@ -278,49 +206,22 @@ int moegps_launch_route_backward(moegps_ctx* ctx, const void* x, const void* w_r
                                  const int32_t* slot_row_off, const int32_t* slot_off, const int32_t* row_pair,
                                  float* dlogit, float* dw_router, float* dbias, void* workspace, cudaStream_t st) {
   const moegps_shape_t& s = ctx->shape;
-  const int chunks = s.D / 8;
   const int64_t Rcap = moegps_rcap_of(s), R = (int64_t)s.T * s.K;
   const int max_units = (int)route_backward::max_units(s);
   const route_backward::Workspace ws = route_backward::carve(s, workspace);
-  const uint4 *xv = static_cast<const uint4*>(x), *rv = static_cast<const uint4*>(w_router);
-  const int slices = route_backward::slices(s);
-  if (s.gate_mode == 1) {
-    const size_t smem = (size_t)s.E * kSliceWords * sizeof(uint4);
-    // at most three blocks for every SM, the number that the slices of 256 experts leave room for: one more would wait
-    // for the others to end.  No block without 32 tokens of its own.
-    int pieces = 3 * ctx->sm_count / slices;
-    if (pieces < 1) pieces = 1;
-    if (pieces > (s.T + 31) / 32) pieces = (s.T + 31) / 32;
-    const int per = (s.T + pieces - 1) / pieces;
-    const dim3 grid(slices, (s.T + per - 1) / per);
-#define MOEGPS_CASE(KT)                                                                                                \
-  case KT:                                                                                                             \
-    if (!ctx->route_backward_attr_done)                                                                                \
-      MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(logits_kernel<KT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)); \
-    logits_kernel<KT><<<grid, kThreads, smem, st>>>(xv, rv, topk_idx, s.T, s.E, chunks, per, ws.part, ctx->d_status);   \
-    break;
-    switch (s.K) {
-      MOEGPS_CASE(1) MOEGPS_CASE(2) MOEGPS_CASE(3) MOEGPS_CASE(4)
-      MOEGPS_CASE(5) MOEGPS_CASE(6) MOEGPS_CASE(7) MOEGPS_CASE(8)
-      default: return MOEGPS_ERR_UNSUPPORTED_SHAPE;
-    }
-#undef MOEGPS_CASE
-    ctx->route_backward_attr_done = true;
-    MOEGPS_AFTER_LAUNCH(ctx);
-  }
-  const int blocks = 1 + (int)((R + kThreads - 1) / kThreads);
-#define MOEGPS_LAUNCH(G)                                                                                             \
-  dlogit_kernel<G><<<blocks, kThreads, 0, st>>>(ws.part, slices, bias, topk_idx, topk_w, dtopk_w, R, s.K, s.E, s.S, Rcap, \
-                                                max_units, slot_row_off, slot_off, dlogit, ws.unit_first, ws.units,  \
-                                                ctx->d_status)
-  if (s.gate_mode == 1) MOEGPS_LAUNCH(true); else MOEGPS_LAUNCH(false);
-#undef MOEGPS_LAUNCH
+  if (s.gate_mode == 1)
+    if (int rc = moegps_launch_route(ctx, x, w_router, bias, nullptr, nullptr, ws.logits, nullptr, nullptr, st)) return rc;
+  MOEGPS_CUDA_TRY(ctx, launch_after(s.gate_mode == 1 ? dlogit_kernel<true> : dlogit_kernel<false>,
+                                    dim3(1 + (unsigned)((R + kThreads - 1) / kThreads)), kThreads, 0, st, ws.logits, topk_idx,
+                                    topk_w, dtopk_w, R, s.K, s.E, s.S, Rcap, max_units, slot_row_off, slot_off, dlogit,
+                                    ws.unit_first, ws.units, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
-  partial_kernel<<<dim3(max_units, (chunks + kPartThreads - 1) / kPartThreads), kPartThreads, 0, st>>>(
-      xv, row_pair, dlogit, R, s.K, s.E, s.D, ws.unit_first, ws.units, ws.part, ws.part_b, dw_router,
-      ctx->d_status);
+  MOEGPS_CUDA_TRY(ctx, launch_after(partial_kernel, dim3(max_units, (s.D / 8 + kPartThreads - 1) / kPartThreads), kPartThreads, 0,
+                                    st, static_cast<const uint4*>(x), row_pair, dlogit, R, s.K, s.E, s.D, ws.unit_first,
+                                    ws.units, ws.part, ws.part_b, dw_router, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
-  reduce_kernel<<<dim3(s.E, (s.D + 127) / 128), kThreads, 0, st>>>(ws.part, ws.part_b, s.D, ws.unit_first, dw_router, dbias);
+  MOEGPS_CUDA_TRY(ctx, launch_after(reduce_kernel, dim3(s.E, (s.D + 127) / 128), kThreads, 0, st, ws.part, ws.part_b, s.D,
+                                    ws.unit_first, dw_router, dbias));
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }

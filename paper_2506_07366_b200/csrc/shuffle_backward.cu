@@ -43,6 +43,8 @@ combine_backward_kernel(const uint4* __restrict__ dout, const uint4* __restrict_
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = threadIdx.x % kTeam;
   const int64_t t = (int64_t)blockIdx.x * (kWarpsPerBlock / W) + warp / W;
   const bool active = t < T;
+  launch_dependents();
+  wait_for_predecessor();
   float dot[KT];
 #pragma unroll
   for (int j = 0; j < KT; ++j) dot[j] = 0.f;
@@ -107,6 +109,8 @@ dispatch_backward_kernel(const uint4* __restrict__ dxp, const int32_t* __restric
   const int warp = threadIdx.x >> 5, l = threadIdx.x % kTeam;
   const int64_t t = (int64_t)blockIdx.x * (kWarpsPerBlock / W) + warp / W;
   if (t >= T) return;
+  launch_dependents();
+  wait_for_predecessor();
   int row[KT], expert[KT];
   float dl[KT];
   load_rows<KT>(row, pair_row, t, Rcap, l == 0, status);
@@ -158,16 +162,15 @@ int moegps_launch_combine_backward(moegps_ctx* ctx, const void* dout, const void
   const bool wide = s.D >= kWideColumns;
   const int per = wide ? 1 : kWarpsPerBlock;
   const int blocks = (s.T + per - 1) / per;
-#define MOEGPS_CASE(KT)                                                                                                     \
-  case KT:                                                                                                                  \
-    if (wide)                                                                                                               \
-      combine_backward_kernel<KT, kWarpsPerBlock><<<blocks, kThreads, 0, st>>>(d, y, pair_row, topk_w, s.T, chunks, Rcap, o, \
-                                                                               dtopk_w, ctx->d_status);                     \
-    else                                                                                                                    \
-      combine_backward_kernel<KT, 1><<<blocks, kThreads, 0, st>>>(d, y, pair_row, topk_w, s.T, chunks, Rcap, o, dtopk_w,    \
-                                                                  ctx->d_status);                                           \
+#define MOEGPS_LAUNCH(KT, W)                                                                                               \
+  MOEGPS_CUDA_TRY(ctx, launch_after(combine_backward_kernel<KT, W>, dim3(blocks), kThreads, 0, st, d, y, pair_row, topk_w, s.T, \
+                                    chunks, Rcap, o, dtopk_w, ctx->d_status))
+#define MOEGPS_CASE(KT)                                                        \
+  case KT:                                                                     \
+    if (wide) MOEGPS_LAUNCH(KT, kWarpsPerBlock); else MOEGPS_LAUNCH(KT, 1);    \
     break;
   MOEGPS_FOR_K(s.K, MOEGPS_CASE)
+#undef MOEGPS_LAUNCH
 #undef MOEGPS_CASE
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
@@ -184,8 +187,8 @@ int moegps_launch_dispatch_backward(moegps_ctx* ctx, const void* dxp, const int3
   const int per = wide ? 1 : kWarpsPerBlock;
   const int blocks = (s.T + per - 1) / per;
 #define MOEGPS_LAUNCH(KT, W, R)                                                                                          \
-  dispatch_backward_kernel<KT, W, R><<<blocks, kThreads, 0, st>>>(v, pair_row, topk_idx, dlogit, r, s.T, s.E, chunks, Rcap, \
-                                                                  o, ctx->d_status)
+  MOEGPS_CUDA_TRY(ctx, launch_after(dispatch_backward_kernel<KT, W, R>, dim3(blocks), kThreads, 0, st, v, pair_row, topk_idx, \
+                                    dlogit, r, s.T, s.E, chunks, Rcap, o, ctx->d_status))
 #define MOEGPS_CASE(KT)                                                                                  \
   case KT:                                                                                               \
     if (dlogit) {                                                                                        \
