@@ -439,10 +439,11 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
       if (!ok) linger();
     }
   } else if (warp == 1) {
-    // The whole warp walks the K blocks: lane 0 waits and issues; at the last block of a slot the other lanes join it
-    // to blank the rows behind the slot's end that the last MMA would read (at most 15, of both operands, since
-    // 0 * NaN is NaN).  A failed wait leaves the loops at the next tile, for all lanes together.
+    // Lane 0 waits for the full K blocks of a slot and issues their MMAs in a loop of its own.  For the block at the slot's
+    // end the other lanes join it, to blank the rows behind the end that the last MMA reads (at most 15, of both operands,
+    // since 0 * NaN is NaN).  A failed wait leaves the loops at the next tile, for all lanes together.
     constexpr uint32_t idesc = idesc_bf16_f32(BM, BNACC, true, true);
+    const uint32_t ring = smem_u32(stage_mem);
     int stage = 0, acc = 0;
     uint32_t phase = 0, acc_phase = 0;
     bool ok = true;
@@ -457,40 +458,57 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
       const uint32_t d_tmem = tmem_base + (uint32_t)acc * BNACC;
       uint32_t accumulate = 0;
       for (int s = first; s < last; ++s) {
-        const int n = sr.ext[s].y;
-        for (int r = 0; r < n; r += BK) {
-          const int valid = min(BK, n - r), steps = (valid + 15) >> 4;
-          if (valid & 15) {
-            __syncwarp();                          // lane 0 has consumed the stages before: the phase is unambiguous
-            const bool here = ok && mbar_wait(&bar.full[stage], phase, bar.abort_flag);
-            ok = __all_sync(0xffffffffu, here);
-            if (ok) {
-              uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
-              const int blank = 16 * steps - valid;         // rows valid .. 16 steps - 1, eight 16-byte words each
-              for (int i = lane; i < 6 * 8 * blank; i += 32) {
-                const int word = i & 7, row = valid + (i >> 3) % blank, box = (i >> 3) / blank;
-                *reinterpret_cast<uint4*>(sa + box * kBoxBytes + row * kRowBytes + word * 16) = make_uint4(0, 0, 0, 0);
-              }
-              fence_proxy_async();
+        const int n = sr.ext[s].y, blocks = n / BK, tail = n % BK;
+        if (lane == 0 && ok) {
+          int st = stage;
+          uint32_t ph = phase;
+          for (int b = 0; b < blocks; ++b) {
+            if (!mbar_wait(&bar.full[st], ph, bar.abort_flag)) { ok = false; break; }
+            tc_fence_after_sync();
+            const uint64_t da = smem_desc_mn(ring + (uint32_t)st * kStageBytes, kBoxBytes);
+            const uint64_t db = smem_desc_mn(ring + (uint32_t)st * kStageBytes + kABytes, kBoxBytes);
+#pragma unroll
+            for (int k = 0; k < BK / 16; ++k) {
+              mma_bf16(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
+              accumulate = 1;
             }
-            __syncwarp();
+            mma_commit(&bar.empty[st]);
+            if (++st == kStages) { st = 0; ph ^= 1u; }
           }
-          if (lane == 0 && ok) {
-            ok = mbar_wait(&bar.full[stage], phase, bar.abort_flag);
-            if (ok) {
-              tc_fence_after_sync();
-              const uint32_t sa = smem_u32(stage_mem + (size_t)stage * kStageBytes);
-              const uint64_t da = smem_desc_mn(sa, kBoxBytes);
-              const uint64_t db = smem_desc_mn(sa + kABytes, kBoxBytes);
-              for (int k = 0; k < steps; ++k) {
-                mma_bf16(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
-                accumulate = 1;
-              }
-              mma_commit(&bar.empty[stage]);
-            }
-          }
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
+        phase ^= ((stage + blocks) / kStages) & 1u;
+        stage = (stage + blocks) % kStages;
+        if (tail == 0) continue;
+        const int steps = (tail + 15) >> 4;
+        if (tail & 15) {
+          __syncwarp();                            // lane 0 has consumed the stages before: the phase is unambiguous
+          const bool here = ok && mbar_wait(&bar.full[stage], phase, bar.abort_flag);
+          ok = __all_sync(0xffffffffu, here);
+          if (ok) {
+            uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
+            // rows tail .. 16 steps - 1 of the six boxes: eight lanes a row, four rows at a time
+            for (int row = tail + (lane >> 3); row < 16 * steps; row += 4)
+#pragma unroll
+              for (int box = 0; box < 6; ++box)
+                *reinterpret_cast<uint4*>(sa + box * kBoxBytes + row * kRowBytes + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+            fence_proxy_async();
+          }
+          __syncwarp();
+        }
+        if (lane == 0 && ok) {
+          ok = mbar_wait(&bar.full[stage], phase, bar.abort_flag);
+          if (ok) {
+            tc_fence_after_sync();
+            const uint64_t da = smem_desc_mn(ring + (uint32_t)stage * kStageBytes, kBoxBytes);
+            const uint64_t db = smem_desc_mn(ring + (uint32_t)stage * kStageBytes + kABytes, kBoxBytes);
+            for (int k = 0; k < steps; ++k) {
+              mma_bf16(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
+              accumulate = 1;
+            }
+            mma_commit(&bar.empty[stage]);
+          }
+        }
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
       ok = __shfl_sync(0xffffffffu, ok, 0);
       if (!ok) break;
