@@ -300,18 +300,29 @@ struct SlotRows {
   int2 ext[kMaxS];
 };
 
-// Tiles are blocks of BM x BNACC elements of one weight gradient.  Per expert: dW1, dW3 (F x D each), then dW2 (D x F).
-// Inside one gradient the order runs over bands of kBand row tiles, column by column: tiles in flight at the same time
-// form a near-square patch of the gradient, so the operand columns they read are shared in L2.
-constexpr int kBand = 12;
+// Tiles are 256 x 256 blocks of one weight gradient, worked by a pair of CTAs (128 rows each; each loads its rows of the
+// left operand and half the columns of the right one, 32 KiB for a K block where a CTA by itself needs 48 KiB for a
+// 128 x 256 tile).  Neither dimension is ragged here, unlike the rows of the other GEMMs.
+// Per expert: dW1, dW3 (F x D each), then dW2 (D x F).  Inside one gradient the order runs over bands of kBand row tiles,
+// column by column: tiles in flight at the same time form a near-square patch of the gradient, so the operand columns
+// they read are shared in L2.
+struct WeightCfg {
+  static constexpr int BM2 = 2 * BM, kAHalf = 2 * kBoxBytes, kStageBytes = 4 * kBoxBytes;     // per CTA
+  static constexpr int kStages = 6, kAccs = 2, kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps, kTmemCols = kAccs * BNACC;
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + sizeof(SlotRows) + 256 +
+                                  (size_t)kEpiWarps * kStagingBytesPerWarp;
+};
+static_assert(WeightCfg::kSmem + 257 * 4 <= 227 * 1024, "one CTA per SM");
+constexpr int kBand = 8;
+
 struct WTile {
   int expert, which, m0, n0, m_dim, n_dim;
 };
 struct WGeom {
   int F, D, per1, per2;              // tiles of dW1 (and dW3), of dW2
   __host__ __device__ WGeom(int F_, int D_) : F(F_), D(D_) {
-    per1 = ((F + BM - 1) / BM) * ((D + BNACC - 1) / BNACC);
-    per2 = ((D + BM - 1) / BM) * ((F + BNACC - 1) / BNACC);
+    per1 = ((F + WeightCfg::BM2 - 1) / WeightCfg::BM2) * ((D + BNACC - 1) / BNACC);
+    per2 = ((D + WeightCfg::BM2 - 1) / WeightCfg::BM2) * ((F + BNACC - 1) / BNACC);
   }
   __host__ __device__ int per_expert() const { return 2 * per1 + per2; }
 };
@@ -323,12 +334,12 @@ __device__ __forceinline__ WTile decode_wtile(const WGeom& g, int tile) {
   q -= t.which * g.per1;
   t.m_dim = t.which == 2 ? g.D : g.F;
   t.n_dim = t.which == 2 ? g.F : g.D;
-  const int mt = (t.m_dim + BM - 1) / BM, nt = (t.n_dim + BNACC - 1) / BNACC;
+  const int mt = (t.m_dim + WeightCfg::BM2 - 1) / WeightCfg::BM2, nt = (t.n_dim + BNACC - 1) / BNACC;
   const int band = q / (kBand * nt);
   q -= band * kBand * nt;
   const int high = min(kBand, mt - band * kBand);
   t.n0 = q / high * BNACC;
-  t.m0 = (band * kBand + q % high) * BM;
+  t.m0 = (band * kBand + q % high) * WeightCfg::BM2;
   return t;
 }
 
@@ -339,22 +350,61 @@ __device__ __forceinline__ int rows_of(const SlotRows& sr, int first, int last) 
   return n;
 }
 
-template <class Cfg>
-__global__ void __launch_bounds__(Cfg::kThreads, Cfg::kCtasPerSm)
+// The barriers.  full counts both CTAs' bytes on the leader; empty and acc_full are signalled in both CTAs by the leader's
+// commits; acc_empty collects both CTAs' epilogue warps on the leader.  At a slot's end, where rows have to be blanked
+// before the MMA, the second CTA's bytes go to its own tail_full, and it reports to the leader's tail_ready when its rows
+// are blank.
+struct PairBars {
+  uint64_t *full, *empty, *tail_full, *tail_ready, *acc_full, *acc_empty;
+  uint32_t* tmem_slot;
+  volatile int* abort_flag;
+  __device__ explicit PairBars(uint8_t* at) {
+    constexpr int n = WeightCfg::kStages;
+    full = reinterpret_cast<uint64_t*>(at);
+    empty = full + n;
+    tail_full = empty + n;
+    tail_ready = tail_full + n;
+    acc_full = tail_ready + n;
+    acc_empty = acc_full + WeightCfg::kAccs;
+    tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + WeightCfg::kAccs);
+    abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  }
+  __device__ void init() const {
+    for (int i = 0; i < 4 * WeightCfg::kStages + WeightCfg::kAccs; ++i) mbar_init(&full[i], 1);
+    for (int i = 0; i < WeightCfg::kAccs; ++i) mbar_init(&acc_empty[i], 2 * WeightCfg::kEpiWarps);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+};
+static_assert((4 * WeightCfg::kStages + 2 * WeightCfg::kAccs) * 8 + 8 <= 256, "barriers fit their space");
+
+// Blanks rows [tail, 16 steps) of a stage's four boxes, by a warp: eight lanes a row, four rows at a time.
+__device__ __forceinline__ void blank_rows(uint8_t* stage, int tail, int steps, int lane) {
+  for (int row = tail + (lane >> 3); row < 16 * steps; row += 4)
+#pragma unroll
+    for (int box = 0; box < 4; ++box)
+      *reinterpret_cast<uint4*>(stage + box * kBoxBytes + row * kRowBytes + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+  fence_proxy_async();
+}
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WeightCfg::kThreads, 1)
 weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __grid_constant__ CUtensorMap tm_dup,
                        const __grid_constant__ CUtensorMap tm_dyp, const __grid_constant__ CUtensorMap tm_xp,
                        const __grid_constant__ CUtensorMap tm_h, const int32_t* __restrict__ slot_row_off,
                        const int32_t* __restrict__ slot_off, const int32_t* __restrict__ row_pair, int S, int E, int F, int D,
                        int row_align, int rcap, __nv_bfloat16* __restrict__ dw_gate, __nv_bfloat16* __restrict__ dw_up,
                        __nv_bfloat16* __restrict__ dw_down, int32_t* __restrict__ status) {
-  constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs, kThreads = Cfg::kThreads;
+  using Cfg = WeightCfg;
+  constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs, kThreads = Cfg::kThreads, kStageBytes = Cfg::kStageBytes;
   extern __shared__ uint8_t smem_raw[];
   __shared__ int32_t s_slot_off[256 + 1];
   uint8_t* stage_mem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   SlotRows& sr = *reinterpret_cast<SlotRows*>(stage_mem + (size_t)kStages * kStageBytes);
-  const Bars<Cfg> bar(stage_mem + (size_t)kStages * kStageBytes + sizeof(SlotRows));
+  const PairBars bar(stage_mem + (size_t)kStages * kStageBytes + sizeof(SlotRows));
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_ctarank();           // 0: leader
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const WGeom geom(F, D);
   const int total_tiles = E * geom.per_expert();
 
@@ -369,8 +419,8 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
   launch_dependents();
   wait_for_predecessor();
   if (warp == 1) {
-    tmem_alloc(bar.tmem_slot, Cfg::kTmemCols);
-    tmem_relinquish();
+    tmem_alloc_pair(bar.tmem_slot, Cfg::kTmemCols);
+    tmem_relinquish_pair();
   }
   for (int s = threadIdx.x; s < S; s += kThreads) {
     const int lo = slot_row_off[s], hi = slot_row_off[s + 1];
@@ -406,8 +456,9 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
     }
     s_slot_off[e] = v;
   }
+  __syncwarp();
   tc_fence_before_sync();
-  __syncthreads();
+  cluster_sync_all();                                // both CTAs' barriers and tables exist
   tc_fence_after_sync();
   const uint32_t tmem_base = *bar.tmem_slot;
 
@@ -416,22 +467,30 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
+      const uint32_t leader_full = map_to_cta(smem_u32(bar.full), 0);
+      for (int tile = pair; ok && tile < total_tiles; tile += pairs) {
         const WTile t = decode_wtile(geom, tile);
         const CUtensorMap* ta = t.which == 0 ? &tm_dgate : t.which == 1 ? &tm_dup : &tm_dyp;
         const CUtensorMap* tbm = t.which == 2 ? &tm_h : &tm_xp;
+        const int m0 = t.m0 + rank * BM, n0 = t.n0 + rank * (BNACC / 2);
         const int last = s_slot_off[t.expert + 1];
         for (int s = s_slot_off[t.expert]; ok && s < last; ++s) {
           const int2 ext = sr.ext[s];
           for (int r = 0; r < ext.y; r += BK) {
             if (!mbar_wait(&bar.empty[stage], phase ^ 1u, bar.abort_flag)) { ok = false; break; }
             uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
-            mbar_arrive_expect_tx(&bar.full[stage], kStageBytes);
+            const bool blank = ext.y - r < BK && ((ext.y - r) & 15) != 0;
+            uint32_t to = leader_full + stage * 8;
+            if (rank == 0) {
+              mbar_arrive_expect_tx(&bar.full[stage], blank ? kStageBytes : 2 * kStageBytes);
+            } else if (blank) {
+              mbar_arrive_expect_tx(&bar.tail_full[stage], kStageBytes);
+              to = map_to_cta(smem_u32(&bar.tail_full[stage]), 1);
+            }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) tma_load_2d(sa + i * kBoxBytes, ta, &bar.full[stage], t.m0 + 64 * i, ext.x + r);
+            for (int i = 0; i < 2; ++i) tma_load_2d_pair(sa + i * kBoxBytes, ta, to, m0 + 64 * i, ext.x + r);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              tma_load_2d(sa + kABytes + i * kBoxBytes, tbm, &bar.full[stage], t.n0 + 64 * i, ext.x + r);
+            for (int i = 0; i < 2; ++i) tma_load_2d_pair(sa + Cfg::kAHalf + i * kBoxBytes, tbm, to, n0 + 64 * i, ext.x + r);
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
         }
@@ -439,40 +498,44 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
       if (!ok) linger();
     }
   } else if (warp == 1) {
-    // Lane 0 waits for the full K blocks of a slot and issues their MMAs in a loop of its own.  For the block at the slot's
-    // end the other lanes join it, to blank the rows behind the end that the last MMA reads (at most 15, of both operands,
-    // since 0 * NaN is NaN).  A failed wait leaves the loops at the next tile, for all lanes together.
-    constexpr uint32_t idesc = idesc_bf16_f32(BM, BNACC, true, true);
+    // Leader: lane 0 waits for the full K blocks of a slot and issues their MMAs in a loop of its own.  For the block at
+    // the slot's end the other lanes join it, to blank the rows behind the end that the last MMA reads (at most 15, of
+    // both operands, since 0 * NaN is NaN); the second CTA's warp does the same for its part.  A failed wait leaves the
+    // loops at the next tile, for all lanes together.
+    constexpr uint32_t idesc = idesc_bf16_f32(Cfg::BM2, BNACC, true, true);
     const uint32_t ring = smem_u32(stage_mem);
+    const uint32_t ready = map_to_cta(smem_u32(bar.tail_ready), 0);
     int stage = 0, acc = 0;
-    uint32_t phase = 0, acc_phase = 0;
+    uint32_t phase = 0, acc_phase = 0, tail_phase = 0;         // tail_phase: a bit for each stage
     bool ok = true;
-    for (int tile = blockIdx.x; tile < total_tiles; tile += gridDim.x) {
+    for (int tile = pair; tile < total_tiles; tile += pairs) {
       const WTile t = decode_wtile(geom, tile);
       const int first = s_slot_off[t.expert], last = s_slot_off[t.expert + 1];
       if (rows_of(sr, first, last) == 0) continue;
-      if (lane == 0) ok = mbar_wait(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag);
-      ok = __shfl_sync(0xffffffffu, ok, 0);
-      if (!ok) break;
-      tc_fence_after_sync();
+      if (rank == 0) {
+        if (lane == 0) ok = mbar_wait_cluster(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag);
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        tc_fence_after_sync();
+      }
       const uint32_t d_tmem = tmem_base + (uint32_t)acc * BNACC;
       uint32_t accumulate = 0;
       for (int s = first; s < last; ++s) {
         const int n = sr.ext[s].y, blocks = n / BK, tail = n % BK;
-        if (lane == 0 && ok) {
+        if (rank == 0 && lane == 0 && ok) {
           int st = stage;
           uint32_t ph = phase;
           for (int b = 0; b < blocks; ++b) {
             if (!mbar_wait(&bar.full[st], ph, bar.abort_flag)) { ok = false; break; }
             tc_fence_after_sync();
             const uint64_t da = smem_desc_mn(ring + (uint32_t)st * kStageBytes, kBoxBytes);
-            const uint64_t db = smem_desc_mn(ring + (uint32_t)st * kStageBytes + kABytes, kBoxBytes);
+            const uint64_t db = smem_desc_mn(ring + (uint32_t)st * kStageBytes + Cfg::kAHalf, kBoxBytes);
 #pragma unroll
             for (int k = 0; k < BK / 16; ++k) {
-              mma_bf16(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
+              mma_bf16_pair(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
               accumulate = 1;
             }
-            mma_commit(&bar.empty[st]);
+            mma_commit_pair(&bar.empty[st]);
             if (++st == kStages) { st = 0; ph ^= 1u; }
           }
         }
@@ -482,37 +545,36 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
         const int steps = (tail + 15) >> 4;
         if (tail & 15) {
           __syncwarp();                            // lane 0 has consumed the stages before: the phase is unambiguous
-          const bool here = ok && mbar_wait(&bar.full[stage], phase, bar.abort_flag);
+          const uint32_t tp = (tail_phase >> stage) & 1u;
+          const bool here = ok && (rank == 0 ? mbar_wait(&bar.full[stage], phase, bar.abort_flag)
+                                             : mbar_wait(&bar.tail_full[stage], tp, bar.abort_flag));
           ok = __all_sync(0xffffffffu, here);
-          if (ok) {
-            uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
-            // rows tail .. 16 steps - 1 of the six boxes: eight lanes a row, four rows at a time
-            for (int row = tail + (lane >> 3); row < 16 * steps; row += 4)
-#pragma unroll
-              for (int box = 0; box < 6; ++box)
-                *reinterpret_cast<uint4*>(sa + box * kBoxBytes + row * kRowBytes + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
-            fence_proxy_async();
-          }
+          if (ok) blank_rows(stage_mem + (size_t)stage * kStageBytes, tail, steps, lane);
           __syncwarp();
+          if (lane == 0 && ok) {
+            if (rank == 1) mbar_arrive_remote(ready + stage * 8);
+            else ok = mbar_wait_cluster(&bar.tail_ready[stage], tp, bar.abort_flag);
+          }
+          tail_phase ^= 1u << stage;
         }
-        if (lane == 0 && ok) {
+        if (rank == 0 && lane == 0 && ok) {
           ok = mbar_wait(&bar.full[stage], phase, bar.abort_flag);
           if (ok) {
             tc_fence_after_sync();
             const uint64_t da = smem_desc_mn(ring + (uint32_t)stage * kStageBytes, kBoxBytes);
-            const uint64_t db = smem_desc_mn(ring + (uint32_t)stage * kStageBytes + kABytes, kBoxBytes);
+            const uint64_t db = smem_desc_mn(ring + (uint32_t)stage * kStageBytes + Cfg::kAHalf, kBoxBytes);
             for (int k = 0; k < steps; ++k) {
-              mma_bf16(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
+              mma_bf16_pair(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
               accumulate = 1;
             }
-            mma_commit(&bar.empty[stage]);
+            mma_commit_pair(&bar.empty[stage]);
           }
         }
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
       ok = __shfl_sync(0xffffffffu, ok, 0);
       if (!ok) break;
-      if (lane == 0) mma_commit(&bar.acc_full[acc]);
+      if (rank == 0 && lane == 0) mma_commit_pair(&bar.acc_full[acc]);
       if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
     }
     if (!ok && lane == 0) linger();
@@ -521,12 +583,13 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
     constexpr int kShare = BNACC / (Cfg::kEpiWarps / 4);
     const int c_begin = ((warp - 2) >> 2) * kShare;
     uint8_t* staging = stage_mem + (size_t)kStages * kStageBytes + sizeof(SlotRows) + 256 + (warp - 2) * kStagingBytesPerWarp;
+    const uint32_t leader_empty = map_to_cta(smem_u32(bar.acc_empty), 0);
     int acc = 0;
     uint32_t acc_phase = 0;
-    for (int tile = blockIdx.x; tile < total_tiles; tile += gridDim.x) {
+    for (int tile = pair; tile < total_tiles; tile += pairs) {
       const WTile t = decode_wtile(geom, tile);
       __nv_bfloat16* out = (t.which == 0 ? dw_gate : t.which == 1 ? dw_up : dw_down) + (size_t)t.expert * t.m_dim * t.n_dim;
-      const int row0 = t.m0 + quarter * 32;
+      const int row0 = t.m0 + rank * BM + quarter * 32;
       if (rows_of(sr, s_slot_off[t.expert], s_slot_off[t.expert + 1]) == 0) {      // no token chose this expert
         drain_plain<true>(0, staging, lane, out, row0, t.m_dim, t.n0, t.n_dim, c_begin, c_begin + kShare);
         continue;
@@ -537,26 +600,20 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
       drain_plain<false>(taddr, staging, lane, out, row0, t.m_dim, t.n0, t.n_dim, c_begin, c_begin + kShare);
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bar.acc_empty[acc]);
+      if (lane == 0) mbar_arrive_remote(leader_empty + acc * 8);
       if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
     }
   }
 
   __syncwarp();
   tc_fence_before_sync();
-  __syncthreads();
+  cluster_sync_all();                                // nobody touches the other CTA's memory after this
   if (threadIdx.x == 0 && *bar.abort_flag) moegps_report(status, MOEGPS_ERR_TIMEOUT, (int)blockIdx.x);
   if (warp == 1) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem_base, Cfg::kTmemCols);
+    tmem_dealloc_pair(tmem_base, Cfg::kTmemCols);
   }
 }
-
-template <class Cfg>
-constexpr size_t weight_smem_bytes() {
-  return 1024 + (size_t)Cfg::kStages * kStageBytes + sizeof(SlotRows) + 256 + (size_t)Cfg::kEpiWarps * kStagingBytesPerWarp;
-}
-static_assert(weight_smem_bytes<WideCfg>() + 257 * 4 <= 227 * 1024, "one CTA per SM");
 
 int tmap_failed(moegps_ctx* ctx) {
   ctx->last_cuda_error = (int)cudaErrorInvalidValue;
@@ -642,13 +699,12 @@ int moegps_launch_ffn_backward_weights(moegps_ctx* ctx, const void* dyp, const v
         moegps_make_tmap_2d(&t_dyp, dyp, rcap, s.D, BK, 64) && moegps_make_tmap_2d(&t_xp, xp, rcap, s.D, BK, 64) &&
         moegps_make_tmap_2d(&t_h, h_ws, rcap, s.F, BK, 64)))
     return tmap_failed(ctx);
-  constexpr size_t smem = weight_smem_bytes<WideCfg>();
+  constexpr size_t smem = WeightCfg::kSmem;
   if (!ctx->weight_gradient_attr_done) {
-    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(weight_gradient_kernel<WideCfg>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                              (int)smem));
+    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(weight_gradient_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     ctx->weight_gradient_attr_done = true;
   }
-  MOEGPS_CUDA_TRY(ctx, launch_after(weight_gradient_kernel<WideCfg>, dim3(ctx->sm_count), WideCfg::kThreads, smem, st, t_dgate,
+  MOEGPS_CUDA_TRY(ctx, launch_after(weight_gradient_kernel, dim3(ctx->sm_count / 2 * 2), WeightCfg::kThreads, smem, st, t_dgate,
                                     t_dup, t_dyp, t_xp, t_h, slot_row_off, slot_off, row_pair, s.S, s.E, s.F, s.D, s.row_align,
                                     (int)rcap, static_cast<__nv_bfloat16*>(dw_gate), static_cast<__nv_bfloat16*>(dw_up),
                                     static_cast<__nv_bfloat16*>(dw_down), ctx->d_status));
