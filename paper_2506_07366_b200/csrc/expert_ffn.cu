@@ -307,6 +307,11 @@ bool moegps_make_tmap_3d(CUtensorMap* tm, const void* base, uint64_t batch, uint
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// bf16 [batch, rows, cols]; box = 32 columns x 32 rows x 1, 64-byte swizzle: what an epilogue warp stores at a time.
+bool moegps_make_tmap_store(CUtensorMap* tm, void* base, uint64_t batch, uint64_t rows, uint64_t cols) {
+  return moegps_make_tmap_3d(tm, base, batch, rows, cols, 32, 32);
+}
+
 namespace {
 
 int tmap_failed(moegps_ctx* ctx) {

@@ -114,23 +114,16 @@ __device__ __forceinline__ void drain_act(uint32_t taddr, uint8_t* staging, int 
   }
 }
 
-// Epilogue of (2) and (3): accumulator -> bf16 -> global.  kZero: the sum has no terms.
-template <bool kZero>
+// Epilogue of (2): accumulator -> bf16 -> global.
 __device__ __forceinline__ void drain_plain(uint32_t taddr, uint8_t* staging, int lane, __nv_bfloat16* out, int row0,
                                             int row_end, int col0, int n_dim, int c_begin, int c_end) {
 #pragma unroll 1
   for (int c0 = c_begin; c0 < c_end; c0 += 32) {
-    uint32_t o[16];
-    if constexpr (kZero) {
+    uint32_t o[16], a[32];
+    tmem_ld32(taddr + c0, a);
+    tmem_ld_wait();
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[i] = 0;
-    } else {
-      uint32_t a[32];
-      tmem_ld32(taddr + c0, a);
-      tmem_ld_wait();
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[i] = pack_bf16(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1]));
-    }
+    for (int i = 0; i < 16; ++i) o[i] = pack_bf16(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1]));
     store_chunk(o, staging, lane, out, row0, row_end, col0 + c0, n_dim);
   }
 }
@@ -275,7 +268,7 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
       if constexpr (kAct)
         drain_act(taddr, staging, lane, kept, block, act_out, row0, tc.row_end, col0, n_dim, c_begin, c_begin + kShare, rcap);
       else
-        drain_plain<false>(taddr, staging, lane, out, row0, tc.row_end, col0, n_dim, c_begin, c_begin + kShare);
+        drain_plain(taddr, staging, lane, out, row0, tc.row_end, col0, n_dim, c_begin, c_begin + kShare);
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bar.acc_empty[acc]);
@@ -300,60 +293,70 @@ struct SlotRows {
   int2 ext[kMaxS];
 };
 
-// Tiles are 256 x 256 blocks of one weight gradient, worked by a pair of CTAs (128 rows each; each loads its rows of the
-// left operand and half the columns of the right one, 32 KiB for a K block where a CTA by itself needs 48 KiB for a
-// 128 x 256 tile).  Neither dimension is ragged here, unlike the rows of the other GEMMs.
-// Per expert: dW1, dW3 (F x D each), then dW2 (D x F).  Inside one gradient the order runs over bands of kBand row tiles,
-// column by column: tiles in flight at the same time form a near-square patch of the gradient, so the operand columns
-// they read are shared in L2.
+// A tile is 256 x 256, worked by a pair of CTAs: each has 128 of the rows, loads them and half the columns of the right
+// operand (32 KiB for a K block, where a CTA by itself needs 48 KiB for a 128 x 256 tile), and keeps its part of the sum in
+// its own TMEM.  Neither dimension is ragged here, unlike the rows of the other GEMMs.
+// Per expert there are two problems: dgate and dup above one another, times xp (dW1 and dW3; an even number of 128-row
+// granules, whichever gradient each belongs to, so no pair has an idle half), and dyp times h (dW2).  A last column tile with
+// at most 128 columns is worked as 256 x 128.  Inside a problem the order runs over bands of kBand tiles in M, column by
+// column: tiles in flight at the same time form a near-square patch, so the operand columns they read are shared in L2.
 struct WeightCfg {
-  static constexpr int BM2 = 2 * BM, kAHalf = 2 * kBoxBytes, kStageBytes = 4 * kBoxBytes;     // per CTA
-  static constexpr int kStages = 6, kAccs = 2, kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps, kTmemCols = kAccs * BNACC;
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + sizeof(SlotRows) + 256 +
-                                  (size_t)kEpiWarps * kStagingBytesPerWarp;
+  static constexpr int kAHalf = 2 * kBoxBytes, kStageBytes = 4 * kBoxBytes;                  // per CTA
+  static constexpr int kStages = 6, kAccs = 2, kEpiWarps = 8, kTmemCols = kAccs * BNACC;
+  static constexpr int kBlankWarp = 2 + kEpiWarps, kThreads = 32 * (3 + kEpiWarps);          // producer, MMA, epilogue, blank
+  static constexpr int kOutBytes = 32 * 64;                                  // of an epilogue warp: 32 rows x 32 columns, bf16
+  static constexpr int kAhead = 8;                                           // > tiles that the producer can be ahead: kStages
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kOutBytes + 8 * kMaxS + 256;
 };
-static_assert(WeightCfg::kSmem + 257 * 4 <= 227 * 1024, "one CTA per SM");
+static_assert(WeightCfg::kSmem + 2 * 257 * 4 <= 227 * 1024, "one CTA per SM");
 constexpr int kBand = 8;
 
 struct WTile {
-  int expert, which, m0, n0, m_dim, n_dim;
+  int expert, problem, m, n0;       // m: tile in M; n0: first column
 };
 struct WGeom {
-  int F, D, per1, per2;              // tiles of dW1 (and dW3), of dW2
-  __host__ __device__ WGeom(int F_, int D_) : F(F_), D(D_) {
-    per1 = ((F + WeightCfg::BM2 - 1) / WeightCfg::BM2) * ((D + BNACC - 1) / BNACC);
-    per2 = ((D + WeightCfg::BM2 - 1) / WeightCfg::BM2) * ((F + BNACC - 1) / BNACC);
+  int F, D, granules_f, mt[2], nt[2], per[2];     // tiles in M and N of the two problems, and in all
+  __device__ WGeom(int F_, int D_) : F(F_), D(D_) {
+    granules_f = (F + BM - 1) / BM;
+    mt[0] = granules_f;
+    mt[1] = ((D + BM - 1) / BM + 1) / 2;
+    nt[0] = (D + BNACC - 1) / BNACC;
+    nt[1] = (F + BNACC - 1) / BNACC;
+    per[0] = mt[0] * nt[0];
+    per[1] = mt[1] * nt[1];
   }
-  __host__ __device__ int per_expert() const { return 2 * per1 + per2; }
+  __device__ WTile decode(int tile) const {
+    WTile t;
+    const int all = per[0] + per[1];
+    t.expert = tile / all;
+    int q = tile - t.expert * all;
+    t.problem = q >= per[0];
+    const int p_mt = t.problem ? mt[1] : mt[0], p_nt = t.problem ? nt[1] : nt[0];
+    if (t.problem) q -= per[0];
+    const int band = q / (kBand * p_nt);
+    q -= band * kBand * p_nt;
+    const int high = min(kBand, p_mt - band * kBand), col = q / high;
+    t.n0 = col * BNACC;
+    t.m = band * kBand + q - col * high;
+    return t;
+  }
+  // columns that a tile works
+  __device__ int width(const WTile& t) const { return (t.problem ? F : D) - t.n0 > BNACC / 2 ? BNACC : BNACC / 2; }
+  // which gradient (0 dW1, 1 dW3, 2 dW2) and first row of it a CTA of the pair has
+  __device__ void rows(const WTile& t, int rank, int& which, int& m0) const {
+    int g = 2 * t.m + rank;
+    which = 2;
+    if (t.problem == 0) {
+      which = g >= granules_f;
+      g -= which * granules_f;
+    }
+    m0 = g * BM;
+  }
 };
-__device__ __forceinline__ WTile decode_wtile(const WGeom& g, int tile) {
-  WTile t;
-  t.expert = tile / g.per_expert();
-  int q = tile - t.expert * g.per_expert();
-  t.which = q < g.per1 ? 0 : q < 2 * g.per1 ? 1 : 2;
-  q -= t.which * g.per1;
-  t.m_dim = t.which == 2 ? g.D : g.F;
-  t.n_dim = t.which == 2 ? g.F : g.D;
-  const int mt = (t.m_dim + WeightCfg::BM2 - 1) / WeightCfg::BM2, nt = (t.n_dim + BNACC - 1) / BNACC;
-  const int band = q / (kBand * nt);
-  q -= band * kBand * nt;
-  const int high = min(kBand, mt - band * kBand);
-  t.n0 = q / high * BNACC;
-  t.m0 = (band * kBand + q % high) * WeightCfg::BM2;
-  return t;
-}
-
-// occupied rows of expert e's slots [first, last)
-__device__ __forceinline__ int rows_of(const SlotRows& sr, int first, int last) {
-  int n = 0;
-  for (int s = first; s < last; ++s) n += sr.ext[s].y;
-  return n;
-}
 
 // The barriers.  full counts both CTAs' bytes on the leader; empty and acc_full are signalled in both CTAs by the leader's
 // commits; acc_empty collects both CTAs' epilogue warps on the leader.  At a slot's end, where rows have to be blanked
-// before the MMA, the second CTA's bytes go to its own tail_full, and it reports to the leader's tail_ready when its rows
-// are blank.
+// before the MMA, each CTA's bytes go to its own tail_full, and the warps that blank report to the leader's tail_ready.
 struct PairBars {
   uint64_t *full, *empty, *tail_full, *tail_ready, *acc_full, *acc_empty;
   uint32_t* tmem_slot;
@@ -370,51 +373,50 @@ struct PairBars {
     abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   }
   __device__ void init() const {
-    for (int i = 0; i < 4 * WeightCfg::kStages + WeightCfg::kAccs; ++i) mbar_init(&full[i], 1);
-    for (int i = 0; i < WeightCfg::kAccs; ++i) mbar_init(&acc_empty[i], 2 * WeightCfg::kEpiWarps);
+    for (int i = 0; i < WeightCfg::kStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+      mbar_init(&tail_full[i], 1);
+      mbar_init(&tail_ready[i], 2);
+    }
+    for (int i = 0; i < WeightCfg::kAccs; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_empty[i], 2 * WeightCfg::kEpiWarps);
+    }
     *abort_flag = 0;
     fence_mbar_init();
   }
 };
 static_assert((4 * WeightCfg::kStages + 2 * WeightCfg::kAccs) * 8 + 8 <= 256, "barriers fit their space");
 
-// Blanks rows [tail, 16 steps) of a stage's four boxes, by a warp: eight lanes a row, four rows at a time.
-__device__ __forceinline__ void blank_rows(uint8_t* stage, int tail, int steps, int lane) {
-  for (int row = tail + (lane >> 3); row < 16 * steps; row += 4)
-#pragma unroll
-    for (int box = 0; box < 4; ++box)
-      *reinterpret_cast<uint4*>(stage + box * kBoxBytes + row * kRowBytes + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
-  fence_proxy_async();
-}
-
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WeightCfg::kThreads, 1)
 weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __grid_constant__ CUtensorMap tm_dup,
                        const __grid_constant__ CUtensorMap tm_dyp, const __grid_constant__ CUtensorMap tm_xp,
-                       const __grid_constant__ CUtensorMap tm_h, const int32_t* __restrict__ slot_row_off,
-                       const int32_t* __restrict__ slot_off, const int32_t* __restrict__ row_pair, int S, int E, int F, int D,
-                       int row_align, int rcap, __nv_bfloat16* __restrict__ dw_gate, __nv_bfloat16* __restrict__ dw_up,
-                       __nv_bfloat16* __restrict__ dw_down, int32_t* __restrict__ status) {
+                       const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_dw_gate,
+                       const __grid_constant__ CUtensorMap tm_dw_up, const __grid_constant__ CUtensorMap tm_dw_down,
+                       const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_off,
+                       const int32_t* __restrict__ row_pair, int S, int E, int F, int D, int row_align, int rcap,
+                       int32_t* __restrict__ status) {
   using Cfg = WeightCfg;
   constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs, kThreads = Cfg::kThreads, kStageBytes = Cfg::kStageBytes;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ int32_t s_slot_off[256 + 1];
+  __shared__ int32_t s_slot_off[256 + 1], s_rows[256];       // first slot and occupied rows of every expert
+  __shared__ int s_width[WeightCfg::kAhead];                 // of the tiles that the producer is ahead
   uint8_t* stage_mem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  SlotRows& sr = *reinterpret_cast<SlotRows*>(stage_mem + (size_t)kStages * kStageBytes);
-  const PairBars bar(stage_mem + (size_t)kStages * kStageBytes + sizeof(SlotRows));
+  uint8_t* out_mem = stage_mem + (size_t)kStages * kStageBytes;
+  SlotRows& sr = *reinterpret_cast<SlotRows*>(out_mem + Cfg::kEpiWarps * Cfg::kOutBytes);
+  const PairBars bar(reinterpret_cast<uint8_t*>(&sr) + sizeof(SlotRows));
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();           // 0: leader
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const WGeom geom(F, D);
-  const int total_tiles = E * geom.per_expert();
+  const int total_tiles = E * (geom.per[0] + geom.per[1]);
 
   if (threadIdx.x == 0) {
     bar.init();
-    prefetch_tensormap(&tm_dgate);
-    prefetch_tensormap(&tm_dup);
-    prefetch_tensormap(&tm_dyp);
-    prefetch_tensormap(&tm_xp);
-    prefetch_tensormap(&tm_h);
+    for (const CUtensorMap* m : {&tm_dgate, &tm_dup, &tm_dyp, &tm_xp, &tm_h, &tm_dw_gate, &tm_dw_up, &tm_dw_down})
+      prefetch_tensormap(m);
   }
   launch_dependents();
   wait_for_predecessor();
@@ -456,6 +458,12 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
     }
     s_slot_off[e] = v;
   }
+  __syncthreads();
+  for (int e = threadIdx.x; e < E; e += kThreads) {
+    int n = 0;
+    for (int s = s_slot_off[e]; s < s_slot_off[e + 1]; ++s) n += sr.ext[s].y;
+    s_rows[e] = n;
+  }
   __syncwarp();
   tc_fence_before_sync();
   cluster_sync_all();                                // both CTAs' barriers and tables exist
@@ -464,33 +472,42 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
 
   if (warp == 0) {
     if (lane == 0) {
-      int stage = 0;
+      int stage = 0, ahead = 0;
       uint32_t phase = 0;
       bool ok = true;
       const uint32_t leader_full = map_to_cta(smem_u32(bar.full), 0);
+      const uint32_t own_tail = map_to_cta(smem_u32(bar.tail_full), rank);
       for (int tile = pair; ok && tile < total_tiles; tile += pairs) {
-        const WTile t = decode_wtile(geom, tile);
-        const CUtensorMap* ta = t.which == 0 ? &tm_dgate : t.which == 1 ? &tm_dup : &tm_dyp;
-        const CUtensorMap* tbm = t.which == 2 ? &tm_h : &tm_xp;
-        const int m0 = t.m0 + rank * BM, n0 = t.n0 + rank * (BNACC / 2);
+        const WTile t = geom.decode(tile);
+        if (s_rows[t.expert] == 0) continue;
+        int which, m0;
+        geom.rows(t, rank, which, m0);
+        const CUtensorMap* ta = which == 0 ? &tm_dgate : which == 1 ? &tm_dup : &tm_dyp;
+        const CUtensorMap* tbm = t.problem ? &tm_h : &tm_xp;
+        const int width = geom.width(t), n0 = t.n0 + rank * (width / 2);
+        const uint32_t bytes = Cfg::kAHalf + (width / 128) * kBoxBytes;
         const int last = s_slot_off[t.expert + 1];
+        // (the entry is free: the tile that had it last has given back all its stages, or this one would have to wait)
+        bool first = true;
         for (int s = s_slot_off[t.expert]; ok && s < last; ++s) {
           const int2 ext = sr.ext[s];
           for (int r = 0; r < ext.y; r += BK) {
             if (!mbar_wait(&bar.empty[stage], phase ^ 1u, bar.abort_flag)) { ok = false; break; }
+            if (first) s_width[ahead++ % Cfg::kAhead] = width;         // published by the arrival on full below
+            first = false;
             uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
             const bool blank = ext.y - r < BK && ((ext.y - r) & 15) != 0;
-            uint32_t to = leader_full + stage * 8;
-            if (rank == 0) {
-              mbar_arrive_expect_tx(&bar.full[stage], blank ? kStageBytes : 2 * kStageBytes);
-            } else if (blank) {
-              mbar_arrive_expect_tx(&bar.tail_full[stage], kStageBytes);
-              to = map_to_cta(smem_u32(&bar.tail_full[stage]), 1);
+            const uint32_t to = (blank ? own_tail : leader_full) + stage * 8;
+            if (blank) {
+              mbar_arrive_expect_tx(&bar.tail_full[stage], bytes);
+              if (rank == 0) mbar_arrive(&bar.full[stage]);            // its phase passes; nobody waits for it
+            } else if (rank == 0) {
+              mbar_arrive_expect_tx(&bar.full[stage], 2 * bytes);
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) tma_load_2d_pair(sa + i * kBoxBytes, ta, to, m0 + 64 * i, ext.x + r);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) tma_load_2d_pair(sa + Cfg::kAHalf + i * kBoxBytes, tbm, to, n0 + 64 * i, ext.x + r);
+            tma_load_2d_pair(sa + Cfg::kAHalf, tbm, to, n0, ext.x + r);
+            if (width == BNACC) tma_load_2d_pair(sa + Cfg::kAHalf + kBoxBytes, tbm, to, n0 + 64, ext.x + r);
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
         }
@@ -498,111 +515,154 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
       if (!ok) linger();
     }
   } else if (warp == 1) {
-    // Leader: lane 0 waits for the full K blocks of a slot and issues their MMAs in a loop of its own.  For the block at
-    // the slot's end the other lanes join it, to blank the rows behind the end that the last MMA reads (at most 15, of
-    // both operands, since 0 * NaN is NaN); the second CTA's warp does the same for its part.  A failed wait leaves the
-    // loops at the next tile, for all lanes together.
-    constexpr uint32_t idesc = idesc_bf16_f32(Cfg::BM2, BNACC, true, true);
-    const uint32_t ring = smem_u32(stage_mem);
-    const uint32_t ready = map_to_cta(smem_u32(bar.tail_ready), 0);
-    int stage = 0, acc = 0;
-    uint32_t phase = 0, acc_phase = 0, tail_phase = 0;         // tail_phase: a bit for each stage
-    bool ok = true;
-    for (int tile = pair; tile < total_tiles; tile += pairs) {
-      const WTile t = decode_wtile(geom, tile);
-      const int first = s_slot_off[t.expert], last = s_slot_off[t.expert + 1];
-      if (rows_of(sr, first, last) == 0) continue;
-      if (rank == 0) {
-        if (lane == 0) ok = mbar_wait_cluster(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag);
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) break;
+    if (rank == 0 && lane == 0) {
+      const uint32_t ring = smem_u32(stage_mem);
+      int stage = 0, acc = 0, expert = 0, ahead = 0;
+      uint32_t phase = 0, acc_phase = 0, tail_phase = 0;       // tail_phase: a bit for each stage
+      bool ok = true;
+      // The tensor core holds a few MMAs at most, so what this thread does between two tiles is time lost: it takes a
+      // tile's expert by counting and its width from the producer instead of decoding the tile (600 cycles).
+      const int all = geom.per[0] + geom.per[1];
+      int q = pair;
+      for (int tile = pair; tile < total_tiles; tile += pairs, q += pairs) {
+        for (; q >= all; q -= all) ++expert;
+        if (s_rows[expert] == 0) continue;
+        if (!mbar_wait(&bar.full[stage], phase, bar.abort_flag)) { ok = false; break; }
+        const uint32_t idesc = s_width[ahead++ % Cfg::kAhead] == BNACC ? idesc_bf16_f32(2 * BM, BNACC, true, true)
+                                                                       : idesc_bf16_f32(2 * BM, BNACC / 2, true, true);
+        if (!mbar_wait_cluster(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
-      }
-      const uint32_t d_tmem = tmem_base + (uint32_t)acc * BNACC;
-      uint32_t accumulate = 0;
-      for (int s = first; s < last; ++s) {
-        const int n = sr.ext[s].y, blocks = n / BK, tail = n % BK;
-        if (rank == 0 && lane == 0 && ok) {
-          int st = stage;
-          uint32_t ph = phase;
-          for (int b = 0; b < blocks; ++b) {
-            if (!mbar_wait(&bar.full[st], ph, bar.abort_flag)) { ok = false; break; }
-            tc_fence_after_sync();
-            const uint64_t da = smem_desc_mn(ring + (uint32_t)st * kStageBytes, kBoxBytes);
-            const uint64_t db = smem_desc_mn(ring + (uint32_t)st * kStageBytes + Cfg::kAHalf, kBoxBytes);
-#pragma unroll
-            for (int k = 0; k < BK / 16; ++k) {
-              mma_bf16_pair(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
-              accumulate = 1;
-            }
-            mma_commit_pair(&bar.empty[st]);
-            if (++st == kStages) { st = 0; ph ^= 1u; }
-          }
-        }
-        phase ^= ((stage + blocks) / kStages) & 1u;
-        stage = (stage + blocks) % kStages;
-        if (tail == 0) continue;
-        const int steps = (tail + 15) >> 4;
-        if (tail & 15) {
-          __syncwarp();                            // lane 0 has consumed the stages before: the phase is unambiguous
-          const uint32_t tp = (tail_phase >> stage) & 1u;
-          const bool here = ok && (rank == 0 ? mbar_wait(&bar.full[stage], phase, bar.abort_flag)
-                                             : mbar_wait(&bar.tail_full[stage], tp, bar.abort_flag));
-          ok = __all_sync(0xffffffffu, here);
-          if (ok) blank_rows(stage_mem + (size_t)stage * kStageBytes, tail, steps, lane);
-          __syncwarp();
-          if (lane == 0 && ok) {
-            if (rank == 1) mbar_arrive_remote(ready + stage * 8);
-            else ok = mbar_wait_cluster(&bar.tail_ready[stage], tp, bar.abort_flag);
-          }
-          tail_phase ^= 1u << stage;
-        }
-        if (rank == 0 && lane == 0 && ok) {
-          ok = mbar_wait(&bar.full[stage], phase, bar.abort_flag);
-          if (ok) {
-            tc_fence_after_sync();
+        const uint32_t d_tmem = tmem_base + (uint32_t)acc * BNACC;
+        const int last = s_slot_off[expert + 1];
+        uint32_t accumulate = 0;
+        for (int s = s_slot_off[expert]; ok && s < last; ++s) {
+          int left = sr.ext[s].y;
+          for (; left > 0; left -= BK) {
             const uint64_t da = smem_desc_mn(ring + (uint32_t)stage * kStageBytes, kBoxBytes);
             const uint64_t db = smem_desc_mn(ring + (uint32_t)stage * kStageBytes + Cfg::kAHalf, kBoxBytes);
-            for (int k = 0; k < steps; ++k) {
-              mma_bf16_pair(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
-              accumulate = 1;
+            if (left >= BK) {
+              if (!mbar_wait(&bar.full[stage], phase, bar.abort_flag)) { ok = false; break; }
+              tc_fence_after_sync();
+#pragma unroll
+              for (int k = 0; k < BK / 16; ++k) {
+                mma_bf16_pair(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
+                accumulate = 1;
+              }
+            } else {
+              if (left & 15) {
+                ok = mbar_wait_cluster(&bar.tail_ready[stage], (tail_phase >> stage) & 1u, bar.abort_flag);
+                tail_phase ^= 1u << stage;
+              } else {
+                ok = mbar_wait(&bar.full[stage], phase, bar.abort_flag);
+              }
+              if (!ok) break;
+              tc_fence_after_sync();
+              for (int k = 0; 16 * k < left; ++k) {
+                mma_bf16_pair(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
+                accumulate = 1;
+              }
             }
             mma_commit_pair(&bar.empty[stage]);
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
         }
-        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        if (!ok) break;
+        mma_commit_pair(&bar.acc_full[acc]);
+        if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
       }
-      ok = __shfl_sync(0xffffffffu, ok, 0);
-      if (!ok) break;
-      if (rank == 0 && lane == 0) mma_commit_pair(&bar.acc_full[acc]);
-      if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+      if (!ok) linger();
     }
-    if (!ok && lane == 0) linger();
+  } else if (warp == Cfg::kBlankWarp) {
+    // Blanks, in this CTA's part of a slot's last K block, the rows behind the slot's end that the last MMA reads (at most
+    // 15, of both operands, since 0 * NaN is NaN): as soon as they have landed, while earlier blocks are being multiplied.
+    const uint32_t ready = map_to_cta(smem_u32(bar.tail_ready), 0);
+    int stage = 0;
+    uint32_t tail_phase = 0;
+    bool ok = true;
+    for (int tile = pair; ok && tile < total_tiles; tile += pairs) {
+      const int expert = tile / (geom.per[0] + geom.per[1]), last = s_slot_off[expert + 1];
+      for (int s = s_slot_off[expert]; ok && s < last; ++s) {
+        const int n = sr.ext[s].y, tail = n % BK;
+        stage = (stage + n / BK) % kStages;
+        if (tail & 15) {
+          const bool here = mbar_wait(&bar.tail_full[stage], (tail_phase >> stage) & 1u, bar.abort_flag, 100);
+          ok = __all_sync(0xffffffffu, here);
+          if (!ok) break;
+          uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
+          for (int row = tail + (lane >> 3); row < (tail + 15) / 16 * 16; row += 4)       // eight lanes a row
+#pragma unroll
+            for (int box = 0; box < 4; ++box)
+              *reinterpret_cast<uint4*>(sa + box * kBoxBytes + row * kRowBytes + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote(ready + stage * 8);
+          tail_phase ^= 1u << stage;
+        }
+        if (tail) stage = (stage + 1) % kStages;
+      }
+    }
   } else {
-    const int quarter = warp & 3;
-    constexpr int kShare = BNACC / (Cfg::kEpiWarps / 4);
-    const int c_begin = ((warp - 2) >> 2) * kShare;
-    uint8_t* staging = stage_mem + (size_t)kStages * kStageBytes + sizeof(SlotRows) + 256 + (warp - 2) * kStagingBytesPerWarp;
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    uint8_t* staging = out_mem + (warp - 2) * Cfg::kOutBytes;
     const uint32_t leader_empty = map_to_cta(smem_u32(bar.acc_empty), 0);
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int tile = pair; tile < total_tiles; tile += pairs) {
-      const WTile t = decode_wtile(geom, tile);
-      __nv_bfloat16* out = (t.which == 0 ? dw_gate : t.which == 1 ? dw_up : dw_down) + (size_t)t.expert * t.m_dim * t.n_dim;
-      const int row0 = t.m0 + rank * BM + quarter * 32;
-      if (rows_of(sr, s_slot_off[t.expert], s_slot_off[t.expert + 1]) == 0) {      // no token chose this expert
-        drain_plain<true>(0, staging, lane, out, row0, t.m_dim, t.n0, t.n_dim, c_begin, c_begin + kShare);
-        continue;
+      const WTile t = geom.decode(tile);
+      int which, m0;
+      geom.rows(t, rank, which, m0);
+      const CUtensorMap* to = which == 0 ? &tm_dw_gate : which == 1 ? &tm_dw_up : &tm_dw_down;
+      const int row0 = m0 + quarter * 32, m_dim = t.problem ? D : F, n_dim = t.problem ? F : D, share = geom.width(t) / 2;
+      uint32_t o[4][16];                               // 128 columns of this lane's row, packed
+      const int rows = s_rows[t.expert];
+      if (rows != 0) {
+        // (a short sum is awaited closely; through a long one the warps sleep, polling costs power that the MMAs need)
+        if (!mbar_wait(&bar.acc_full[acc], acc_phase, bar.abort_flag, rows > 1024 ? 256 : 32)) break;
+        tc_fence_after_sync();
+        // the accumulator is emptied into registers at one go and handed back, then the columns are stored: for an
+        // expert with few rows the next sums are ready before the stores are out
+        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * BNACC + half * share;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          if (32 * c < share) {
+            uint32_t a[32];
+            tmem_ld32(taddr + 32 * c, a);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[c][i] = pack_bf16(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1]));
+          }
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_remote(leader_empty + acc * 8);
+        if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+      } else {                                         // no token chose this expert
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[c][i] = 0;
       }
-      if (!mbar_wait(&bar.acc_full[acc], acc_phase, bar.abort_flag, 256)) break;
-      tc_fence_after_sync();
-      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * BNACC;
-      drain_plain<false>(taddr, staging, lane, out, row0, t.m_dim, t.n0, t.n_dim, c_begin, c_begin + kShare);
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_remote(leader_empty + acc * 8);
-      if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int col = t.n0 + half * share + 32 * c;
+        if (32 * c >= share || col >= n_dim || row0 >= m_dim) break;
+        // 32 rows of 64 bytes in the store's 64-byte swizzle (16-byte word w of row r at w ^ (r / 2 % 4)), which also
+        // keeps the lanes' writes free of bank conflicts; the TMA unit writes the box
+        if (lane == 0) bulk_wait_read<0>();
+        __syncwarp();
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          *reinterpret_cast<uint4*>(staging + lane * 64 + ((w ^ ((lane >> 1) & 3)) << 4)) =
+              make_uint4(o[c][4 * w], o[c][4 * w + 1], o[c][4 * w + 2], o[c][4 * w + 3]);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_3d(to, staging, col, row0, t.expert);
+          bulk_commit();
+        }
+      }
     }
+    if (lane == 0) bulk_wait_all();
   }
 
   __syncwarp();
@@ -694,10 +754,11 @@ int moegps_launch_ffn_backward_weights(moegps_ctx* ctx, const void* dyp, const v
                                        const int32_t* row_pair, void* dw_gate, void* dw_up, void* dw_down, cudaStream_t st) {
   const moegps_shape_t& s = ctx->shape;
   const uint64_t rcap = (uint64_t)moegps_rcap_of(s);
-  CUtensorMap t_dgate, t_dup, t_dyp, t_xp, t_h;
+  CUtensorMap t_dgate, t_dup, t_dyp, t_xp, t_h, o_gate, o_up, o_down;
   if (!(moegps_make_tmap_2d(&t_dgate, dgate, rcap, s.F, BK, 64) && moegps_make_tmap_2d(&t_dup, dup, rcap, s.F, BK, 64) &&
         moegps_make_tmap_2d(&t_dyp, dyp, rcap, s.D, BK, 64) && moegps_make_tmap_2d(&t_xp, xp, rcap, s.D, BK, 64) &&
-        moegps_make_tmap_2d(&t_h, h_ws, rcap, s.F, BK, 64)))
+        moegps_make_tmap_2d(&t_h, h_ws, rcap, s.F, BK, 64) && moegps_make_tmap_store(&o_gate, dw_gate, s.E, s.F, s.D) &&
+        moegps_make_tmap_store(&o_up, dw_up, s.E, s.F, s.D) && moegps_make_tmap_store(&o_down, dw_down, s.E, s.D, s.F)))
     return tmap_failed(ctx);
   constexpr size_t smem = WeightCfg::kSmem;
   if (!ctx->weight_gradient_attr_done) {
@@ -705,9 +766,8 @@ int moegps_launch_ffn_backward_weights(moegps_ctx* ctx, const void* dyp, const v
     ctx->weight_gradient_attr_done = true;
   }
   MOEGPS_CUDA_TRY(ctx, launch_after(weight_gradient_kernel, dim3(ctx->sm_count / 2 * 2), WeightCfg::kThreads, smem, st, t_dgate,
-                                    t_dup, t_dyp, t_xp, t_h, slot_row_off, slot_off, row_pair, s.S, s.E, s.F, s.D, s.row_align,
-                                    (int)rcap, static_cast<__nv_bfloat16*>(dw_gate), static_cast<__nv_bfloat16*>(dw_up),
-                                    static_cast<__nv_bfloat16*>(dw_down), ctx->d_status));
+                                    t_dup, t_dyp, t_xp, t_h, o_gate, o_up, o_down, slot_row_off, slot_off, row_pair, s.S, s.E, s.F,
+                                    s.D, s.row_align, (int)rcap, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }

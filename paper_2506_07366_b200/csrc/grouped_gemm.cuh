@@ -153,3 +153,5 @@ bool moegps_make_tmap_2d(CUtensorMap* tm, const void* base, uint64_t rows, uint6
 // bf16 [batch, rows, cols]; box = box_cols columns x box_rows rows x 1 batch entry.
 bool moegps_make_tmap_3d(CUtensorMap* tm, const void* base, uint64_t batch, uint64_t rows, uint64_t cols,
                          uint32_t box_rows, uint32_t box_cols);
+// the same with the box that an epilogue warp stores: 32 columns x 32 rows
+bool moegps_make_tmap_store(CUtensorMap* tm, void* base, uint64_t batch, uint64_t rows, uint64_t cols);
