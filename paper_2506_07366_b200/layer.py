@@ -7,7 +7,7 @@ from __future__ import annotations
 
 import torch
 
-from .binding import Context, Shape, workspace_bytes
+from .binding import Context, Shape, route_backward_workspace_bytes, workspace_bytes
 
 # Row alignment of the slot buckets that the benchmark and the serving examples use: slot starts are
 # multiples of 16 rows.  The grouped GEMM accepts any alignment (its tiles start at the slot's first
@@ -131,6 +131,64 @@ class MoeLayer:
         out = self.forward(self.x, stream)
         out_host.copy_(out, non_blocking=True)
         return out_host
+
+
+class MoeTrainLayer(MoeLayer):
+    """MoeLayer with a backward pass, on the same plan, permutation and buffers.
+
+    forward_train() is forward() except that the gate and up products are kept in 8 bits (2 bytes for each hidden value
+    and row instead of the 6 of gate, up and hidden activations in bf16); backward() turns the gradient of the output
+    into the gradients of the input, the experts and the router.  The layer owns every buffer; what a call returns is
+    overwritten by the next call.
+    """
+
+    def __init__(self, shape: Shape, w_router, bias, w_gate, w_up, w_down, device=None):
+        super().__init__(shape, w_router, bias, w_gate, w_up, w_down, device)
+        s, dev = shape, w_router.device
+        bf, u8 = dict(dtype=torch.bfloat16, device=dev), dict(dtype=torch.uint8, device=dev)
+        f32 = dict(dtype=torch.float32, device=dev)
+        self.kept = (torch.empty(s.Rcap, s.P, **u8), torch.empty(s.Rcap, s.P, **u8),              # gate8, up8
+                     torch.empty(s.P // 32, s.Rcap, **u8), torch.empty(s.P // 32, s.Rcap, **u8))  # gate_scale, up_scale
+        self.dgate, self.dup = torch.empty(s.Rcap, s.F, **bf), torch.empty(s.Rcap, s.F, **bf)
+        self.dyp, self.dxp = torch.empty(s.Rcap, s.D, **bf), torch.empty(s.Rcap, s.D, **bf)
+        self.dtopk_w, self.dlogit = torch.empty(s.T, s.K, **f32), torch.empty(s.T, s.K, **f32)
+        self.grads = dict(x=torch.empty(s.T, s.D, **bf), w_gate=torch.empty_like(w_gate), w_up=torch.empty_like(w_up),
+                          w_down=torch.empty_like(w_down), w_router=torch.empty(s.E, s.D, **f32),
+                          bias=torch.empty(s.E, **f32))
+        self.route_workspace = torch.empty(max(16, route_backward_workspace_bytes(s)), **u8)
+        self._trained_x = None
+
+    def forward_train(self, x, stream=None, out=None):
+        """forward() that keeps what backward() needs; x must stay as it is until then."""
+        if not self._planned:
+            raise RuntimeError("call plan(predicted_hist) before forward_train()")
+        c = self.ctx
+        out = self.out if out is None else out
+        c.route_prepare(x, self.w_router, self.bias, self.topk_idx, self.topk_w, self.hist, self.workspace, stream)
+        c.dispatch_prepared(x, self.topk_idx, self.hist, self.replicas, self.slot_off, self.slot_row_off,
+                            self.row_pair, self.pair_row, self.xp, self.workspace, stream)
+        c.expert_ffn_gate_up_save(self.xp, self.slot_row_off, self.slot_expert, self.w_gate, self.w_up, self.h_ws,
+                                  *self.kept, stream=stream)
+        c.expert_ffn_down(self.h_ws, self.slot_row_off, self.slot_expert, self.w_down, self.yp, stream)
+        c.combine(self.yp, self.pair_row, self.topk_w, out, stream)
+        self._trained_x = x
+        return out
+
+    def backward(self, dout, stream=None):
+        """Gradients for the last forward_train(): dict of x [T,D], w_gate, w_up [E,F,D], w_down [E,D,F] (bf16) and
+        w_router [E,D], bias [E] (fp32).  dout: bf16 [T,D].  The plan must not have changed in between."""
+        if self._trained_x is None:
+            raise RuntimeError("call forward_train() before backward()")
+        c, x, g = self.ctx, self._trained_x, self.grads
+        c.combine_backward(dout, self.yp, self.pair_row, self.topk_w, self.dyp, self.dtopk_w, stream)
+        c.expert_ffn_backward(self.dyp, self.xp, self.slot_row_off, self.slot_off, self.slot_expert, self.row_pair,
+                              self.w_gate, self.w_up, self.w_down, *self.kept, self.dgate, self.dup, self.h_ws, self.dxp,
+                              g["w_gate"], g["w_up"], g["w_down"], stream)
+        c.route_backward(x, self.w_router, self.bias, self.topk_idx, self.topk_w, self.dtopk_w, self.slot_row_off,
+                         self.slot_off, self.row_pair, self.dlogit, g["w_router"], g["bias"], self.route_workspace, stream)
+        c.dispatch_backward(self.dxp, self.pair_row, self.topk_idx, self.dlogit, self.w_router, g["x"], stream)
+        self._trained_x = None
+        return g
 
 
 class HostPipeline:
