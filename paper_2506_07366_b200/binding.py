@@ -170,7 +170,32 @@ def _stream(stream):
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
-    return int(stream)
+    return int(stream if isinstance(stream, int) else stream.cuda_stream)
+
+
+def _marshal():
+    """The compiled argument checks (csrc/marshal.cpp), or None where they have not been built."""
+    try:
+        from . import _marshal as module
+    except ImportError:
+        return None
+    return module
+
+
+def _training_call(entry, handle: int, specs):
+    """A callable (stream, *tensors) that checks every tensor against its spec (type, shape, name, may be None), calls the C
+    entry point and returns its code.  The compiled form costs a few microseconds less for each call; both raise the
+    exceptions of _ptr."""
+    module = _marshal()
+    if module is not None:
+        return module.Call(ctypes.cast(entry, ctypes.c_void_p).value, handle, _ptr, tuple(specs))
+
+    def run(stream, *tensors):
+        if len(tensors) != len(specs):
+            raise TypeError(f"expected a stream and {len(specs)} tensors")
+        return entry(handle, *[_ptr(t, *spec) for t, spec in zip(tensors, specs)], _stream(stream))
+
+    return run
 
 
 class Context:
@@ -181,14 +206,6 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("moegps needs a CUDA device (sm_100a); there is no CPU path")
         self.shape = shape
-        # shapes of the training step's tensors
-        rows = shape.Rcap
-        self._td, self._tk, self._ed = (shape.T, shape.D), (shape.T, shape.K), (shape.E, shape.D)
-        self._rows, self._rows_d, self._rows_f = (rows,), (rows, shape.D), (rows, shape.F)
-        self._codes, self._scales = (rows, shape.P), (shape.P // 32, rows)
-        self._efd, self._edf = (shape.E, shape.F, shape.D), (shape.E, shape.D, shape.F)
-        self._s, self._s1, self._e, self._e1 = (shape.S,), (shape.S + 1,), (shape.E,), (shape.E + 1,)
-        self._route_backward_bytes = route_backward_workspace_bytes(shape)
         self.device = torch.cuda.current_device() if device is None else int(device)
         self._h = ctypes.c_void_p()
         cs = shape.c_struct()
@@ -196,11 +213,13 @@ class Context:
         if rc != OK:
             self._h = ctypes.c_void_p()
             raise MoegpsError(rc, "moegps_create")
+        self._bind_training_calls()
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:
             _lib().moegps_destroy(self._h)
             self._h = ctypes.c_void_p()
+            self._bind_training_calls()                  # to the null context, which every entry point refuses
 
     def __del__(self):
         try:
@@ -396,97 +415,104 @@ class Context:
             _ptr(out, torch.bfloat16, (s.T, s.D), "out"), _stream(stream)), "moegps_combine")
 
     # -- the training step --------------------------------------------------------------------
+    def _bind_training_calls(self):
+        """What each tensor of these calls has to be: (type, shape or None, name, may be None)."""
+        s = self.shape
+        bf16, i32, u8, f32 = torch.bfloat16, torch.int32, torch.uint8, torch.float32
+
+        def t(name, dtype, *shape, optional=False):
+            return (dtype, shape or None, name, optional)
+
+        def rows(*names, width=None, dtype=bf16):
+            return tuple(t(n, dtype, s.Rcap, width) for n in names)
+
+        row_off, slot_off, expert = t("slot_row_off", i32, s.S + 1), t("slot_off", i32, s.E + 1), t("slot_expert", i32, s.S)
+        row_pair, pair_row = t("row_pair", i32, s.Rcap), t("pair_row", i32, s.T, s.K)
+        up = tuple(t(n, bf16, s.E, s.F, s.D) for n in ("w_gate", "w_up"))
+        down = (t("w_down", bf16, s.E, s.D, s.F),)
+        d_up = tuple(t(n, bf16, s.E, s.F, s.D) for n in ("dw_gate", "dw_up")) + (t("dw_down", bf16, s.E, s.D, s.F),)
+        kept = rows("gate8", "up8", width=s.P, dtype=u8) + tuple(t(n, u8, s.P // 32, s.Rcap) for n in ("gate_scale", "up_scale"))
+        mid, h = rows("dgate", "dup", width=s.F), rows("h_ws", width=s.F)
+        xp, dyp, dxp, yp = (rows(n, width=s.D) for n in ("xp", "dyp", "dxp", "yp"))
+        topk_idx, topk_w, dtopk_w, dlogit = (t(n, d, s.T, s.K) for n, d in
+                                             (("topk_idx", i32), ("topk_w", f32), ("dtopk_w", f32), ("dlogit", f32)))
+        w_router, dx = t("w_router", bf16, s.E, s.D), t("dx", bf16, s.T, s.D)
+        softmax = s.gate_mode == 0                       # then w_router, bias and topk_idx are not read
+        maybe = lambda spec: spec[:3] + (softmax,)  # noqa: E731
+
+        def call(name, *specs):
+            return _training_call(getattr(_lib(), "moegps_" + name), self._h.value or 0, specs)
+
+        self._gate_up_save = call("expert_ffn_gate_up_save", *xp, row_off, expert, *up, *h, *kept)
+        self._ffn_backward = call("expert_ffn_backward", *dyp, *xp, row_off, slot_off, expert, row_pair, *up, *down, *kept, *mid,
+                                  *h, *dxp, *d_up)
+        self._ffn_backward_act = call("expert_ffn_backward_act", *dyp, row_off, expert, *down, *kept, *mid, *h)
+        self._ffn_backward_input = call("expert_ffn_backward_input", *mid, row_off, expert, *up, *dxp)
+        self._ffn_backward_weights = call("expert_ffn_backward_weights", *dyp, *xp, *mid, *h, row_off, slot_off, row_pair, *d_up)
+        self._combine_backward = call("combine_backward", t("dout", bf16, s.T, s.D), *yp, pair_row, topk_w, *dyp, dtopk_w)
+        none = (f32, None, "", True)
+        self._dispatch_backward = call("dispatch_backward", *dxp, pair_row, none, none, none, dx)
+        self._dispatch_backward_router = call("dispatch_backward", *dxp, pair_row, topk_idx, dlogit, w_router, dx)
+        self._route_backward = call("route_backward", t("x", bf16, s.T, s.D), maybe(w_router),
+                                    t("bias", f32, s.E, optional=True), maybe(topk_idx), topk_w, dtopk_w, row_off, slot_off,
+                                    row_pair, dlogit, t("dw_router", f32, s.E, s.D), t("dbias", f32, s.E),
+                                    t("workspace", u8))
+        self._route_backward_bytes = route_backward_workspace_bytes(s)
+
     def expert_ffn_gate_up_save(self, xp, slot_row_off, slot_expert, w_gate, w_up, h_ws, gate8, up8, gate_scale, up_scale,
                                 stream=None):
-        bf16, i32, u8 = torch.bfloat16, torch.int32, torch.uint8
-        self._check(_lib().moegps_expert_ffn_gate_up_save(
-            self._h, _ptr(xp, bf16, self._rows_d, "xp"), _ptr(slot_row_off, i32, self._s1, "slot_row_off"),
-            _ptr(slot_expert, i32, self._s, "slot_expert"), _ptr(w_gate, bf16, self._efd, "w_gate"),
-            _ptr(w_up, bf16, self._efd, "w_up"), _ptr(h_ws, bf16, self._rows_f, "h_ws"),
-            _ptr(gate8, u8, self._codes, "gate8"), _ptr(up8, u8, self._codes, "up8"),
-            _ptr(gate_scale, u8, self._scales, "gate_scale"), _ptr(up_scale, u8, self._scales, "up_scale"),
-            _stream(stream)), "moegps_expert_ffn_gate_up_save")
+        rc = self._gate_up_save(stream, xp, slot_row_off, slot_expert, w_gate, w_up, h_ws, gate8, up8, gate_scale, up_scale)
+        if rc:
+            self._check(rc, "moegps_expert_ffn_gate_up_save")
 
     def expert_ffn_backward(self, dyp, xp, slot_row_off, slot_off, slot_expert, row_pair, w_gate, w_up, w_down, gate8, up8,
                             gate_scale, up_scale, dgate, dup, h_ws, dxp, dw_gate, dw_up, dw_down, stream=None):
-        bf16, i32, u8 = torch.bfloat16, torch.int32, torch.uint8
-        self._check(_lib().moegps_expert_ffn_backward(
-            self._h, _ptr(dyp, bf16, self._rows_d, "dyp"), _ptr(xp, bf16, self._rows_d, "xp"),
-            _ptr(slot_row_off, i32, self._s1, "slot_row_off"), _ptr(slot_off, i32, self._e1, "slot_off"),
-            _ptr(slot_expert, i32, self._s, "slot_expert"), _ptr(row_pair, i32, self._rows, "row_pair"),
-            _ptr(w_gate, bf16, self._efd, "w_gate"), _ptr(w_up, bf16, self._efd, "w_up"),
-            _ptr(w_down, bf16, self._edf, "w_down"), _ptr(gate8, u8, self._codes, "gate8"),
-            _ptr(up8, u8, self._codes, "up8"), _ptr(gate_scale, u8, self._scales, "gate_scale"),
-            _ptr(up_scale, u8, self._scales, "up_scale"), _ptr(dgate, bf16, self._rows_f, "dgate"),
-            _ptr(dup, bf16, self._rows_f, "dup"), _ptr(h_ws, bf16, self._rows_f, "h_ws"),
-            _ptr(dxp, bf16, self._rows_d, "dxp"), _ptr(dw_gate, bf16, self._efd, "dw_gate"),
-            _ptr(dw_up, bf16, self._efd, "dw_up"), _ptr(dw_down, bf16, self._edf, "dw_down"),
-            _stream(stream)), "moegps_expert_ffn_backward")
+        rc = self._ffn_backward(stream, dyp, xp, slot_row_off, slot_off, slot_expert, row_pair, w_gate, w_up, w_down, gate8, up8,
+                                gate_scale, up_scale, dgate, dup, h_ws, dxp, dw_gate, dw_up, dw_down)
+        if rc:
+            self._check(rc, "moegps_expert_ffn_backward")
 
     def expert_ffn_backward_act(self, dyp, slot_row_off, slot_expert, w_down, gate8, up8, gate_scale, up_scale, dgate, dup,
                                 h_ws, stream=None):
-        bf16, i32, u8 = torch.bfloat16, torch.int32, torch.uint8
-        self._check(_lib().moegps_expert_ffn_backward_act(
-            self._h, _ptr(dyp, bf16, self._rows_d, "dyp"), _ptr(slot_row_off, i32, self._s1, "slot_row_off"),
-            _ptr(slot_expert, i32, self._s, "slot_expert"), _ptr(w_down, bf16, self._edf, "w_down"),
-            _ptr(gate8, u8, self._codes, "gate8"), _ptr(up8, u8, self._codes, "up8"),
-            _ptr(gate_scale, u8, self._scales, "gate_scale"), _ptr(up_scale, u8, self._scales, "up_scale"),
-            _ptr(dgate, bf16, self._rows_f, "dgate"), _ptr(dup, bf16, self._rows_f, "dup"),
-            _ptr(h_ws, bf16, self._rows_f, "h_ws"), _stream(stream)), "moegps_expert_ffn_backward_act")
+        rc = self._ffn_backward_act(stream, dyp, slot_row_off, slot_expert, w_down, gate8, up8, gate_scale, up_scale, dgate, dup,
+                                    h_ws)
+        if rc:
+            self._check(rc, "moegps_expert_ffn_backward_act")
 
     def expert_ffn_backward_input(self, dgate, dup, slot_row_off, slot_expert, w_gate, w_up, dxp, stream=None):
-        bf16, i32 = torch.bfloat16, torch.int32
-        self._check(_lib().moegps_expert_ffn_backward_input(
-            self._h, _ptr(dgate, bf16, self._rows_f, "dgate"), _ptr(dup, bf16, self._rows_f, "dup"),
-            _ptr(slot_row_off, i32, self._s1, "slot_row_off"), _ptr(slot_expert, i32, self._s, "slot_expert"),
-            _ptr(w_gate, bf16, self._efd, "w_gate"), _ptr(w_up, bf16, self._efd, "w_up"),
-            _ptr(dxp, bf16, self._rows_d, "dxp"), _stream(stream)), "moegps_expert_ffn_backward_input")
+        rc = self._ffn_backward_input(stream, dgate, dup, slot_row_off, slot_expert, w_gate, w_up, dxp)
+        if rc:
+            self._check(rc, "moegps_expert_ffn_backward_input")
 
     def expert_ffn_backward_weights(self, dyp, xp, dgate, dup, h_ws, slot_row_off, slot_off, row_pair, dw_gate, dw_up, dw_down,
                                     stream=None):
-        bf16, i32 = torch.bfloat16, torch.int32
-        self._check(_lib().moegps_expert_ffn_backward_weights(
-            self._h, _ptr(dyp, bf16, self._rows_d, "dyp"), _ptr(xp, bf16, self._rows_d, "xp"),
-            _ptr(dgate, bf16, self._rows_f, "dgate"), _ptr(dup, bf16, self._rows_f, "dup"),
-            _ptr(h_ws, bf16, self._rows_f, "h_ws"), _ptr(slot_row_off, i32, self._s1, "slot_row_off"),
-            _ptr(slot_off, i32, self._e1, "slot_off"), _ptr(row_pair, i32, self._rows, "row_pair"),
-            _ptr(dw_gate, bf16, self._efd, "dw_gate"), _ptr(dw_up, bf16, self._efd, "dw_up"),
-            _ptr(dw_down, bf16, self._edf, "dw_down"), _stream(stream)), "moegps_expert_ffn_backward_weights")
+        rc = self._ffn_backward_weights(stream, dyp, xp, dgate, dup, h_ws, slot_row_off, slot_off, row_pair, dw_gate, dw_up,
+                                        dw_down)
+        if rc:
+            self._check(rc, "moegps_expert_ffn_backward_weights")
 
     def combine_backward(self, dout, yp, pair_row, topk_w, dyp, dtopk_w, stream=None):
-        bf16, f32 = torch.bfloat16, torch.float32
-        self._check(_lib().moegps_combine_backward(
-            self._h, _ptr(dout, bf16, self._td, "dout"), _ptr(yp, bf16, self._rows_d, "yp"),
-            _ptr(pair_row, torch.int32, self._tk, "pair_row"), _ptr(topk_w, f32, self._tk, "topk_w"),
-            _ptr(dyp, bf16, self._rows_d, "dyp"), _ptr(dtopk_w, f32, self._tk, "dtopk_w"), _stream(stream)),
-            "moegps_combine_backward")
+        rc = self._combine_backward(stream, dout, yp, pair_row, topk_w, dyp, dtopk_w)
+        if rc:
+            self._check(rc, "moegps_combine_backward")
 
     def dispatch_backward(self, dxp, pair_row, topk_idx, dlogit, w_router, dx, stream=None):
         """dlogit None: without the router's part (topk_idx and w_router are not read)."""
-        bf16, i32 = torch.bfloat16, torch.int32
-        part = dlogit is not None
-        self._check(_lib().moegps_dispatch_backward(
-            self._h, _ptr(dxp, bf16, self._rows_d, "dxp"), _ptr(pair_row, i32, self._tk, "pair_row"),
-            _ptr(topk_idx, i32, self._tk, "topk_idx") if part else None,
-            _ptr(dlogit, torch.float32, self._tk, "dlogit") if part else None,
-            _ptr(w_router, bf16, self._ed, "w_router") if part else None,
-            _ptr(dx, bf16, self._td, "dx"), _stream(stream)), "moegps_dispatch_backward")
+        if dlogit is None:
+            rc = self._dispatch_backward(stream, dxp, pair_row, None, None, None, dx)
+        else:
+            rc = self._dispatch_backward_router(stream, dxp, pair_row, topk_idx, dlogit, w_router, dx)
+        if rc:
+            self._check(rc, "moegps_dispatch_backward")
 
     def route_backward(self, x, w_router, bias, topk_idx, topk_w, dtopk_w, slot_row_off, slot_off, row_pair, dlogit,
                        dw_router, dbias, workspace, stream=None):
-        if workspace is None or workspace.numel() * workspace.element_size() < self._route_backward_bytes:
+        if workspace is None or workspace.nbytes < self._route_backward_bytes:
             raise MoegpsError(ERR_WORKSPACE_TOO_SMALL, "moegps_route_backward")
-        bf16, i32, f32 = torch.bfloat16, torch.int32, torch.float32
-        softmax = self.shape.gate_mode == 0              # then w_router, bias and topk_idx are not read
-        self._check(_lib().moegps_route_backward(
-            self._h, _ptr(x, bf16, self._td, "x"), _ptr(w_router, bf16, self._ed, "w_router", allow_none=softmax),
-            _ptr(bias, f32, self._e, "bias", allow_none=True),
-            _ptr(topk_idx, i32, self._tk, "topk_idx", allow_none=softmax), _ptr(topk_w, f32, self._tk, "topk_w"),
-            _ptr(dtopk_w, f32, self._tk, "dtopk_w"), _ptr(slot_row_off, i32, self._s1, "slot_row_off"),
-            _ptr(slot_off, i32, self._e1, "slot_off"), _ptr(row_pair, i32, self._rows, "row_pair"),
-            _ptr(dlogit, f32, self._tk, "dlogit"), _ptr(dw_router, f32, self._ed, "dw_router"),
-            _ptr(dbias, f32, self._e, "dbias"), _ptr(workspace, workspace.dtype, None, "workspace"),
-            _stream(stream)), "moegps_route_backward")
+        rc = self._route_backward(stream, x, w_router, bias, topk_idx, topk_w, dtopk_w, slot_row_off, slot_off, row_pair, dlogit,
+                                  dw_router, dbias, workspace)
+        if rc:
+            self._check(rc, "moegps_route_backward")
 
     def predictor_update(self, hist, state, predicted_hist, stream=None):
         s = self.shape

@@ -1,15 +1,19 @@
-"""Builds libmoegps.so (the C-ABI library, sm_100a only) in-tree with nvcc."""
+"""Builds libmoegps.so (the C-ABI library, sm_100a only) in-tree with nvcc, and with the host compiler the Python module
+_marshal (argument checks of the training step's calls, csrc/marshal.cpp)."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libmoegps.so")
+MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
+MARSHAL_PATH = os.path.join(PKG_DIR, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.cu", "route.cu", "histogram.cu", "plan.cu", "pack.cu", "dispatch.cu", "expert_ffn.cu", "combine.cu",
            "predictor.cu", "selftest.cu", "expert_ffn_backward.cu", "shuffle_backward.cu", "route_backward.cu"]
 HEADERS = ["common.cuh", "sm100.cuh", "route_epilogue.cuh", "slot_offsets.cuh", "grouped_gemm.cuh", "act8.cuh", "bf16x8.cuh",
@@ -31,8 +35,31 @@ def needs_build() -> bool:
     return any(os.path.getmtime(d) > built for d in deps)
 
 
+def build_marshal(force: bool = False) -> str:
+    """Compile _marshal against the installed torch; returns its path."""
+    if not force and os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_SOURCE) <= os.path.getmtime(MARSHAL_PATH):
+        return MARSHAL_PATH
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
+    cmd = [
+        "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+        f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+        "-I", os.path.join(home, "include"), "-I", os.path.join(home, "include", "torch", "csrc", "api", "include"),
+        "-I", cuda, "-I", sysconfig.get_path("include"), MARSHAL_SOURCE,
+        "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", MARSHAL_PATH + ".tmp",
+    ]
+    proc = subprocess.run(cmd, capture_output=True, text=True)
+    if proc.returncode != 0:
+        sys.stderr.write(proc.stdout + proc.stderr)
+        raise RuntimeError("g++ failed building _marshal")
+    os.replace(MARSHAL_PATH + ".tmp", MARSHAL_PATH)
+    return MARSHAL_PATH
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu of the library for sm_100a into one shared object; returns its path."""
+    """Compile every .cu of the library for sm_100a into one shared object (and _marshal); returns its path."""
+    build_marshal(force)
     if not force and not needs_build():
         return LIB_PATH
     cmd = [

@@ -411,3 +411,32 @@ def test_bad_tables_are_reported():
     dx = torch.empty_like(dout)
     c.ctx.dispatch_backward(dyp2, rows, None, None, None, dx)
     assert c.ctx.status() == binding.ERR_BAD_INDEX
+
+
+def test_checks_without_the_compiled_module(monkeypatch):
+    """Where _marshal has not been built the same checks run in Python: same results, same refusals."""
+    assert binding._marshal() is not None
+    monkeypatch.setattr(binding, "_marshal", lambda: None)
+    c = Case(64, 64, 64, 4, 2, 4, 16, seed=20)
+    s, t = c.shape, c.t
+    dout, yp = bf(c.rng.standard_normal((s.T, s.D))), c.rows(0.5, s.D)
+    got = torch.zeros_like(yp), torch.empty(s.T, s.K, device=DEV)
+    c.ctx.combine_backward(dout, yp, t["pair_row"], t["w"], *got)
+    monkeypatch.undo()
+    other = binding.Context(s)
+    want = torch.zeros_like(yp), torch.empty(s.T, s.K, device=DEV)
+    other.combine_backward(dout, yp, t["pair_row"], t["w"], *want, stream=torch.cuda.current_stream())
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for ctx in (c.ctx, other):
+        with pytest.raises(TypeError, match="topk_w must be torch.float32"):
+            ctx.combine_backward(dout, yp, t["pair_row"], t["w"].double(), *got)
+        with pytest.raises(ValueError, match="dtopk_w must have shape"):
+            ctx.combine_backward(dout, yp, t["pair_row"], t["w"], got[0], got[1][:-1])
+        with pytest.raises(TypeError, match="yp must be a CUDA tensor"):
+            ctx.combine_backward(dout, "yp", t["pair_row"], t["w"], *got)
+        with pytest.raises(AttributeError):
+            ctx.combine_backward(dout, yp, t["pair_row"], t["w"], *got, stream=object())
+        ctx.close()
+        with pytest.raises(binding.MoegpsError) as err:
+            ctx.combine_backward(dout, yp, t["pair_row"], t["w"], *got)
+        assert err.value.code == binding.ERR_INVALID_ARG
