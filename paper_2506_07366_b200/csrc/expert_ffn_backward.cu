@@ -66,6 +66,16 @@ __device__ __forceinline__ void load_block(KeptBlock& b, const KeptActs& kept, i
   }
 }
 
+// 1 / (1 + exp(-x)) by the hardware's exp2 and reciprocal (relative error a few 2^-22; the results are rounded to bf16,
+// 2^-8).  The forms that flush subnormals: exp(-x) is 0 or infinite far out, where the sigmoid is 1 or 0 to fp32 anyway,
+// and without the flush each costs several instructions more in the longest epilogue here.
+__device__ __forceinline__ float sigmoid_fast(float x) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-1.4426950408889634f * x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
+}
+
 // The four values of one code word each, with their part of dh -> packed dgate, dup, h.
 __device__ __forceinline__ void act_gradient(uint32_t gw, uint32_t uw, float gs, float us, const uint32_t* dh, uint32_t* dgate,
                                              uint32_t* dup, uint32_t* h) {
@@ -76,7 +86,7 @@ __device__ __forceinline__ void act_gradient(uint32_t gw, uint32_t uw, float gs,
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float d = __uint_as_float(dh[i]);
-    const float s = __fdividef(1.f, 1.f + __expf(-g[i]));
+    const float s = sigmoid_fast(g[i]);
     const float a = g[i] * s;                       // silu
     dg[i] = d * u[i] * fmaf(a, 1.f - s, s);         // s (1 + g (1 - s)) = s + a (1 - s)
     du[i] = d * a;
