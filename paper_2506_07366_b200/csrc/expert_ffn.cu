@@ -134,7 +134,7 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 2 * kAccs);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
   const int cols_per_tile = kSwiGLU ? 128 : 256;
   const int n_tiles = (n_dim + cols_per_tile - 1) / cols_per_tile;
   const int num_kb = (k_dim + BK - 1) / BK;
@@ -186,36 +186,37 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      constexpr uint32_t idesc = idesc_bf16_f32(BM, BNACC);
-      int stage = 0;
-      uint32_t phase = 0;
-      int acc = 0;
-      uint32_t acc_phase = 0;
-      bool ok = true;
-      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
-        if (!mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag)) { ok = false; break; }
+    constexpr uint32_t idesc = idesc_bf16_f32(BM, BNACC);
+    const uint32_t ring = smem_u32(stage_mem);
+    int stage = 0;
+    uint32_t phase = 0;
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    bool ok = true;
+    for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
+      if (!warp_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag)) { ok = false; break; }
+      tc_fence_after_sync();
+      const uint32_t d_tmem = tmem_base + (uint32_t)acc * BNACC;
+      for (int kb = 0; kb < num_kb; ++kb) {
+        if (!warp_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
-        const uint32_t d_tmem = tmem_base + (uint32_t)acc * BNACC;
-        for (int kb = 0; kb < num_kb; ++kb) {
-          if (!mbar_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
-          tc_fence_after_sync();
-          const uint32_t sa = smem_u32(stage_mem + (size_t)stage * kStageBytes);
-          const uint64_t da = smem_desc_k<kRowBytes>(sa);
-          const uint64_t db = smem_desc_k<kRowBytes>(sa + kABytes);
+        const uint32_t sa = ring + (uint32_t)stage * kStageBytes;
+        const uint64_t da = smem_desc_k<kRowBytes>(sa);
+        const uint64_t db = smem_desc_k<kRowBytes>(sa + kABytes);
+        if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < BK / 16; ++k)      // 16 bf16 = 32 bytes per MMA along K
             mma_bf16(d_tmem, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (kb | k) != 0);
           mma_commit(&empty[stage]);             // frees the stage when these MMAs have read it
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
-        if (!ok) break;
-        mma_commit(&acc_full[acc]);              // accumulator complete
-        if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
-      if (!ok) {
-        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
-      }
+      if (!ok) break;
+      if (elect_one()) mma_commit(&acc_full[acc]);             // accumulator complete
+      if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+    }
+    if (!ok) {
+      for (int i = 0; i < 1000; ++i) __nanosleep(1000);
     }
   } else {
     const int quarter = warp & 3;                 // TMEM lanes this warp may read

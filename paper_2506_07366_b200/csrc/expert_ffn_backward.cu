@@ -100,27 +100,49 @@ __device__ __forceinline__ void act_gradient(uint32_t gw, uint32_t uw, float gs,
   }
 }
 
-// Epilogue of (1) for one warp: 32 rows x [c_begin, c_end) columns of dh.  The codes of a chunk are loaded while the
-// chunk before it is worked on (the first one before the accumulator is complete).
-__device__ __forceinline__ void drain_act(uint32_t taddr, uint8_t* staging, int lane, const KeptActs& kept, KeptBlock& next,
-                                          const ActOutputs& out, int row0, int row_end, int col0, int n_dim, int c_begin,
-                                          int c_end, int rcap) {
+// 16 consecutive bf16 of one row; the first and the second eight may lie beyond the row's end.
+__device__ __forceinline__ void store16(__nv_bfloat16* at, const uint32_t (&o)[8], bool first, bool second, bool whole_sectors) {
+  if (whole_sectors && second) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]),
+                 "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7])
+                 : "memory");
+  } else {
+    if (first) *reinterpret_cast<uint4*>(at) = make_uint4(o[0], o[1], o[2], o[3]);
+    if (second) *reinterpret_cast<uint4*>(at + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+  }
+}
+
+// Epilogue of (1) for one warp: 32 rows x [c_begin, c_end) columns of dh, one row for each lane.  The codes of a chunk are
+// loaded while the chunk before it is worked on (the first one before the accumulator is complete).  A lane stores 16
+// columns of its row at a time, a whole 32-byte sector, straight from its registers: with three results to store, keeping
+// a chunk of each for the staging buffer that the other epilogues use costs more registers than there are.
+__device__ __forceinline__ void drain_act(uint32_t taddr, int lane, const KeptActs& kept, KeptBlock& next, const ActOutputs& out,
+                                          int row0, int row_end, int col0, int n_dim, int c_begin, int c_end, int rcap,
+                                          bool whole_sectors) {
+  const int row = row0 + lane;
 #pragma unroll 1
   for (int c0 = c_begin; c0 < c_end; c0 += 32) {
     const KeptBlock cur = next;
-    if (c0 + 32 < c_end) load_block(next, kept, row0 + lane, row_end, col0 + c0 + 32, n_dim, rcap);
+    if (c0 + 32 < c_end) load_block(next, kept, row, row_end, col0 + c0 + 32, n_dim, rcap);
     uint32_t acc[32];
     tmem_ld32(taddr + c0, acc);
     tmem_ld_wait();
     const float gs = act8::scale_of(cur.gs), us = act8::scale_of(cur.us);
-    const uint32_t gw[8] = {cur.g[0].x, cur.g[0].y, cur.g[0].z, cur.g[0].w, cur.g[1].x, cur.g[1].y, cur.g[1].z, cur.g[1].w};
-    const uint32_t uw[8] = {cur.u[0].x, cur.u[0].y, cur.u[0].z, cur.u[0].w, cur.u[1].x, cur.u[1].y, cur.u[1].z, cur.u[1].w};
-    uint32_t dgate[16], dup[16], h[16];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) act_gradient(gw[i], uw[i], gs, us, acc + 4 * i, dgate + 2 * i, dup + 2 * i, h + 2 * i);
-    store_chunk(dgate, staging, lane, out.dgate, row0, row_end, col0 + c0, n_dim);
-    store_chunk(dup, staging, lane, out.dup, row0, row_end, col0 + c0, n_dim);
-    store_chunk(h, staging, lane, out.h, row0, row_end, col0 + c0, n_dim);
+    for (int half = 0; half < 2; ++half) {
+      const uint32_t gw[4] = {cur.g[half].x, cur.g[half].y, cur.g[half].z, cur.g[half].w};
+      const uint32_t uw[4] = {cur.u[half].x, cur.u[half].y, cur.u[half].z, cur.u[half].w};
+      uint32_t dgate[8], dup[8], h[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        act_gradient(gw[i], uw[i], gs, us, acc + 16 * half + 4 * i, dgate + 2 * i, dup + 2 * i, h + 2 * i);
+      const int col = col0 + c0 + 16 * half;
+      const bool first = row < row_end && col + 8 <= n_dim, second = row < row_end && col + 16 <= n_dim;
+      const size_t at = (size_t)row * n_dim + col;
+      store16(out.dgate + at, dgate, first, second, whole_sectors);
+      store16(out.dup + at, dup, first, second, whole_sectors);
+      store16(out.h + at, h, first, second, whole_sectors);
+    }
   }
 }
 
@@ -182,7 +204,7 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
   Tables& tb = *reinterpret_cast<Tables*>(stage_mem + (size_t)kStages * kStageBytes);
   const Bars<Cfg> bar(stage_mem + (size_t)kStages * kStageBytes + sizeof(Tables));
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
   const int n_tiles = (n_dim + BN - 1) / BN;
   const int kb_per_pair = (k_dim + BK - 1) / BK;
   const int num_kb = kAct ? kb_per_pair : 2 * kb_per_pair;
@@ -232,38 +254,42 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
       if (!ok) linger();
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      constexpr uint32_t idesc = idesc_bf16_f32(BM, BN, false, true);
-      int stage = 0, acc = 0;
-      uint32_t phase = 0, acc_phase = 0;
-      bool ok = true;
-      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
-        if (!mbar_wait(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag)) { ok = false; break; }
+    constexpr uint32_t idesc = idesc_bf16_f32(BM, BN, false, true);
+    const uint32_t ring = smem_u32(stage_mem);
+    int stage = 0, acc = 0;
+    uint32_t phase = 0, acc_phase = 0;
+    bool ok = true;
+    for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
+      if (!warp_wait(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag)) { ok = false; break; }
+      tc_fence_after_sync();
+      const uint32_t d_tmem = tmem_base + (uint32_t)acc * BN;
+      for (int kb = 0; kb < num_kb; ++kb) {
+        if (!warp_wait(&bar.full[stage], phase, bar.abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
-        const uint32_t d_tmem = tmem_base + (uint32_t)acc * BN;
-        for (int kb = 0; kb < num_kb; ++kb) {
-          if (!mbar_wait(&bar.full[stage], phase, bar.abort_flag)) { ok = false; break; }
-          tc_fence_after_sync();
-          const uint32_t sa = smem_u32(stage_mem + (size_t)stage * kStageBytes);
-          const uint64_t da = smem_desc_k<kRowBytes>(sa);
-          const uint64_t db = smem_desc_mn(sa + kABytes, kBoxBytes);
+        const uint32_t sa = ring + (uint32_t)stage * kStageBytes;
+        const uint64_t da = smem_desc_k<kRowBytes>(sa);
+        const uint64_t db = smem_desc_mn(sa + kABytes, kBoxBytes);
+        if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < BK / 16; ++k)      // A advances 32 bytes along its rows, B 16 rows of 128 bytes
             mma_bf16(d_tmem, da + (uint64_t)(k * 2), db + (uint64_t)(k * 128), idesc, (kb | k) != 0);
           mma_commit(&bar.empty[stage]);
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
-        if (!ok) break;
-        mma_commit(&bar.acc_full[acc]);
-        if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
-      if (!ok) linger();
+      if (!ok) break;
+      if (elect_one()) mma_commit(&bar.acc_full[acc]);
+      if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
     }
+    if (!ok) linger();
   } else {
     const int quarter = warp & 3;                 // TMEM lanes this warp may read
     constexpr int kShare = BN / (Cfg::kEpiWarps / 4);
     const int c_begin = ((warp - 2) >> 2) * kShare;
     uint8_t* staging = stage_mem + (size_t)kStages * kStageBytes + sizeof(Tables) + 256 + (warp - 2) * kStagingBytesPerWarp;
+    [[maybe_unused]] const bool whole_sectors =
+        ((reinterpret_cast<uintptr_t>(act_out.dgate) | reinterpret_cast<uintptr_t>(act_out.dup) |
+          reinterpret_cast<uintptr_t>(act_out.h) | (uintptr_t)n_dim * 2) & 31) == 0;
     int acc = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
@@ -276,7 +302,7 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
       tc_fence_after_sync();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * BN;
       if constexpr (kAct)
-        drain_act(taddr, staging, lane, kept, block, act_out, row0, tc.row_end, col0, n_dim, c_begin, c_begin + kShare, rcap);
+        drain_act(taddr, lane, kept, block, act_out, row0, tc.row_end, col0, n_dim, c_begin, c_begin + kShare, rcap, whole_sectors);
       else
         drain_plain(taddr, staging, lane, out, row0, tc.row_end, col0, n_dim, c_begin, c_begin + kShare);
       tc_fence_before_sync();
@@ -417,7 +443,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
   SlotRows& sr = *reinterpret_cast<SlotRows*>(out_mem + Cfg::kEpiWarps * Cfg::kOutBytes);
   const PairBars bar(reinterpret_cast<uint8_t*>(&sr) + sizeof(SlotRows));
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();           // 0: leader
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const WGeom geom(F, D);
@@ -525,59 +551,51 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
       if (!ok) linger();
     }
   } else if (warp == 1) {
-    if (rank == 0 && lane == 0) {
+    if (rank == 0) {
       const uint32_t ring = smem_u32(stage_mem);
       int stage = 0, acc = 0, expert = 0, ahead = 0;
       uint32_t phase = 0, acc_phase = 0, tail_phase = 0;       // tail_phase: a bit for each stage
       bool ok = true;
-      // The tensor core holds a few MMAs at most, so what this thread does between two tiles is time lost: it takes a
+      // The tensor core holds a few MMAs at most, so what this warp does between two tiles is time lost: it takes a
       // tile's expert by counting and its width from the producer instead of decoding the tile (600 cycles).
       const int all = geom.per[0] + geom.per[1];
       int q = pair;
       for (int tile = pair; tile < total_tiles; tile += pairs, q += pairs) {
         for (; q >= all; q -= all) ++expert;
         if (s_rows[expert] == 0) continue;
-        if (!mbar_wait(&bar.full[stage], phase, bar.abort_flag)) { ok = false; break; }
+        if (!warp_wait(&bar.full[stage], phase, bar.abort_flag)) { ok = false; break; }
         const uint32_t idesc = s_width[ahead++ % Cfg::kAhead] == BNACC ? idesc_bf16_f32(2 * BM, BNACC, true, true)
                                                                        : idesc_bf16_f32(2 * BM, BNACC / 2, true, true);
-        if (!mbar_wait_cluster(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag)) { ok = false; break; }
+        if (!warp_wait_cluster(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
         const uint32_t d_tmem = tmem_base + (uint32_t)acc * BNACC;
         const int last = s_slot_off[expert + 1];
-        uint32_t accumulate = 0;
+        uint32_t more = 0;                                     // 0: the tile's first block, whose first MMA starts the sum
         for (int s = s_slot_off[expert]; ok && s < last; ++s) {
-          int left = sr.ext[s].y;
-          for (; left > 0; left -= BK) {
+          for (int left = sr.ext[s].y; left > 0; left -= BK) {
+            if (left < BK && (left & 15)) {
+              ok = warp_wait_cluster(&bar.tail_ready[stage], (tail_phase >> stage) & 1u, bar.abort_flag);
+              tail_phase ^= 1u << stage;
+            } else {
+              ok = warp_wait(&bar.full[stage], phase, bar.abort_flag);
+            }
+            if (!ok) break;
+            tc_fence_after_sync();
             const uint64_t da = smem_desc_mn(ring + (uint32_t)stage * kStageBytes, kBoxBytes);
             const uint64_t db = smem_desc_mn(ring + (uint32_t)stage * kStageBytes + Cfg::kAHalf, kBoxBytes);
-            if (left >= BK) {
-              if (!mbar_wait(&bar.full[stage], phase, bar.abort_flag)) { ok = false; break; }
-              tc_fence_after_sync();
+            if (elect_one()) {
 #pragma unroll
-              for (int k = 0; k < BK / 16; ++k) {
-                mma_bf16_pair(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
-                accumulate = 1;
-              }
-            } else {
-              if (left & 15) {
-                ok = mbar_wait_cluster(&bar.tail_ready[stage], (tail_phase >> stage) & 1u, bar.abort_flag);
-                tail_phase ^= 1u << stage;
-              } else {
-                ok = mbar_wait(&bar.full[stage], phase, bar.abort_flag);
-              }
-              if (!ok) break;
-              tc_fence_after_sync();
-              for (int k = 0; 16 * k < left; ++k) {
-                mma_bf16_pair(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, accumulate);
-                accumulate = 1;
-              }
+              for (int k = 0; k < BK / 16; ++k)
+                if (16 * k < left)
+                  mma_bf16_pair(d_tmem, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, k > 0 ? 1u : more);
+              mma_commit_pair(&bar.empty[stage]);
             }
-            mma_commit_pair(&bar.empty[stage]);
+            more = 1;
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
         }
         if (!ok) break;
-        mma_commit_pair(&bar.acc_full[acc]);
+        if (elect_one()) mma_commit_pair(&bar.acc_full[acc]);
         if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
       }
       if (!ok) linger();
