@@ -149,6 +149,8 @@ grouped_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
     prefetch_tensormap(&tm_b0);
     prefetch_tensormap(&tm_b1);
   }
+  launch_dependents();
+  wait_for_predecessor();
   if (warp == 1) {
     tmem_alloc(tmem_slot, Cfg::kTmemCols);
     tmem_relinquish();
@@ -331,9 +333,9 @@ int launch_gemm(moegps_ctx* ctx, bool* attr_done, const CUtensorMap& ta, const C
                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     *attr_done = true;
   }
-  grouped_gemm_kernel<kSwiGLU, kSave, Cfg><<<ctx->sm_count * Cfg::kCtasPerSm, Cfg::kThreads, smem, st>>>(
-      ta, tb0, tb1, slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim, (int)moegps_rcap_of(s),
-      static_cast<__nv_bfloat16*>(out), save, ctx->d_status);
+  MOEGPS_CUDA_TRY(ctx, launch_after(grouped_gemm_kernel<kSwiGLU, kSave, Cfg>, dim3(ctx->sm_count * Cfg::kCtasPerSm),
+                                    Cfg::kThreads, smem, st, ta, tb0, tb1, slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim,
+                                    (int)moegps_rcap_of(s), static_cast<__nv_bfloat16*>(out), save, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }

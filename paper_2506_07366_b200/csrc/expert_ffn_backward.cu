@@ -112,6 +112,12 @@ __device__ __forceinline__ void store16(__nv_bfloat16* at, const uint32_t (&o)[8
   }
 }
 
+// whether 16 columns that start at a multiple of 16 are a whole 32-byte sector in all three results
+__device__ __forceinline__ bool act_whole_sectors(const ActOutputs& out, int n_dim) {
+  return ((reinterpret_cast<uintptr_t>(out.dgate) | reinterpret_cast<uintptr_t>(out.dup) | reinterpret_cast<uintptr_t>(out.h) |
+           (uintptr_t)n_dim * 2) & 31) == 0;
+}
+
 // Epilogue of (1) for one warp: 32 rows x [c_begin, c_end) columns of dh, one row for each lane.  The codes of a chunk are
 // loaded while the chunk before it is worked on (the first one before the accumulator is complete).  A lane stores 16
 // columns of its row at a time, a whole 32-byte sector, straight from its registers: with three results to store, keeping
@@ -287,9 +293,7 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
     constexpr int kShare = BN / (Cfg::kEpiWarps / 4);
     const int c_begin = ((warp - 2) >> 2) * kShare;
     uint8_t* staging = stage_mem + (size_t)kStages * kStageBytes + sizeof(Tables) + 256 + (warp - 2) * kStagingBytesPerWarp;
-    [[maybe_unused]] const bool whole_sectors =
-        ((reinterpret_cast<uintptr_t>(act_out.dgate) | reinterpret_cast<uintptr_t>(act_out.dup) |
-          reinterpret_cast<uintptr_t>(act_out.h) | (uintptr_t)n_dim * 2) & 31) == 0;
+    [[maybe_unused]] const bool whole_sectors = act_whole_sectors(act_out, n_dim);
     int acc = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
@@ -322,6 +326,196 @@ data_gradient_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_con
   }
 }
 
+// The barriers of a kernel whose tiles are worked by pairs of CTAs.  full counts both CTAs' bytes on the leader; empty and
+// acc_full are signalled in both CTAs by the leader's commits; acc_empty collects both CTAs' epilogue warps on the leader.
+// tail_full, tail_ready (weight_gradient_kernel only): at a slot's end, where rows have to be blanked before the MMA, each
+// CTA's bytes go to its own tail_full, and the warps that blank report to the leader's tail_ready.
+struct PairCfg {
+  static constexpr int kStages = 6, kAccs = 2, kEpiWarps = 8, kTmemCols = kAccs * BNACC;
+  static constexpr int kAHalf = 2 * kBoxBytes, kStageBytes = 4 * kBoxBytes;        // per CTA: 128 rows of A, 128 columns of B
+};
+struct PairBars {
+  uint64_t *full, *empty, *tail_full, *tail_ready, *acc_full, *acc_empty;
+  uint32_t* tmem_slot;
+  volatile int* abort_flag;
+  __device__ explicit PairBars(uint8_t* at) {
+    constexpr int n = PairCfg::kStages;
+    full = reinterpret_cast<uint64_t*>(at);
+    empty = full + n;
+    tail_full = empty + n;
+    tail_ready = tail_full + n;
+    acc_full = tail_ready + n;
+    acc_empty = acc_full + PairCfg::kAccs;
+    tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + PairCfg::kAccs);
+    abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  }
+  __device__ void init() const {
+    for (int i = 0; i < PairCfg::kStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+      mbar_init(&tail_full[i], 1);
+      mbar_init(&tail_ready[i], 2);
+    }
+    for (int i = 0; i < PairCfg::kAccs; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_empty[i], 2 * PairCfg::kEpiWarps);
+    }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+};
+static_assert((4 * PairCfg::kStages + 2 * PairCfg::kAccs) * 8 + 8 <= 256, "barriers fit their space");
+
+// ------------------------------------------------------------------------------------------------ (1) and (2), by pairs
+// The same products on 256 x 256 tiles of a slot: each CTA of a pair has 128 of the rows, loads them and half the columns
+// of the weights, 32 KiB for a K block instead of 48.  For slots of several hundred rows and more: the last tile of a slot
+// leaves the second CTA idle when it has at most 128 rows.  Measured, whole gradient: 2048 rows a slot (16384 tokens, 16
+// slots) 20.4 -> 19.8 ms, 614 rows a slot (64 experts, 80 slots) 1.96 -> 1.94 ms, 137 rows a slot not faster.
+struct PairDataCfg : PairCfg {
+  static constexpr int kThreads = 64 + 32 * kEpiWarps;
+  static constexpr size_t kSmem =
+      1024 + (size_t)kStages * kStageBytes + sizeof(Tables) + 256 + (size_t)kEpiWarps * kStagingBytesPerWarp;
+};
+static_assert(PairDataCfg::kSmem <= 227 * 1024, "one CTA per SM");
+
+template <bool kAct>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairDataCfg::kThreads, 1)
+data_gradient_pair_kernel(const __grid_constant__ CUtensorMap tm_a0, const __grid_constant__ CUtensorMap tm_b0,
+                          const __grid_constant__ CUtensorMap tm_a1, const __grid_constant__ CUtensorMap tm_b1,
+                          const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert, int S, int E,
+                          int n_dim, int k_dim, int rcap, const KeptActs kept, const ActOutputs act_out,
+                          __nv_bfloat16* __restrict__ out, int32_t* __restrict__ status) {
+  using Cfg = PairDataCfg;
+  constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs, kStageBytes = Cfg::kStageBytes;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* stage_mem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  Tables& tb = *reinterpret_cast<Tables*>(stage_mem + (size_t)kStages * kStageBytes);
+  const PairBars bar(stage_mem + (size_t)kStages * kStageBytes + sizeof(Tables));
+
+  const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
+  const int rank = (int)cluster_ctarank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int n_tiles = (n_dim + BNACC - 1) / BNACC;
+  const int kb_per_pair = (k_dim + BK - 1) / BK;
+  const int num_kb = kAct ? kb_per_pair : 2 * kb_per_pair;
+
+  if (threadIdx.x == 0) {
+    bar.init();
+    prefetch_tensormap(&tm_a0);
+    prefetch_tensormap(&tm_b0);
+    if (!kAct) { prefetch_tensormap(&tm_a1); prefetch_tensormap(&tm_b1); }
+  }
+  launch_dependents();
+  wait_for_predecessor();
+  if (warp == 1) {
+    tmem_alloc_pair(bar.tmem_slot, Cfg::kTmemCols);
+    tmem_relinquish_pair();
+  }
+  build_tables<Cfg::kThreads, 2 * BM>(tb, slot_row_off, slot_expert, S, E, n_tiles, rcap, status);
+  __syncwarp();
+  tc_fence_before_sync();
+  cluster_sync_all();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *bar.tmem_slot;
+  const int total_tiles = tb.tile_base[S];
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      const uint32_t leader_full = map_to_cta(smem_u32(bar.full), 0);
+      for (int tile = pair; ok && tile < total_tiles; tile += pairs) {
+        const TileCoord tc = decode_tile<2 * BM>(tb, slot_row_off, slot_expert, S, tile, n_tiles);
+        const int m0 = tc.m0 + rank * BM, n0 = tc.n_tile * BNACC + rank * (BNACC / 2);
+        for (int kb = 0; kb < num_kb; ++kb) {
+          if (!mbar_wait(&bar.empty[stage], phase ^ 1u, bar.abort_flag)) { ok = false; break; }
+          uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
+          if (rank == 0) mbar_arrive_expect_tx(&bar.full[stage], 2 * kStageBytes);
+          const bool second = !kAct && kb >= kb_per_pair;
+          const int k0 = (second ? kb - kb_per_pair : kb) * BK;
+          const CUtensorMap* ta = second ? &tm_a1 : &tm_a0;
+          const CUtensorMap* tbm = second ? &tm_b1 : &tm_b0;
+          const uint32_t to = leader_full + stage * 8;
+          tma_load_2d_pair(sa, ta, to, k0, m0);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) tma_load_3d_pair(sa + Cfg::kAHalf + i * kBoxBytes, tbm, to, n0 + 64 * i, k0, tc.expert);
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (!ok) linger();
+    }
+  } else if (warp == 1) {
+    if (rank == 0) {
+      constexpr uint32_t idesc = idesc_bf16_f32(2 * BM, BNACC, false, true);
+      const uint32_t ring = smem_u32(stage_mem);
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = true;
+      for (int tile = pair; ok && tile < total_tiles; tile += pairs) {
+        if (!warp_wait_cluster(&bar.acc_empty[acc], acc_phase ^ 1u, bar.abort_flag)) { ok = false; break; }
+        tc_fence_after_sync();
+        const uint32_t d_tmem = tmem_base + (uint32_t)acc * BNACC;
+        for (int kb = 0; kb < num_kb; ++kb) {
+          if (!warp_wait(&bar.full[stage], phase, bar.abort_flag)) { ok = false; break; }
+          tc_fence_after_sync();
+          const uint32_t sa = ring + (uint32_t)stage * kStageBytes;
+          const uint64_t da = smem_desc_k<kRowBytes>(sa);
+          const uint64_t db = smem_desc_mn(sa + Cfg::kAHalf, kBoxBytes);
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < BK / 16; ++k)
+              mma_bf16_pair(d_tmem, da + (uint64_t)(k * 2), db + (uint64_t)(k * 128), idesc, (kb | k) != 0);
+            mma_commit_pair(&bar.empty[stage]);
+          }
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        if (elect_one()) mma_commit_pair(&bar.acc_full[acc]);
+        if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+      }
+      if (!ok) linger();
+    }
+  } else {
+    const int quarter = warp & 3;
+    constexpr int kShare = BNACC / (Cfg::kEpiWarps / 4);
+    const int c_begin = ((warp - 2) >> 2) * kShare;
+    uint8_t* staging = stage_mem + (size_t)kStages * kStageBytes + sizeof(Tables) + 256 + (warp - 2) * kStagingBytesPerWarp;
+    const uint32_t leader_empty = map_to_cta(smem_u32(bar.acc_empty), 0);
+    [[maybe_unused]] const bool whole_sectors = act_whole_sectors(act_out, n_dim);
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    for (int tile = pair; tile < total_tiles; tile += pairs) {
+      const TileCoord tc = decode_tile<2 * BM>(tb, slot_row_off, slot_expert, S, tile, n_tiles);
+      const int row0 = tc.m0 + rank * BM + quarter * 32, col0 = tc.n_tile * BNACC;
+      [[maybe_unused]] KeptBlock block;
+      if constexpr (kAct) load_block(block, kept, row0 + lane, tc.row_end, col0 + c_begin, n_dim, rcap);
+      if (!mbar_wait(&bar.acc_full[acc], acc_phase, bar.abort_flag, 256)) break;
+      tc_fence_after_sync();
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * BNACC;
+      if (row0 < tc.row_end) {                       // (a warp without rows of the slot has nothing to store)
+        if constexpr (kAct)
+          drain_act(taddr, lane, kept, block, act_out, row0, tc.row_end, col0, n_dim, c_begin, c_begin + kShare, rcap,
+                    whole_sectors);
+        else
+          drain_plain(taddr, staging, lane, out, row0, tc.row_end, col0, n_dim, c_begin, c_begin + kShare);
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_remote(leader_empty + acc * 8);
+      if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+    }
+  }
+
+  __syncwarp();
+  tc_fence_before_sync();
+  cluster_sync_all();                                // nobody touches the other CTA's memory after this
+  if (threadIdx.x == 0 && *bar.abort_flag) moegps_report(status, MOEGPS_ERR_TIMEOUT, (int)blockIdx.x);
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc_pair(tmem_base, Cfg::kTmemCols);
+  }
+}
+
 // ------------------------------------------------------------------------------------------------ (3)
 // Occupied rows of every slot: first row and count.  The padding that dispatch leaves at a slot's end (row_pair < 0)
 // holds no token and must not enter the sums, whatever its memory holds.
@@ -336,9 +530,7 @@ struct SlotRows {
 // granules, whichever gradient each belongs to, so no pair has an idle half), and dyp times h (dW2).  A last column tile with
 // at most 128 columns is worked as 256 x 128.  Inside a problem the order runs over bands of kBand tiles in M, column by
 // column: tiles in flight at the same time form a near-square patch, so the operand columns they read are shared in L2.
-struct WeightCfg {
-  static constexpr int kAHalf = 2 * kBoxBytes, kStageBytes = 4 * kBoxBytes;                  // per CTA
-  static constexpr int kStages = 6, kAccs = 2, kEpiWarps = 8, kTmemCols = kAccs * BNACC;
+struct WeightCfg : PairCfg {
   static constexpr int kBlankWarp = 2 + kEpiWarps, kThreads = 32 * (3 + kEpiWarps);          // producer, MMA, epilogue, blank
   static constexpr int kOutBytes = 32 * 64;                                  // of an epilogue warp: 32 rows x 32 columns, bf16
   static constexpr int kAhead = 8;                                           // > tiles that the producer can be ahead: kStages
@@ -389,41 +581,6 @@ struct WGeom {
     m0 = g * BM;
   }
 };
-
-// The barriers.  full counts both CTAs' bytes on the leader; empty and acc_full are signalled in both CTAs by the leader's
-// commits; acc_empty collects both CTAs' epilogue warps on the leader.  At a slot's end, where rows have to be blanked
-// before the MMA, each CTA's bytes go to its own tail_full, and the warps that blank report to the leader's tail_ready.
-struct PairBars {
-  uint64_t *full, *empty, *tail_full, *tail_ready, *acc_full, *acc_empty;
-  uint32_t* tmem_slot;
-  volatile int* abort_flag;
-  __device__ explicit PairBars(uint8_t* at) {
-    constexpr int n = WeightCfg::kStages;
-    full = reinterpret_cast<uint64_t*>(at);
-    empty = full + n;
-    tail_full = empty + n;
-    tail_ready = tail_full + n;
-    acc_full = tail_ready + n;
-    acc_empty = acc_full + WeightCfg::kAccs;
-    tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + WeightCfg::kAccs);
-    abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  }
-  __device__ void init() const {
-    for (int i = 0; i < WeightCfg::kStages; ++i) {
-      mbar_init(&full[i], 1);
-      mbar_init(&empty[i], 1);
-      mbar_init(&tail_full[i], 1);
-      mbar_init(&tail_ready[i], 2);
-    }
-    for (int i = 0; i < WeightCfg::kAccs; ++i) {
-      mbar_init(&acc_full[i], 1);
-      mbar_init(&acc_empty[i], 2 * WeightCfg::kEpiWarps);
-    }
-    *abort_flag = 0;
-    fence_mbar_init();
-  }
-};
-static_assert((4 * WeightCfg::kStages + 2 * WeightCfg::kAccs) * 8 + 8 <= 256, "barriers fit their space");
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WeightCfg::kThreads, 1)
 weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __grid_constant__ CUtensorMap tm_dup,
@@ -727,22 +884,55 @@ int launch_data_gradient(moegps_ctx* ctx, const CUtensorMap& a0, const CUtensorM
   return MOEGPS_OK;
 }
 
-// Tile width for n_dim output columns: the widest with a tile for every SM.  The slots' loads are on the device; a layer
-// has at least R / BM row tiles, and about one for each slot.
-int tile_width(const moegps_ctx* ctx, int n_dim) {
+template <bool kAct>
+int launch_data_gradient_pair(moegps_ctx* ctx, const CUtensorMap& a0, const CUtensorMap& b0, const CUtensorMap& a1,
+                              const CUtensorMap& b1, const int32_t* slot_row_off, const int32_t* slot_expert, int n_dim,
+                              int k_dim, const KeptActs& kept, const ActOutputs& act_out, void* out, cudaStream_t st) {
+  using Cfg = PairDataCfg;
   const moegps_shape_t& s = ctx->shape;
-  const int64_t R = (int64_t)s.T * s.K, spread = s.S < R ? s.S : R, full = (R + BM - 1) / BM;
-  const int64_t row_tiles = full > spread ? full : spread;
-  for (int bn : {256, 128})
-    if (row_tiles * ((n_dim + bn - 1) / bn) >= ctx->sm_count) return bn;
-  return 64;
+  bool& done = ctx->data_gradient_attr_done[kAct ? 0 : 1][3];
+  if (!done) {
+    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(data_gradient_pair_kernel<kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                              (int)Cfg::kSmem));
+    done = true;
+  }
+  MOEGPS_CUDA_TRY(ctx, launch_after(data_gradient_pair_kernel<kAct>, dim3(ctx->sm_count / 2 * 2), Cfg::kThreads, Cfg::kSmem, st,
+                                    a0, b0, a1, b1, slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim, (int)moegps_rcap_of(s),
+                                    kept, act_out, static_cast<__nv_bfloat16*>(out), ctx->d_status));
+  MOEGPS_AFTER_LAUNCH(ctx);
+  return MOEGPS_OK;
+}
+
+enum class Tiles { kPair, k256, k128, k64 };
+
+// The tiles for n_dim output columns: what needs the fewest rounds of tiles over the SMs, weighted with a round's time
+// (relative to 128 x 256; measured cycles for a K block 690-860, 400, 330 and 600).  The slots' loads are on the device:
+// the estimate is that of evenly loaded slots, whose last tile is half full.
+Tiles choose_tiles(const moegps_ctx* ctx, int n_dim) {
+  const moegps_shape_t& s = ctx->shape;
+  const double R = (double)s.T * s.K, slots = s.S < R ? s.S : R;
+  Tiles best = Tiles::k256;
+  double least = 1e300;
+  const struct { Tiles tiles; int rows, cols, sms; double time; } all[] = {
+      {Tiles::k256, BM, 256, 1, 1.0}, {Tiles::k128, BM, 128, 1, 0.6}, {Tiles::k64, BM, 64, 1, 0.5}, {Tiles::kPair, 2 * BM, 256, 2, 0.85}};
+  for (const auto& t : all) {
+    const double rounds = (R / t.rows + 0.5 * slots) * ((n_dim + t.cols - 1) / t.cols) / (ctx->sm_count / t.sms);
+    // (many rounds even out, a few do not)
+    const double time = (rounds < 8 ? (double)(int64_t)(rounds + 0.999) : rounds) * t.time;
+    if (time < least) {
+      least = time;
+      best = t.tiles;
+    }
+  }
+  return best;
 }
 
 template <bool kAct, typename... Args>
 int launch_data_gradient_any(moegps_ctx* ctx, int n_dim, Args... args) {
-  switch (tile_width(ctx, n_dim)) {
-    case 256: return launch_data_gradient<kAct, 256>(ctx, args...);
-    case 128: return launch_data_gradient<kAct, 128>(ctx, args...);
+  switch (choose_tiles(ctx, n_dim)) {
+    case Tiles::kPair: return launch_data_gradient_pair<kAct>(ctx, args...);
+    case Tiles::k256: return launch_data_gradient<kAct, 256>(ctx, args...);
+    case Tiles::k128: return launch_data_gradient<kAct, 128>(ctx, args...);
     default: return launch_data_gradient<kAct, 64>(ctx, args...);
   }
 }

@@ -55,6 +55,7 @@ struct TileCoord {
   int expert;
 };
 
+template <int kRows = BM>
 __device__ __forceinline__ TileCoord decode_tile(const Tables& tb, const int32_t* __restrict__ slot_row_off,
                                                const int32_t* __restrict__ slot_expert, int S, int tile, int n_tiles) {
   int lo = 0, hi = S;                 // find s with tile_base[s] <= tile < tile_base[s+1]
@@ -69,7 +70,7 @@ __device__ __forceinline__ TileCoord decode_tile(const Tables& tb, const int32_t
   c.n_tile = local / mt;
   // (the slot tables are a few KiB that every CTA reads: they stay in L1/L2; only slots that passed
   // the checks of the table build own tiles, so these values are in range)
-  c.m0 = __ldg(slot_row_off + s) + (local % mt) * BM;
+  c.m0 = __ldg(slot_row_off + s) + (local % mt) * kRows;
   c.row_end = __ldg(slot_row_off + s + 1);
   c.expert = __ldg(slot_expert + s);
   return c;
@@ -105,7 +106,7 @@ __device__ __forceinline__ void store_chunk(const uint32_t (&o)[16], uint8_t* st
 // all 1024 this took over 2 us of a 12 us launch on an 8-slot layer.
 // A slot whose extent is not inside [0, rcap] (offsets negative, decreasing or past the buffers) gets no
 // tiles: nothing is read or written for it, and the caller is told.
-template <int kThreads>
+template <int kThreads, int kRows = BM>       // kRows: rows of a tile
 __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restrict__ slot_row_off,
                                              const int32_t* __restrict__ slot_expert, int S, int E, int n_tiles, int rcap,
                                              int32_t* __restrict__ status) {
@@ -116,7 +117,7 @@ __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restri
     if (lo < 0 || hi < lo || hi > rcap) {
       if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
     } else if (hi > lo && e >= 0 && e < E) {
-      cnt = ((hi - lo + BM - 1) / BM) * n_tiles;
+      cnt = ((hi - lo + kRows - 1) / kRows) * n_tiles;
     } else if (hi > lo && e >= E) {
       if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
     }
