@@ -69,9 +69,10 @@ inline void moegps_trace_launch(const moegps_ctx* ctx, const char* where) {
 
 // Launches a kernel that may start while the stream's previous kernel still runs, as far as its own
 // wait_for_predecessor(): the launch and the set-up in front of that call overlap the predecessor's end.
+// early = false: an ordinary launch.
 template <typename... KArgs, typename... Args>
-static inline cudaError_t launch_after(void (*kernel)(KArgs...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st,
-                                       Args... args) {
+static inline cudaError_t launch_after_if(bool early, void (*kernel)(KArgs...), dim3 grid, unsigned threads, size_t smem,
+                                          cudaStream_t st, Args... args) {
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
@@ -81,8 +82,13 @@ static inline cudaError_t launch_after(void (*kernel)(KArgs...), dim3 grid, unsi
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = early ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+template <typename... KArgs, typename... Args>
+static inline cudaError_t launch_after(void (*kernel)(KArgs...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st,
+                                       Args... args) {
+  return launch_after_if(true, kernel, grid, threads, smem, st, args...);
 }
 
 static inline bool moegps_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

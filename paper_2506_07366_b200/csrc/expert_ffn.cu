@@ -333,7 +333,11 @@ int launch_gemm(moegps_ctx* ctx, bool* attr_done, const CUtensorMap& ta, const C
                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     *attr_done = true;
   }
-  MOEGPS_CUDA_TRY(ctx, launch_after(grouped_gemm_kernel<kSwiGLU, kSave, Cfg>, dim3(ctx->sm_count * Cfg::kCtasPerSm),
+  // An early launch saves 1.1 of the 10.3 us of gate_up_save on an 8-expert layer of 512 pairs, and costs 2 % (597 -> 608
+  // us) on 64 experts and 49152 pairs, where a launch runs some 30 rounds of tiles: only up to four rounds.
+  const int64_t tiles = ((int64_t)s.T * s.K / BM + s.S) * ((n_dim + (kSwiGLU ? 127 : 255)) / (kSwiGLU ? 128 : 256));
+  const bool early = tiles <= 4 * (int64_t)ctx->sm_count;
+  MOEGPS_CUDA_TRY(ctx, launch_after_if(early, grouped_gemm_kernel<kSwiGLU, kSave, Cfg>, dim3(ctx->sm_count * Cfg::kCtasPerSm),
                                     Cfg::kThreads, smem, st, ta, tb0, tb1, slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim,
                                     (int)moegps_rcap_of(s), static_cast<__nv_bfloat16*>(out), save, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
