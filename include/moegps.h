@@ -343,10 +343,11 @@ MOEGPS_API int moegps_dispatch_backward(moegps_ctx_t* ctx, const void* dxp, cons
  *   gate_mode 0: dlogit[t,j] = topk_w (dtopk_w - m);  gate_mode 1: times 1 - sigmoid(logit), the K selected logits being
  *   computed again from x, w_router and bias.  Logits that were not selected have no gradient.
  *   dw_router[e] = sum dlogit x[t], dbias[e] = sum dlogit over the pairs of e (zero for an expert without pairs).
- * x: bf16 [T,D]; w_router: bf16 [E,D], bias: fp32 [E] or NULL and topk_idx: int32 [T,K] are read in gate_mode 1 only
- * (w_router and topk_idx may be NULL otherwise); topk_w, dtopk_w: fp32 [T,K]; slot_row_off, row_pair from dispatch,
- * slot_off from the plan (they list the pairs by expert); dlogit: fp32 [T,K]; dw_router: fp32 [E,D]; dbias: fp32 [E].
- * fp32 throughout, fixed summation order.  workspace: moegps_route_backward_workspace_bytes(shape) bytes, contents
+ * x: bf16 [T,D]; w_router: bf16 [E,D] and bias: fp32 [E] or NULL are read in gate_mode 1 only (w_router may be NULL
+ * otherwise); topk_idx: int32 [T,K] (NULL in gate_mode 0: found from the tables, two launches more); topk_w, dtopk_w: fp32
+ * [T,K]; slot_row_off, row_pair from dispatch, slot_off from the plan (they list the pairs by expert); dlogit: fp32 [T,K];
+ * dw_router: fp32 [E,D]; dbias: fp32 [E].
+ * fp32 throughout, fixed summation order; what a token's x holds enters only the rows of the experts it chose.  workspace: moegps_route_backward_workspace_bytes(shape) bytes, contents
  * irrelevant; its size cannot be checked here. */
 MOEGPS_API int moegps_route_backward(moegps_ctx_t* ctx, const void* x, const void* w_router, const float* bias,
                                      const int32_t* topk_idx, const float* topk_w, const float* dtopk_w,

@@ -437,7 +437,7 @@ class Context:
         topk_idx, topk_w, dtopk_w, dlogit = (t(n, d, s.T, s.K) for n, d in
                                              (("topk_idx", i32), ("topk_w", f32), ("dtopk_w", f32), ("dlogit", f32)))
         w_router, dx = t("w_router", bf16, s.E, s.D), t("dx", bf16, s.T, s.D)
-        softmax = s.gate_mode == 0                       # then w_router, bias and topk_idx are not read
+        softmax = s.gate_mode == 0                       # then w_router and topk_idx may be missing
         maybe = lambda spec: spec[:3] + (softmax,)  # noqa: E731
 
         def call(name, *specs):

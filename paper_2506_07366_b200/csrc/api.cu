@@ -52,7 +52,7 @@ int moegps_create(moegps_ctx_t** out, const moegps_shape_t* shape, int device) {
   for (bool& b : ctx->ffn_attr_done) b = false;
   for (auto& v : ctx->data_gradient_attr_done)
     for (bool& b : v) b = false;
-  ctx->weight_gradient_attr_done = false;
+  ctx->weight_gradient_attr_done = ctx->router_weight_attr_done = false;
   ctx->rt_valid = false;
   ctx->route_attr_done = false;
   ctx->dispatch_attr_done = false;
@@ -353,6 +353,7 @@ int moegps_route_backward(moegps_ctx_t* ctx, const void* x, const void* w_router
   }
   if (!all_ok(x, topk_w, dtopk_w, slot_row_off, slot_off, row_pair, dlogit, workspace)) return MOEGPS_ERR_INVALID_ARG;
   if (s.gate_mode == 1 && !all_ok(w_router, topk_idx)) return MOEGPS_ERR_INVALID_ARG;
+  if (topk_idx && !all_ok(topk_idx)) return MOEGPS_ERR_INVALID_ARG;
   if (bias && (reinterpret_cast<uintptr_t>(bias) & 3u)) return MOEGPS_ERR_INVALID_ARG;
   return moegps_launch_route_backward(ctx, x, w_router, bias, topk_idx, topk_w, dtopk_w, slot_row_off, slot_off, row_pair,
                                       dlogit, dw_router, dbias, workspace, st);

@@ -27,7 +27,7 @@ struct moegps_ctx {
   bool tm2_valid;
   bool ffn_attr_done[3]; // dynamic shared-memory limit raised: gate+up, down, gate+up with kept activations
   bool data_gradient_attr_done[2][4];   // the same for the gradient's kernels: (act, input) x tile shapes
-  bool weight_gradient_attr_done;
+  bool weight_gradient_attr_done, router_weight_attr_done;
   // cached TMA descriptors of the router
   const void* rt_key[2];
   CUtensorMap tm_rx, tm_rw;

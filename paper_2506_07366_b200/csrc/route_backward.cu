@@ -9,76 +9,37 @@
 //                logits again (route.cu), bit for bit those that the selection was made on.  Its tensor-core sums cost
 //                26 us on 4096 tokens x 7168 and 256 experts; 8 dot products for each token on the CUDA cores took 83 us
 //                with Wr from L2, and 40 + 6 us with slices of it in shared memory.
-//   2. dlogit  : one thread per pair.  One more block lists the units of the next step.
-//   3. partial : dlogit is sparse (K of E), so dWr is a weighted sum of rows rather than a matrix
-//                product: the pairs of one expert are consecutive in the permuted order, and a unit is
-//                up to kUnitRows of them.  Its rows of x are gathered through row_pair (x is read K
-//                times, but from L2: it is the unpermuted tensor) and summed in fp32.
-//   4. reduce  : the units of an expert are added in order.
+//   2. dlogit  : one thread per pair.
+//   3. weights : dWr = dl^T x on the tensor cores, dl as a dense [tokens x experts] matrix that exists only in shared
+//                memory, tile by tile.  A dl is split into three bf16 (8 + 8 + 8 bits: all of its 24), so the products are
+//                exact and the sums are fp32: three MMAs for one, but x is read once.  Summing each expert's rows of x
+//                instead, gathered K times from L2, ran at L2's rate (10 TB/s) and took 21 us + 8 us for joining the parts
+//                on 8192 tokens x 2048, 6 of 64 experts, and 41 + 12 us on 4096 x 7168, 8 of 256.
+//   4. reduce  : adds the parts of the tokens.  In the dense product a token that did not choose an expert adds 0 x, which
+//                is NaN where x is not finite: a sum that is not finite is therefore computed again from the expert's own
+//                pairs alone (they are consecutive in the permuted order), and is what the definition gives.
 // No atomics: the sums have a fixed order.  Each kernel is launched while the one before it drains (launch_after).
-#include "bf16x8.cuh"
 #include "common.cuh"
+#include "grouped_gemm.cuh"
 #include "route_backward.cuh"
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kUnitRows = route_backward::kUnitRows;
+using namespace sm100;
+using route_backward::kTileD;
+using route_backward::kTileE;
+using route_backward::kTileT;
 
-// Lists the units: expert e owns rows slot_row_off[slot_off[e]] .. slot_row_off[slot_off[e+1]], cut into
-// pieces of kUnitRows.  One block; thread e takes expert e (E <= 256).
-__device__ void list_units(int E, int S, int64_t Rcap, int max_units, const int32_t* __restrict__ slot_row_off,
-                           const int32_t* __restrict__ slot_off, int32_t* __restrict__ unit_first,
-                           int4* __restrict__ units, int32_t* status) {
-  __shared__ int32_t warp_tot[kWarps];
-  const int e = threadIdx.x, lane = e & 31, warp = e >> 5;
-  int lo = 0, hi = 0;
-  if (e < E) {
-    const int a = slot_off[e], b = slot_off[e + 1];
-    if (a < 0 || b < a || b > S) {
-      moegps_report(status, MOEGPS_ERR_BAD_INDEX, e);
-    } else {
-      lo = slot_row_off[a];
-      hi = slot_row_off[b];
-      if (lo < 0 || hi < lo || hi > Rcap) {
-        moegps_report(status, MOEGPS_ERR_BAD_INDEX, e);
-        lo = hi = 0;
-      }
-    }
-  }
-  const int n = (hi - lo + kUnitRows - 1) / kUnitRows;
-  int incl = n;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int o = __shfl_up_sync(0xffffffffu, incl, d);
-    if (lane >= d) incl += o;
-  }
-  if (lane == 31) warp_tot[warp] = incl;
-  __syncthreads();
-  int first = incl - n;
-  for (int v = 0; v < warp; ++v) first += warp_tot[v];
-  if (e < E) unit_first[e] = min(first, max_units);
-  if (e == E - 1) unit_first[E] = min(first + n, max_units);
-  // extents that overlap (a table no plan makes) could ask for more units than there is room for
-  if (first + n > max_units) moegps_report(status, MOEGPS_ERR_BAD_INDEX, e);
-  for (int i = 0; i < n && first + i < max_units; ++i)
-    units[first + i] = make_int4(e, lo + i * kUnitRows, min(hi, lo + (i + 1) * kUnitRows), 0);
-}
+constexpr int kThreads = 256;
 
 template <bool kSigmoid>
 __global__ void __launch_bounds__(kThreads)
-dlogit_kernel(const float* __restrict__ logits, const int32_t* __restrict__ topk_idx, const float* __restrict__ topk_w, const float* __restrict__ dtopk_w,
-              int64_t R, int K, int E, int S, int64_t Rcap, int max_units, const int32_t* __restrict__ slot_row_off,
-              const int32_t* __restrict__ slot_off, float* __restrict__ dlogit, int32_t* __restrict__ unit_first,
-              int4* __restrict__ units, int32_t* __restrict__ status) {
+dlogit_kernel(const float* __restrict__ logits, const int32_t* __restrict__ topk_idx, const float* __restrict__ topk_w,
+              const float* __restrict__ dtopk_w, int64_t R, int K, int E, float* __restrict__ dlogit,
+              int32_t* __restrict__ status) {
   launch_dependents();
   wait_for_predecessor();
-  if (blockIdx.x == 0) {
-    list_units(E, S, Rcap, max_units, slot_row_off, slot_off, unit_first, units, status);
-    return;
-  }
-  const int64_t p = ((int64_t)blockIdx.x - 1) * kThreads + threadIdx.x;
+  const int64_t p = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   if (p >= R) return;
   const int64_t p0 = p / K * K;
   float m = 0.f;
@@ -95,107 +56,302 @@ dlogit_kernel(const float* __restrict__ logits, const int32_t* __restrict__ topk
   dlogit[p] = d;
 }
 
-// block (u, c): columns [1024 c, 1024 c + 1024) of unit u; a thread sums eight columns over the unit's rows, eight rows
-// in flight at a time.  An expert with one unit needs no second pass: its sums are the result.
-constexpr int kPartThreads = 128;
+// ------------------------------------------------------------------------------------------------ dWr
+struct RouterCfg {
+  static constexpr int kBoxBytes = 64 * kTileT * 2;                  // 64 contiguous elements x 64 tokens
+  static constexpr int kSplitBytes = kTileE * kTileT * 2;            // one of the three parts of a dl tile
+  static constexpr int kABytes = 3 * kSplitBytes, kAStages = 2;      // built in shared memory
+  static constexpr int kBBytes = kTileD / 64 * kBoxBytes, kBStages = 3;
+  static constexpr int kBuilders = 4, kThreads = 32 * (2 + kBuilders), kPairs = kTileT * 8 / (32 * kBuilders);
+  static constexpr size_t kSmem = 1024 + kAStages * kABytes + kBStages * kBBytes + 256;
+};
+static_assert(RouterCfg::kSmem <= 227 * 1024, "fits an SM");
 
-__global__ void __launch_bounds__(kPartThreads)
-partial_kernel(const uint4* __restrict__ x, const int32_t* __restrict__ row_pair, const float* __restrict__ dlogit, int64_t R,
-               int K, int E, int D, const int32_t* __restrict__ unit_first, const int4* __restrict__ units,
-               float* __restrict__ part, float* __restrict__ part_b, float* __restrict__ dw_router,
-               int32_t* __restrict__ status) {
-  static_assert(kUnitRows == 64, "two warps list the unit's rows");
-  __shared__ float s_dl[kUnitRows];
-  __shared__ int s_t[kUnitRows];
-  __shared__ int s_n[2];
-  launch_dependents();
-  wait_for_predecessor();
-  const int u = blockIdx.x;
-  if (u >= unit_first[E]) return;
-  const int4 unit = units[u];
-  const int tid = threadIdx.x, lane = tid & 31;
-  // the unit's tokens in order, without its padding rows
-  int p = -1;
-  unsigned have = 0;
-  if (tid < kUnitRows) {
-    if (unit.y + tid < unit.z) p = row_pair[unit.y + tid];
-    if (p >= R) {
-      moegps_report(status, MOEGPS_ERR_BAD_INDEX, unit.y + tid);
-      p = -1;
-    }
-    have = __ballot_sync(0xffffffffu, p >= 0);
-    if (lane == 0) s_n[tid >> 5] = __popc(have);
-  }
-  __syncthreads();
-  const int n = s_n[0] + s_n[1];
-  if (p >= 0) {
-    const int at = (tid >= 32 ? s_n[0] : 0) + __popc(have & ((1u << lane) - 1));
-    s_dl[at] = dlogit[p];
-    s_t[at] = p / K;
-  }
-  __syncthreads();
-  const int chunks = D / 8, c = blockIdx.y * kPartThreads + tid;
-  if (blockIdx.y == 0 && tid == 0) {
-    float b = 0.f;
-    for (int r = 0; r < n; ++r) b += s_dl[r];
-    part_b[u] = b;
-  }
-  if (c >= chunks) return;
-  float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  const uint4* xc = x + c;
-  int r = 0;
-  for (; r + 8 <= n; r += 8) {
-    uint4 v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = xc[(int64_t)s_t[r + i] * chunks];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) fma8(acc, s_dl[r + i], v[i]);
-  }
-  for (; r < n; ++r) fma8(acc, s_dl[r], xc[(int64_t)s_t[r] * chunks]);
-  const bool only = unit_first[unit.x + 1] - unit_first[unit.x] == 1;
-  float4* o = reinterpret_cast<float4*>((only ? dw_router + (int64_t)unit.x * D : part + (int64_t)u * D) + 8 * c);
-  o[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-  o[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+// Byte offset of (token k, expert m) in an MN-major tile with the 128-byte swizzle: see smem_desc_mn.
+__device__ __forceinline__ uint32_t dl_offset(int k, int m) {
+  return (uint32_t)((m >> 6) * RouterCfg::kBoxBytes + k * 128 + ((((m >> 3) & 7) ^ (k & 7)) << 4) + (m & 7) * 2);
 }
 
-// The units of expert e are shared by W warps (each takes every W-th one, their sums are added in order), W growing with
-// their number, and a block's other warps take further groups of 128 columns: block (e, y) adds columns
-// [128 G y, 128 G y + 128 G), G = 8 / W.  The grid has room for G = 1; blocks beyond an expert's columns end at once.
-__global__ void __launch_bounds__(kThreads)
-reduce_kernel(const float* __restrict__ part, const float* __restrict__ part_b, int D,
-              const int32_t* __restrict__ unit_first, float* __restrict__ dw_router, float* __restrict__ dbias) {
-  __shared__ float4 s_acc[kWarps][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// block (expert tile x, column tile y, split z): warp 0 loads x, warp 1 multiplies, warps 2..5 build the dl tiles and, at
+// the end, store the sums.
+__global__ void __launch_bounds__(RouterCfg::kThreads, 1)
+router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __restrict__ pair_expert,
+                     const float* __restrict__ dlogit, int T, int K, int E, int D, int per, float* __restrict__ part,
+                     int32_t* __restrict__ status) {
+  using Cfg = RouterCfg;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* a_mem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* b_mem = a_mem + Cfg::kAStages * Cfg::kABytes;
+  uint64_t* a_full = reinterpret_cast<uint64_t*>(b_mem + Cfg::kBStages * Cfg::kBBytes);
+  uint64_t* a_empty = a_full + Cfg::kAStages;
+  uint64_t* b_full = a_empty + Cfg::kAStages;
+  uint64_t* b_empty = b_full + Cfg::kBStages;
+  uint64_t* done = b_empty + Cfg::kBStages;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
+  const int e0 = blockIdx.x * kTileE, d0 = blockIdx.y * kTileD;
+  const int first = blockIdx.z * per, steps = min(per, (T + kTileT - 1) / kTileT - first);
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < Cfg::kAStages; ++i) { mbar_init(&a_full[i], Cfg::kBuilders); mbar_init(&a_empty[i], 1); }
+    for (int i = 0; i < Cfg::kBStages; ++i) { mbar_init(&b_full[i], 1); mbar_init(&b_empty[i], 1); }
+    mbar_init(done, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    prefetch_tensormap(&tm_x);
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, kTileD);
+    tmem_relinquish();
+  }
+  // the dl tiles are zero but for the entries of the present tokens
+  for (int i = threadIdx.x; i < Cfg::kAStages * Cfg::kABytes / 16; i += Cfg::kThreads)
+    reinterpret_cast<uint4*>(a_mem)[i] = make_uint4(0, 0, 0, 0);
+  fence_proxy_async();
   launch_dependents();
   wait_for_predecessor();
-  const int e = blockIdx.x;
-  const int first = unit_first[e], last = unit_first[e + 1], n = last - first;
-  const int W = n <= 4 ? 1 : n <= 8 ? 2 : n <= 16 ? 4 : 8;
-  const int group = blockIdx.y * (kWarps / W) + warp / W, col = 128 * group + 4 * lane;
-  if (blockIdx.y * (kWarps / W) * 128 >= D || (n == 1 && blockIdx.y > 0)) return;
-  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (col < D && n != 1) {
-#pragma unroll 8
-    for (int u = first + warp % W; u < last; u += W) {
-      const float4 v = *reinterpret_cast<const float4*>(part + (int64_t)u * D + col);
-      a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int i = 0; i < steps; ++i) {
+        if (!mbar_wait(&b_empty[stage], phase ^ 1u, abort_flag)) { ok = false; break; }
+        uint8_t* sb = b_mem + stage * Cfg::kBBytes;
+        mbar_arrive_expect_tx(&b_full[stage], Cfg::kBBytes);
+#pragma unroll
+        for (int c = 0; c < kTileD / 64; ++c)
+          tma_load_2d(sb + c * Cfg::kBoxBytes, &tm_x, &b_full[stage], d0 + 64 * c, (first + i) * kTileT);
+        if (++stage == Cfg::kBStages) { stage = 0; phase ^= 1u; }
+      }
+      if (!ok)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+    }
+  } else if (warp == 1) {
+    constexpr uint32_t idesc = idesc_bf16_f32(kTileE, kTileD, true, true);
+    const uint32_t a_ring = smem_u32(a_mem), b_ring = smem_u32(b_mem);
+    int as = 0, bs = 0;
+    uint32_t a_phase = 0, b_phase = 0;
+    bool ok = true;
+    for (int i = 0; i < steps; ++i) {
+      if (!warp_wait(&b_full[bs], b_phase, abort_flag) || !warp_wait(&a_full[as], a_phase, abort_flag)) { ok = false; break; }
+      tc_fence_after_sync();
+      const uint64_t db = smem_desc_mn(b_ring + bs * Cfg::kBBytes, Cfg::kBoxBytes);
+      const uint64_t da = smem_desc_mn(a_ring + as * Cfg::kABytes, Cfg::kBoxBytes);
+      if (elect_one()) {
+#pragma unroll
+        for (int split = 0; split < 3; ++split)
+#pragma unroll
+          for (int k = 0; k < kTileT / 16; ++k)
+            mma_bf16(tmem_base, da + (uint64_t)(split * (Cfg::kSplitBytes >> 4) + k * 128), db + (uint64_t)(k * 128), idesc,
+                     (i | split | k) != 0);
+        mma_commit(&a_empty[as]);
+        mma_commit(&b_empty[bs]);
+      }
+      if (++as == Cfg::kAStages) { as = 0; a_phase ^= 1u; }
+      if (++bs == Cfg::kBStages) { bs = 0; b_phase ^= 1u; }
+    }
+    if (ok && elect_one()) mma_commit(done);
+    if (!ok)
+      for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+  } else {
+    const int builder = threadIdx.x - 64;
+    // the entries that this thread has set in each stage; -1: none
+    int set[Cfg::kAStages][Cfg::kPairs];
+#pragma unroll
+    for (int s = 0; s < Cfg::kAStages; ++s)
+#pragma unroll
+      for (int i = 0; i < Cfg::kPairs; ++i) set[s][i] = -1;
+    // this thread's pairs of a step: q = builder + 128 n, of token q / K; the next step's are loaded while this one's wait
+    // for their stage (all at once: one after the other, each behind the other's branch, they took longer than the MMAs)
+    int token[Cfg::kPairs], next_e[Cfg::kPairs];
+    float next_dl[Cfg::kPairs];
+#pragma unroll
+    for (int n = 0; n < Cfg::kPairs; ++n) token[n] = (builder + 32 * Cfg::kBuilders * n) / K;
+    auto fetch = [&](int i) {
+      const int64_t p0 = (int64_t)(first + i) * kTileT * K;
+#pragma unroll
+      for (int n = 0; n < Cfg::kPairs; ++n) {
+        const int64_t p = p0 + builder + 32 * Cfg::kBuilders * n;
+        const bool in = i < steps && token[n] < kTileT && p < (int64_t)T * K;
+        next_e[n] = in ? pair_expert[p] : -1;
+        next_dl[n] = in ? dlogit[p] : 0.f;
+      }
+    };
+    fetch(0);
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int i0 = 0; i0 < steps; i0 += Cfg::kAStages, phase ^= 1u) {
+#pragma unroll
+      for (int as = 0; as < Cfg::kAStages; ++as) {
+        const int i = i0 + as;
+        if (i < steps) {
+          int at[Cfg::kPairs];
+          float dl[Cfg::kPairs];
+#pragma unroll
+          for (int n = 0; n < Cfg::kPairs; ++n) {
+            const int m = next_e[n] - e0;
+            at[n] = next_e[n] >= 0 && m >= 0 && m < kTileE ? (int)dl_offset(token[n], m) : -1;
+            dl[n] = next_dl[n];
+          }
+          fetch(i + 1);
+          ok = ok && warp_wait(&a_empty[as], phase ^ 1u, abort_flag);
+          uint8_t* sa = a_mem + as * Cfg::kABytes;
+#pragma unroll
+          for (int n = 0; n < Cfg::kPairs; ++n)
+            if (ok && set[as][n] >= 0)
+#pragma unroll
+              for (int split = 0; split < 3; ++split)
+                *reinterpret_cast<__nv_bfloat16*>(sa + split * Cfg::kSplitBytes + set[as][n]) = __float2bfloat16(0.f);
+          // no entry is set before all old ones are gone (a warp whose wait failed comes here too: the count stays right)
+          asm volatile("bar.sync 1, %0;" ::"n"(32 * Cfg::kBuilders) : "memory");
+#pragma unroll
+          for (int n = 0; n < Cfg::kPairs; ++n) {
+            set[as][n] = at[n];
+            if (ok && at[n] >= 0) {
+              float rest = dl[n];
+#pragma unroll
+              for (int split = 0; split < 3; ++split) {
+                const __nv_bfloat16 v = __float2bfloat16(rest);       // nearest; what is left is exact in fp32
+                *reinterpret_cast<__nv_bfloat16*>(sa + split * Cfg::kSplitBytes + at[n]) = v;
+                rest -= __bfloat162float(v);
+              }
+            }
+          }
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&a_full[as]);
+        }
+      }
+    }
+    // ---- the sums: a lane's row is an expert ----
+    if (ok && mbar_wait(done, 0, abort_flag, 64)) {
+      tc_fence_after_sync();
+      const int quarter = warp & 3, e = e0 + quarter * 32 + lane;
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
+      float* row = part + ((int64_t)blockIdx.z * E + e) * D + d0;
+#pragma unroll 1
+      for (int c = 0; c < kTileD; c += 32) {
+        uint32_t v[32];
+        tmem_ld32(taddr + c, v);
+        tmem_ld_wait();
+        if (e < E) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 8)
+            if (d0 + c + i < D)                          // (D is a multiple of 8)
+              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + c + i), "r"(v[i]), "r"(v[i + 1]),
+                           "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
+                           : "memory");
+        }
+      }
     }
   }
-  s_acc[warp][lane] = a;
+
+  __syncwarp();
+  tc_fence_before_sync();
   __syncthreads();
-  if (warp % W == 0 && col < D && n != 1) {        // (one unit: partial_kernel has stored the result)
-    for (int v = 1; v < W; ++v) {
-      const float4 b = s_acc[warp + v][lane];
-      a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+  if (threadIdx.x == 0 && *abort_flag) moegps_report(status, MOEGPS_ERR_TIMEOUT, (int)blockIdx.x);
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, kTileD);
+  }
+}
+
+// Without topk_idx (the softmax form does not need it otherwise): the expert of every pair from the tables of the permutation.
+__global__ void __launch_bounds__(kThreads)
+pair_expert_kernel(const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_off,
+                   const int32_t* __restrict__ row_pair, int64_t R, int64_t Rcap, int S, int32_t* __restrict__ pair_expert,
+                   int32_t* __restrict__ status) {
+  const int e = blockIdx.x;
+  const int a = slot_off[e], b = slot_off[e + 1];
+  if (a < 0 || b < a || b > S) {
+    if (threadIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, e);
+    return;
+  }
+  const int lo = slot_row_off[a], hi = slot_row_off[b];
+  if (lo < 0 || hi < lo || hi > Rcap) {
+    if (threadIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, e);
+    return;
+  }
+  for (int r = lo + threadIdx.x; r < hi; r += kThreads) {
+    const int p = row_pair[r];
+    if (p >= 0 && p < R) pair_expert[p] = e;
+  }
+}
+
+// block (e, c): columns [1024 c, 1024 c + 1024) of expert e, four for each thread; the blocks behind the last columns add
+// dbias, a thread's pairs 16 at a time (their indices, then their values, in two round trips to memory)
+__global__ void __launch_bounds__(kThreads)
+reduce_kernel(const float* __restrict__ part, int splits, const __nv_bfloat16* __restrict__ x, const float* __restrict__ dlogit,
+              const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_off,
+              const int32_t* __restrict__ row_pair, int64_t R, int64_t Rcap, int K, int E, int S, int D,
+              float* __restrict__ dw_router, float* __restrict__ dbias, int32_t* __restrict__ status) {
+  __shared__ float s_sum[kThreads / 32];
+  launch_dependents();
+  wait_for_predecessor();
+  const int e = blockIdx.x, tid = threadIdx.x, col = blockIdx.y * 1024 + 4 * tid;
+  // the rows of the expert's pairs
+  int lo = 0, hi = 0;
+  {
+    const int a = slot_off[e], b = slot_off[e + 1];
+    bool valid = a >= 0 && b >= a && b <= S;
+    if (valid) {
+      lo = slot_row_off[a];
+      hi = slot_row_off[b];
+      valid = lo >= 0 && hi >= lo && hi <= Rcap;
+    }
+    if (!valid) {
+      if (tid == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, e);
+      lo = hi = 0;
+    }
+  }
+  if (col < D) {
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) {
+      const float4 v = *reinterpret_cast<const float4*>(part + ((int64_t)s * E + e) * D + col);
+      a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+    }
+    if (!(isfinite(a.x) && isfinite(a.y) && isfinite(a.z) && isfinite(a.w))) {
+      a = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int r = lo; r < hi; ++r) {
+        const int p = row_pair[r];
+        if (p < 0 || p >= R) continue;
+        const uint2 v = *reinterpret_cast<const uint2*>(x + (int64_t)(p / K) * D + col);
+        const float dl = dlogit[p];
+        a.x = fmaf(dl, __uint_as_float(v.x << 16), a.x);
+        a.y = fmaf(dl, __uint_as_float(v.x & 0xffff0000u), a.y);
+        a.z = fmaf(dl, __uint_as_float(v.y << 16), a.z);
+        a.w = fmaf(dl, __uint_as_float(v.y & 0xffff0000u), a.w);
+      }
     }
     *reinterpret_cast<float4*>(dw_router + (int64_t)e * D + col) = a;
   }
-  if (warp == 1 && blockIdx.y == 0) {
+  if (blockIdx.y == gridDim.y - 1) {
     float b = 0.f;
-    for (int u = first + lane; u < last; u += 32) b += part_b[u];
+    for (int r0 = lo + tid; r0 < hi; r0 += 16 * kThreads) {
+      int p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = r0 + i * kThreads < hi ? row_pair[r0 + i * kThreads] : -1;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) b += p[i] >= 0 && p[i] < R ? dlogit[p[i]] : 0.f;
+    }
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) b += __shfl_xor_sync(0xffffffffu, b, s);
-    if (lane == 0) dbias[e] = b;
+    if ((tid & 31) == 0) s_sum[tid >> 5] = b;
+    __syncthreads();
+    if (tid == 0) {
+#pragma unroll
+      for (int v = 1; v < kThreads / 32; ++v) b += s_sum[v];
+      dbias[e] = b;
+    }
   }
 }
 
@@ -205,23 +361,40 @@ int moegps_launch_route_backward(moegps_ctx* ctx, const void* x, const void* w_r
                                  const int32_t* topk_idx, const float* topk_w, const float* dtopk_w,
                                  const int32_t* slot_row_off, const int32_t* slot_off, const int32_t* row_pair,
                                  float* dlogit, float* dw_router, float* dbias, void* workspace, cudaStream_t st) {
+  using Cfg = RouterCfg;
   const moegps_shape_t& s = ctx->shape;
   const int64_t Rcap = moegps_rcap_of(s), R = (int64_t)s.T * s.K;
-  const int max_units = (int)route_backward::max_units(s);
   const route_backward::Workspace ws = route_backward::carve(s, workspace);
+  const route_backward::Splits sp = route_backward::splits_of(s);
+  CUtensorMap tm_x;
+  if (!moegps_make_tmap_2d(&tm_x, x, (uint64_t)s.T, (uint64_t)s.D, kTileT, 64)) {
+    ctx->last_cuda_error = (int)cudaErrorInvalidValue;
+    return MOEGPS_ERR_CUDA;
+  }
+  if (!ctx->router_weight_attr_done) {
+    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(router_weight_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
+    ctx->router_weight_attr_done = true;
+  }
+  const int32_t* pair_expert = topk_idx;
+  if (!pair_expert) {                                   // the softmax form without topk_idx
+    MOEGPS_CUDA_TRY(ctx, cudaMemsetAsync(ws.pair_expert, 0xff, (size_t)R * sizeof(int32_t), st));
+    pair_expert_kernel<<<s.E, kThreads, 0, st>>>(slot_row_off, slot_off, row_pair, R, Rcap, s.S, ws.pair_expert, ctx->d_status);
+    MOEGPS_AFTER_LAUNCH(ctx);
+    pair_expert = ws.pair_expert;
+  }
   if (s.gate_mode == 1)
     if (int rc = moegps_launch_route(ctx, x, w_router, bias, nullptr, nullptr, ws.logits, nullptr, nullptr, st)) return rc;
   MOEGPS_CUDA_TRY(ctx, launch_after(s.gate_mode == 1 ? dlogit_kernel<true> : dlogit_kernel<false>,
-                                    dim3(1 + (unsigned)((R + kThreads - 1) / kThreads)), kThreads, 0, st, ws.logits, topk_idx,
-                                    topk_w, dtopk_w, R, s.K, s.E, s.S, Rcap, max_units, slot_row_off, slot_off, dlogit,
-                                    ws.unit_first, ws.units, ctx->d_status));
+                                    dim3((unsigned)((R + kThreads - 1) / kThreads)), kThreads, 0, st, ws.logits, topk_idx, topk_w,
+                                    dtopk_w, R, s.K, s.E, dlogit, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
-  MOEGPS_CUDA_TRY(ctx, launch_after(partial_kernel, dim3(max_units, (s.D / 8 + kPartThreads - 1) / kPartThreads), kPartThreads, 0,
-                                    st, static_cast<const uint4*>(x), row_pair, dlogit, R, s.K, s.E, s.D, ws.unit_first,
-                                    ws.units, ws.part, ws.part_b, dw_router, ctx->d_status));
+  MOEGPS_CUDA_TRY(ctx, launch_after(router_weight_kernel,
+                                    dim3((s.E + kTileE - 1) / kTileE, (s.D + kTileD - 1) / kTileD, sp.splits), Cfg::kThreads,
+                                    Cfg::kSmem, st, tm_x, pair_expert, dlogit, s.T, s.K, s.E, s.D, sp.per, ws.part, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
-  MOEGPS_CUDA_TRY(ctx, launch_after(reduce_kernel, dim3(s.E, (s.D + 127) / 128), kThreads, 0, st, ws.part, ws.part_b, s.D,
-                                    ws.unit_first, dw_router, dbias));
+  MOEGPS_CUDA_TRY(ctx, launch_after(reduce_kernel, dim3(s.E, (s.D + 1023) / 1024 + 1), kThreads, 0, st, ws.part, sp.splits,
+                                    static_cast<const __nv_bfloat16*>(x), dlogit, slot_row_off, slot_off, row_pair, R, Rcap,
+                                    s.K, s.E, s.S, s.D, dw_router, dbias, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }

@@ -5,41 +5,39 @@
 
 namespace route_backward {
 
-constexpr int kUnitRows = 64;      // rows of one expert that one block sums
+constexpr int kTileE = 128, kTileD = 256, kTileT = 64;   // experts, columns and tokens of a block's products
+constexpr int kBlocks = 148;                             // that run at the same time: one for each SM
 
-// every expert may end in a partly filled unit
-static inline int64_t max_units(const moegps_shape_t& s) { return s.E + moegps_rcap_of(s) / kUnitRows; }
-
-static inline size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
+// The tokens are cut into `splits` parts of `per` tiles, so that (expert tiles x column tiles x splits) blocks fill the SMs.
+struct Splits {
+  int splits, per;
+};
+static inline Splits splits_of(const moegps_shape_t& s) {
+  const int64_t tiles = (int64_t)((s.E + kTileE - 1) / kTileE) * ((s.D + kTileD - 1) / kTileD);
+  const int64_t steps = ((int64_t)s.T + kTileT - 1) / kTileT;
+  int64_t n = kBlocks / tiles;
+  if (n > steps) n = steps;
+  if (n < 1) n = 1;
+  const int64_t per = (steps + n - 1) / n;
+  return {per ? (int)((steps + per - 1) / per) : 1, (int)per};
+}
 
 struct Workspace {
-  int32_t* unit_first;   // [E+1] first unit of each expert, and their number
-  int4* units;           // [max_units] expert, first row, end row
-  float* part;           // [max_units][D] partial sums of dw_router
-  float* part_b;         // [max_units] partial sums of dbias
+  float* part;           // [splits][E][D] partial sums of dw_router
   float* logits;         // [T][E], sigmoid form only
+  int32_t* pair_expert;  // [T K], softmax form only
 };
 
+static inline size_t part_bytes(const moegps_shape_t& s) { return (size_t)splits_of(s).splits * s.E * s.D * sizeof(float); }
 static inline size_t bytes(const moegps_shape_t& s) {
-  const size_t n = (size_t)max_units(s);
-  return up16((s.E + 1) * sizeof(int32_t)) + n * sizeof(int4) + n * s.D * sizeof(float) + up16(n * sizeof(float)) +
-         (s.gate_mode == 1 ? up16((size_t)s.T * s.E * sizeof(float)) : 0);
+  return 32 + part_bytes(s) + (size_t)s.T * (s.gate_mode == 1 ? s.E : s.K) * 4;
 }
 
 static inline Workspace carve(const moegps_shape_t& s, void* base) {
-  const size_t n = (size_t)max_units(s);
-  char* p = static_cast<char*>(base);
-  Workspace w;
-  w.unit_first = reinterpret_cast<int32_t*>(p);
-  p += up16((s.E + 1) * sizeof(int32_t));
-  w.units = reinterpret_cast<int4*>(p);
-  p += n * sizeof(int4);
-  w.part = reinterpret_cast<float*>(p);
-  p += n * s.D * sizeof(float);
-  w.part_b = reinterpret_cast<float*>(p);
-  p += up16(n * sizeof(float));
-  w.logits = reinterpret_cast<float*>(p);
-  return w;
+  // partial sums are stored 32 bytes at a time
+  char* p = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(base) + 31) & ~(uintptr_t)31);
+  char* rest = p + part_bytes(s);
+  return {reinterpret_cast<float*>(p), reinterpret_cast<float*>(rest), reinterpret_cast<int32_t*>(rest)};
 }
 
 }  // namespace route_backward

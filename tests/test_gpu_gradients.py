@@ -440,3 +440,32 @@ def test_checks_without_the_compiled_module(monkeypatch):
         with pytest.raises(binding.MoegpsError) as err:
             ctx.combine_backward(dout, yp, t["pair_row"], t["w"], *got)
         assert err.value.code == binding.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("given", [True, False])
+def test_route_backward_keeps_bad_tokens_to_their_experts(given):
+    """A token with infinities or NaN in x adds nothing to the experts that it did not choose."""
+    T, D, _, E, K, S, A = 500, 264, 8, 20, 3, 24, 16
+    c = Case(T, D, 8, E, K, S, A, seed=21)
+    dw = c.rng.standard_normal((T, K)).astype(np.float32)
+    x = c.x.clone()
+    x[7, 3], x[7, 200], x[499] = float("inf"), float("nan"), float("nan")
+    dl, dwr, db = (torch.full(d, float("nan"), device=DEV) for d in ((T, K), (E, D), (E,)))
+    ws = torch.empty(binding.route_backward_workspace_bytes(c.shape), dtype=torch.uint8, device=DEV)
+    c.ctx.route_backward(x, None, None, c.t["idx"] if given else None, c.t["w"], torch.from_numpy(dw).to(DEV),
+                         c.t["slot_row_off"], c.t["slot_off"], c.t["row_pair"], dl, dwr, db, ws)
+    c.ctx.check_status()
+    xz = f64(x)
+    bad = np.zeros((E, D), dtype=bool)
+    for t, cols in ((7, [3, 200]), (499, range(D))):
+        for e in c.idx[t]:
+            bad[e, list(cols)] = True
+    xz[~np.isfinite(xz)] = 0
+    want = oracle.route_backward(xz, hz.bits(c.wr), c.bias, c.idx, c.w, dw, 0)
+    got = f64(dwr)
+    assert (~np.isfinite(got) == bad).all()
+    dense = np.zeros((T, E))
+    np.put_along_axis(dense, c.idx.astype(np.int64), np.abs(want[0]) + np.abs(c.w) * np.abs(dw).sum(1, keepdims=True), 1)
+    bound = (96 + T) * 2.0 ** -24 * dense.T @ np.abs(xz) + 1e-37      # one sum of up to T terms
+    assert (np.abs(got - want[1]) <= bound)[~bad].all()
+    assert torch.isfinite(db).all()
