@@ -12,8 +12,10 @@
 //   2. dlogit  : one thread per pair.
 //   3. weights : dWr = dl^T x on the tensor cores, dl as a dense [tokens x experts] matrix that exists only in shared
 //                memory, tile by tile.  A dl is split into three bf16 (8 + 8 + 8 bits: all of its 24), so the products are
-//                exact and the sums are fp32: three MMAs for one, but x is read once.  Summing each expert's rows of x
-//                instead, gathered K times from L2, ran at L2's rate (10 TB/s) and took 21 us + 8 us for joining the parts
+//                exact and the sums are fp32: three MMAs for one, but x is read once.  An accumulation on the tensor core
+//                truncates, so its error grows with their number: the small second and third parts have a sum of their own,
+//                and no sum runs over more than 1024 tokens.  (256 experts, 4096 tokens: 5.5e-6 of the norm with one sum over
+//                2048 tokens, fp32 sums on the CUDA cores 2e-7.)  Summing each expert's rows of x instead, gathered K times from L2, ran at L2's rate (10 TB/s) and took 21 us + 8 us for joining the parts
 //                on 8192 tokens x 2048, 6 of 64 experts, and 41 + 12 us on 4096 x 7168, 8 of 256.
 //   4. reduce  : adds the parts of the tokens.  In the dense product a token that did not choose an expert adds 0 x, which
 //                is NaN where x is not finite: a sum that is not finite is therefore computed again from the expert's own
@@ -76,7 +78,7 @@ __device__ __forceinline__ uint32_t dl_offset(int k, int m) {
 // the end, store the sums.
 __global__ void __launch_bounds__(RouterCfg::kThreads, 1)
 router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __restrict__ pair_expert,
-                     const float* __restrict__ dlogit, int T, int K, int E, int D, int per, float* __restrict__ part,
+                     const float* __restrict__ dlogit, int T, int K, int E, int D, int cols, int per, float* __restrict__ part,
                      int32_t* __restrict__ status) {
   using Cfg = RouterCfg;
   extern __shared__ uint8_t smem_raw[];
@@ -91,7 +93,7 @@ router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
-  const int e0 = blockIdx.x * kTileE, d0 = blockIdx.y * kTileD;
+  const int e0 = blockIdx.x * kTileE, d0 = blockIdx.y * cols;
   const int first = blockIdx.z * per, steps = min(per, (T + kTileT - 1) / kTileT - first);
 
   if (threadIdx.x == 0) {
@@ -103,7 +105,7 @@ router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __
     prefetch_tensormap(&tm_x);
   }
   if (warp == 1) {
-    tmem_alloc(tmem_slot, kTileD);
+    tmem_alloc(tmem_slot, 2 * kTileD);
     tmem_relinquish();
   }
   // the dl tiles are zero but for the entries of the present tokens
@@ -135,7 +137,7 @@ router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
     }
   } else if (warp == 1) {
-    constexpr uint32_t idesc = idesc_bf16_f32(kTileE, kTileD, true, true);
+    const uint32_t idesc = idesc_bf16_f32(kTileE, cols, true, true);
     const uint32_t a_ring = smem_u32(a_mem), b_ring = smem_u32(b_mem);
     int as = 0, bs = 0;
     uint32_t a_phase = 0, b_phase = 0;
@@ -149,9 +151,9 @@ router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __
 #pragma unroll
         for (int split = 0; split < 3; ++split)
 #pragma unroll
-          for (int k = 0; k < kTileT / 16; ++k)
-            mma_bf16(tmem_base, da + (uint64_t)(split * (Cfg::kSplitBytes >> 4) + k * 128), db + (uint64_t)(k * 128), idesc,
-                     (i | split | k) != 0);
+          for (int k = 0; k < kTileT / 16; ++k)            // the first part's sum, and the other two's
+            mma_bf16(tmem_base + (split ? kTileD : 0), da + (uint64_t)(split * (Cfg::kSplitBytes >> 4) + k * 128),
+                     db + (uint64_t)(k * 128), idesc, i != 0 || k != 0 || split == 2);
         mma_commit(&a_empty[as]);
         mma_commit(&b_empty[bs]);
       }
@@ -238,14 +240,17 @@ router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
       float* row = part + ((int64_t)blockIdx.z * E + e) * D + d0;
 #pragma unroll 1
-      for (int c = 0; c < kTileD; c += 32) {
-        uint32_t v[32];
+      for (int c = 0; c < cols; c += 32) {
+        uint32_t v[32], w[32];
         tmem_ld32(taddr + c, v);
+        tmem_ld32(taddr + kTileD + c, w);
         tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
         if (e < E) {
 #pragma unroll
           for (int i = 0; i < 32; i += 8)
-            if (d0 + c + i < D)                          // (D is a multiple of 8)
+            if (c + i < cols && d0 + c + i < D)          // (both multiples of 8)
               asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + c + i), "r"(v[i]), "r"(v[i + 1]),
                            "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
                            : "memory");
@@ -260,7 +265,7 @@ router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __
   if (threadIdx.x == 0 && *abort_flag) moegps_report(status, MOEGPS_ERR_TIMEOUT, (int)blockIdx.x);
   if (warp == 1) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem_base, kTileD);
+    tmem_dealloc(tmem_base, 2 * kTileD);
   }
 }
 
@@ -365,7 +370,7 @@ int moegps_launch_route_backward(moegps_ctx* ctx, const void* x, const void* w_r
   const moegps_shape_t& s = ctx->shape;
   const int64_t Rcap = moegps_rcap_of(s), R = (int64_t)s.T * s.K;
   const route_backward::Workspace ws = route_backward::carve(s, workspace);
-  const route_backward::Splits sp = route_backward::splits_of(s);
+  const route_backward::Cut cut = route_backward::cut_of(s);
   CUtensorMap tm_x;
   if (!moegps_make_tmap_2d(&tm_x, x, (uint64_t)s.T, (uint64_t)s.D, kTileT, 64)) {
     ctx->last_cuda_error = (int)cudaErrorInvalidValue;
@@ -389,10 +394,10 @@ int moegps_launch_route_backward(moegps_ctx* ctx, const void* x, const void* w_r
                                     dtopk_w, R, s.K, s.E, dlogit, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
   MOEGPS_CUDA_TRY(ctx, launch_after(router_weight_kernel,
-                                    dim3((s.E + kTileE - 1) / kTileE, (s.D + kTileD - 1) / kTileD, sp.splits), Cfg::kThreads,
-                                    Cfg::kSmem, st, tm_x, pair_expert, dlogit, s.T, s.K, s.E, s.D, sp.per, ws.part, ctx->d_status));
+                                    dim3((s.E + kTileE - 1) / kTileE, (s.D + cut.cols - 1) / cut.cols, cut.splits), Cfg::kThreads,
+                                    Cfg::kSmem, st, tm_x, pair_expert, dlogit, s.T, s.K, s.E, s.D, cut.cols, cut.per, ws.part, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
-  MOEGPS_CUDA_TRY(ctx, launch_after(reduce_kernel, dim3(s.E, (s.D + 1023) / 1024 + 1), kThreads, 0, st, ws.part, sp.splits,
+  MOEGPS_CUDA_TRY(ctx, launch_after(reduce_kernel, dim3(s.E, (s.D + 1023) / 1024 + 1), kThreads, 0, st, ws.part, cut.splits,
                                     static_cast<const __nv_bfloat16*>(x), dlogit, slot_row_off, slot_off, row_pair, R, Rcap,
                                     s.K, s.E, s.S, s.D, dw_router, dbias, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
