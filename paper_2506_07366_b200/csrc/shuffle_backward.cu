@@ -16,8 +16,12 @@ namespace {
 
 constexpr int kWarpsPerBlock = 4;
 constexpr int kThreads = kWarpsPerBlock * 32;
-// Columns from which a token is spread over the block's four warps.
-constexpr int kWideColumns = 2048;
+// Whether a token is spread over the block's four warps: for wide rows, and for few tokens, whose blocks all run at once
+// and only the length of one counts.  Measured, us a call in a graph, four warps / one (combine, dispatch):
+//   256 tokens x 512, K 2: 1.6 / 1.7, 1.2 / 1.5     1024 x 1024, K 4: 3.7 / 5.0, 2.3 / 2.5    64 x 4096, K 2: 2.3 / 5.3, 1.9 / 4.5
+//   4096 x 512, K 2: 5.5 / 3.7, 4.7 / 2.6           8192 x 1024, K 4: 30.8 / 26.8, 14.2 / 15.7
+//   8192 x 2048, K 6: 67 / 69, 37.4 / 37.8          4096 x 7168, K 8: 153 / 159, 81 / 91 (floor 153, 81)
+bool is_wide(const moegps_ctx* ctx) { return ctx->shape.D >= 2048 || ctx->shape.T <= 8 * ctx->sm_count; }
 
 // The rows of token t's pairs; one outside the buffer is reported and becomes -1.
 template <int KT>
@@ -159,7 +163,7 @@ int moegps_launch_combine_backward(moegps_ctx* ctx, const void* dout, const void
   const int64_t Rcap = moegps_rcap_of(s);
   const uint4 *d = static_cast<const uint4*>(dout), *y = static_cast<const uint4*>(yp);
   uint4* o = static_cast<uint4*>(dyp);
-  const bool wide = s.D >= kWideColumns;
+  const bool wide = is_wide(ctx);
   const int per = wide ? 1 : kWarpsPerBlock;
   const int blocks = (s.T + per - 1) / per;
 #define MOEGPS_LAUNCH(KT, W)                                                                                               \
@@ -183,7 +187,7 @@ int moegps_launch_dispatch_backward(moegps_ctx* ctx, const void* dxp, const int3
   const int64_t Rcap = moegps_rcap_of(s);
   const uint4 *v = static_cast<const uint4*>(dxp), *r = static_cast<const uint4*>(w_router);
   uint4* o = static_cast<uint4*>(dx);
-  const bool wide = s.D >= kWideColumns;
+  const bool wide = is_wide(ctx);
   const int per = wide ? 1 : kWarpsPerBlock;
   const int blocks = (s.T + per - 1) / per;
 #define MOEGPS_LAUNCH(KT, W, R)                                                                                          \
