@@ -44,16 +44,16 @@ dlogit_kernel(const float* __restrict__ logits, const int32_t* __restrict__ topk
   const int64_t p = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   if (p >= R) return;
   const int64_t p0 = p / K * K;
+  const int e = kSigmoid || topk_idx ? topk_idx[p] : 0;
+  const bool valid = e >= 0 && e < E;
+  const float logit = kSigmoid && valid ? logits[p / K * E + e] : 0.f;
   float m = 0.f;
   for (int j = 0; j < K; ++j) m = fmaf(topk_w[p0 + j], dtopk_w[p0 + j], m);
   float d = topk_w[p] * (dtopk_w[p] - m);
-  if constexpr (kSigmoid) {
-    const int e = topk_idx[p];
-    const bool valid = e >= 0 && e < E;
-    if (!valid) moegps_report(status, MOEGPS_ERR_BAD_INDEX, (int)(p / K));
-    const float logit = valid ? logits[p / K * E + e] : 0.f;
-    if (!valid) d = 0.f;
-    d *= 1.f / (1.f + expf(logit));                   // 1 - sigmoid
+  if constexpr (kSigmoid) d *= 1.f / (1.f + expf(logit));            // 1 - sigmoid
+  if (!valid) {
+    moegps_report(status, MOEGPS_ERR_BAD_INDEX, (int)(p / K));
+    d = 0.f;
   }
   dlogit[p] = d;
 }
@@ -341,13 +341,18 @@ reduce_kernel(const float* __restrict__ part, int splits, const __nv_bfloat16* _
   }
   if (blockIdx.y == gridDim.y - 1) {
     float b = 0.f;
+    bool bad = false;
     for (int r0 = lo + tid; r0 < hi; r0 += 16 * kThreads) {
       int p[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = r0 + i * kThreads < hi ? row_pair[r0 + i * kThreads] : -1;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) b += p[i] >= 0 && p[i] < R ? dlogit[p[i]] : 0.f;
+      for (int i = 0; i < 16; ++i) {
+        bad |= p[i] >= R;
+        b += p[i] >= 0 && p[i] < R ? dlogit[p[i]] : 0.f;
+      }
     }
+    if (bad) moegps_report(status, MOEGPS_ERR_BAD_INDEX, e);      // (inside the loop it would part the loads)
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) b += __shfl_xor_sync(0xffffffffu, b, s);
     if ((tid & 31) == 0) s_sum[tid >> 5] = b;

@@ -469,3 +469,33 @@ def test_route_backward_keeps_bad_tokens_to_their_experts(given):
     bound = (96 + T) * 2.0 ** -24 * dense.T @ np.abs(xz) + 1e-37      # one sum of up to T terms
     assert (np.abs(got - want[1]) <= bound)[~bad].all()
     assert torch.isfinite(db).all()
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+def test_route_backward_reports_bad_indices(mode):
+    c = Case(200, 64, 8, 6, 2, 6, 16, mode=mode, seed=22)
+    s, t = c.shape, c.t
+    f32 = dict(dtype=torch.float32, device=DEV)
+    dw = torch.randn(s.T, s.K, **f32)
+    ws = torch.empty(binding.route_backward_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+
+    def run(idx, row_pair):
+        out = torch.empty(s.T, s.K, **f32), torch.empty(s.E, s.D, **f32), torch.empty(s.E, **f32)
+        c.ctx.route_backward(c.x, c.wr, torch.from_numpy(c.bias).to(DEV), idx, t["w"], dw, t["slot_row_off"], t["slot_off"],
+                             row_pair, *out, ws)
+        return out
+
+    good = run(t["idx"], t["row_pair"])
+    c.ctx.check_status()
+    idx = t["idx"].clone()
+    e = int(idx[9, 1])
+    idx[9, 1] = s.E
+    dl, dwr, _ = run(idx, t["row_pair"])
+    assert c.ctx.status() == binding.ERR_BAD_INDEX
+    assert dl[9, 1] == 0 and torch.equal(dl[9, 0], good[0][9, 0])
+    others = [i for i in range(s.E) if i != e]
+    assert torch.equal(dwr[others], good[1][others]) and torch.isfinite(dwr).all()
+    rows = t["row_pair"].clone()
+    rows[0] = s.R
+    _, dwr, _ = run(t["idx"], rows)
+    assert c.ctx.status() == binding.ERR_BAD_INDEX and torch.equal(dwr, good[1])
