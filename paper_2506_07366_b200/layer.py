@@ -108,7 +108,7 @@ class MoeLayer:
             raise RuntimeError("call plan(predicted_hist) first or pass predicted_hist")
         side = torch.cuda.Stream(x.device)
         side.wait_stream(torch.cuda.current_stream())
-        graph = torch.cuda.CUDAGraph()
+        graph = self._new_graph()
 
         def step():
             if predicted_hist is not None:
@@ -125,6 +125,9 @@ class MoeLayer:
         torch.cuda.current_stream().wait_stream(side)
         return graph
 
+    def _new_graph(self):
+        return torch.cuda.CUDAGraph()
+
     def forward_host(self, x_host, out_host, stream=None):
         """Same, with (pinned) host tensors: copies x in, runs the layer, copies the result out."""
         self.x.copy_(x_host, non_blocking=True)
@@ -133,13 +136,22 @@ class MoeLayer:
         return out_host
 
 
+class _InferenceGraph(torch.cuda.CUDAGraph):
+    """A MoeTrainLayer's captured forward pass: a replay writes the layer's buffers as forward() does."""
+
+    def replay(self):
+        self.layer._trained_x = None
+        super().replay()
+
+
 class MoeTrainLayer(MoeLayer):
     """MoeLayer with a backward pass, on the same plan, permutation and buffers.
 
     forward_train() is forward() except that the gate and up products are kept in 8 bits (2 bytes for each hidden value
     and row instead of the 6 of gate, up and hidden activations in bf16); backward() turns the gradient of the output
     into the gradients of the input, the experts and the router.  The layer owns every buffer; what a call returns is
-    overwritten by the next call.
+    overwritten by the next call.  forward(), what is built on it (a captured graph's replay too) and plan() write the tables
+    and buffers that backward() reads: after any of them backward() refuses until the next forward_train().
     """
 
     def __init__(self, shape: Shape, w_router, bias, w_gate, w_up, w_down, device=None):
@@ -156,10 +168,28 @@ class MoeTrainLayer(MoeLayer):
                           w_down=torch.empty_like(w_down), w_router=torch.empty(s.E, s.D, **f32),
                           bias=torch.empty(s.E, **f32))
         self.route_workspace = torch.empty(max(16, route_backward_workspace_bytes(s)), **u8)
+        self._trained_x = None                           # the x that the buffers belong to, while they do
+
+    def plan(self, predicted_hist, stream=None):
         self._trained_x = None
+        super().plan(predicted_hist, stream)
+
+    def start_prediction(self, replan_every: int = 1, ema_shift: int | None = None):
+        self._trained_x = None
+        super().start_prediction(replan_every, ema_shift)
+
+    def forward(self, x, stream=None, out=None):
+        self._trained_x = None
+        return super().forward(x, stream, out)
+
+    def _new_graph(self):
+        graph = _InferenceGraph()
+        graph.layer = self
+        return graph
 
     def forward_train(self, x, stream=None, out=None):
         """forward() that keeps what backward() needs; x must stay as it is until then."""
+        self._trained_x = None
         if not self._planned:
             raise RuntimeError("call plan(predicted_hist) before forward_train()")
         c = self.ctx
@@ -176,9 +206,9 @@ class MoeTrainLayer(MoeLayer):
 
     def backward(self, dout, stream=None):
         """Gradients for the last forward_train(): dict of x [T,D], w_gate, w_up [E,F,D], w_down [E,D,F] (bf16) and
-        w_router [E,D], bias [E] (fp32).  dout: bf16 [T,D].  The plan must not have changed in between."""
+        w_router [E,D], bias [E] (fp32).  dout: bf16 [T,D].  No other forward pass and no new plan in between."""
         if self._trained_x is None:
-            raise RuntimeError("call forward_train() before backward()")
+            raise RuntimeError("call forward_train() before backward(), with no other forward pass and no plan() in between")
         c, x, g = self.ctx, self._trained_x, self.grads
         c.combine_backward(dout, self.yp, self.pair_row, self.topk_w, self.dyp, self.dtopk_w, stream)
         c.expert_ffn_backward(self.dyp, self.xp, self.slot_row_off, self.slot_off, self.slot_expert, self.row_pair,

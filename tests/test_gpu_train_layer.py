@@ -132,3 +132,23 @@ def test_step_in_a_graph():
 def test_finetune_example_learns():
     losses = finetune(steps=20, log=lambda s: None)
     assert np.isfinite(losses).all() and losses[-1] < 0.7 * losses[0]
+
+
+def test_backward_refuses_another_batchs_buffers():
+    """A validation batch, a replay of a captured forward pass or a new plan in the middle of a step."""
+    x, _, _, _, layer = build(*CASES[0])
+    xd = x.to(DEV)
+    dout = torch.randn(layer.shape.T, layer.shape.D, device=DEV).to(torch.bfloat16)
+    graph = layer.capture(xd.flip(0).contiguous())
+    layer.forward_train(xd)
+    want = {k: v.clone() for k, v in layer.backward(dout).items()}
+    for between in (lambda: layer.forward(xd.flip(0).contiguous()), graph.replay, lambda: layer.plan(layer.hist)):
+        layer.forward_train(xd)
+        between()
+        with pytest.raises(RuntimeError, match="forward_train"):
+            layer.backward(dout)
+    layer.plan(layer.hist)
+    layer.forward_train(xd)
+    got = layer.backward(dout)
+    layer.ctx.check_status()
+    assert all(torch.equal(got[k], want[k]) for k in want)
