@@ -79,6 +79,9 @@ combine_backward_kernel(const uint4* __restrict__ dout, const uint4* __restrict_
         if (row[j] >= 0) dyp[(int64_t)row[j] * chunks + c] = pack8(o);
       }
     }
+#pragma unroll
+    for (int j = 0; j < KT; ++j)
+      if (row[j] < 0) dot[j] = 0.f;                    // (the sum of 0 dout is not 0 where dout is not finite)
   }
 #pragma unroll
   for (int j = 0; j < KT; ++j) {
@@ -129,6 +132,7 @@ dispatch_backward_kernel(const uint4* __restrict__ dxp, const int32_t* __restric
       if (expert[j] < 0 || expert[j] >= E) {
         if (l == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, (int)t);
         expert[j] = -1;
+        dl[j] = 0.f;                                   // (its product with the row read as zero may not be 0)
       }
   }
 #pragma unroll 2

@@ -499,3 +499,30 @@ def test_route_backward_reports_bad_indices(mode):
     rows[0] = s.R
     _, dwr, _ = run(t["idx"], rows)
     assert c.ctx.status() == binding.ERR_BAD_INDEX and torch.equal(dwr, good[1])
+
+
+@pytest.mark.parametrize("T", [64, 1300])                         # four warps for each token, and one
+def test_skipped_pairs_add_nothing_where_values_are_not_finite(T):
+    """A pair whose row or expert is outside its range is skipped: its dtopk_w is 0, and dx is the other pairs' sum, also
+    where the value that it would have been multiplied with is an infinity or a NaN."""
+    c = Case(T, 64, 8, 4, 2, 4, 16, seed=23)
+    s, t = c.shape, c.t
+    yp, dxp = c.rows(1.0, s.D), c.rows(1.0, s.D)
+    dout = bf(c.rng.standard_normal((s.T, s.D)))
+    dout[5, 3], dout[6, 1] = float("inf"), float("nan")
+    rows = t["pair_row"].clone()
+    rows[5, 1], rows[6, 0] = s.Rcap, -1
+    dyp, dw = torch.zeros_like(yp), torch.empty(s.T, s.K, device=DEV)
+    c.ctx.combine_backward(dout, yp, rows, t["w"], dyp, dw)
+    assert c.ctx.status() == binding.ERR_BAD_INDEX
+    assert dw[5, 1] == 0 and dw[6, 0] == 0
+    assert not torch.isfinite(dw[5, 0]) and not torch.isfinite(dw[6, 1])
+    idx, dl = t["idx"].clone(), torch.randn(s.T, s.K, device=DEV)
+    idx[7, 1], idx[8, 0], dl[7, 1], dl[8, 0] = s.E, -1, float("inf"), float("nan")
+    got, want = torch.empty_like(dout), torch.empty_like(dout)
+    c.ctx.dispatch_backward(dxp, t["pair_row"], idx, dl, c.wr, got)
+    assert c.ctx.status() == binding.ERR_BAD_INDEX
+    dl[7, 1] = dl[8, 0] = 0
+    c.ctx.dispatch_backward(dxp, t["pair_row"], t["idx"], dl, c.wr, want)
+    c.ctx.check_status()
+    assert torch.equal(got, want)
