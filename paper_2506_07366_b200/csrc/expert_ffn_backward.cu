@@ -545,6 +545,10 @@ struct WeightCfg : PairCfg {
 static_assert(WeightCfg::kSmem + 2 * 257 * 4 <= 227 * 1024, "one CTA per SM");
 constexpr int kBand = 8;
 
+// Limit of a wait that lasts as long as the sums over `rows` rows.  A K block of 64 rows takes 600 to 1700 cycles; 64 cycles are
+// allowed for each row.  The plain limit, about a second, is passed by a sum over 2 10^8 rows (8 columns: 600 cycles a block).
+__device__ __forceinline__ long long wait_limit(long long rows) { return kWaitLimitCycles + 64 * rows; }
+
 struct WTile {
   int expert, problem, m, n0;       // m: tile in M; n0: first column
 };
@@ -769,14 +773,17 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
     const uint32_t ready = map_to_cta(smem_u32(bar.tail_ready), 0);
     int stage = 0;
     uint32_t tail_phase = 0;
+    long long rows = 0;                                // that are multiplied before the next rows to blank are loaded, at most
     bool ok = true;
     for (int tile = pair; ok && tile < total_tiles; tile += pairs) {
       const int expert = tile / (geom.per[0] + geom.per[1]), last = s_slot_off[expert + 1];
       for (int s = s_slot_off[expert]; ok && s < last; ++s) {
         const int n = sr.ext[s].y, tail = n % BK;
+        rows += n;
         stage = (stage + n / BK) % kStages;
         if (tail & 15) {
-          const bool here = mbar_wait(&bar.tail_full[stage], (tail_phase >> stage) & 1u, bar.abort_flag, 100);
+          const bool here =
+              mbar_wait(&bar.tail_full[stage], (tail_phase >> stage) & 1u, bar.abort_flag, 100, wait_limit(rows));
           ok = __all_sync(0xffffffffu, here);
           if (!ok) break;
           uint8_t* sa = stage_mem + (size_t)stage * kStageBytes;
@@ -808,7 +815,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap tm_dgate, const __gri
       const int rows = s_rows[t.expert];
       if (rows != 0) {
         // (a short sum is awaited closely; through a long one the warps sleep, polling costs power that the MMAs need)
-        if (!mbar_wait(&bar.acc_full[acc], acc_phase, bar.abort_flag, rows > 1024 ? 256 : 32)) break;
+        if (!mbar_wait(&bar.acc_full[acc], acc_phase, bar.abort_flag, rows > 1024 ? 256 : 32, wait_limit(rows))) break;
         tc_fence_after_sync();
         // the accumulator is emptied into registers at one go and handed back, then the columns are stored: for an
         // expert with few rows the next sums are ready before the stores are out

@@ -526,3 +526,29 @@ def test_skipped_pairs_add_nothing_where_values_are_not_finite(T):
     c.ctx.dispatch_backward(dxp, t["pair_row"], t["idx"], dl, c.wr, want)
     c.ctx.check_status()
     assert torch.equal(got, want)
+
+
+def test_weight_gradient_over_more_rows_than_a_second_lasts():
+    """400 million tokens, all but a thousand of one expert: its sums take longer than the kernels' plain waiting limit.  All
+    rows are zero but for some, whose products are small whole numbers: the sums are exact."""
+    T, D, F = 400_000_005, 8, 8
+    first = T - 1001                                              # neither part is whole blocks of 16 rows
+    shape = binding.Shape(T, D, F, 2, 1, 2, 0, 1)
+    ctx = binding.Context(shape)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    dyp, xp, dgate, dup, h = (torch.zeros(T, 8, dtype=torch.bfloat16, device=DEV) for _ in range(5))
+    rows = [0, 15, 77_777_777, 268_435_456, first - 1, first, T - 2, T - 1]
+    rng = np.random.default_rng(24)
+    small = rng.integers(-3, 4, (5, len(rows), 8)).astype(np.float64)
+    for t, v in zip((dyp, xp, dgate, dup, h), small):
+        t[rows] = bf(v)
+    dw = [torch.full((2, 8, 8), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(3)]
+    ctx.expert_ffn_backward_weights(dyp, xp, dgate, dup, h, torch.tensor([0, first, T], **i32), torch.tensor([0, 1, 2], **i32),
+                                    torch.arange(T, **i32), *dw)
+    ctx.check_status()
+    dy, x, dg, du, hh = small
+    for e, part in enumerate((slice(0, 5), slice(5, 8))):
+        for got, want in zip(dw, (dg[part].T @ x[part], du[part].T @ x[part], dy[part].T @ hh[part])):
+            assert np.array_equal(f64(got[e]), want)
+    del dyp, xp, dgate, dup, h
+    torch.cuda.empty_cache()
