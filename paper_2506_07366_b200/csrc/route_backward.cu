@@ -33,6 +33,7 @@ using route_backward::kTileE;
 using route_backward::kTileT;
 
 constexpr int kThreads = 256;
+static_assert(kTileE >= 128, "at most 256 experts are one or two tiles");
 
 template <bool kSigmoid>
 __global__ void __launch_bounds__(kThreads)
@@ -74,12 +75,12 @@ __device__ __forceinline__ uint32_t dl_offset(int k, int m) {
   return (uint32_t)((m >> 6) * RouterCfg::kBoxBytes + k * 128 + ((((m >> 3) & 7) ^ (k & 7)) << 4) + (m & 7) * 2);
 }
 
-// block (expert tile x, column tile y, split z): warp 0 loads x, warp 1 multiplies, warps 2..5 build the dl tiles and, at
-// the end, store the sums.
+// Block = split x tiles + tile, tile = column tile x expert tiles + expert tile: one grid dimension, since there may be more
+// than 65535 splits.  Warp 0 loads x, warp 1 multiplies, warps 2..5 build the dl tiles and, at the end, store the sums.
 __global__ void __launch_bounds__(RouterCfg::kThreads, 1)
 router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __restrict__ pair_expert,
-                     const float* __restrict__ dlogit, int T, int K, int E, int D, int cols, int per, float* __restrict__ part,
-                     int32_t* __restrict__ status) {
+                     const float* __restrict__ dlogit, int T, int K, int E, int D, int cols, int tiles, int per,
+                     float* __restrict__ part, int32_t* __restrict__ status) {
   using Cfg = RouterCfg;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* a_mem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -93,8 +94,9 @@ router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
-  const int e0 = blockIdx.x * kTileE, d0 = blockIdx.y * cols;
-  const int first = blockIdx.z * per, steps = min(per, (T + kTileT - 1) / kTileT - first);
+  const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
+  const int e_shift = E > kTileE, e0 = (tile & e_shift) * kTileE, d0 = (tile >> e_shift) * cols;      // (one expert tile or two)
+  const int first = split * per, steps = min(per, (T + kTileT - 1) / kTileT - first);
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < Cfg::kAStages; ++i) { mbar_init(&a_full[i], Cfg::kBuilders); mbar_init(&a_empty[i], 1); }
@@ -149,11 +151,11 @@ router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __
       const uint64_t da = smem_desc_mn(a_ring + as * Cfg::kABytes, Cfg::kBoxBytes);
       if (elect_one()) {
 #pragma unroll
-        for (int split = 0; split < 3; ++split)
+        for (int dl_part = 0; dl_part < 3; ++dl_part)
 #pragma unroll
           for (int k = 0; k < kTileT / 16; ++k)            // the first part's sum, and the other two's
-            mma_bf16(tmem_base + (split ? kTileD : 0), da + (uint64_t)(split * (Cfg::kSplitBytes >> 4) + k * 128),
-                     db + (uint64_t)(k * 128), idesc, i != 0 || k != 0 || split == 2);
+            mma_bf16(tmem_base + (dl_part ? kTileD : 0), da + (uint64_t)(dl_part * (Cfg::kSplitBytes >> 4) + k * 128),
+                     db + (uint64_t)(k * 128), idesc, i != 0 || k != 0 || dl_part == 2);
         mma_commit(&a_empty[as]);
         mma_commit(&b_empty[bs]);
       }
@@ -210,8 +212,8 @@ router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __
           for (int n = 0; n < Cfg::kPairs; ++n)
             if (ok && set[as][n] >= 0)
 #pragma unroll
-              for (int split = 0; split < 3; ++split)
-                *reinterpret_cast<__nv_bfloat16*>(sa + split * Cfg::kSplitBytes + set[as][n]) = __float2bfloat16(0.f);
+              for (int dl_part = 0; dl_part < 3; ++dl_part)
+                *reinterpret_cast<__nv_bfloat16*>(sa + dl_part * Cfg::kSplitBytes + set[as][n]) = __float2bfloat16(0.f);
           // no entry is set before all old ones are gone (a warp whose wait failed comes here too: the count stays right)
           asm volatile("bar.sync 1, %0;" ::"n"(32 * Cfg::kBuilders) : "memory");
 #pragma unroll
@@ -220,9 +222,9 @@ router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __
             if (ok && at[n] >= 0) {
               float rest = dl[n];
 #pragma unroll
-              for (int split = 0; split < 3; ++split) {
+              for (int dl_part = 0; dl_part < 3; ++dl_part) {
                 const __nv_bfloat16 v = __float2bfloat16(rest);       // nearest; what is left is exact in fp32
-                *reinterpret_cast<__nv_bfloat16*>(sa + split * Cfg::kSplitBytes + at[n]) = v;
+                *reinterpret_cast<__nv_bfloat16*>(sa + dl_part * Cfg::kSplitBytes + at[n]) = v;
                 rest -= __bfloat162float(v);
               }
             }
@@ -238,7 +240,7 @@ router_weight_kernel(const __grid_constant__ CUtensorMap tm_x, const int32_t* __
       tc_fence_after_sync();
       const int quarter = warp & 3, e = e0 + quarter * 32 + lane;
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
-      float* row = part + ((int64_t)blockIdx.z * E + e) * D + d0;
+      float* row = part + ((int64_t)split * E + e) * D + d0;
 #pragma unroll 1
       for (int c = 0; c < cols; c += 32) {
         uint32_t v[32], w[32];
@@ -398,9 +400,9 @@ int moegps_launch_route_backward(moegps_ctx* ctx, const void* x, const void* w_r
                                     dim3((unsigned)((R + kThreads - 1) / kThreads)), kThreads, 0, st, ws.logits, topk_idx, topk_w,
                                     dtopk_w, R, s.K, s.E, dlogit, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
-  MOEGPS_CUDA_TRY(ctx, launch_after(router_weight_kernel,
-                                    dim3((s.E + kTileE - 1) / kTileE, (s.D + cut.cols - 1) / cut.cols, cut.splits), Cfg::kThreads,
-                                    Cfg::kSmem, st, tm_x, pair_expert, dlogit, s.T, s.K, s.E, s.D, cut.cols, cut.per, ws.part, ctx->d_status));
+  const int tiles = (s.E + kTileE - 1) / kTileE * ((s.D + cut.cols - 1) / cut.cols);
+  MOEGPS_CUDA_TRY(ctx, launch_after(router_weight_kernel, dim3((unsigned)tiles * (unsigned)cut.splits),
+                                    Cfg::kThreads, Cfg::kSmem, st, tm_x, pair_expert, dlogit, s.T, s.K, s.E, s.D, cut.cols, tiles, cut.per, ws.part, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx);
   MOEGPS_CUDA_TRY(ctx, launch_after(reduce_kernel, dim3(s.E, (s.D + 1023) / 1024 + 1), kThreads, 0, st, ws.part, cut.splits,
                                     static_cast<const __nv_bfloat16*>(x), dlogit, slot_row_off, slot_off, row_pair, R, Rcap,

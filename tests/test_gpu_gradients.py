@@ -552,3 +552,30 @@ def test_weight_gradient_over_more_rows_than_a_second_lasts():
             assert np.array_equal(f64(got[e]), want)
     del dyp, xp, dgate, dup, h
     torch.cuda.empty_cache()
+
+
+def test_route_backward_of_many_short_parts():
+    """67.2 million tokens: more parts than a grid's second or third dimension holds.  dl is zero but for some tokens, whose
+    products are exact."""
+    T, D, E = 67_200_000, 8, 2
+    shape = binding.Shape(T, D, 8, E, 2, E, 0, 1)
+    ctx = binding.Context(shape)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    x, dw = torch.zeros(T, D, dtype=torch.bfloat16, device=DEV), torch.zeros(T, 2, device=DEV)
+    rng = np.random.default_rng(25)
+    at = [0, 63, 64, 1023, 1024, 33_554_432, 67_107_839, 67_107_840, T - 1]      # (the 65536th part starts at 67107840)
+    xs, ds = rng.integers(-3, 4, (len(at), D)).astype(np.float64), rng.integers(-8, 9, len(at)).astype(np.float64) * 4
+    x[at] = bf(xs)
+    dw[at, 0] = torch.from_numpy(ds).float().to(DEV)
+    idx = torch.tensor([[0, 1]], **i32).expand(T, 2).contiguous()
+    w = torch.full((T, 2), 0.5, device=DEV)
+    row_pair = torch.arange(2 * T, **i32).view(T, 2).T.contiguous().view(-1)
+    off, slot_off = torch.tensor([0, T, 2 * T], **i32), torch.tensor([0, 1, 2], **i32)
+    dl, dwr, db = (torch.full(d, float("nan"), device=DEV) for d in ((T, 2), (E, D), (E,)))
+    ws = torch.empty(binding.route_backward_workspace_bytes(shape), dtype=torch.uint8, device=DEV)
+    ctx.route_backward(x, None, None, idx, w, dw, off, slot_off, row_pair, dl, dwr, db, ws)
+    ctx.check_status()
+    assert np.array_equal(f64(dl[at]), np.stack([ds / 4, -ds / 4], 1)) and int((dl != 0).sum()) == 2 * int((ds != 0).sum())
+    assert np.array_equal(f64(dwr), np.stack([ds @ xs, -ds @ xs]) / 4) and np.array_equal(f64(db), np.array([1, -1]) * ds.sum() / 4)
+    del x, dw, idx, w, row_pair, dl, ws
+    torch.cuda.empty_cache()
