@@ -170,7 +170,12 @@ def _stream(stream):
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
-    return int(stream if isinstance(stream, int) else stream.cuda_stream)
+    if hasattr(stream, "cuda_stream"):
+        return int(stream.cuda_stream)
+    try:
+        return int(stream)                               # a handle
+    except TypeError:
+        raise AttributeError(f"{stream!r} is neither a stream nor a stream's handle") from None
 
 
 def _marshal():

@@ -63,14 +63,24 @@ bool matches(const Spec& s, PyObject* o, void** out) {
   return true;
 }
 
-// a stream argument as binding.py takes it: None (the current stream), a torch.cuda.Stream or its handle
+// A stream argument as binding.py takes it: None (the current stream), a stream object or whatever int() makes a handle of.
 bool stream_of(PyObject* o, void** out) {
   if (o == Py_None) {
     *out = c10::cuda::getCurrentCUDAStream().stream();
     return true;
   }
-  PyObject* handle = PyLong_Check(o) ? Py_NewRef(o) : PyObject_GetAttrString(o, "cuda_stream");
-  if (!handle) return false;
+  PyObject* held = PyLong_Check(o) ? Py_NewRef(o) : PyObject_GetAttrString(o, "cuda_stream");
+  if (!held && PyErr_ExceptionMatches(PyExc_AttributeError)) {
+    PyErr_Clear();
+    held = Py_NewRef(o);
+  }
+  PyObject* handle = held ? PyNumber_Long(held) : nullptr;
+  Py_XDECREF(held);
+  if (!handle) {
+    if (PyErr_ExceptionMatches(PyExc_TypeError))
+      PyErr_Format(PyExc_AttributeError, "%R is neither a stream nor a stream's handle", o);
+    return false;
+  }
   *out = PyLong_AsVoidPtr(handle);
   Py_DECREF(handle);
   return !PyErr_Occurred();
