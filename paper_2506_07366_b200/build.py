@@ -58,10 +58,21 @@ def build_marshal(force: bool = False) -> str:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu of the library for sm_100a into one shared object (and _marshal); returns its path."""
-    build_marshal(force)
-    if not force and not needs_build():
-        return LIB_PATH
+    """Compile every .cu of the library for sm_100a into one shared object (and _marshal); returns its path.
+
+    _marshal is optional (binding.py makes the same checks): where it cannot be compiled that is said, and no old one stays."""
+    if force or needs_build():
+        _build_library(verbose)
+    try:
+        build_marshal(force)
+    except (RuntimeError, OSError) as e:
+        sys.stderr.write(f"_marshal was not built ({e}): tensors are checked in Python, some microseconds a call slower\n")
+        if os.path.exists(MARSHAL_PATH):
+            os.remove(MARSHAL_PATH)
+    return LIB_PATH
+
+
+def _build_library(verbose: bool) -> None:
     cmd = [
         _nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
         "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
@@ -77,7 +88,6 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if verbose:
         sys.stderr.write(proc.stdout + proc.stderr)
     os.replace(LIB_PATH + ".tmp", LIB_PATH)
-    return LIB_PATH
 
 
 if __name__ == "__main__":
