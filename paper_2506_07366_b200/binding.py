@@ -179,12 +179,12 @@ def _stream(stream):
 
 
 def _marshal():
-    """The compiled argument checks (csrc/marshal.cpp), or None where they have not been built."""
+    """The compiled argument checks (csrc/marshal.cpp), or None where they have not been built for this torch."""
     try:
         from . import _marshal as module
     except ImportError:
         return None
-    return module
+    return module if getattr(module, "built_for", None) == _build.marshal_marker() else None
 
 
 def _training_call(entry, handle: int, specs):

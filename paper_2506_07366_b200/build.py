@@ -35,16 +35,29 @@ def needs_build() -> bool:
     return any(os.path.getmtime(d) > built for d in deps)
 
 
+def marshal_marker() -> str:
+    """What a _marshal of this torch carries (its attribute `built_for`): it reads torch's C++ objects directly."""
+    import torch
+    return f"moegps _marshal for torch {torch.__version__}"
+
+
+def _marshal_is_current() -> bool:
+    if not os.path.exists(MARSHAL_PATH) or os.path.getmtime(MARSHAL_SOURCE) > os.path.getmtime(MARSHAL_PATH):
+        return False
+    with open(MARSHAL_PATH, "rb") as f:
+        return marshal_marker().encode() in f.read()
+
+
 def build_marshal(force: bool = False) -> str:
     """Compile _marshal against the installed torch; returns its path."""
-    if not force and os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_SOURCE) <= os.path.getmtime(MARSHAL_PATH):
+    if not force and _marshal_is_current():
         return MARSHAL_PATH
     import torch
     home = os.path.dirname(torch.__file__)
     cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
     cmd = [
         "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
-        f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+        f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", f'-DMOEGPS_BUILT_FOR="{marshal_marker()}"',
         "-I", os.path.join(home, "include"), "-I", os.path.join(home, "include", "torch", "csrc", "api", "include"),
         "-I", cuda, "-I", sysconfig.get_path("include"), MARSHAL_SOURCE,
         "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", MARSHAL_PATH + ".tmp",

@@ -189,7 +189,9 @@ PyMODINIT_FUNC PyInit__marshal() {
   if (PyType_Ready(&call_type) < 0) return nullptr;
   PyObject* m = PyModule_Create(&module_def);
   if (!m) return nullptr;
-  if (PyModule_AddObjectRef(m, "Call", reinterpret_cast<PyObject*>(&call_type)) < 0) {
+  // (the module depends on the layout of torch's objects: build.py and binding.py compare this with the installed version)
+  if (PyModule_AddObjectRef(m, "Call", reinterpret_cast<PyObject*>(&call_type)) < 0 ||
+      PyModule_AddStringConstant(m, "built_for", MOEGPS_BUILT_FOR) < 0) {
     Py_DECREF(m);
     return nullptr;
   }

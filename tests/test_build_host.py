@@ -2,8 +2,9 @@
 import subprocess
 
 import pytest
+import torch
 
-from paper_2506_07366_b200 import build
+from paper_2506_07366_b200 import binding, build
 
 
 @pytest.fixture
@@ -49,3 +50,22 @@ def test_library_failure_is_an_error(compilers):
     compilers.broken = {"nvcc"}
     with pytest.raises(RuntimeError, match="nvcc"):
         build.build(force=True)
+
+
+def test_marshal_of_another_torch_is_not_used_and_is_rebuilt(compilers, monkeypatch):
+    """It reads torch's C++ objects, whose layout belongs to one version."""
+    build.build()
+    open(build.MARSHAL_PATH, "wb").write(b"..." + build.marshal_marker().encode() + b"...")
+    compilers.ran.clear()
+    build.build()
+    assert compilers.ran == []                            # both are current
+    monkeypatch.setattr(torch, "__version__", "0.0.1")
+    build.build()
+    assert compilers.ran == ["g++"]
+
+
+def test_binding_ignores_a_marshal_of_another_torch(monkeypatch):
+    build.build_marshal()
+    assert binding._marshal() is not None
+    monkeypatch.setattr(torch, "__version__", "0.0.1")
+    assert binding._marshal() is None
