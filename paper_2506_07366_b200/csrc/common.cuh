@@ -4,6 +4,7 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <stdarg.h>
 #include <stdint.h>
 #include <stdio.h>
 
@@ -38,12 +39,21 @@ struct moegps_ctx {
   bool trace;               // MOEGPS_TRACE was set when the context was created: log every launch to stderr
 };
 
-// Host-side launch log (off unless the environment asked for it): ordinal, launcher, shape.
-inline void moegps_trace_launch(const moegps_ctx* ctx, const char* where) {
+// Host-side launch log (off unless the environment asked for it): ordinal, launcher, shape, and what was chosen for the launch
+// (printf form) where there is a choice.
+__attribute__((format(printf, 3, 4))) inline void moegps_trace_launch(const moegps_ctx* ctx, const char* where,
+                                                                      const char* choice = nullptr, ...) {
   if (!ctx->trace) return;
   const moegps_shape_t& s = ctx->shape;
-  fprintf(stderr, "[moegps] launch %lld %s T=%d D=%d F=%d E=%d K=%d S=%d A=%d\n", (long long)ctx->launches, where, s.T, s.D,
-          s.F, s.E, s.K, s.S, s.row_align);
+  char more[128] = "";
+  if (choice) {
+    va_list args;
+    va_start(args, choice);
+    vsnprintf(more, sizeof(more), choice, args);
+    va_end(args);
+  }
+  fprintf(stderr, "[moegps] launch %lld %s T=%d D=%d F=%d E=%d K=%d S=%d A=%d%s%s\n", (long long)ctx->launches, where, s.T, s.D,
+          s.F, s.E, s.K, s.S, s.row_align, choice ? " " : "", more);
 }
 
 #define MOEGPS_CUDA_TRY(ctx, expr)                                   \
@@ -55,11 +65,11 @@ inline void moegps_trace_launch(const moegps_ctx* ctx, const char* where) {
     }                                                                \
   } while (0)
 
-// Records a launch (and its launch error, if any).
-#define MOEGPS_AFTER_LAUNCH(ctx)                                     \
+// Records a launch (and its launch error, if any); further arguments: what was chosen for it, see moegps_trace_launch.
+#define MOEGPS_AFTER_LAUNCH(ctx, ...)                                \
   do {                                                               \
     (ctx)->launches += 1;                                            \
-    moegps_trace_launch((ctx), __func__);                            \
+    moegps_trace_launch((ctx), __func__, ##__VA_ARGS__);             \
     cudaError_t _e = cudaGetLastError();                             \
     if (_e != cudaSuccess) {                                         \
       (ctx)->last_cuda_error = (int)_e;                              \

@@ -403,7 +403,7 @@ int moegps_launch_route_backward(moegps_ctx* ctx, const void* x, const void* w_r
   const int tiles = (s.E + kTileE - 1) / kTileE * ((s.D + cut.cols - 1) / cut.cols);
   MOEGPS_CUDA_TRY(ctx, launch_after(router_weight_kernel, dim3((unsigned)tiles * (unsigned)cut.splits),
                                     Cfg::kThreads, Cfg::kSmem, st, tm_x, pair_expert, dlogit, s.T, s.K, s.E, s.D, cut.cols, tiles, cut.per, ws.part, ctx->d_status));
-  MOEGPS_AFTER_LAUNCH(ctx);
+  MOEGPS_AFTER_LAUNCH(ctx, "cols=%d parts=%d steps=%d", cut.cols, cut.splits, cut.per);
   MOEGPS_CUDA_TRY(ctx, launch_after(reduce_kernel, dim3(s.E, (s.D + 1023) / 1024 + 1), kThreads, 0, st, ws.part, cut.splits,
                                     static_cast<const __nv_bfloat16*>(x), dlogit, slot_row_off, slot_off, row_pair, R, Rcap,
                                     s.K, s.E, s.S, s.D, dw_router, dbias, ctx->d_status));

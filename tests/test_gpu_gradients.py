@@ -579,3 +579,68 @@ def test_route_backward_of_many_short_parts():
     assert np.array_equal(f64(dwr), np.stack([ds @ xs, -ds @ xs]) / 4) and np.array_equal(f64(db), np.array([1, -1]) * ds.sum() / 4)
     del x, dw, idx, w, row_pair, dl, ws
     torch.cuda.empty_cache()
+
+
+def traced(monkeypatch, shape):
+    """A context whose launches are logged to stderr."""
+    monkeypatch.setenv("MOEGPS_TRACE", "1")
+    ctx = binding.Context(shape)
+    monkeypatch.delenv("MOEGPS_TRACE")
+    return ctx
+
+
+# T, D, E, K and the cut: columns of a tile, parts of the tokens, steps of 64 tokens in a part.  (The last part has 13, 12, 8 and
+# 9 steps, so the ring of dl tiles ends on either stage; no T is whole steps.)
+LONG_ROUTES = [
+    (4099, 7168, 256, 8, 256, 5, 13),
+    (3401, 7160, 250, 3, 208, 4, 14),
+    (8131, 2048, 64, 6, 128, 9, 15),
+    (5003, 2056, 130, 1, 176, 6, 14),
+]
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("dims", LONG_ROUTES, ids=lambda d: "x".join(map(str, d)))
+def test_route_backward_over_many_steps(dims, mode, monkeypatch, capfd):
+    """Sums over many steps of 64 tokens, as training batches have them, against the definition in 64 bits on the GPU.
+
+    Bounds for dw_router, M being the sum of the terms' magnitudes: an accumulation on the tensor core truncates, so it is off
+    by at most 2^-23 of the running sum, as is each of the 16 products that it aligns with it; a sum runs over at most 64
+    accumulations, the sum of the two small parts of dl over 128 of 2^-8 the size.  (64 + 1)(16 + 1) 2^-23 M at worst.  The
+    2-norm of the error is held to 64 2^-24 of the result's: 64 truncations by half a unit on average of a running sum, which
+    is smaller than the result on average.  dbias: fp32, at most T K terms in 256 threads and a tree."""
+    T, D, E, K, cols, parts, steps = dims
+    gen = torch.Generator(device=DEV).manual_seed(26)
+    rnd = lambda *s: torch.randn(*s, generator=gen, device=DEV)  # noqa: E731
+    x, wr, bias = rnd(T, D).to(torch.bfloat16), (rnd(E, D) / D ** 0.5).to(torch.bfloat16), -torch.log1p(torch.arange(E, device=DEV).float())
+    logits = x.double() @ wr.double().T + bias.double()
+    top, idx = torch.topk(logits, K, dim=1)
+    s = torch.sigmoid(top)
+    w = (torch.softmax(top, 1) if mode == 0 else s / s.sum(1, keepdim=True)).float()
+    dw = rnd(T, K)
+    # the pairs in the order of their experts, one slot for each
+    order = torch.argsort(idx.view(-1), stable=True)
+    off = torch.nn.functional.pad(torch.bincount(idx.view(-1), minlength=E).cumsum(0), (1, 0)).to(torch.int32)
+    shape = binding.Shape(T, D, 8, E, K, E, mode, 1)
+    ctx = traced(monkeypatch, shape)
+    dl, dwr, db = (torch.full(d, float("nan"), device=DEV) for d in ((T, K), (E, D), (E,)))
+    ws = torch.full((binding.route_backward_workspace_bytes(shape),), 0xFF, dtype=torch.uint8, device=DEV)
+    idx32, slot_off = idx.to(torch.int32), torch.arange(E + 1, dtype=torch.int32, device=DEV)
+    for given in ([idx32] if mode else [idx32, None]):
+        capfd.readouterr()
+        ctx.route_backward(x, wr, bias, given, w, dw, off, slot_off, order.to(torch.int32), dl, dwr, db, ws)
+        ctx.check_status()
+        assert f"cols={cols} parts={parts} steps={steps}" in capfd.readouterr().err
+        m = (w.double() * dw.double()).sum(1, keepdim=True)
+        want = w.double() * (dw.double() - m) * (1 if mode == 0 else 1 - torch.sigmoid(top))
+        err = 16 * 2.0 ** -24 * w.double() * (dw.abs().double() + (w * dw.abs()).double().sum(1, keepdim=True))
+        if mode:
+            z = (x.double().abs() @ wr.double().abs().T + bias.abs()).gather(1, idx)
+            err += want.abs() * ((D / 32 + 8) * 2.0 ** -24 * z + 2.0 ** -20)
+        within(f64(dl), f64(want), f64(err), "dlogit")
+        # the sums, of the dl that the call itself has returned
+        dense = torch.zeros(T, E, dtype=torch.float64, device=DEV).scatter_(1, idx, dl.double())
+        ref, mag = dense.T @ x.double(), dense.abs().T @ x.double().abs()
+        within(f64(dwr), f64(ref), f64(65 * 17 * 2.0 ** -23 * mag) + 1e-37, "dw_router")
+        assert (dwr.double() - ref).norm() <= 64 * 2.0 ** -24 * ref.norm()
+        within(f64(db), f64(dense.sum(0)), f64((T * K / 256 + 16) * 2.0 ** -24 * dense.abs().sum(0)) + 1e-37, "dbias")
