@@ -644,3 +644,77 @@ def test_route_backward_over_many_steps(dims, mode, monkeypatch, capfd):
         within(f64(dwr), f64(ref), f64(65 * 17 * 2.0 ** -23 * mag) + 1e-37, "dw_router")
         assert (dwr.double() - ref).norm() <= 64 * 2.0 ** -24 * ref.norm()
         within(f64(db), f64(dense.sum(0)), f64((T * K / 256 + 16) * 2.0 ** -24 * dense.abs().sum(0)) + 1e-37, "dbias")
+
+
+def test_weight_gradients_over_long_sums():
+    """90001 rows of one expert in two of its three slots and 70 of another, all values checked against 64 bits.  A running sum is truncated
+    at each of up to 5626 accumulations (2^-24 of it on average) and the result rounded to bf16 (1.7e-3 of the norm):
+    together below 2e-3."""
+    D, F = 264, 328
+    off = [0, 50_001, 50_001, 90_001, 90_071]                     # the second slot of the first expert is empty
+    R = off[-1]
+    shape = binding.Shape(R, D, F, 2, 1, 4, 0, 1)
+    ctx = binding.Context(shape)
+    gen = torch.Generator(device=DEV).manual_seed(27)
+    rnd = lambda n: torch.randn(R, n, generator=gen, device=DEV).to(torch.bfloat16)  # noqa: E731
+    dyp, xp, dgate, dup, h = rnd(D), rnd(D), rnd(F), rnd(F), rnd(F)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    dw = [torch.full(s, float("nan"), dtype=torch.bfloat16, device=DEV) for s in ((2, F, D), (2, F, D), (2, D, F))]
+    ctx.expert_ffn_backward_weights(dyp, xp, dgate, dup, h, torch.tensor(off, **i32), torch.tensor([0, 3, 4], **i32),
+                                    torch.arange(R, **i32), *dw)
+    ctx.check_status()
+    for e, part in enumerate((slice(0, off[3]), slice(off[3], R))):
+        for got, a, b in zip(dw, (dgate, dup, dyp), (xp, xp, h)):
+            ref = a[part].double().T @ b[part].double()
+            assert (got[e].double() - ref).norm() <= 2e-3 * ref.norm()
+
+
+def test_expert_gradient_of_a_large_layer_with_idle_experts():
+    """4096 tokens over 6 of 40 experts (13 to 3458 pairs each): the others have no rows in slots of their own, and zero weight gradients.  Against 64
+    bits on the GPU, to 4e-3 of the norm as above."""
+    T, D, F, E, K, S, A = 4096, 1000, 712, 40, 2, 48, 16
+    rng = np.random.default_rng(28)
+    busy = rng.permutation(E)[:11]
+    score = rng.random((T, 11)) + np.linspace(0, 2, 11)
+    idx = busy[np.argsort(-score, axis=1)[:, :K]].astype(np.int32)
+    hist = oracle.histogram(idx, E)
+    assert (hist == 0).sum() == E - 6
+    _, slot_off, slot_expert, _ = oracle.plan(hist, S)
+    slot_row_off, row_pair, _, _ = oracle.dispatch(None, idx, hist, np.diff(slot_off), slot_off, S, A)
+    i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a).astype(np.int32)).to(DEV)  # noqa: E731
+    ctx = binding.Context(binding.Shape(T, D, F, E, K, S, 0, A))
+    s = ctx.shape
+    gen = torch.Generator(device=DEV).manual_seed(29)
+    occ = i32(row_pair) >= 0
+
+    def rows(n, std):
+        v = torch.randn(s.Rcap, n, generator=gen, device=DEV) * std
+        v[~occ] = float("nan")
+        return v.to(torch.bfloat16)
+
+    xp, dyp = rows(D, 1.0), rows(D, 0.01)
+    ws = [(torch.randn(d, generator=gen, device=DEV) * 0.03).to(torch.bfloat16) for d in ((E, F, D), (E, F, D), (E, D, F))]
+    u8 = dict(dtype=torch.uint8, device=DEV)
+    kept = [torch.empty(d, **u8) for d in ((s.Rcap, s.P), (s.Rcap, s.P), (s.P // 32, s.Rcap), (s.P // 32, s.Rcap))]
+    nan = lambda *d: torch.full(d, float("nan"), dtype=torch.bfloat16, device=DEV)  # noqa: E731
+    mid, dxp, dw = [nan(s.Rcap, F) for _ in range(3)], nan(s.Rcap, D), [nan(E, F, D), nan(E, F, D), nan(E, D, F)]
+    off, expert = i32(slot_row_off), i32(slot_expert)
+    ctx.expert_ffn_gate_up_save(xp, off, expert, ws[0], ws[1], mid[2], *kept)
+    ctx.expert_ffn_backward(dyp, xp, off, i32(slot_off), expert, i32(row_pair), *ws, *kept, *mid, dxp, *dw)
+    ctx.check_status()
+    unit = lambda c, sc: c.view(torch.float8_e4m3fn).double() * torch.exp2(sc.double() - 127).T.repeat_interleave(32, 1)  # noqa: E731
+    close = lambda got, ref, tol: (got.double() - ref).norm() <= tol * ref.norm()  # noqa: E731
+    for e in range(E):
+        at = torch.arange(slot_row_off[slot_off[e]], slot_row_off[slot_off[e + 1]], device=DEV)
+        at = at[occ[at]]
+        if at.numel() == 0:
+            assert hist[e] == 0 and all((v[e] == 0).all() for v in dw)
+            continue
+        g, u = (unit(c[at], sc[:, at])[:, :F] for c, sc in ((kept[0], kept[2]), (kept[1], kept[3])))
+        x, dy, w1, w3, w2 = (v.double() for v in (xp[at], dyp[at], ws[0][e], ws[1][e], ws[2][e]))
+        sig = torch.sigmoid(g)
+        dh = dy @ w2
+        dg, du = dh * u * sig * (1 + g * (1 - sig)), dh * g * sig
+        assert close(dxp[at], dg @ w1 + du @ w3, 4e-3)
+        assert close(dw[0][e], dg.T @ x, 4e-3) and close(dw[1][e], du.T @ x, 4e-3)
+        assert close(dw[2][e], dy.T @ (g * sig * u), 4e-3)
