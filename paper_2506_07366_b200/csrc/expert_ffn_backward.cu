@@ -373,8 +373,8 @@ static_assert((4 * PairCfg::kStages + 2 * PairCfg::kAccs) * 8 + 8 <= 256, "barri
 
 // ------------------------------------------------------------------------------------------------ (1) and (2), by pairs
 // The same products on 256 x 256 tiles of a slot: each CTA of a pair has 128 of the rows, loads them and half the columns
-// of the weights, 32 KiB for a K block instead of 48.  For slots of several hundred rows and more: the last tile of a slot
-// leaves the second CTA idle when it has at most 128 rows.  Measured, whole gradient: 2048 rows a slot (16384 tokens, 16
+// of the weights, 32 KiB for a K block instead of 48.  For long slots (choose_tiles): the last tile of a slot leaves the
+// second CTA idle when it has at most 128 rows.  Measured, whole gradient: 2048 rows a slot (16384 tokens, 16
 // slots) 20.4 -> 19.8 ms, 614 rows a slot (64 experts, 80 slots) 1.96 -> 1.94 ms, 137 rows a slot not faster.
 struct PairDataCfg : PairCfg {
   static constexpr int kThreads = 64 + 32 * kEpiWarps;
@@ -893,7 +893,7 @@ int launch_data_gradient(moegps_ctx* ctx, const CUtensorMap& a0, const CUtensorM
   MOEGPS_CUDA_TRY(ctx, launch_after(data_gradient_kernel<kAct, Cfg>, dim3(ctx->sm_count), Cfg::kThreads, Cfg::kSmem, st, a0, b0,
                                     a1, b1, slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim, (int)moegps_rcap_of(s), kept,
                                     act_out, static_cast<__nv_bfloat16*>(out), ctx->d_status));
-  MOEGPS_AFTER_LAUNCH(ctx);
+  MOEGPS_AFTER_LAUNCH(ctx, "%s tile=%dx%d", kAct ? "act" : "input", BM, BN);
   return MOEGPS_OK;
 }
 
@@ -912,7 +912,7 @@ int launch_data_gradient_pair(moegps_ctx* ctx, const CUtensorMap& a0, const CUte
   MOEGPS_CUDA_TRY(ctx, launch_after(data_gradient_pair_kernel<kAct>, dim3(ctx->sm_count / 2 * 2), Cfg::kThreads, Cfg::kSmem, st,
                                     a0, b0, a1, b1, slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim, (int)moegps_rcap_of(s),
                                     kept, act_out, static_cast<__nv_bfloat16*>(out), ctx->d_status));
-  MOEGPS_AFTER_LAUNCH(ctx);
+  MOEGPS_AFTER_LAUNCH(ctx, "%s tile=%dx%d", kAct ? "act" : "input", 2 * BM, BNACC);
   return MOEGPS_OK;
 }
 
@@ -920,7 +920,9 @@ enum class Tiles { kPair, k256, k128, k64 };
 
 // The tiles for n_dim output columns: what needs the fewest rounds of tiles over the SMs, weighted with a round's time
 // (relative to 128 x 256; measured cycles for a K block 690-860, 400, 330 and 600).  The slots' loads are on the device:
-// the estimate is that of evenly loaded slots, whose last tile is half full.
+// the estimate is that of evenly loaded slots, whose last tile is half full, and which have one tile at least.  Measured,
+// all four forced on 16 layers of 3 to 307 rows a slot, even and skewed loads: the choice is the fastest to 1 % in 55 of 64 launches and
+// within 14 % of it in the others, the worst the act kernel on 777 x 1000, F 1416, 17 slots (42.5 us by pairs, 37.4 by 128).
 Tiles choose_tiles(const moegps_ctx* ctx, int n_dim) {
   const moegps_shape_t& s = ctx->shape;
   const double R = (double)s.T * s.K, slots = s.S < R ? s.S : R;
@@ -929,7 +931,8 @@ Tiles choose_tiles(const moegps_ctx* ctx, int n_dim) {
   const struct { Tiles tiles; int rows, cols, sms; double time; } all[] = {
       {Tiles::k256, BM, 256, 1, 1.0}, {Tiles::k128, BM, 128, 1, 0.6}, {Tiles::k64, BM, 64, 1, 0.5}, {Tiles::kPair, 2 * BM, 256, 2, 0.85}};
   for (const auto& t : all) {
-    const double rounds = (R / t.rows + 0.5 * slots) * ((n_dim + t.cols - 1) / t.cols) / (ctx->sm_count / t.sms);
+    const double of_a_slot = R / slots / t.rows + 0.5, row_tiles = slots * (of_a_slot > 1.0 ? of_a_slot : 1.0);
+    const double rounds = row_tiles * ((n_dim + t.cols - 1) / t.cols) / (ctx->sm_count / t.sms);
     // (many rounds even out, a few do not)
     const double time = (rounds < 8 ? (double)(int64_t)(rounds + 0.999) : rounds) * t.time;
     if (time < least) {
