@@ -132,7 +132,6 @@ dispatch_backward_kernel(const uint4* __restrict__ dxp, const int32_t* __restric
       if (expert[j] < 0 || expert[j] >= E) {
         if (l == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, (int)t);
         expert[j] = -1;
-        dl[j] = 0.f;                                   // (its product with the row read as zero may not be 0)
       }
   }
 #pragma unroll 2
@@ -147,7 +146,8 @@ dispatch_backward_kernel(const uint4* __restrict__ dxp, const int32_t* __restric
 #pragma unroll
     for (int j = 0; j < KT; ++j) {
       fma8(acc, 1.f, v[j]);
-      if constexpr (kRouter) fma8(acc, dl[j], r[j]);
+      if constexpr (kRouter)
+        if (expert[j] >= 0) fma8(acc, dl[j], r[j]);    // (not the product with a row read as zero: dl may be infinite)
     }
     dx[t * chunks + c] = pack8(acc);
   }
