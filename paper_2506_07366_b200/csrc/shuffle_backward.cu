@@ -17,11 +17,23 @@ namespace {
 constexpr int kWarpsPerBlock = 4;
 constexpr int kThreads = kWarpsPerBlock * 32;
 // Whether a token is spread over the block's four warps: for wide rows, and for few tokens, whose blocks all run at once
-// and only the length of one counts.  Measured, us a call in a graph, four warps / one (combine, dispatch):
-//   256 tokens x 512, K 2: 1.6 / 1.7, 1.2 / 1.5     1024 x 1024, K 4: 3.7 / 5.0, 2.3 / 2.5    64 x 4096, K 2: 2.3 / 5.3, 1.9 / 4.5
-//   4096 x 512, K 2: 5.5 / 3.7, 4.7 / 2.6           8192 x 1024, K 4: 30.8 / 26.8, 14.2 / 15.7
-//   8192 x 2048, K 6: 67 / 69, 37.4 / 37.8          4096 x 7168, K 8: 153 / 159, 81 / 91 (floor 153, 81)
-bool is_wide(const moegps_ctx* ctx) { return ctx->shape.D >= 2048 || ctx->shape.T <= 8 * ctx->sm_count; }
+// and only the length of one counts.  Measured, us a call in a graph, four warps / one:
+//                                   combine        dispatch       dispatch with the router's part
+//     256 tokens x  512, K 2      1.7 /   1.9    1.4 /   1.7      1.8 /   2.1
+//    1200        x 1024, K 4      4.2 /   5.4    2.5 /   2.6      4.2 /   4.5
+//    4096        x 1024, K 4     16.5 /  15.6    5.8 /   6.1     11.4 /  10.5
+//    8192        x 1024, K 2     16.1 /  15.7    9.6 /   7.8     13.5 /  11.2
+//    8192        x 1024, K 4     30.7 /  27.0   14.2 /  15.8     31.5 /  22.6
+//    4096        x 1536, K 2     12.6 /  11.9    4.9 /   6.5      7.2 /   7.0
+//    8192        x 1536, K 8     75.2 /  68.1   42.6 /  37.4     75.1 /  50.3
+//    8192        x 2048, K 6     67.1 /  68.4   37.8 /  38.2     55.8 /  48.7
+//    4096        x 3584, K 4     41.8 /  45.9   23.7 /  24.8     36.1 /  41.0
+//    4096        x 7168, K 8    152.8 / 159.8   81.4 /  91.7    117.1 / 131.0    (floors 153, 81, 82)
+bool is_wide(const moegps_ctx* ctx, int least_width) {
+  return ctx->shape.D >= least_width || ctx->shape.T <= 8 * ctx->sm_count;
+}
+constexpr int kCombineWidth = 2048, kRouterWidth = 2056;      // (widths are multiples of 8: wider than 2048)
+int dispatch_width(int K) { return K > 4 ? 2048 : K > 2 ? 1024 : 1536; }
 
 // The rows of token t's pairs; one outside the buffer is reported and becomes -1.
 template <int KT>
@@ -167,7 +179,7 @@ int moegps_launch_combine_backward(moegps_ctx* ctx, const void* dout, const void
   const int64_t Rcap = moegps_rcap_of(s);
   const uint4 *d = static_cast<const uint4*>(dout), *y = static_cast<const uint4*>(yp);
   uint4* o = static_cast<uint4*>(dyp);
-  const bool wide = is_wide(ctx);
+  const bool wide = is_wide(ctx, kCombineWidth);
   const int per = wide ? 1 : kWarpsPerBlock;
   const int blocks = (s.T + per - 1) / per;
 #define MOEGPS_LAUNCH(KT, W)                                                                                               \
@@ -180,7 +192,7 @@ int moegps_launch_combine_backward(moegps_ctx* ctx, const void* dout, const void
   MOEGPS_FOR_K(s.K, MOEGPS_CASE)
 #undef MOEGPS_LAUNCH
 #undef MOEGPS_CASE
-  MOEGPS_AFTER_LAUNCH(ctx);
+  MOEGPS_AFTER_LAUNCH(ctx, "warps=%d", wide ? kWarpsPerBlock : 1);
   return MOEGPS_OK;
 }
 
@@ -191,7 +203,7 @@ int moegps_launch_dispatch_backward(moegps_ctx* ctx, const void* dxp, const int3
   const int64_t Rcap = moegps_rcap_of(s);
   const uint4 *v = static_cast<const uint4*>(dxp), *r = static_cast<const uint4*>(w_router);
   uint4* o = static_cast<uint4*>(dx);
-  const bool wide = is_wide(ctx);
+  const bool wide = is_wide(ctx, dlogit ? kRouterWidth : dispatch_width(s.K));
   const int per = wide ? 1 : kWarpsPerBlock;
   const int blocks = (s.T + per - 1) / per;
 #define MOEGPS_LAUNCH(KT, W, R)                                                                                          \
@@ -208,6 +220,6 @@ int moegps_launch_dispatch_backward(moegps_ctx* ctx, const void* dxp, const int3
   MOEGPS_FOR_K(s.K, MOEGPS_CASE)
 #undef MOEGPS_CASE
 #undef MOEGPS_LAUNCH
-  MOEGPS_AFTER_LAUNCH(ctx);
+  MOEGPS_AFTER_LAUNCH(ctx, "warps=%d", wide ? kWarpsPerBlock : 1);
   return MOEGPS_OK;
 }

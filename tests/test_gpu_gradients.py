@@ -750,3 +750,48 @@ def test_expert_gradient_on_every_tile_shape(dims, monkeypatch, capfd):
     check_layer(ctx, idx, 31)
     err = capfd.readouterr().err
     assert f"act tile={act}\n" in err and f"input tile={data}\n" in err
+
+
+# T, D, K and the warps that a token gets in combine, in dispatch and in dispatch with the router's part
+SHUFFLES = [
+    (1301, 72, 1, 1, 1, 1), (1301, 136, 2, 1, 1, 1), (1301, 520, 3, 1, 1, 1), (1301, 264, 5, 1, 1, 1), (1301, 1032, 8, 1, 1, 1),
+    (1301, 1032, 4, 1, 4, 1), (1301, 1544, 2, 1, 4, 1), (1301, 2048, 6, 4, 4, 1), (1301, 2056, 7, 4, 4, 4), (9, 8, 2, 4, 4, 4),
+]
+
+
+@pytest.mark.parametrize("dims", SHUFFLES, ids=lambda d: "x".join(map(str, d[:3])))
+def test_shuffle_gradients_with_every_team_of_warps(dims, monkeypatch, capfd):
+    """Against 64 bits on the GPU.  dyp is one product rounded once; dtopk_w a sum of D terms, (D / 32 + 8) 2^-24 of their
+    magnitudes; dx an fp32 sum of at most 2 K terms rounded once."""
+    T, D, K, *warps = dims
+    E, S, A = 9, 11, 16
+    idx = np.argsort(np.random.default_rng(32).random((T, E)), axis=1)[:, :K].astype(np.int32)
+    hist = oracle.histogram(idx, E)
+    replicas, slot_off, _, _ = oracle.plan(hist, S)
+    _, row_pair, pair_row, _ = oracle.dispatch(None, idx, hist, replicas, slot_off, S, A)
+    ctx = traced(monkeypatch, binding.Shape(T, D, 8, E, K, S, 0, A))
+    if torch.cuda.get_device_properties(0).multi_processor_count != 148:
+        pytest.skip("the teams are those for 148 SMs")
+    gen = torch.Generator(device=DEV).manual_seed(33)
+    rnd = lambda *s: torch.randn(*s, generator=gen, device=DEV)  # noqa: E731
+    i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a).astype(np.int32)).to(DEV)  # noqa: E731
+    rows, at, pad = i32(pair_row).view(T, K), i32(pair_row).view(T, K).long(), i32(row_pair) < 0
+    dout, wr, w, dl = rnd(T, D).to(torch.bfloat16), rnd(E, D).to(torch.bfloat16), torch.softmax(rnd(T, K), 1), rnd(T, K)
+    buf = rnd(ctx.shape.Rcap, D).to(torch.bfloat16)
+    buf[pad] = float("nan")
+    dyp, dw, dx = torch.full_like(buf, 7.0), torch.full((T, K), float("nan"), device=DEV), torch.full_like(dout, float("nan"))
+    capfd.readouterr()
+    ctx.combine_backward(dout, buf, rows, w, dyp, dw)
+    assert f"warps={warps[0]}\n" in capfd.readouterr().err
+    assert torch.equal(dyp[at], (w[..., None] * dout[:, None].float()).to(torch.bfloat16)) and (dyp[pad] == 7).all()
+    terms = buf[at].double() * dout[:, None].double()
+    assert ((dw.double() - terms.sum(-1)).abs() <= (D / 32 + 8) * 2.0 ** -24 * terms.abs().sum(-1)).all()
+    ctx.dispatch_backward(buf, rows, None, None, None, dx)
+    assert f"warps={warps[1]}\n" in capfd.readouterr().err
+    parts = buf[at].double()
+    off = lambda p: (dx.double() - p.sum(1)).abs() - U * p.sum(1).abs() - 17 * 2.0 ** -24 * p.abs().sum(1)  # noqa: E731
+    assert off(parts).max() <= 0
+    ctx.dispatch_backward(buf, rows, i32(idx), dl, wr, dx)
+    assert f"warps={warps[2]}\n" in capfd.readouterr().err
+    assert off(torch.cat([parts, dl[..., None].double() * wr[i32(idx).long()].double()], 1)).max() <= 0
+    ctx.check_status()
