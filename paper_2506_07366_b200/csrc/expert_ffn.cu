@@ -31,8 +31,9 @@ namespace {
 using namespace sm100;
 using namespace grouped_gemm;
 
-// silu(g) = g / (1 + exp(-g)) = g * (0.5 + 0.5 tanh(g / 2)), with the hardware tanh approximation
-// (relative error about 2^-11; the product is rounded to bf16, 2^-9, right after).
+// silu(g) = g / (1 + exp(-g)) = g * (0.5 + 0.5 tanh(g / 2)), with the hardware tanh approximation.  For negative g the
+// sum cancels; measured over [-20, 20] against 64 bits, after the rounding to bf16: nothing but that rounding (2^-8 at most)
+// for g >= -6, 5e-3 of the value down to -8, 1e-2 down to -12, and beyond, where silu is below 8e-5, 2e-6 in absolute terms.
 __device__ __forceinline__ float silu_fast(float g) {
   float t;
   asm("tanh.approx.f32 %0, %1;" : "=f"(t) : "f"(0.5f * g));

@@ -8,7 +8,9 @@
 namespace route_backward {
 
 constexpr int kTileE = 128, kTileD = 256, kTileT = 64;   // experts, columns (at most) and tokens of a block's products
-constexpr int kBlocks = 148;                             // that run at the same time: one for each SM
+// That run at the same time, one for each SM.  A constant: the cut decides the workspace's size, which is asked for by shape,
+// without a device.
+constexpr int kBlocks = 148;
 
 // Most token tiles that one sum runs over: the tensor core truncates at every accumulation.
 constexpr int kMostSteps = 16;
