@@ -12,11 +12,11 @@
 //   2. dlogit  : one thread per pair.
 //   3. weights : dWr = dl^T x on the tensor cores, dl as a dense [tokens x experts] matrix that exists only in shared
 //                memory, tile by tile.  A dl is split into three bf16 (8 + 8 + 8 bits: all of its 24), so the products are
-//                exact and the sums are fp32: three MMAs for one, but x is read once.  An accumulation on the tensor core
-//                truncates, so its error grows with their number: the small second and third parts have a sum of their own,
-//                and no sum runs over more than 1024 tokens.  Measured against 64 bits, of the norm: 8.1e-7 on 8192 tokens and 64
-//                experts, 9.1e-7 on 4096 tokens and 256, 7.8e-7 on 16384 tokens and 8 (a 32-bit library product of the same
-//                dl: 4.6e-7, 1.2e-6, 4.5e-7); with sums over 2048 tokens 1.4e-6 to 1.8e-6.
+//                exact and the sums are fp32: three MMAs for one, but x is read once for each 128 experts.  An accumulation
+//                on the tensor core truncates, so its error grows with their number: the small second and third parts have
+//                a sum of their own, and no sum runs over more than 1024 tokens.  Measured against 64 bits, of the norm:
+//                8.1e-7 on 8192 tokens and 64 experts, 9.1e-7 on 4096 tokens and 256, 7.8e-7 on 16384 tokens and 8 (a
+//                32-bit library product of the same dl: 4.6e-7, 1.2e-6, 4.5e-7); with sums over 2048 tokens 1.4e-6 to 1.8e-6.
 //                Summing each expert's rows of x instead, gathered K times from L2, ran at L2's rate (10 TB/s) and took
 //                21 us + 8 us for joining the parts on 8192 tokens x 2048, 6 of 64 experts, and 41 + 12 us on 4096 x 7168,
 //                8 of 256.
