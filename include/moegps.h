@@ -361,6 +361,41 @@ MOEGPS_API int moegps_route_backward(moegps_ctx_t* ctx, const void* x, const voi
 /* Bytes of `workspace` for moegps_route_backward (0 for an invalid shape). */
 MOEGPS_API size_t moegps_route_backward_workspace_bytes(const moegps_shape_t* shape);
 
+/* ---- experts in 4 bits: what serving reads is the experts' weights, and these are a quarter of the bytes ----
+ * A matrix of N outputs x C inputs for each expert (gate, up: N = F, C = D; down: N = D, C = F).  32 consecutive inputs of an
+ * output form a block with one power-of-two scale 2^k, k the smallest integer >= -127 with max|w| <= 6 * 2^k (at most 125:
+ * weights beyond 1.5 * 2^127 become that); a code is w * 2^-k rounded to e2m1 {0, .5, 1, 1.5, 2, 3, 4, 6} (nearest, ties to
+ * the even code; bit 3 the sign), the scale byte is k + 127 (0 for a block of zeros).  A block that holds an infinity or a NaN
+ * has scale byte 255 and its 32 weights decode to NaN.
+ * Codes: uint8 [E, N, C4 / 2], two to a byte, the even input in the low half; C4 = C rounded up to a multiple of 128, filled up
+ * with zero codes.  32-byte aligned.
+ * Scales: uint8 [E, N4 / 128, C4 / 128, 512], N4 = N rounded up to a multiple of 128: the byte of output n and inputs
+ * 32 b .. 32 b + 31 is [e, n / 128, b / 4, (n % 32) * 16 + n / 32 % 4 * 4 + b % 4] (0 for outputs that do not exist).
+ * moegps_weights4_bytes / _scale_bytes give the sizes (0 for an invalid shape); down != 0: of the down matrices.
+ *
+ * weights_quantize4 - w: bf16 [E, N, C] -> w4, w4_scale.  weights_dequantize4 - back, exactly (every value is a bf16).
+ * All experts in one launch.  Shapes with more than 2^31-1 tiles of 128 x 128 weights: MOEGPS_ERR_UNSUPPORTED_SHAPE. */
+MOEGPS_API size_t moegps_weights4_bytes(const moegps_shape_t* shape, int32_t down);
+MOEGPS_API size_t moegps_weights4_scale_bytes(const moegps_shape_t* shape, int32_t down);
+MOEGPS_API int moegps_weights_quantize4(moegps_ctx_t* ctx, const void* w, int32_t down, void* w4, void* w4_scale, void* stream);
+MOEGPS_API int moegps_weights_dequantize4(moegps_ctx_t* ctx, const void* w4, const void* w4_scale, int32_t down, void* w,
+                                          void* stream);
+
+/* expert_ffn4 - moegps_expert_ffn on 4-bit weights: for every row rho of slot s with e = slot_expert[s], W4 what the codes
+ * stand for:  h = silu(gate4[e] xp[rho]) * (up4[e] xp[rho]);   yp[rho] = down4[e] h.
+ * The products are exact (a row is split into two e4m3 terms that add up to it, see csrc/mx4.cuh; values below 2^-15 of the
+ * largest of their 32 neighbours are off by at most 2^-21 of that), sums are fp32, h is kept to 2^-9 relative and yp is rounded
+ * once to bf16.  A row that holds an infinity or a NaN gives NaN.
+ * xp, slot_row_off, slot_expert, yp as in moegps_expert_ffn: padding rows of a slot yield unspecified values, rows outside every
+ * slot and slots with slot_expert < 0 are not written, a slot with an extent outside [0, Rcap] is skipped and
+ * MOEGPS_ERR_BAD_INDEX recorded.
+ * workspace: moegps_expert_ffn4_workspace_bytes(shape) bytes, 16-byte aligned, contents irrelevant; its size cannot be checked
+ * here.  Calls that may overlap on the GPU need a workspace each. */
+MOEGPS_API size_t moegps_expert_ffn4_workspace_bytes(const moegps_shape_t* shape);
+MOEGPS_API int moegps_expert_ffn4(moegps_ctx_t* ctx, const void* xp, const int32_t* slot_row_off, const int32_t* slot_expert,
+                                  const void* gate4, const void* up4, const void* down4, const void* gate4_scale,
+                                  const void* up4_scale, const void* down4_scale, void* yp, void* workspace, void* stream);
+
 /* predictor_update - state of Distribution-Only Prediction across batches (paper, Section 3.2.1:
  * the maximum-likelihood estimate p_e = n_e / N of Eq. 1, averaged over the batches seen).  state[e] += hist[e]; state / sum(state) is then Eq. 1 over all tokens
  * seen.  predicted_hist = state divided by the smallest power of two that makes its largest entry fit

@@ -35,3 +35,8 @@ from .moe_gradients import (  # noqa: F401
     gate_up,
     route_backward,
 )
+from .experts4 import (  # noqa: F401
+    weights4_decode,
+    weights4_encode,
+    weights4_pack,
+)

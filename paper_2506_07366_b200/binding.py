@@ -47,6 +47,12 @@ class Shape:
         """Columns of a row of 8-bit activations: F rounded up to whole blocks of 32."""
         return (self.F + 31) // 32 * 32
 
+    def w4_shapes(self, down: bool = False):
+        """Shapes of 4-bit expert matrices: (codes, scales), both uint8.  down False: gate or up [E, F, D]; True: [E, D, F]."""
+        n, c = (self.D, self.F) if down else (self.F, self.D)
+        tiles, chunks = (n + 127) // 128, (c + 127) // 128
+        return (self.E, n, 64 * chunks), (self.E, tiles, chunks, 512)
+
     def c_struct(self) -> moegps_shape_t:
         return moegps_shape_t(*(getattr(self, f[0]) for f in moegps_shape_t._fields_))
 
@@ -65,6 +71,8 @@ EXPORTS = (
     "moegps_expert_ffn_gate_up_save", "moegps_expert_ffn_backward", "moegps_expert_ffn_backward_act",
     "moegps_expert_ffn_backward_input", "moegps_expert_ffn_backward_weights", "moegps_combine_backward",
     "moegps_dispatch_backward", "moegps_route_backward", "moegps_route_backward_workspace_bytes",
+    "moegps_weights4_bytes", "moegps_weights4_scale_bytes", "moegps_weights_quantize4", "moegps_weights_dequantize4",
+    "moegps_expert_ffn4", "moegps_expert_ffn4_workspace_bytes",
 )
 
 
@@ -126,6 +134,12 @@ def _lib():
         "moegps_dispatch_backward": (ctypes.c_int, [vp] * 8),
         "moegps_route_backward": (ctypes.c_int, [vp] * 15),
         "moegps_route_backward_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(moegps_shape_t)]),
+        "moegps_weights4_bytes": (ctypes.c_size_t, [ctypes.POINTER(moegps_shape_t), i32]),
+        "moegps_weights4_scale_bytes": (ctypes.c_size_t, [ctypes.POINTER(moegps_shape_t), i32]),
+        "moegps_weights_quantize4": (ctypes.c_int, [vp, vp, i32, vp, vp, vp]),
+        "moegps_weights_dequantize4": (ctypes.c_int, [vp, vp, vp, i32, vp, vp]),
+        "moegps_expert_ffn4": (ctypes.c_int, [vp] * 13),
+        "moegps_expert_ffn4_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(moegps_shape_t)]),
         "moegps_selftest_bounded_wait": (ctypes.c_int, [vp, i64, vp]),
         "moegps_predictor_update": (ctypes.c_int, [vp] * 5),
         "moegps_predictor_update_ema": (ctypes.c_int, [vp, vp, vp, i32, vp, vp]),
@@ -463,6 +477,11 @@ class Context:
                                     row_pair, dlogit, t("dw_router", f32, s.E, s.D), t("dbias", f32, s.E),
                                     t("workspace", u8))
         self._route_backward_bytes = route_backward_workspace_bytes(s)
+        (up_codes, up_scales), (down_codes, down_scales) = s.w4_shapes(), s.w4_shapes(down=True)
+        self._expert_ffn4 = call("expert_ffn4", *xp, row_off, expert, t("gate4", u8, *up_codes), t("up4", u8, *up_codes),
+                                 t("down4", u8, *down_codes), t("gate4_scale", u8, *up_scales), t("up4_scale", u8, *up_scales),
+                                 t("down4_scale", u8, *down_scales), *yp, t("workspace", u8))
+        self._ffn4_bytes = expert_ffn4_workspace_bytes(s)
 
     def expert_ffn_gate_up_save(self, xp, slot_row_off, slot_expert, w_gate, w_up, h_ws, gate8, up8, gate_scale, up_scale,
                                 stream=None):
@@ -519,6 +538,34 @@ class Context:
         if rc:
             self._check(rc, "moegps_route_backward")
 
+    # -- experts in 4 bits --------------------------------------------------------------------
+    def weights_quantize4(self, w, w4, w4_scale, down=False, stream=None):
+        """w: bf16 [E, F, D] (down: [E, D, F]) -> codes and scales of Shape.w4_shapes(down)."""
+        s = self.shape
+        codes, scales = s.w4_shapes(down)
+        self._check(_lib().moegps_weights_quantize4(
+            self._h, _ptr(w, torch.bfloat16, (s.E, s.D, s.F) if down else (s.E, s.F, s.D), "w"), int(bool(down)),
+            _ptr(w4, torch.uint8, codes, "w4"), _ptr(w4_scale, torch.uint8, scales, "w4_scale"), _stream(stream)),
+            "moegps_weights_quantize4")
+
+    def weights_dequantize4(self, w4, w4_scale, w, down=False, stream=None):
+        """What the codes stand for, exactly, into w: bf16 [E, F, D] (down: [E, D, F])."""
+        s = self.shape
+        codes, scales = s.w4_shapes(down)
+        self._check(_lib().moegps_weights_dequantize4(
+            self._h, _ptr(w4, torch.uint8, codes, "w4"), _ptr(w4_scale, torch.uint8, scales, "w4_scale"), int(bool(down)),
+            _ptr(w, torch.bfloat16, (s.E, s.D, s.F) if down else (s.E, s.F, s.D), "w"), _stream(stream)),
+            "moegps_weights_dequantize4")
+
+    def expert_ffn4(self, xp, slot_row_off, slot_expert, gate4, up4, down4, gate4_scale, up4_scale, down4_scale, yp, workspace,
+                    stream=None):
+        if workspace is None or workspace.nbytes < self._ffn4_bytes:
+            raise MoegpsError(ERR_WORKSPACE_TOO_SMALL, "moegps_expert_ffn4")
+        rc = self._expert_ffn4(stream, xp, slot_row_off, slot_expert, gate4, up4, down4, gate4_scale, up4_scale, down4_scale, yp,
+                               workspace)
+        if rc:
+            self._check(rc, "moegps_expert_ffn4")
+
     def predictor_update(self, hist, state, predicted_hist, stream=None):
         s = self.shape
         self._check(_lib().moegps_predictor_update(
@@ -574,6 +621,21 @@ def workspace_bytes(shape: Shape) -> int:
 def route_backward_workspace_bytes(shape: Shape) -> int:
     cs = shape.c_struct()
     return int(_lib().moegps_route_backward_workspace_bytes(ctypes.byref(cs)))
+
+
+def expert_ffn4_workspace_bytes(shape: Shape) -> int:
+    cs = shape.c_struct()
+    return int(_lib().moegps_expert_ffn4_workspace_bytes(ctypes.byref(cs)))
+
+
+def w4_scale_tiles(scale):
+    """Scale bytes [E, N, C / 32 rounded up] (one for each 32 inputs of an output, as a checkpoint holds them) in the order of
+    Shape.w4_shapes: [E, tiles, chunks, 512]."""
+    e, n, b = scale.shape
+    tiles, chunks = (n + 127) // 128, (b + 3) // 4
+    full = torch.zeros(e, tiles * 128, chunks * 4, dtype=scale.dtype, device=scale.device)
+    full[:, :n, :b] = scale
+    return full.view(e, tiles, 4, 32, chunks, 4).permute(0, 1, 4, 3, 2, 5).reshape(e, tiles, chunks, 512)
 
 
 def error_string(code: int) -> str:

@@ -15,9 +15,10 @@ LIB_PATH = os.path.join(PKG_DIR, "libmoegps.so")
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
 MARSHAL_PATH = os.path.join(PKG_DIR, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.cu", "route.cu", "histogram.cu", "plan.cu", "pack.cu", "dispatch.cu", "expert_ffn.cu", "combine.cu",
-           "predictor.cu", "selftest.cu", "expert_ffn_backward.cu", "shuffle_backward.cu", "route_backward.cu"]
+           "predictor.cu", "selftest.cu", "expert_ffn_backward.cu", "shuffle_backward.cu", "route_backward.cu",
+           "experts4.cu", "expert_ffn4.cu"]
 HEADERS = ["common.cuh", "sm100.cuh", "route_epilogue.cuh", "slot_offsets.cuh", "grouped_gemm.cuh", "act8.cuh", "bf16x8.cuh",
-           "route_backward.cuh"]
+           "route_backward.cuh", "mx4.cuh"]
 
 
 def _nvcc() -> str:
@@ -88,7 +89,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
 def _build_library(verbose: bool) -> None:
     cmd = [
         _nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-        "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
+        "--threads", "8", "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
         "-I", os.path.join(ROOT, "include"), "-I", CSRC,
     ]
     if verbose:

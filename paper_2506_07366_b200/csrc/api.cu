@@ -5,6 +5,7 @@
 #include <stdlib.h>
 
 #include "common.cuh"
+#include "mx4.cuh"
 #include "route_backward.cuh"
 
 namespace {
@@ -28,6 +29,14 @@ bool all_ok(P... ptrs) {
   for (const void* p : a)
     if (p == nullptr || !moegps_aligned16(p)) return false;
   return true;
+}
+
+bool aligned32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
+
+// 4-bit weights: a launch has one block for each tile of a matrix's chunk
+bool tiles4_fit(const moegps_shape_t& s) {
+  return (int64_t)s.E * mx4::tiles_of(s.F) * mx4::chunks_of(s.D) <= INT32_MAX &&
+         (int64_t)s.E * mx4::tiles_of(s.D) * mx4::chunks_of(s.F) <= INT32_MAX;
 }
 
 }  // namespace
@@ -357,6 +366,50 @@ int moegps_route_backward(moegps_ctx_t* ctx, const void* x, const void* w_router
   if (bias && (reinterpret_cast<uintptr_t>(bias) & 3u)) return MOEGPS_ERR_INVALID_ARG;
   return moegps_launch_route_backward(ctx, x, w_router, bias, topk_idx, topk_w, dtopk_w, slot_row_off, slot_off, row_pair,
                                       dlogit, dw_router, dbias, workspace, st);
+}
+
+size_t moegps_weights4_bytes(const moegps_shape_t* shape, int32_t down) {
+  if (check_shape(shape) != MOEGPS_OK) return 0;
+  const size_t rows = down ? shape->D : shape->F;
+  return (size_t)shape->E * rows * mx4::chunks_of(down ? shape->F : shape->D) * (mx4::kChunk / 2);
+}
+
+size_t moegps_weights4_scale_bytes(const moegps_shape_t* shape, int32_t down) {
+  if (check_shape(shape) != MOEGPS_OK) return 0;
+  return (size_t)shape->E * mx4::tiles_of(down ? shape->D : shape->F) * mx4::chunks_of(down ? shape->F : shape->D) *
+         mx4::kScaleTile;
+}
+
+int moegps_weights_quantize4(moegps_ctx_t* ctx, const void* w, int32_t down, void* w4, void* w4_scale, void* stream) {
+  if (!ctx || !all_ok(w, w4, w4_scale) || !aligned32(w4)) return MOEGPS_ERR_INVALID_ARG;
+  if (int rc = moegps_check_device(ctx)) return rc;
+  if (!tiles4_fit(ctx->shape)) return MOEGPS_ERR_UNSUPPORTED_SHAPE;
+  return moegps_launch_weights_quantize4(ctx, w, down != 0, w4, w4_scale, (cudaStream_t)stream);
+}
+
+int moegps_weights_dequantize4(moegps_ctx_t* ctx, const void* w4, const void* w4_scale, int32_t down, void* w, void* stream) {
+  if (!ctx || !all_ok(w, w4, w4_scale) || !aligned32(w4)) return MOEGPS_ERR_INVALID_ARG;
+  if (int rc = moegps_check_device(ctx)) return rc;
+  if (!tiles4_fit(ctx->shape)) return MOEGPS_ERR_UNSUPPORTED_SHAPE;
+  return moegps_launch_weights_dequantize4(ctx, w4, w4_scale, down != 0, w, (cudaStream_t)stream);
+}
+
+size_t moegps_expert_ffn4_workspace_bytes(const moegps_shape_t* shape) {
+  return check_shape(shape) == MOEGPS_OK ? mx4::layout_of(*shape).total : 0;
+}
+
+int moegps_expert_ffn4(moegps_ctx_t* ctx, const void* xp, const int32_t* slot_row_off, const int32_t* slot_expert,
+                       const void* gate4, const void* up4, const void* down4, const void* gate4_scale, const void* up4_scale,
+                       const void* down4_scale, void* yp, void* workspace, void* stream) {
+  if (!ctx) return MOEGPS_ERR_INVALID_ARG;
+  if (int rc = moegps_check_device(ctx)) return rc;
+  if (ctx->shape.T == 0) return MOEGPS_OK;
+  if (!all_ok(xp, slot_row_off, slot_expert, gate4, up4, down4, gate4_scale, up4_scale, down4_scale, yp, workspace) ||
+      !aligned32(gate4) || !aligned32(up4) || !aligned32(down4))
+    return MOEGPS_ERR_INVALID_ARG;
+  if (!tiles4_fit(ctx->shape)) return MOEGPS_ERR_UNSUPPORTED_SHAPE;
+  return moegps_launch_expert_ffn4(ctx, xp, slot_row_off, slot_expert, gate4, up4, down4, gate4_scale, up4_scale, down4_scale, yp,
+                                   workspace, (cudaStream_t)stream);
 }
 
 int moegps_status(moegps_ctx_t* ctx, void* stream, int32_t* host_status) {

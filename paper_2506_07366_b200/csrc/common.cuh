@@ -174,3 +174,8 @@ int moegps_launch_route_backward(moegps_ctx* ctx, const void* x, const void* w_r
                                  const int32_t* topk_idx, const float* topk_w, const float* dtopk_w,
                                  const int32_t* slot_row_off, const int32_t* slot_off, const int32_t* row_pair,
                                  float* dlogit, float* dw_router, float* dbias, void* workspace, cudaStream_t st);
+int moegps_launch_weights_quantize4(moegps_ctx* ctx, const void* w, bool down, void* w4, void* w4_scale, cudaStream_t st);
+int moegps_launch_weights_dequantize4(moegps_ctx* ctx, const void* w4, const void* w4_scale, bool down, void* w, cudaStream_t st);
+int moegps_launch_expert_ffn4(moegps_ctx* ctx, const void* xp, const int32_t* slot_row_off, const int32_t* slot_expert,
+                              const void* gate4, const void* up4, const void* down4, const void* gate4_scale, const void* up4_scale,
+                              const void* down4_scale, void* yp, void* workspace, cudaStream_t st);

@@ -7,7 +7,7 @@ from __future__ import annotations
 
 import torch
 
-from .binding import Context, Shape, route_backward_workspace_bytes, workspace_bytes
+from .binding import Context, Shape, expert_ffn4_workspace_bytes, route_backward_workspace_bytes, workspace_bytes
 
 # Row alignment of the slot buckets that the benchmark and the serving examples use: slot starts are
 # multiples of 16 rows.  The grouped GEMM accepts any alignment (its tiles start at the slot's first
@@ -22,7 +22,7 @@ class MoeLayer:
         self.ctx = Context(shape, device)
         dev = w_router.device
         self.w_router, self.bias = w_router, bias
-        self.w_gate, self.w_up, self.w_down = w_gate, w_up, w_down
+        self._set_experts(w_gate, w_up, w_down)
         i32 = dict(dtype=torch.int32, device=dev)
         bf = dict(dtype=torch.bfloat16, device=dev)
         self.x = torch.empty(s.T, s.D, **bf)             # staging for host inputs
@@ -37,12 +37,20 @@ class MoeLayer:
         self.row_pair = torch.empty(s.Rcap, **i32)
         self.pair_row = torch.empty(s.T, s.K, **i32)
         self.xp = torch.empty(s.Rcap, s.D, **bf)
-        self.h_ws = torch.empty(s.Rcap, s.F, **bf)
         self.yp = torch.empty(s.Rcap, s.D, **bf)
         self.out = torch.empty(s.T, s.D, **bf)
         self.workspace = torch.empty(max(16, workspace_bytes(s)), dtype=torch.uint8, device=dev)
         self.pred = torch.empty(s.E, **i32)
         self._planned = False
+
+    def _set_experts(self, w_gate, w_up, w_down):
+        s = self.shape
+        self.w_gate, self.w_up, self.w_down = w_gate, w_up, w_down
+        self.h_ws = torch.empty(s.Rcap, s.F, dtype=torch.bfloat16, device=self.w_router.device)
+
+    def _expert_ffn(self, stream):
+        self.ctx.expert_ffn(self.xp, self.slot_row_off, self.slot_expert, self.w_gate, self.w_up, self.w_down, self.h_ws, self.yp,
+                            stream)
 
     def plan(self, predicted_hist, stream=None):
         """Replica plan from a predicted histogram (int32 [E], device or host tensor)."""
@@ -62,8 +70,7 @@ class MoeLayer:
         c.route_prepare(x, self.w_router, self.bias, self.topk_idx, self.topk_w, self.hist, self.workspace, stream)
         c.dispatch_prepared(x, self.topk_idx, self.hist, self.replicas, self.slot_off, self.slot_row_off,
                             self.row_pair, self.pair_row, self.xp, self.workspace, stream)
-        c.expert_ffn(self.xp, self.slot_row_off, self.slot_expert, self.w_gate, self.w_up,
-                     self.w_down, self.h_ws, self.yp, stream)
+        self._expert_ffn(stream)
         c.combine(self.yp, self.pair_row, self.topk_w, out, stream)
         return out
 
@@ -219,6 +226,43 @@ class MoeTrainLayer(MoeLayer):
         c.dispatch_backward(self.dxp, self.pair_row, self.topk_idx, self.dlogit, self.w_router, g["x"], stream)
         self._trained_x = None
         return g
+
+
+class MoeLayer4(MoeLayer):
+    """MoeLayer with its experts in 4 bits: a quarter of the memory, and of the bytes that a step of few tokens reads.
+
+    Each of w_gate, w_up [E, F, D] and w_down [E, D, F] is a bf16 tensor, rounded to 4 bits here, or the pair (codes, scales)
+    of one that is in 4 bits already (Shape.w4_shapes; binding.w4_scale_tiles brings a checkpoint's scale bytes into that order).
+    The layer keeps the pairs.  dense_experts() gives the weights back as bf16, for instance to train on what was rounded.
+    """
+
+    def _set_experts(self, w_gate, w_up, w_down):
+        self.w_gate, self.w_up, self.w_down = (self._in_4_bits(w, down) for w, down in
+                                               ((w_gate, False), (w_up, False), (w_down, True)))
+        self.ffn_workspace = torch.empty(max(16, expert_ffn4_workspace_bytes(self.shape)), dtype=torch.uint8,
+                                         device=self.w_router.device)
+
+    def _in_4_bits(self, w, down):
+        if not isinstance(w, torch.Tensor):
+            codes, scales = w
+            return codes, scales
+        pair = tuple(torch.empty(n, dtype=torch.uint8, device=w.device) for n in self.shape.w4_shapes(down))
+        self.ctx.weights_quantize4(w, *pair, down)
+        return pair
+
+    def _expert_ffn(self, stream):
+        (gate, gate_scale), (up, up_scale), (down, down_scale) = self.w_gate, self.w_up, self.w_down
+        self.ctx.expert_ffn4(self.xp, self.slot_row_off, self.slot_expert, gate, up, down, gate_scale, up_scale, down_scale, self.yp,
+                             self.ffn_workspace, stream)
+
+    def dense_experts(self, stream=None):
+        """(w_gate, w_up, w_down) in bf16: exactly what the layer computes with."""
+        s, out = self.shape, []
+        for pair, down in ((self.w_gate, False), (self.w_up, False), (self.w_down, True)):
+            w = torch.empty((s.E, s.D, s.F) if down else (s.E, s.F, s.D), dtype=torch.bfloat16, device=pair[0].device)
+            self.ctx.weights_dequantize4(*pair, w, down, stream)
+            out.append(w)
+        return tuple(out)
 
 
 class HostPipeline:
