@@ -6,11 +6,14 @@
 // The products are block-scaled MMAs (e2m1 x e4m3, fp32 accumulators in tensor memory) with the WEIGHTS as the 128-row
 // operand and the slot's rows as the other one, so that a slot of few rows costs few columns.  A weight tile is expanded to 16-byte
 // groups by the TMA load that brings it (8 bytes of codes, 8 unused): 8 KB of memory traffic for 16 KB of shared memory,
-// and no thread touches a weight.
+// and no thread touches a weight.  The scales of the rows lie in the workspace as tensor memory wants them, tile by tile.
 //
-// Warps: 0 loads weights, their scales and the rows' codes (TMA), 2 the rows' scales (the words of a tile's rows go to
-// the places where tensor memory wants them, 4-byte asynchronous copies), 1 issues scale copies and MMAs, 4..7 drain the
-// accumulators (two, so that a tile's epilogue overlaps the next one's products).  Every wait is bounded.
+// Two kernels, by rows for each slot (mx4::cut_of):
+//  narrow_kernel (up to 48): bound by reading weights.  The K steps of all tiles are dealt evenly to the SMs, whatever their
+//    number; a tile that several SMs share is joined by the one that finishes last.  Both terms of a row are columns of one
+//    MMA (an MMA of few columns takes 40 clocks whatever their number, it waits for its 128 weight rows).
+//  wide_kernel: bound by products.  Pairs of CTAs, 256 weight rows x 224 rows of the slot, two MMAs for the two terms.
+// Every wait is bounded.
 #include "common.cuh"
 #include "grouped_gemm.cuh"
 #include "mx4.cuh"
@@ -20,36 +23,79 @@ namespace {
 
 using namespace sm100;
 using grouped_gemm::build_tables;
-using grouped_gemm::decode_tile;
+using grouped_gemm::kMaxS;
 using grouped_gemm::Tables;
-using grouped_gemm::TileCoord;
+using mx4::kChunk;
+using mx4::kScaleTile;
+using mx4::kTile;
+
+__host__ __device__ constexpr int round_up(int n, int to) { return (n + to - 1) / to * to; }
+
+// A tile: rows row0 .. row0 + rows - 1 of one slot, times tile m of its expert's outputs.
+struct Tile {
+  int row0, rows, m, expert, row_tile;
+};
+
+// tb: first row tile of each slot.  Tiles are ordered by slot, then outputs, then rows, so that neighbours share weights.
+template <int kRows>
+__device__ __forceinline__ Tile tile_at(const Tables& tb, const int32_t* __restrict__ slot_row_off,
+                                        const int32_t* __restrict__ slot_expert, int S, int64_t t, int m_tiles) {
+  int lo = 0, hi = S;                 // find s with base[s] * m_tiles <= t < base[s + 1] * m_tiles
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if ((int64_t)tb.tile_base[mid] * m_tiles <= t) lo = mid; else hi = mid;
+  }
+  const int base = tb.tile_base[lo], n = tb.tile_base[lo + 1] - base;
+  const int local = (int)(t - (int64_t)base * m_tiles);       // below n * m_tiles of one slot
+  Tile c;
+  c.m = local / n;
+  const int j = local - c.m * n;
+  c.row0 = __ldg(slot_row_off + lo) + j * kRows;
+  c.rows = min(kRows, __ldg(slot_row_off + lo + 1) - c.row0);
+  c.expert = __ldg(slot_expert + lo);
+  c.row_tile = base + j;
+  return c;
+}
+
+__device__ __forceinline__ void linger() {
+  for (int i = 0; i < 1000; ++i) __nanosleep(1000);           // let copies in flight land before the block retires
+}
 
 // ------------------------------------------------------------------------------------------- split
-constexpr int kSplitRows = 8;      // rows of a block: one for each warp
-constexpr int kSplitCols = 1024;   // columns of a block
+constexpr int kSplitThreads = 256;
+constexpr int kSplitRows = 8;      // rows of a block's unit: one for each warp
+constexpr int kSplitCols = 1024;   // its columns
 
-__global__ void __launch_bounds__(256) split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off,
-                                                    int S, int D, int rcap, int pitch, const mx4::Rows out) {
-  __shared__ int last_row;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+template <int kRows>
+__global__ void __launch_bounds__(kSplitThreads)
+split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert,
+             int S, int E, int D, int rcap, const mx4::Rows out, int32_t* __restrict__ arrived, int32_t* __restrict__ status) {
+  static_assert(kRows % kSplitRows == 0, "a unit's rows belong to one tile");
+  __shared__ Tables units, tiles;                     // groups of kSplitRows rows, tiles of rows
   launch_dependents();
   wait_for_predecessor();
-  if (threadIdx.x == 0) last_row = 0;
+  build_tables<kSplitThreads, kSplitRows>(units, slot_row_off, slot_expert, S, E, 1, rcap, status);
+  build_tables<kSplitThreads, kRows>(tiles, slot_row_off, slot_expert, S, E, 1, rcap, status);
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < 2 * mx4::kMaxCtas; i += kSplitThreads) arrived[i] = 0;
   __syncthreads();
-  // one past the last row of any slot (slots with an extent outside the buffers have no rows)
-  int last = 0;
-  for (int s = threadIdx.x; s < S; s += blockDim.x) {
-    const int lo = slot_row_off[s], hi = slot_row_off[s + 1];
-    if (lo >= 0 && hi > lo && hi <= rcap) last = max(last, hi);
-  }
-  if (last) atomicMax(&last_row, last);
-  __syncthreads();
-  const int rows = last_row, chunks = mx4::chunks_of(D);
-  const int col_blocks = (chunks * mx4::kChunk + kSplitCols - 1) / kSplitCols;
-  const int64_t work = (int64_t)((rows + kSplitRows - 1) / kSplitRows) * col_blocks;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int chunks = mx4::chunks_of(D);
+  const int col_blocks = (chunks * kChunk + kSplitCols - 1) / kSplitCols;
+  const int64_t work = (int64_t)units.tile_base[S] * col_blocks;
   for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
-    const int row = (int)(b / col_blocks) * kSplitRows + warp, col0 = (int)(b % col_blocks) * kSplitCols;
-    if (row >= rows) continue;
+    const int group = (int)(b / col_blocks), col0 = (int)(b - (int64_t)group * col_blocks) * kSplitCols;
+    int lo = 0, hi = S;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (units.tile_base[mid] <= group) lo = mid; else hi = mid;
+    }
+    const int first = __ldg(slot_row_off + lo), slot_rows = __ldg(slot_row_off + lo + 1) - first;
+    const int r = (group - units.tile_base[lo]) * kSplitRows + warp;      // row of the slot
+    if (r >= slot_rows) continue;
+    const int row = first + r, in_tile = r % kRows, tile = tiles.tile_base[lo] + r / kRows;
+    const int rows_in_tile = min(kRows, slot_rows - (r - in_tile));
+    const int at1 = mx4::row_scale_at<kRows>(in_tile, 0, rows_in_tile), at2 = mx4::row_scale_at<kRows>(in_tile, 1, rows_in_tile);
     uint4 v[kSplitCols / 256];
 #pragma unroll
     for (int i = 0; i < kSplitCols / 256; ++i) {
@@ -78,85 +124,146 @@ __global__ void __launch_bounds__(256) split_kernel(const __nv_bfloat16* __restr
       w2 |= __shfl_xor_sync(0xffffffffu, w2, 4);
       w1 |= __shfl_xor_sync(0xffffffffu, w1, 8);
       w2 |= __shfl_xor_sync(0xffffffffu, w2, 8);
-      if (col < chunks * mx4::kChunk) {
-        const size_t at = (size_t)row * (chunks * mx4::kChunk) + col;
+      if (col < chunks * kChunk) {
+        const size_t at = (size_t)row * (chunks * kChunk) + col;
         *reinterpret_cast<uint2*>(out.code[0] + at) = make_uint2(c1[0] | c1[1] << 16, c1[2] | c1[3] << 16);
         *reinterpret_cast<uint2*>(out.code[1] + at) = make_uint2(c2[0] | c2[1] << 16, c2[2] | c2[3] << 16);
         if ((lane & 15) == 0) {
-          const size_t word = (size_t)(col / mx4::kChunk) * pitch + row;
-          out.scale[0][word] = w1;
-          out.scale[1][word] = w2;
+          uint8_t* scales = out.scale + ((size_t)tile * chunks + col / kChunk) * mx4::kRowScaleBytes<kRows>;
+          *reinterpret_cast<uint32_t*>(scales + at1) = w1;
+          *reinterpret_cast<uint32_t*>(scales + at2) = w2;
         }
       }
     }
   }
 }
 
-// ------------------------------------------------------------------------------------------- products
-__host__ __device__ constexpr int round_up(int n, int to) { return (n + to - 1) / to * to; }
+// ------------------------------------------------------------------------------------------- epilogues
+__device__ __forceinline__ float silu(float g) { return __fdividef(g, 1.0f + __expf(-g)); }
 
-template <int kN_, bool kGateUp_, int kStages_>
-struct Cfg {
-  static constexpr int kN = kN_;                       // rows of a tile at most
+// What a warp holds of 16 rows (a lane has one column of each) goes to memory through 1 KB of shared memory: 16 bytes a lane in
+// runs of 32 or 64, where a store of one byte or bf16 by each lane for each row held the epilogue up (gate + up on 49152
+// rows x 2048, F 1408, 64 experts: 1030 us, 755 without the stores).
+constexpr int kStaging = 1024;
+
+// 16 rows of h for a warp's 32 outputs (one for each lane, one block): codes and scales.  row: the first one's place in the
+// buffers, in_tile: in its tile of `rows`; col0: the first lane's column; block: which of the chunk's four.
+template <int kRows>
+__device__ __forceinline__ void store_h(const mx4::Rows& h, const uint32_t (&g)[16], const uint32_t (&u)[16], uint8_t* staging,
+                                        int row, int in_tile, int rows, size_t pitch, int col0, uint8_t* scales, int block, int lane) {
+  uint32_t bytes = 0;                                  // lane i: scale of row i's first term, lane 16 + i: of its second
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float v = silu(__uint_as_float(g[i])) * __uint_as_float(u[i]);
+    const uint32_t b1 = mx4::term_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
+    const uint32_t b2 = mx4::second_scale(b1);
+    uint32_t c1, c2;
+    mx4::split2(v, 0.0f, mx4::inverse_scale(b1), mx4::scale_ratio(b1, b2), c1, c2);
+    staging[i * 32 + lane] = (uint8_t)c1;
+    staging[512 + i * 32 + lane] = (uint8_t)c2;
+    if ((lane & 15) == i) bytes = lane < 16 ? b1 : b2;
+  }
+  __syncwarp();
+  const int r = lane >> 1;                             // two lanes for each row
+  if (in_tile + r < rows) {
+    const size_t at = (size_t)(row + r) * pitch + col0 + 16 * (lane & 1);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      *reinterpret_cast<uint4*>(h.code[t] + at) = *reinterpret_cast<const uint4*>(staging + 512 * t + 16 * lane);
+  }
+  if (in_tile + (lane & 15) < rows)
+    scales[mx4::row_scale_at<kRows>(in_tile + (lane & 15), lane >> 4, rows) + block] = (uint8_t)bytes;
+  __syncwarp();
+}
+
+// 16 rows of y for a warp's 32 outputs, col0 the first
+__device__ __forceinline__ void store_y(__nv_bfloat16* __restrict__ y, const uint32_t (&v)[16], uint8_t* staging, int row, int in_tile,
+                                        int rows, int D, int col0, int lane) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    reinterpret_cast<__nv_bfloat16*>(staging)[i * 32 + lane] = __float2bfloat16_rn(__uint_as_float(v[i]));
+  __syncwarp();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int r = 8 * k + (lane >> 2), col = col0 + 8 * (lane & 3);      // four lanes for each row; D is a multiple of 8
+    if (in_tile + r < rows && col < D)
+      *reinterpret_cast<uint4*>(y + (size_t)(row + r) * D + col) = *reinterpret_cast<const uint4*>(staging + 512 * k + 16 * lane);
+  }
+  __syncwarp();
+}
+
+// ------------------------------------------------------------------------------------------- narrow
+template <int kRows_, bool kGateUp_, int kStages_>
+struct Narrow {
+  static constexpr int kRows = kRows_;                 // of a tile at most
   static constexpr bool kGateUp = kGateUp_;
   static constexpr int kStages = kStages_;
   static constexpr int kMats = kGateUp ? 2 : 1;        // weight matrices that share the rows
-  static constexpr int kBoxRows = 16;                  // rows of one TMA box
-  static constexpr int kABytes = mx4::kTile * mx4::kChunk;      // of shared memory; half of them are loaded
-  static constexpr int kALoaded = kABytes / 2;
-  static constexpr int kBBytes = kN * mx4::kChunk;
-  static constexpr int kScaleTiles = (kN + 127) / 128;          // 512-byte groups of a term's scales
-  static constexpr int kTermScaleBytes = kScaleTiles * mx4::kScaleTile;
-  static constexpr int kScaleOffset = kMats * kABytes + 2 * kBBytes;
-  static constexpr int kStageBytes = round_up(kScaleOffset + kMats * mx4::kScaleTile + 2 * kTermScaleBytes, 1024);
-  static constexpr int kScaleCols = 4 * kMats + 8 * kScaleTiles;
-  static constexpr int kAccCols = kMats * kN;
+  static constexpr int kCols = 2 * kRows;              // accumulator columns of a matrix: both terms
+  static constexpr int kABytes = kTile * kChunk;       // of shared memory; half of them are loaded
+  static constexpr int kBBytes = kCols * kChunk;
+  static constexpr int kScaleOffset = kMats * kABytes + kBBytes;
+  static constexpr int kStageBytes = round_up(kScaleOffset + (kMats + 1) * kScaleTile, 1024);
+  static constexpr int kScaleCols = 4 * (kMats + 1);
+  static constexpr int kAccCols = kMats * kCols;
   static constexpr int kColsUsed = 2 * kAccCols + kStages * kScaleCols;
   static constexpr int kTmemCols = kColsUsed <= 128 ? 128 : kColsUsed <= 256 ? 256 : 512;
-  static constexpr int kThreads = 256;
-  // the loader of the rows' scales runs this many stages ahead of what it hands over
-  static constexpr int kScaleLag = kStages - 1 < 3 ? kStages - 1 : 3;
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + sizeof(Tables) + 256;
-  static_assert(kN % 16 == 0 && kN <= 256 && kColsUsed <= 512 && kSmem <= 227 * 1024 && kStages >= 2, "does not fit");
+  static constexpr int kThreads = 192;                 // loads, MMAs, four epilogue warps
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + sizeof(Tables) + 256 + 4 * kStaging;
+  static_assert(kRows % 16 == 0 && kCols <= 128 && kColsUsed <= 512 && kSmem <= 227 * 1024, "does not fit");
 };
 
-struct Operands {
-  const uint8_t* w_scale[2];        // gate, up; or down
-  const uint32_t* row_scale[2];     // the two terms
-  int pitch;                        // words of a chunk of row_scale
+struct Weights {
+  const uint8_t* scale[2];          // gate, up; or down
 };
 
-__device__ __forceinline__ float silu(float g) { return __fdividef(g, 1.0f + __expf(-g)); }
+// What a block does of all K steps, [begin, end) of the tiles one after the other, and who shares a tile with it.
+struct Share {
+  int64_t steps;                    // of all tiles
+  int blocks;                       // that have any
+  int64_t begin, end;
+  __device__ Share(int64_t steps_, int grid, int block) : steps(steps_), blocks((int)min((int64_t)grid, steps_)) {
+    begin = end = 0;
+    if (block < blocks) {
+      begin = steps * block / blocks;
+      end = steps * (block + 1) / blocks;
+    }
+  }
+  // the block that has step p: the last one that begins at or before it
+  __device__ int owner(int64_t p) const { return (int)(((p + 1) * blocks - 1) / steps); }
+};
 
-// kGateUp: h = silu(g) u as two terms into `h`; otherwise y = accumulator into `y` [rcap, n_dim].
 template <class Cfg>
 __global__ void __launch_bounds__(Cfg::kThreads, 1)
-product4_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ CUtensorMap tm_w1,
-                const __grid_constant__ CUtensorMap tm_r0, const __grid_constant__ CUtensorMap tm_r1, const Operands op,
-                const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert, int S, int E, int n_dim, int k_dim,
-                int rcap, const mx4::Rows h, __nv_bfloat16* __restrict__ y, int32_t* __restrict__ status) {
-  constexpr int kStages = Cfg::kStages, kN = Cfg::kN, kMats = Cfg::kMats;
+narrow_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ CUtensorMap tm_w1,
+              const __grid_constant__ CUtensorMap tm_r0, const __grid_constant__ CUtensorMap tm_r1, const Weights w,
+              const uint8_t* __restrict__ row_scale, const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert,
+              int S, int E, int n_dim, int k_dim, int rcap, const mx4::Rows h, __nv_bfloat16* __restrict__ y,
+              int32_t* __restrict__ arrived, float* __restrict__ partial, int32_t* __restrict__ status) {
+  constexpr int kStages = Cfg::kStages, kRows = Cfg::kRows, kMats = Cfg::kMats;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   Tables& tb = *reinterpret_cast<Tables*>(smem + (size_t)kStages * Cfg::kStageBytes);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)kStages * Cfg::kStageBytes + sizeof(Tables));
-  uint64_t* full = bars;                     // [kStages]  loaders -> MMA
-  uint64_t* empty = bars + kStages;          // [kStages]  MMA -> loaders
+  uint64_t* full = bars;                     // [kStages]  loads -> MMA
+  uint64_t* empty = bars + kStages;          // [kStages]  MMA -> loads
   uint64_t* acc_full = bars + 2 * kStages;   // [2]  MMA -> epilogue
   uint64_t* acc_empty = acc_full + 2;        // [2]  epilogue -> MMA
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* is_last = abort_flag + 1;
+  static_assert((2 * kStages + 4) * 8 + 12 <= 256, "barriers fit their space");
 
   const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
   const int m_tiles = mx4::tiles_of(n_dim), chunks = mx4::chunks_of(k_dim);
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 2); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); }
     *abort_flag = 0;
     fence_mbar_init();
     prefetch_tensormap(&tm_w0);
-    prefetch_tensormap(&tm_w1);
+    if (kMats == 2) prefetch_tensormap(&tm_w1);
     prefetch_tensormap(&tm_r0);
     prefetch_tensormap(&tm_r1);
   }
@@ -166,24 +273,27 @@ product4_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant
     tmem_alloc(tmem_slot, Cfg::kTmemCols);
     tmem_relinquish();
   }
-  build_tables<Cfg::kThreads, kN>(tb, slot_row_off, slot_expert, S, E, m_tiles, rcap, status);
+  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status);
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  const int total_tiles = tb.tile_base[S];
+  const Share share((int64_t)tb.tile_base[S] * m_tiles * chunks, gridDim.x, blockIdx.x);
 
   if (warp == 0) {
     if (lane == 0) {
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
-        const TileCoord tc = decode_tile<kN>(tb, slot_row_off, slot_expert, S, tile, m_tiles);
-        const int boxes = (min(kN, tc.row_end - tc.m0) + Cfg::kBoxRows - 1) / Cfg::kBoxRows;
-        const uint32_t bytes = kMats * (Cfg::kALoaded + mx4::kScaleTile) + 2 * boxes * Cfg::kBoxRows * mx4::kChunk;
-        const size_t scale_at = ((size_t)tc.expert * m_tiles + tc.n_tile) * chunks * mx4::kScaleTile;
-        for (int c = 0; c < chunks; ++c) {
+      for (int64_t p = share.begin; ok && p < share.end;) {
+        const int64_t t = p / chunks;
+        const int k0 = (int)(p - t * chunks), k1 = (int)min((int64_t)chunks, k0 + share.end - p);
+        const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+        const int padded = round_up(tc.rows, 16);
+        const uint32_t bytes = kMats * (Cfg::kABytes / 2 + kScaleTile) + 2 * padded * kChunk + kScaleTile;
+        const size_t scale_at = ((size_t)tc.expert * m_tiles + tc.m) * chunks * kScaleTile;
+        const uint8_t* rows_at = row_scale + (size_t)tc.row_tile * chunks * kScaleTile;
+        for (int c = k0; c < k1; ++c) {
           if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag)) { ok = false; break; }
           uint8_t* a = smem + (size_t)stage * Cfg::kStageBytes;
           uint8_t* b = a + kMats * Cfg::kABytes;
@@ -191,93 +301,51 @@ product4_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant
           mbar_arrive_expect_tx(&full[stage], bytes);
 #pragma unroll
           for (int m = 0; m < kMats; ++m) {
-            tma_load_3d(a + m * Cfg::kABytes, m ? &tm_w1 : &tm_w0, &full[stage], c * mx4::kChunk, tc.n_tile * mx4::kTile,
-                        tc.expert);
-            bulk_load(sc + m * mx4::kScaleTile, op.w_scale[m] + scale_at + (size_t)c * mx4::kScaleTile, mx4::kScaleTile,
-                      &full[stage]);
+            tma_load_3d(a + m * Cfg::kABytes, m ? &tm_w1 : &tm_w0, &full[stage], c * kChunk, tc.m * kTile, tc.expert);
+            bulk_load(sc + m * kScaleTile, w.scale[m] + scale_at + (size_t)c * kScaleTile, kScaleTile, &full[stage]);
           }
-          for (int i = 0; i < boxes; ++i) {
-            const int r = i * Cfg::kBoxRows;
-            tma_load_2d(b + r * mx4::kChunk, &tm_r0, &full[stage], c * mx4::kChunk, tc.m0 + r);
-            tma_load_2d(b + Cfg::kBBytes + r * mx4::kChunk, &tm_r1, &full[stage], c * mx4::kChunk, tc.m0 + r);
+          for (int r = 0; r < padded; r += 16) {
+            tma_load_2d(b + r * kChunk, &tm_r0, &full[stage], c * kChunk, tc.row0 + r);
+            tma_load_2d(b + (padded + r) * kChunk, &tm_r1, &full[stage], c * kChunk, tc.row0 + r);
           }
+          bulk_load(sc + kMats * kScaleTile, rows_at + (size_t)c * kScaleTile, kScaleTile, &full[stage]);
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
+        p += k1 - k0;
       }
-      if (!ok) {
-        for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // let copies in flight land before the block retires
-      }
+      if (!ok) linger();
     }
-  } else if (warp == 2) {
-    constexpr int kLag = Cfg::kScaleLag;
-    int stage = 0, pending = 0, done = 0;      // copies issued and not handed over; stage of the next one to hand over
-    uint32_t phase = 0;
-    bool ok = true;
-    auto hand_over = [&]() {                   // the copies of stage `done` have landed in this thread's view
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&full[done]);
-      done = done + 1 == kStages ? 0 : done + 1;
-      --pending;
-    };
-    for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
-      const TileCoord tc = decode_tile<kN>(tb, slot_row_off, slot_expert, S, tile, m_tiles);
-      const int rows = min(kN, tc.row_end - tc.m0);
-      for (int c = 0; c < chunks; ++c) {
-        if (!__all_sync(0xffffffffu, mbar_wait(&empty[stage], phase ^ 1u, abort_flag))) { ok = false; break; }
-        const uint32_t dst = smem_u32(smem + (size_t)stage * Cfg::kStageBytes + Cfg::kScaleOffset + kMats * mx4::kScaleTile);
-        const size_t src = (size_t)c * op.pitch + tc.m0;
-        for (int r = lane; r < round_up(rows, 32); r += 32) {
-          const uint32_t at = dst + (r / 128) * mx4::kScaleTile + mx4::scale_byte_at(r % 128);
-          const size_t from = src + (r < rows ? r : 0);
-          copy_async4(at, op.row_scale[0] + from, r < rows ? 4 : 0);
-          copy_async4(at + Cfg::kTermScaleBytes, op.row_scale[1] + from, r < rows ? 4 : 0);
-        }
-        copy_async_commit();
-        ++pending;
-        if (pending > kLag) {
-          copy_async_wait<kLag>();
-          hand_over();
-        }
-        if (++stage == kStages) { stage = 0; phase ^= 1u; }
-      }
-    }
-    copy_async_wait<0>();
-    while (pending > 0) hand_over();
   } else if (warp == 1) {
     const uint32_t ring = smem_u32(smem);
     const uint32_t scale_cols = tmem_base + 2 * Cfg::kAccCols;
     int stage = 0, acc = 0;
     uint32_t phase = 0, acc_phase = 0;
     bool ok = true;
-    for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
-      const TileCoord tc = decode_tile<kN>(tb, slot_row_off, slot_expert, S, tile, m_tiles);
-      const uint32_t idesc = idesc_mx_e2m1_e4m3(mx4::kTile, round_up(min(kN, tc.row_end - tc.m0), 16));
-      if (!warp_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag)) { ok = false; break; }
+    for (int64_t p = share.begin; ok && p < share.end;) {
+      const int64_t t = p / chunks;
+      const int k0 = (int)(p - t * chunks), k1 = (int)min((int64_t)chunks, k0 + share.end - p);
+      const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+      const uint32_t idesc = idesc_mx_e2m1_e4m3(kTile, 2 * round_up(tc.rows, 16));
+      if (!warp_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag)) break;
       tc_fence_after_sync();
       const uint32_t d = tmem_base + (uint32_t)acc * Cfg::kAccCols;
-      for (int c = 0; c < chunks; ++c) {
+      for (int c = k0; c < k1; ++c) {
         if (!warp_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
         const uint32_t a = ring + (uint32_t)stage * Cfg::kStageBytes;
         const uint32_t sc = a + Cfg::kScaleOffset;
-        const uint64_t da = smem_desc_k_sw128(a);
-        const uint64_t db = smem_desc_k_sw128(a + kMats * Cfg::kABytes);
-        const uint32_t ts = scale_cols + (uint32_t)stage * Cfg::kScaleCols;
+        const uint64_t da = smem_desc_k_sw128(a), db = smem_desc_k_sw128(a + kMats * Cfg::kABytes);
+        const uint32_t ts = scale_cols + (uint32_t)stage * Cfg::kScaleCols;     // (the ring frees a stage's columns with it)
         if (elect_one()) {
 #pragma unroll
-          for (int i = 0; i < kMats + 2 * Cfg::kScaleTiles; ++i)
-            copy_scales(ts + 4 * i, smem_desc_scales(sc + i * mx4::kScaleTile));
+          for (int i = 0; i < kMats + 1; ++i) copy_scales(ts + 4 * i, smem_desc_scales(sc + i * kScaleTile));
 #pragma unroll
-          for (int j = 0; j < mx4::kChunk / mx4::kBlock; ++j) {
+          for (int m = 0; m < kMats; ++m) {
 #pragma unroll
-            for (int m = 0; m < kMats; ++m) {
-#pragma unroll
-              for (int t = 0; t < 2; ++t)
-                mma_mx(d + m * kN, da + (uint64_t)((m * Cfg::kABytes + j * mx4::kBlock) >> 4),
-                       db + (uint64_t)((t * Cfg::kBBytes + j * mx4::kBlock) >> 4), idesc | idesc_mx_block(j), ts + 4 * m,
-                       ts + 4 * kMats + 4 * Cfg::kScaleTiles * t, (c | j | t) != 0);
-            }
+            for (int j = 0; j < kChunk / mx4::kBlock; ++j)
+              mma_mx(d + m * Cfg::kCols, da + (uint64_t)((m * Cfg::kABytes + j * mx4::kBlock) >> 4),
+                     db + (uint64_t)((j * mx4::kBlock) >> 4), idesc | idesc_mx_block(j), ts + 4 * m, ts + 4 * kMats,
+                     (c - k0) | j);
           }
           mma_commit(&empty[stage]);
         }
@@ -287,50 +355,53 @@ product4_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant
       if (elect_one()) mma_commit(&acc_full[acc]);
       acc ^= 1;
       if (acc == 0) acc_phase ^= 1u;
+      p += k1 - k0;
     }
-    if (!ok) {
-      for (int i = 0; i < 1000; ++i) __nanosleep(1000);
-    }
-  } else if (warp >= 4) {
-    const int quarter = warp & 3;
-    const int k_pitch = m_tiles * mx4::kChunk;         // bytes of a row of h
+    if (*abort_flag) linger();
+  } else {
+    const int quarter = warp & 3, thread = quarter * 32 + lane;
+    uint8_t* staging = smem + (size_t)kStages * Cfg::kStageBytes + sizeof(Tables) + 256 + quarter * kStaging;
+    const size_t h_pitch = (size_t)m_tiles * kChunk;
     int acc = 0;
     uint32_t acc_phase = 0;
-    for (int tile = blockIdx.x; tile < total_tiles; tile += gridDim.x) {
-      const TileCoord tc = decode_tile<kN>(tb, slot_row_off, slot_expert, S, tile, m_tiles);
-      const int rows = min(kN, tc.row_end - tc.m0);
-      if (!mbar_wait(&acc_full[acc], acc_phase, abort_flag, 64)) break;
+    bool ok = true;                  // a warp whose wait ran out still meets the others at every barrier below
+    for (int64_t p = share.begin; p < share.end;) {
+      const int64_t t = p / chunks;
+      const int k0 = (int)(p - t * chunks), k1 = (int)min((int64_t)chunks, k0 + share.end - p);
+      const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+      const int padded = round_up(tc.rows, 16);
+      const bool whole = k1 - k0 == chunks;
+      const int first = whole ? 0 : share.owner(t * chunks), last = whole ? 0 : share.owner((t + 1) * chunks - 1);
+      // a block's unfinished tiles: the one that it begins and does not end, and the one that another block began
+      auto part = [&](int block) { return partial + ((size_t)2 * block + (block == first)) * kMats * kRows * kTile; };
+      const int col0 = tc.m * kTile + quarter * 32;    // this warp's first output
+      uint8_t* scales = h.scale + ((size_t)tc.row_tile * m_tiles + tc.m) * kScaleTile;
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, 64));
       tc_fence_after_sync();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * Cfg::kAccCols;
-      const int out = tc.n_tile * mx4::kTile + quarter * 32 + lane;        // this thread's output
-      for (int c0 = 0; c0 < rows; c0 += 16) {
-        uint32_t g[16];
-        tmem_ld16(taddr + c0, g);
-        if constexpr (Cfg::kGateUp) {
-          uint32_t u[16];
-          tmem_ld16(taddr + kN + c0, u);
-          tmem_ld_wait();
+      for (int r = 0; ok && r < tc.rows; r += 16) {
+        uint32_t v[kMats][16], second[kMats][16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            if (c0 + i < rows) {                       // the same for the whole warp
-              const float v = silu(__uint_as_float(g[i])) * __uint_as_float(u[i]);
-              const uint32_t b1 = mx4::term_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
-              const uint32_t b2 = mx4::second_scale(b1);
-              uint32_t c1, c2;
-              mx4::split2(v, 0.0f, mx4::inverse_scale(b1), mx4::scale_ratio(b1, b2), c1, c2);
-              const size_t row = tc.m0 + c0 + i;
-              h.code[0][row * k_pitch + out] = (uint8_t)c1;
-              h.code[1][row * k_pitch + out] = (uint8_t)c2;
-              if (lane < 2)
-                reinterpret_cast<uint8_t*>(h.scale[lane] + (size_t)tc.n_tile * op.pitch + row)[quarter] = (uint8_t)(lane ? b2 : b1);
-            }
-          }
+        for (int m = 0; m < kMats; ++m) {
+          tmem_ld16(taddr + m * Cfg::kCols + r, v[m]);
+          tmem_ld16(taddr + m * Cfg::kCols + padded + r, second[m]);
+        }
+        tmem_ld_wait();
+#pragma unroll
+        for (int m = 0; m < kMats; ++m)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[m][i] = __float_as_uint(__uint_as_float(v[m][i]) + __uint_as_float(second[m][i]));
+        if (!whole) {
+          float* to = part(blockIdx.x);
+#pragma unroll
+          for (int m = 0; m < kMats; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (r + i < tc.rows) __stcg(to + (m * kRows + r + i) * kTile + thread, __uint_as_float(v[m][i]));
+        } else if constexpr (Cfg::kGateUp) {
+          store_h<kRows>(h, v[0], v[kMats - 1], staging, tc.row0 + r, r, tc.rows, h_pitch, col0, scales, quarter, lane);
         } else {
-          tmem_ld_wait();
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (c0 + i < rows && out < n_dim)
-              y[(size_t)(tc.m0 + c0 + i) * n_dim + out] = __float2bfloat16_rn(__uint_as_float(g[i]));
+          store_y(y, v[0], staging, tc.row0 + r, r, tc.rows, n_dim, col0, lane);
         }
       }
       tc_fence_before_sync();
@@ -338,6 +409,38 @@ product4_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant
       if (lane == 0) mbar_arrive(&acc_empty[acc]);
       acc ^= 1;
       if (acc == 0) acc_phase ^= 1u;
+      if (!whole) {
+        // the block that comes last adds the parts up, in the order of the blocks
+        __threadfence();
+        named_sync(1, 128);
+        if (thread == 0) *is_last = !*abort_flag && atomicAdd(&arrived[first], 1) == last - first;
+        named_sync(1, 128);
+        if (*is_last) {
+          __threadfence();
+          for (int r = 0; r < tc.rows; r += 16) {
+            uint32_t v[kMats][16];
+#pragma unroll
+            for (int m = 0; m < kMats; ++m)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) v[m][i] = 0;
+            for (int b = first; b <= last; ++b) {
+              const float* from = part(b);
+#pragma unroll
+              for (int m = 0; m < kMats; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                  if (r + i < tc.rows)
+                    v[m][i] = __float_as_uint(__uint_as_float(v[m][i]) + __ldcg(from + (m * kRows + r + i) * kTile + thread));
+            }
+            if constexpr (Cfg::kGateUp)
+              store_h<kRows>(h, v[0], v[kMats - 1], staging, tc.row0 + r, r, tc.rows, h_pitch, col0, scales, quarter, lane);
+            else
+              store_y(y, v[0], staging, tc.row0 + r, r, tc.rows, n_dim, col0, lane);
+          }
+        }
+        named_sync(1, 128);                            // is_last is read before it is written again
+      }
+      p += k1 - k0;
     }
   }
 
@@ -351,23 +454,381 @@ product4_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant
   }
 }
 
+// ------------------------------------------------------------------------------------------- wide
+// A pair of CTAs works 256 weight rows x up to 224 rows of a slot; each CTA loads its 128 weight rows and half of the slot's
+// rows.  Gate + up: a CTA's 128 weight rows are 64 gate rows and the 64 up rows of the same outputs, so that a tile needs
+// 224 accumulator columns and not twice that, and two tiles fit tensor memory; in the epilogue the warps of the gate's
+// lanes and of the up's exchange half of their values through shared memory.
+// Shared memory is what feeds the MMAs: one of 224 columns takes 112 clocks and reads 128 + 112 rows of 32 bytes, 60 clocks
+// of shared memory's 128 bytes; the loads write 44 KB for eight of them, 352 clocks of 896.  (One CTA by itself reads all 224 rows, and
+// at 112 columns for each of two accumulators it was 60 clocks of reads for 56 of products: 0.99 PFLOP/s for gate + up, 0.65
+// for down, on 16384 tokens x 4096, F 14336, 8 experts.)
+template <bool kGateUp_>
+struct Wide {
+  static constexpr bool kGateUp = kGateUp_;
+  static constexpr int kRows = 224, kStages = 4;
+  static constexpr int kABytes = kTile * kChunk;       // half of them are loaded
+  static constexpr int kBBytes = kRows / 2 * kChunk;   // of a term
+  static constexpr int kRowScales = mx4::kRowScaleBytes<kRows>;
+  static constexpr int kScaleOffset = kABytes + 2 * kBBytes;             // rows' scales, (down) weights' scales
+  static constexpr int kStageBytes = round_up(kScaleOffset + kRowScales + (kGateUp ? 0 : kScaleTile), 1024);
+  // (gate + up) the weights' scales have a ring of their own, kGroup chunks at a time
+  static constexpr int kGroup = 4, kGroups = kGateUp ? 4 : 0;
+  static constexpr int kGroupBytes = kGroup * kScaleTile;
+  static constexpr int kScaleCols = 4 + 4 * kRowScales / kScaleTile;
+  static constexpr int kScaleBufs = 3;                 // tensor memory has no room for four
+  static constexpr int kOutputs = kGateUp ? 128 : 256; // of a pair's tile
+  static constexpr int kExchange = kGateUp ? 4 * 2 * 16 * 32 * 4 : 0;     // two buffers of 16 x 32 fp32 for each epilogue warp
+  static constexpr int kThreads = 256;
+  static constexpr size_t kSmem =
+      1024 + (size_t)kStages * kStageBytes + kGroups * kGroupBytes + kExchange + sizeof(Tables) + 256 + 4 * kStaging;
+  static constexpr int kBigBox = kRows / 2;            // rows of a TMA box where a CTA has more than half as many, else 16
+  static_assert(2 * kRows + kScaleBufs * kScaleCols <= 512 && kSmem <= 227 * 1024, "does not fit");
+};
+
 template <class Cfg>
-int launch_product(moegps_ctx* ctx, const CUtensorMap& w0, const CUtensorMap& w1, const CUtensorMap& r0, const CUtensorMap& r1,
-                   const Operands& op, const int32_t* slot_row_off, const int32_t* slot_expert, int n_dim, int k_dim,
-                   const mx4::Rows& h, void* y, cudaStream_t st) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Cfg::kThreads, 1)
+wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ CUtensorMap tm_w1,
+            const __grid_constant__ CUtensorMap tm_r0, const __grid_constant__ CUtensorMap tm_r1,
+            const __grid_constant__ CUtensorMap tm_big0, const __grid_constant__ CUtensorMap tm_big1,
+            const __grid_constant__ CUtensorMap tm_ws, const __grid_constant__ CUtensorMap tm_rs, const Weights w,
+            const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert, int S, int E, int n_dim, int k_dim,
+            int rcap, const mx4::Rows h, __nv_bfloat16* __restrict__ y, int32_t* __restrict__ status) {
+  constexpr int kStages = Cfg::kStages, kRows = Cfg::kRows;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* w_scales = smem + (size_t)kStages * Cfg::kStageBytes;
+  float* exchange = reinterpret_cast<float*>(w_scales + Cfg::kGroups * Cfg::kGroupBytes);
+  Tables& tb = *reinterpret_cast<Tables*>(reinterpret_cast<uint8_t*>(exchange) + Cfg::kExchange);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(&tb) + sizeof(Tables));
+  uint64_t* full = bars;                     // [kStages]  both CTAs' loads -> MMA, on the leader
+  uint64_t* empty = bars + kStages;          // [kStages]  MMA -> loads, in both
+  uint64_t* acc_full = bars + 2 * kStages;   // [2]  MMA -> epilogue, in both
+  uint64_t* acc_empty = acc_full + 2;        // [2]  both epilogues -> MMA, on the leader
+  uint64_t* scales_full = acc_empty + 2;               // [kGroups]  both CTAs' copies -> MMA, on the leader
+  uint64_t* scales_empty = scales_full + Cfg::kGroups; // [kGroups]  MMA -> copies, in both
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(scales_empty + Cfg::kGroups);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  static_assert((2 * kStages + 4 + 2 * Cfg::kGroups) * 8 + 8 <= 256, "barriers fit their space");
+
+  const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
+  const int rank = (int)cluster_ctarank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int m_tiles = (n_dim + Cfg::kOutputs - 1) / Cfg::kOutputs, chunks = mx4::chunks_of(k_dim);
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < Cfg::kGroups; ++i) { mbar_init(&scales_full[i], 2); mbar_init(&scales_empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 8); }
+    *abort_flag = 0;
+    fence_mbar_init();
+    prefetch_tensormap(&tm_w0);
+    prefetch_tensormap(&tm_w1);
+    prefetch_tensormap(&tm_r0);
+    prefetch_tensormap(&tm_r1);
+    prefetch_tensormap(&tm_ws);
+    prefetch_tensormap(&tm_rs);
+  }
+  launch_dependents();
+  wait_for_predecessor();
+  if (warp == 1) {
+    tmem_alloc_pair(tmem_slot, 512);
+    tmem_relinquish_pair();
+  }
+  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status);
+  __syncwarp();
+  tc_fence_before_sync();
+  cluster_sync_all();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  const int64_t total = (int64_t)tb.tile_base[S] * m_tiles;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      const uint32_t leader_full = map_to_cta(smem_u32(full), 0);
+      for (int64_t t = pair; ok && t < total; t += pairs) {
+        const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+        const int half = round_up(tc.rows, 32) / 2, row0 = tc.row0 + rank * half;
+        const bool big = half > Cfg::kBigBox / 2;
+        const uint32_t bytes = 2 * (Cfg::kABytes / 2 + 2 * (big ? Cfg::kBigBox : half) * kChunk + Cfg::kRowScales + (Cfg::kGateUp ? 0 : kScaleTile));
+        const int out0 = tc.m * Cfg::kOutputs + rank * (Cfg::kOutputs / 2);
+        // (down) rows of 128 bytes of the weights' scales; outputs behind the last tile meet zero weights, whatever their scales
+        const int ws0 = ((tc.expert * mx4::tiles_of(n_dim) + out0 / kTile) * chunks) * (kScaleTile / 128);
+        const int rs0 = tc.row_tile * chunks * (Cfg::kRowScales / 128);
+        for (int c = 0; c < chunks; ++c) {
+          if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag)) { ok = false; break; }
+          uint8_t* a = smem + (size_t)stage * Cfg::kStageBytes;
+          uint8_t* b = a + Cfg::kABytes;
+          uint8_t* sc = a + Cfg::kScaleOffset;
+          if (rank == 0) mbar_arrive_expect_tx(&full[stage], bytes);
+          const uint32_t to = leader_full + stage * 8;
+          if constexpr (Cfg::kGateUp) {
+            tma_load_3d_pair(a, &tm_w0, to, c * kChunk, out0, tc.expert);
+            tma_load_3d_pair(a + Cfg::kABytes / 2, &tm_w1, to, c * kChunk, out0, tc.expert);
+          } else {
+            tma_load_3d_pair(a, &tm_w0, to, c * kChunk, out0, tc.expert);
+            tma_load_2d_pair(sc + Cfg::kRowScales, &tm_ws, to, 0, ws0 + c * (kScaleTile / 128));
+          }
+          if (big) {
+            tma_load_2d_pair(b, &tm_big0, to, c * kChunk, row0);
+            tma_load_2d_pair(b + Cfg::kBBytes, &tm_big1, to, c * kChunk, row0);
+          }
+          for (int r = big ? half : 0; r < half; r += 16) {
+            tma_load_2d_pair(b + r * kChunk, &tm_r0, to, c * kChunk, row0 + r);
+            tma_load_2d_pair(b + Cfg::kBBytes + r * kChunk, &tm_r1, to, c * kChunk, row0 + r);
+          }
+          tma_load_2d_pair(sc, &tm_rs, to, 0, rs0 + c * (Cfg::kRowScales / 128));
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (!ok) linger();
+    }
+  } else if (Cfg::kGateUp && warp == 2) {
+    // scales of 64 gate rows and 64 up rows: 8 of the 16 bytes of each lane, of either matrix.  Some twelve chunks ahead of the
+    // products and four at a time: what a step costs here (a wait, a proxy fence, an arrival) would hold up each of theirs (gate
+    // + up on 16384 tokens 9.1 ms with these copies as part of a stage, 6.2 without them).
+    constexpr int kAhead = Cfg::kGroups - 2;           // groups under way when one is handed over
+    int group = 0, pending = 0, done = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    const uint32_t leader_full = map_to_cta(smem_u32(scales_full), 0);
+    auto hand_over = [&]() {
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_remote(leader_full + done * 8);
+      if (++done == Cfg::kGroups) done = 0;
+      --pending;
+    };
+    for (int64_t t = pair; ok && t < total; t += pairs) {
+      const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+      const size_t at = ((size_t)tc.expert * m_tiles + tc.m) * chunks * kScaleTile + 16 * lane + 8 * rank;
+      for (int c = 0; c < chunks; c += Cfg::kGroup) {
+        if (!__all_sync(0xffffffffu, mbar_wait(&scales_empty[group], phase ^ 1u, abort_flag))) { ok = false; break; }
+        const uint32_t to = smem_u32(w_scales + group * Cfg::kGroupBytes) + 16 * lane;
+#pragma unroll
+        for (int i = 0; i < Cfg::kGroup; ++i) {
+          if (c + i < chunks) {
+            copy_async8(to + i * kScaleTile, w.scale[0] + at + (size_t)(c + i) * kScaleTile);
+            copy_async8(to + i * kScaleTile + 8, w.scale[1] + at + (size_t)(c + i) * kScaleTile);
+          }
+        }
+        copy_async_commit();
+        if (++pending > kAhead) {
+          copy_async_wait<kAhead>();
+          hand_over();
+        }
+        if (++group == Cfg::kGroups) { group = 0; phase ^= 1u; }
+      }
+    }
+    copy_async_wait<0>();
+    while (pending > 0) hand_over();
+  } else if (warp == 1) {
+    if (rank == 0) {
+      const uint32_t ring = smem_u32(smem);
+      const uint32_t scale_cols = tmem_base + 2 * kRows;
+      int stage = 0, acc = 0, buf = 0, group = 0;
+      uint32_t phase = 0, acc_phase = 0, group_phase = 0;
+      int64_t step = 0;
+      bool ok = true;
+      for (int64_t t = pair; ok && t < total; t += pairs) {
+        const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+        const uint32_t idesc = idesc_mx_e2m1_e4m3(2 * kTile, round_up(tc.rows, 32));
+        if (!warp_wait_cluster(&acc_empty[acc], acc_phase ^ 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after_sync();
+        const uint32_t d = tmem_base + (uint32_t)acc * kRows;
+        for (int c = 0; c < chunks; ++c, ++step) {
+          // the scale columns of three steps ago are free when that step's MMAs are done
+          if (step >= Cfg::kScaleBufs) {
+            const int64_t old = step - Cfg::kScaleBufs;
+            if (!warp_wait(&empty[old % kStages], (uint32_t)(old / kStages) & 1u, abort_flag)) { ok = false; break; }
+          }
+          if (Cfg::kGateUp && c % Cfg::kGroup == 0 && !warp_wait_cluster(&scales_full[group], group_phase, abort_flag)) {
+            ok = false;
+            break;
+          }
+          if (!warp_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
+          tc_fence_after_sync();
+          const uint32_t a = ring + (uint32_t)stage * Cfg::kStageBytes;
+          const uint32_t sc = a + Cfg::kScaleOffset;
+          const uint32_t wsc =
+              Cfg::kGateUp ? smem_u32(w_scales) + group * Cfg::kGroupBytes + (c % Cfg::kGroup) * kScaleTile : sc + Cfg::kRowScales;
+          const uint64_t da = smem_desc_k_sw128(a), db = smem_desc_k_sw128(a + Cfg::kABytes);
+          const uint32_t ts = scale_cols + (uint32_t)buf * Cfg::kScaleCols;
+          const bool group_end = Cfg::kGateUp && (c % Cfg::kGroup == Cfg::kGroup - 1 || c == chunks - 1);
+          if (elect_one()) {
+            copy_scales_pair(ts, smem_desc_scales(wsc));
+#pragma unroll
+            for (int i = 0; i < Cfg::kRowScales / kScaleTile; ++i)
+              copy_scales_pair(ts + 4 + 4 * i, smem_desc_scales(sc + i * kScaleTile));
+#pragma unroll
+            for (int j = 0; j < kChunk / mx4::kBlock; ++j) {
+#pragma unroll
+              for (int term = 0; term < 2; ++term)
+                mma_mx_pair(d, da + (uint64_t)((j * mx4::kBlock) >> 4), db + (uint64_t)((term * Cfg::kBBytes + j * mx4::kBlock) >> 4),
+                            idesc | idesc_mx_block(j), ts, ts + 4 + 8 * term, (c | j | term) != 0);
+            }
+            mma_commit_pair(&empty[stage]);
+            if (group_end) mma_commit_pair(&scales_empty[group]);
+          }
+          if (group_end && ++group == Cfg::kGroups) { group = 0; group_phase ^= 1u; }
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          if (++buf == Cfg::kScaleBufs) buf = 0;
+        }
+        if (!ok) break;
+        if (elect_one()) mma_commit_pair(&acc_full[acc]);
+        acc ^= 1;
+        if (acc == 0) acc_phase ^= 1u;
+      }
+      if (!ok) linger();
+    }
+  } else if (warp >= 4) {
+    const int quarter = warp & 3;
+    uint8_t* staging = reinterpret_cast<uint8_t*>(bars) + 256 + quarter * kStaging;
+    const uint32_t leader_empty = map_to_cta(smem_u32(acc_empty), 0);
+    int acc = 0, turn = 0;
+    uint32_t acc_phase = 0;
+    bool ok = true;                  // a warp whose wait ran out still meets its partner at every barrier below
+    for (int64_t t = pair; t < total; t += pairs) {
+      const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+      const int padded = round_up(tc.rows, 32);
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, 64));
+      tc_fence_after_sync();
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * kRows;
+      if constexpr (Cfg::kGateUp) {
+        const bool up = quarter >= 2;
+        const int block = rank * 2 + (quarter & 1);    // which 32 of the tile's 128 outputs
+        const int col0 = tc.m * kChunk + block * 32;
+        uint8_t* scales = h.scale + ((size_t)tc.row_tile * m_tiles + tc.m) * Cfg::kRowScales;
+        const int half = padded / 2;
+        for (int i = 0; i < half; i += 16) {
+          // the gate's warps finish the first half of the rows, the up's the second
+          const int mine = up ? half + i : i, other = up ? i : half + i;
+          uint32_t v[16], give[16], get[16];
+          if (ok) {
+            tmem_ld16(taddr + other, give);
+            tmem_ld16(taddr + mine, v);
+            tmem_ld_wait();
+          }
+          float* buffer = exchange + turn * 16 * 32 + lane;            // of warp 0; a warp has 2 * 16 * 32
+#pragma unroll
+          for (int j = 0; j < 16; ++j) buffer[quarter * 1024 + j * 32] = __uint_as_float(give[j]);
+          named_sync(1 + (quarter & 1), 64);           // (before a buffer is written again both have met here once more)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) get[j] = __float_as_uint(buffer[(quarter ^ 2) * 1024 + j * 32]);
+          turn ^= 1;
+          if (!ok) continue;
+          if (up)
+            store_h<kRows>(h, get, v, staging, tc.row0 + mine, mine, tc.rows, (size_t)m_tiles * kChunk, col0, scales, block, lane);
+          else
+            store_h<kRows>(h, v, get, staging, tc.row0 + mine, mine, tc.rows, (size_t)m_tiles * kChunk, col0, scales, block, lane);
+        }
+      } else {
+        const int col0 = tc.m * Cfg::kOutputs + rank * kTile + quarter * 32;
+        for (int r = 0; ok && r < tc.rows; r += 16) {
+          uint32_t v[16];
+          tmem_ld16(taddr + r, v);
+          tmem_ld_wait();
+          store_y(y, v, staging, tc.row0 + r, r, tc.rows, n_dim, col0, lane);
+        }
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_remote(leader_empty + acc * 8);
+      acc ^= 1;
+      if (acc == 0) acc_phase ^= 1u;
+    }
+  }
+
+  __syncwarp();
+  tc_fence_before_sync();
+  cluster_sync_all();                                  // nobody touches the other CTA's memory after this
+  if (threadIdx.x == 0 && *abort_flag) moegps_report(status, MOEGPS_ERR_TIMEOUT, (int)blockIdx.x);
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
+// ------------------------------------------------------------------------------------------- host
+struct Call {
+  const void* xp;
+  const int32_t *slot_row_off, *slot_expert;
+  const void *gate4, *up4, *down4;
+  Weights up_scale, down_scale;
+  __nv_bfloat16* yp;
+  uint8_t* workspace;
+  mx4::Layout l;
+  mx4::Rows x, h;
+};
+
+int tmap_failed(moegps_ctx* ctx) {
+  ctx->last_cuda_error = (int)cudaErrorInvalidValue;
+  return MOEGPS_ERR_CUDA;
+}
+
+template <int kRows>
+int launch_split(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   const moegps_shape_t& s = ctx->shape;
-  MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(product4_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
-  MOEGPS_CUDA_TRY(ctx, launch_after(product4_kernel<Cfg>, dim3(ctx->sm_count), Cfg::kThreads, Cfg::kSmem, st, w0, w1, r0, r1, op,
-                                    slot_row_off, slot_expert, s.S, s.E, n_dim, k_dim, (int)moegps_rcap_of(s), h,
-                                    static_cast<__nv_bfloat16*>(y), ctx->d_status));
-  MOEGPS_AFTER_LAUNCH(ctx, "rows=%d", Cfg::kN);
+  const int64_t units = (c.l.rows / kSplitRows + s.S) * ((mx4::chunks_of(s.D) * kChunk + kSplitCols - 1) / kSplitCols);
+  const int64_t resident = 8 * (int64_t)ctx->sm_count;
+  split_kernel<kRows><<<(unsigned)(units < resident ? units : resident), kSplitThreads, 0, st>>>(
+      static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert, s.S, s.E, s.D, (int)c.l.rows, c.x,
+      reinterpret_cast<int32_t*>(c.workspace + c.l.arrived), ctx->d_status);
+  MOEGPS_AFTER_LAUNCH(ctx, "rows=%d", kRows);
   return MOEGPS_OK;
 }
 
-mx4::Rows rows_at(void* workspace, size_t code, size_t code_bytes, size_t scale, size_t scale_bytes) {
-  uint8_t* w = static_cast<uint8_t*>(workspace);
-  return {{w + code, w + code + code_bytes},
-          {reinterpret_cast<uint32_t*>(w + scale), reinterpret_cast<uint32_t*>(w + scale + scale_bytes)}};
+template <class Cfg>
+int launch_narrow(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
+  const moegps_shape_t& s = ctx->shape;
+  const int n_dim = Cfg::kGateUp ? s.F : s.D, k_dim = Cfg::kGateUp ? s.D : s.F;
+  const int cols = mx4::chunks_of(k_dim) * kChunk;
+  const mx4::Rows& in = Cfg::kGateUp ? c.x : c.h;
+  CUtensorMap w0, w1, r0, r1;
+  if (!moegps_make_tmap_codes4(&w0, Cfg::kGateUp ? c.gate4 : c.down4, s.E, n_dim, cols, kTile) ||
+      !moegps_make_tmap_codes4(&w1, Cfg::kGateUp ? c.up4 : c.down4, s.E, n_dim, cols, kTile) ||
+      !moegps_make_tmap_bytes(&r0, in.code[0], c.l.rows, cols, 16, true) ||
+      !moegps_make_tmap_bytes(&r1, in.code[1], c.l.rows, cols, 16, true))
+    return tmap_failed(ctx);
+  MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(narrow_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
+  const int grid = ctx->sm_count < mx4::kMaxCtas ? ctx->sm_count : mx4::kMaxCtas;
+  MOEGPS_CUDA_TRY(ctx, launch_after(narrow_kernel<Cfg>, dim3(grid), Cfg::kThreads, Cfg::kSmem, st, w0, w1, r0, r1,
+                                    Cfg::kGateUp ? c.up_scale : c.down_scale, in.scale, c.slot_row_off, c.slot_expert, s.S, s.E, n_dim,
+                                    k_dim, (int)c.l.rows, c.h, c.yp,
+                                    reinterpret_cast<int32_t*>(c.workspace + c.l.arrived) + (Cfg::kGateUp ? 0 : mx4::kMaxCtas),
+                                    reinterpret_cast<float*>(c.workspace + c.l.partial), ctx->d_status));
+  MOEGPS_AFTER_LAUNCH(ctx, "rows=%d", Cfg::kRows);
+  return MOEGPS_OK;
+}
+
+template <class Cfg>
+int launch_wide(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
+  const moegps_shape_t& s = ctx->shape;
+  const int n_dim = Cfg::kGateUp ? s.F : s.D, k_dim = Cfg::kGateUp ? s.D : s.F;
+  const int chunks = mx4::chunks_of(k_dim), cols = chunks * kChunk;
+  const mx4::Rows& in = Cfg::kGateUp ? c.x : c.h;
+  const Weights& ws = Cfg::kGateUp ? c.up_scale : c.down_scale;
+  CUtensorMap w0, w1, r0, r1, big0, big1, wsm, rsm;
+  const int box = Cfg::kGateUp ? 64 : kTile;
+  if (!moegps_make_tmap_codes4(&w0, Cfg::kGateUp ? c.gate4 : c.down4, s.E, n_dim, cols, box) ||
+      !moegps_make_tmap_codes4(&w1, Cfg::kGateUp ? c.up4 : c.down4, s.E, n_dim, cols, box) ||
+      !moegps_make_tmap_bytes(&r0, in.code[0], c.l.rows, cols, 16, true) ||
+      !moegps_make_tmap_bytes(&r1, in.code[1], c.l.rows, cols, 16, true) ||
+      !moegps_make_tmap_bytes(&big0, in.code[0], c.l.rows, cols, Cfg::kBigBox, true) ||
+      !moegps_make_tmap_bytes(&big1, in.code[1], c.l.rows, cols, Cfg::kBigBox, true) ||
+      !moegps_make_tmap_bytes(&wsm, ws.scale[0], (uint64_t)s.E * mx4::tiles_of(n_dim) * chunks * (kScaleTile / 128), 128,
+                              kScaleTile / 128, false) ||
+      !moegps_make_tmap_bytes(&rsm, in.scale, (uint64_t)c.l.row_tiles * chunks * (Cfg::kRowScales / 128), 128,
+                              Cfg::kRowScales / 128, false))
+    return tmap_failed(ctx);
+  MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(wide_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
+  MOEGPS_CUDA_TRY(ctx, launch_after(wide_kernel<Cfg>, dim3(ctx->sm_count / 2 * 2), Cfg::kThreads, Cfg::kSmem, st, w0, w1, r0, r1,
+                                    big0, big1, wsm, rsm, ws, c.slot_row_off, c.slot_expert, s.S, s.E, n_dim, k_dim, (int)c.l.rows, c.h, c.yp,
+                                    ctx->d_status));
+  MOEGPS_AFTER_LAUNCH(ctx, "rows=%d", Cfg::kRows);
+  return MOEGPS_OK;
 }
 
 }  // namespace
@@ -375,42 +836,30 @@ mx4::Rows rows_at(void* workspace, size_t code, size_t code_bytes, size_t scale,
 int moegps_launch_expert_ffn4(moegps_ctx* ctx, const void* xp, const int32_t* slot_row_off, const int32_t* slot_expert,
                               const void* gate4, const void* up4, const void* down4, const void* gate4_scale, const void* up4_scale,
                               const void* down4_scale, void* yp, void* workspace, cudaStream_t st) {
-  const moegps_shape_t& s = ctx->shape;
-  const mx4::Layout l = mx4::layout_of(s);
-  const mx4::Rows x = rows_at(workspace, l.x_code, l.x_code_bytes, l.x_scale, l.x_scale_bytes);
-  const mx4::Rows h = rows_at(workspace, l.h_code, l.h_code_bytes, l.h_scale, l.h_scale_bytes);
-  const int dc = mx4::chunks_of(s.D) * mx4::kChunk, fc = mx4::chunks_of(s.F) * mx4::kChunk;
-  CUtensorMap tg, tu, td, tx[2], th[2];
-  bool ok = moegps_make_tmap_codes4(&tg, gate4, s.E, s.F, dc, mx4::kTile) && moegps_make_tmap_codes4(&tu, up4, s.E, s.F, dc, mx4::kTile) &&
-            moegps_make_tmap_codes4(&td, down4, s.E, s.D, fc, mx4::kTile);
-  for (int t = 0; t < 2; ++t)
-    ok = ok && moegps_make_tmap_bytes(&tx[t], x.code[t], l.rows, dc, 16) && moegps_make_tmap_bytes(&th[t], h.code[t], l.rows, fc, 16);
-  if (!ok) {
-    ctx->last_cuda_error = (int)cudaErrorInvalidValue;
-    return MOEGPS_ERR_CUDA;
+  Call c = {xp, slot_row_off, slot_expert, gate4, up4, down4,
+            {{static_cast<const uint8_t*>(gate4_scale), static_cast<const uint8_t*>(up4_scale)}},
+            {{static_cast<const uint8_t*>(down4_scale), nullptr}},
+            static_cast<__nv_bfloat16*>(yp), static_cast<uint8_t*>(workspace), mx4::layout_of(ctx->shape), {}, {}};
+  uint8_t* ws = c.workspace;
+  c.x = {{ws + c.l.x_code, ws + c.l.x_code + c.l.x_code_bytes}, ws + c.l.x_scale};
+  c.h = {{ws + c.l.h_code, ws + c.l.h_code + c.l.h_code_bytes}, ws + c.l.h_scale};
+  int rc = MOEGPS_OK;
+  switch (c.l.cut) {
+    case mx4::Cut::k16:
+      rc = launch_split<16>(ctx, c, st);
+      if (rc == MOEGPS_OK) rc = launch_narrow<Narrow<16, true, 5>>(ctx, c, st);
+      if (rc == MOEGPS_OK) rc = launch_narrow<Narrow<16, false, 10>>(ctx, c, st);
+      return rc;
+    case mx4::Cut::k48:
+      rc = launch_split<48>(ctx, c, st);
+      if (rc == MOEGPS_OK) rc = launch_narrow<Narrow<48, true, 4>>(ctx, c, st);
+      if (rc == MOEGPS_OK) rc = launch_narrow<Narrow<48, false, 7>>(ctx, c, st);
+      return rc;
+    case mx4::Cut::k224:
+      rc = launch_split<224>(ctx, c, st);
+      if (rc == MOEGPS_OK) rc = launch_wide<Wide<true>>(ctx, c, st);
+      if (rc == MOEGPS_OK) rc = launch_wide<Wide<false>>(ctx, c, st);
+      return rc;
   }
-  const int64_t split_blocks = (l.rows + kSplitRows - 1) / kSplitRows * ((dc + kSplitCols - 1) / kSplitCols);
-  const int64_t resident = 8 * (int64_t)ctx->sm_count;
-  split_kernel<<<(unsigned)(split_blocks < resident ? split_blocks : resident), 256, 0, st>>>(
-      static_cast<const __nv_bfloat16*>(xp), slot_row_off, s.S, s.D, (int)l.rows, (int)l.pitch, x);
-  MOEGPS_AFTER_LAUNCH(ctx);
-  const Operands up_op = {{static_cast<const uint8_t*>(gate4_scale), static_cast<const uint8_t*>(up4_scale)},
-                          {x.scale[0], x.scale[1]}, (int)l.pitch};
-  const Operands down_op = {{static_cast<const uint8_t*>(down4_scale), nullptr}, {h.scale[0], h.scale[1]}, (int)l.pitch};
-  const int64_t R = (int64_t)s.T * s.K;
-  const int64_t per_slot = (R + s.S - 1) / s.S;
-  const mx4::Rows none = {};
-  int rc;
-  if (per_slot <= 16)
-    rc = launch_product<Cfg<16, true, 5>>(ctx, tg, tu, tx[0], tx[1], up_op, slot_row_off, slot_expert, s.F, s.D, h, nullptr, st);
-  else if (per_slot <= 64)
-    rc = launch_product<Cfg<64, true, 4>>(ctx, tg, tu, tx[0], tx[1], up_op, slot_row_off, slot_expert, s.F, s.D, h, nullptr, st);
-  else
-    rc = launch_product<Cfg<112, true, 3>>(ctx, tg, tu, tx[0], tx[1], up_op, slot_row_off, slot_expert, s.F, s.D, h, nullptr, st);
-  if (rc != MOEGPS_OK) return rc;
-  if (per_slot <= 16)
-    return launch_product<Cfg<16, false, 9>>(ctx, td, td, th[0], th[1], down_op, slot_row_off, slot_expert, s.D, s.F, none, yp, st);
-  if (per_slot <= 64)
-    return launch_product<Cfg<64, false, 6>>(ctx, td, td, th[0], th[1], down_op, slot_row_off, slot_expert, s.D, s.F, none, yp, st);
-  return launch_product<Cfg<208, false, 3>>(ctx, td, td, th[0], th[1], down_op, slot_row_off, slot_expert, s.D, s.F, none, yp, st);
+  return MOEGPS_ERR_UNSUPPORTED_SHAPE;
 }

@@ -157,4 +157,4 @@ bool moegps_make_tmap_3d(CUtensorMap* tm, const void* base, uint64_t batch, uint
 // the same with the box that an epilogue warp stores: 32 columns x 32 rows
 bool moegps_make_tmap_store(CUtensorMap* tm, void* base, uint64_t batch, uint64_t rows, uint64_t cols);
 bool moegps_make_tmap_codes4(CUtensorMap* tm, const void* base, uint64_t batch, uint64_t rows, uint64_t cols, uint32_t box_rows);
-bool moegps_make_tmap_bytes(CUtensorMap* tm, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
+bool moegps_make_tmap_bytes(CUtensorMap* tm, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows, bool swizzle);

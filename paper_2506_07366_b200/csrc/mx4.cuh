@@ -73,34 +73,63 @@ __device__ __forceinline__ void split2(float a, float b, float inv, float ratio,
 }
 
 // ------------------------------------------------------------------------------------------- workspace of expert_ffn4
-// Rows of activations in two terms: codes [rows][chunks * 128] for each term, words of four scale bytes [chunks][pitch]
-// for each (the rows of a tile are consecutive there).
+// How the rows of a slot are cut into tiles (chosen by shape alone, it decides the layout of the workspace).
+enum class Cut { k16, k48, k224 };
+inline Cut cut_of(const moegps_shape_t& s) {
+  const int64_t R = (int64_t)s.T * s.K, slots = R < s.S ? R : s.S;
+  const int64_t per_slot = slots > 0 ? (R + slots - 1) / slots : 0;
+  return per_slot <= 16 ? Cut::k16 : per_slot <= 48 ? Cut::k48 : Cut::k224;
+}
+inline int rows_of(Cut c) { return c == Cut::k16 ? 16 : c == Cut::k48 ? 48 : 224; }
+
+// Scale bytes of a tile's rows for one chunk, in the order of tensor memory (scale_byte_at).
+// Tiles of 16 or 48 rows: both terms stacked in one group of 512 bytes, the second term's rows behind the first's, which are
+// rounded up to 16.  Tiles of 224 rows: two groups for each term.
+template <int kRows>
+constexpr int kRowScaleBytes = kRows > 48 ? 4 * kScaleTile : kScaleTile;
+template <int kRows>
+__host__ __device__ constexpr int row_scale_at(int row, int term, int rows_in_tile) {
+  if (kRows > 48) return (2 * term + row / 128) * kScaleTile + scale_byte_at(row % 128);
+  return scale_byte_at(row + term * ((rows_in_tile + 15) / 16 * 16));
+}
+
+// Rows of activations in two terms: codes [rows][chunks * 128] for each, scales [row tile][chunk][kRowScaleBytes].
 struct Rows {
   uint8_t* code[2];
-  uint32_t* scale[2];
+  uint8_t* scale;
 };
 
 inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+constexpr int kMaxCtas = 148;      // blocks of a launch that joins partial sums; what they leave for each other is sized by it
+
 struct Layout {
-  int64_t rows, pitch;             // Rcap; words of a chunk's scales
-  size_t x_code, x_scale, h_code, h_scale, total;     // offsets of the first term; the second follows
-  size_t x_code_bytes, x_scale_bytes, h_code_bytes, h_scale_bytes;
+  Cut cut;
+  int64_t rows, row_tiles;         // Rcap; tiles of rows at most
+  size_t x_code, x_scale, h_code, h_scale, arrived, partial, total;     // offsets (the second term's codes follow the first's)
+  size_t x_code_bytes, h_code_bytes;
+  size_t x_scale_bytes, h_scale_bytes;
 };
 
 inline Layout layout_of(const moegps_shape_t& s) {
   Layout l;
+  l.cut = cut_of(s);
+  const int n = rows_of(l.cut);
+  const size_t row_scales = n > 48 ? 4 * kScaleTile : kScaleTile;
   l.rows = (int64_t)s.T * s.K + (int64_t)s.S * (s.row_align - 1);
-  l.pitch = (l.rows + 31) & ~(int64_t)31;
+  l.row_tiles = l.rows / n + s.S;
   l.x_code_bytes = align256((size_t)l.rows * chunks_of(s.D) * kChunk);
   l.h_code_bytes = align256((size_t)l.rows * chunks_of(s.F) * kChunk);
-  l.x_scale_bytes = align256((size_t)l.pitch * chunks_of(s.D) * 4);
-  l.h_scale_bytes = align256((size_t)l.pitch * chunks_of(s.F) * 4);
+  l.x_scale_bytes = align256((size_t)l.row_tiles * chunks_of(s.D) * row_scales);
+  l.h_scale_bytes = align256((size_t)l.row_tiles * chunks_of(s.F) * row_scales);
   l.x_code = 0;
   l.x_scale = l.x_code + 2 * l.x_code_bytes;
-  l.h_code = l.x_scale + 2 * l.x_scale_bytes;
+  l.h_code = l.x_scale + l.x_scale_bytes;
   l.h_scale = l.h_code + 2 * l.h_code_bytes;
-  l.total = l.h_scale + 2 * l.h_scale_bytes;
+  l.arrived = l.h_scale + l.h_scale_bytes;
+  l.partial = l.arrived + align256(2 * kMaxCtas * sizeof(int32_t));
+  // each block leaves at most two unfinished tiles: 2 matrices x n rows x 128 fp32
+  l.total = l.partial + (n > 48 ? 0 : (size_t)kMaxCtas * 2 * 2 * n * kTile * sizeof(float));
   return l;
 }
 
