@@ -74,10 +74,11 @@ int moegps_create(moegps_ctx_t** out, const moegps_shape_t* shape, int device) {
   cudaGetDevice(&prev);
   cudaError_t e = cudaSetDevice(device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&ctx->sm_count, cudaDevAttrMultiProcessorCount, device);
-  constexpr size_t kCtxWords = 4 + 2 * 256;      // status word, router accumulators (64-bit)
+  constexpr size_t kCtxWords = 4 + 2 * 256 + 2;  // status word, router accumulators (64-bit), a count (64-bit)
   if (e == cudaSuccess) e = cudaMalloc(&ctx->d_status, kCtxWords * sizeof(int32_t));
   if (e == cudaSuccess) e = cudaMemset(ctx->d_status, 0, kCtxWords * sizeof(int32_t));
   ctx->d_route_acc = ctx->d_status ? reinterpret_cast<unsigned long long*>(ctx->d_status + 4) : nullptr;
+  ctx->d_meetings = ctx->d_status ? ctx->d_route_acc + 256 : nullptr;
   cudaSetDevice(prev);
   if (e != cudaSuccess) {
     if (ctx->d_status) cudaFree(ctx->d_status);

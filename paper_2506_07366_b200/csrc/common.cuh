@@ -17,6 +17,7 @@ struct moegps_ctx {
   int sm_count;
   int32_t* d_status;        // 4 x int32 on the device
   unsigned long long* d_route_acc;   // behind it: 256 64-bit histogram accumulators of the router (all zero between calls)
+  unsigned long long* d_meetings;    // behind them: arrivals of the blocks of expert_ffn4, ever growing
   int64_t launches;         // kernels launched through this context
   int last_cuda_error;
   // cached TMA descriptors of the expert FFN, keyed by the base pointers they were built for

@@ -1,19 +1,17 @@
 // expert_ffn4: the experts' SwiGLU FFN on 4-bit weights (mx4.cuh) over ragged slots, from the few rows of a token being
-// generated to long prompts.  Three launches:
+// generated to long prompts:
 //   split      x = two e4m3 terms with a scale for 32 values (exact, see mx4.cuh)
-//   gate + up  g = x Wg^T, u = x Wu^T, h = silu(g) u, written as two terms
+//   gate + up  g = x Wg^T, u = x Wu^T, h = silu(g) u, as two terms
 //   down       y = h Wd^T
 // The products are block-scaled MMAs (e2m1 x e4m3, fp32 accumulators in tensor memory) with the WEIGHTS as the 128-row
 // operand and the slot's rows as the other one, so that a slot of few rows costs few columns.  A weight tile is expanded to 16-byte
 // groups by the TMA load that brings it (8 bytes of codes, 8 unused): 8 KB of memory traffic for 16 KB of shared memory,
 // and no thread touches a weight.  The scales of the rows lie in the workspace as tensor memory wants them, tile by tile.
 //
-// Two kernels, by rows for each slot (mx4::cut_of):
-//  narrow_kernel (up to 48): bound by reading weights.  The K steps of all tiles are dealt evenly to the SMs, whatever their
-//    number; a tile that several SMs share is joined by the one that finishes last.  Both terms of a row are columns of one
-//    MMA (an MMA of few columns takes 40 clocks whatever their number, it waits for its 128 weight rows).
-//  wide_kernel: bound by products.  Pairs of CTAs, 256 weight rows x 224 rows of the slot, two MMAs for the two terms.
-// Every wait is bounded.
+// Two ways, by rows for each slot (mx4::cut_of): up to 48 one launch that is bound by reading weights (short_kernel), beyond
+// that three that are bound by products (split_kernel, wide_kernel twice).  Every wait is bounded.
+#include <type_traits>
+
 #include "common.cuh"
 #include "grouped_gemm.cuh"
 #include "mx4.cuh"
@@ -66,18 +64,55 @@ constexpr int kSplitThreads = 256;
 constexpr int kSplitRows = 8;      // rows of a block's unit: one for each warp
 constexpr int kSplitCols = 1024;   // its columns
 
+// Columns col0 .. col0 + 1023 of a row by a warp: codes(column, first term's eight codes, second term's) for each lane's
+// eight columns, scales(chunk, word of the first term's four scale bytes, of the second's) once for each chunk.
+template <class Codes, class Scales>
+__device__ __forceinline__ void split_row(const __nv_bfloat16* __restrict__ x, int D, int col0, int lane, Codes&& codes, Scales&& scales) {
+  uint4 v[kSplitCols / 256];
+#pragma unroll
+  for (int i = 0; i < kSplitCols / 256; ++i) {
+    const int col = col0 + 256 * i + 8 * lane;
+    v[i] = make_uint4(0, 0, 0, 0);
+    if (col < D) v[i] = *reinterpret_cast<const uint4*>(x + col);
+  }
+#pragma unroll
+  for (int i = 0; i < kSplitCols / 256; ++i) {
+    const int col = col0 + 256 * i + 8 * lane;        // a warp's 256 columns are two chunks: whole half-warps are inside or not
+    const uint32_t words[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+    const uint32_t m2 = __vmaxu2(__vmaxu2(words[0] & 0x7fff7fffu, words[1] & 0x7fff7fffu),
+                                 __vmaxu2(words[2] & 0x7fff7fffu, words[3] & 0x7fff7fffu));
+    uint32_t m = max(m2 & 0xffffu, m2 >> 16);         // as integers, NaN and infinity are the largest
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));   // over the four lanes of a block
+    const uint32_t b1 = mx4::term_scale(m << 16), b2 = mx4::second_scale(b1);
+    const float inv = mx4::inverse_scale(b1), ratio = mx4::scale_ratio(b1, b2);
+    uint32_t c1[4], c2[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      mx4::split2(__uint_as_float(words[j] << 16), __uint_as_float(words[j] & 0xffff0000u), inv, ratio, c1[j], c2[j]);
+    // the four scale bytes of a chunk, from lanes 0, 4, 8, 12 of its half-warp
+    uint32_t w1 = b1 << (8 * ((lane >> 2) & 3)), w2 = b2 << (8 * ((lane >> 2) & 3));
+    w1 |= __shfl_xor_sync(0xffffffffu, w1, 4);
+    w2 |= __shfl_xor_sync(0xffffffffu, w2, 4);
+    w1 |= __shfl_xor_sync(0xffffffffu, w1, 8);
+    w2 |= __shfl_xor_sync(0xffffffffu, w2, 8);
+    if (col < (D + kChunk - 1) / kChunk * kChunk) {
+      codes(col, make_uint2(c1[0] | c1[1] << 16, c1[2] | c1[3] << 16), make_uint2(c2[0] | c2[1] << 16, c2[2] | c2[3] << 16));
+      if ((lane & 15) == 0) scales(col / kChunk, w1, w2);
+    }
+  }
+}
+
 template <int kRows>
 __global__ void __launch_bounds__(kSplitThreads)
 split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert,
-             int S, int E, int D, int rcap, const mx4::Rows out, int32_t* __restrict__ arrived, int32_t* __restrict__ status) {
+             int S, int E, int D, int rcap, const mx4::Rows out, int32_t* __restrict__ status) {
   static_assert(kRows % kSplitRows == 0, "a unit's rows belong to one tile");
   __shared__ Tables units, tiles;                     // groups of kSplitRows rows, tiles of rows
   launch_dependents();
   wait_for_predecessor();
   build_tables<kSplitThreads, kSplitRows>(units, slot_row_off, slot_expert, S, E, 1, rcap, status);
   build_tables<kSplitThreads, kRows>(tiles, slot_row_off, slot_expert, S, E, 1, rcap, status);
-  if (blockIdx.x == 0)
-    for (int i = threadIdx.x; i < 2 * mx4::kMaxCtas; i += kSplitThreads) arrived[i] = 0;
   __syncthreads();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int chunks = mx4::chunks_of(D);
@@ -95,46 +130,15 @@ split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ s
     if (r >= slot_rows) continue;
     const int row = first + r, in_tile = r % kRows, tile = tiles.tile_base[lo] + r / kRows;
     const int rows_in_tile = min(kRows, slot_rows - (r - in_tile));
-    const int at1 = mx4::row_scale_at<kRows>(in_tile, 0, rows_in_tile), at2 = mx4::row_scale_at<kRows>(in_tile, 1, rows_in_tile);
-    uint4 v[kSplitCols / 256];
-#pragma unroll
-    for (int i = 0; i < kSplitCols / 256; ++i) {
-      const int col = col0 + 256 * i + 8 * lane;
-      v[i] = make_uint4(0, 0, 0, 0);
-      if (col < D) v[i] = *reinterpret_cast<const uint4*>(xp + (size_t)row * D + col);
-    }
-#pragma unroll
-    for (int i = 0; i < kSplitCols / 256; ++i) {
-      const int col = col0 + 256 * i + 8 * lane;      // a warp's 256 columns are two chunks: whole half-warps are inside or not
-      const uint32_t words[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-      const uint32_t m2 = __vmaxu2(__vmaxu2(words[0] & 0x7fff7fffu, words[1] & 0x7fff7fffu),
-                                   __vmaxu2(words[2] & 0x7fff7fffu, words[3] & 0x7fff7fffu));
-      uint32_t m = max(m2 & 0xffffu, m2 >> 16);
-      m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-      m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-      const uint32_t b1 = mx4::term_scale(m << 16), b2 = mx4::second_scale(b1);
-      const float inv = mx4::inverse_scale(b1), ratio = mx4::scale_ratio(b1, b2);
-      uint32_t c1[4], c2[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        mx4::split2(__uint_as_float(words[j] << 16), __uint_as_float(words[j] & 0xffff0000u), inv, ratio, c1[j], c2[j]);
-      // the four scale bytes of a chunk, from lanes 0, 4, 8, 12 of its half-warp
-      uint32_t w1 = b1 << (8 * ((lane >> 2) & 3)), w2 = b2 << (8 * ((lane >> 2) & 3));
-      w1 |= __shfl_xor_sync(0xffffffffu, w1, 4);
-      w2 |= __shfl_xor_sync(0xffffffffu, w2, 4);
-      w1 |= __shfl_xor_sync(0xffffffffu, w1, 8);
-      w2 |= __shfl_xor_sync(0xffffffffu, w2, 8);
-      if (col < chunks * kChunk) {
-        const size_t at = (size_t)row * (chunks * kChunk) + col;
-        *reinterpret_cast<uint2*>(out.code[0] + at) = make_uint2(c1[0] | c1[1] << 16, c1[2] | c1[3] << 16);
-        *reinterpret_cast<uint2*>(out.code[1] + at) = make_uint2(c2[0] | c2[1] << 16, c2[2] | c2[3] << 16);
-        if ((lane & 15) == 0) {
-          uint8_t* scales = out.scale + ((size_t)tile * chunks + col / kChunk) * mx4::kRowScaleBytes<kRows>;
-          *reinterpret_cast<uint32_t*>(scales + at1) = w1;
-          *reinterpret_cast<uint32_t*>(scales + at2) = w2;
-        }
-      }
-    }
+    split_row(xp + (size_t)row * D, D, col0, lane, [&](int col, uint2 c1, uint2 c2) {
+      const size_t at = (size_t)row * (chunks * kChunk) + col;
+      *reinterpret_cast<uint2*>(out.code[0] + at) = c1;
+      *reinterpret_cast<uint2*>(out.code[1] + at) = c2;
+    }, [&](int chunk, uint32_t w1, uint32_t w2) {
+      uint8_t* scales = out.scale + ((size_t)tile * chunks + chunk) * mx4::kRowScaleBytes<kRows>;
+      *reinterpret_cast<uint32_t*>(scales + mx4::row_scale_at<kRows>(in_tile, 0, rows_in_tile)) = w1;
+      *reinterpret_cast<uint32_t*>(scales + mx4::row_scale_at<kRows>(in_tile, 1, rows_in_tile)) = w2;
+    });
   }
 }
 
@@ -146,12 +150,10 @@ __device__ __forceinline__ float silu(float g) { return __fdividef(g, 1.0f + __e
 // rows x 2048, F 1408, 64 experts: 1030 us, 755 without the stores).
 constexpr int kStaging = 1024;
 
-// 16 rows of h for a warp's 32 outputs (one for each lane, one block): codes and scales.  row: the first one's place in the
-// buffers, in_tile: in its tile of `rows`; col0: the first lane's column; block: which of the chunk's four.
-template <int kRows>
-__device__ __forceinline__ void store_h(const mx4::Rows& h, const uint32_t (&g)[16], const uint32_t (&u)[16], uint8_t* staging,
-                                        int row, int in_tile, int rows, size_t pitch, int col0, uint8_t* scales, int block, int lane) {
-  uint32_t bytes = 0;                                  // lane i: scale of row i's first term, lane 16 + i: of its second
+// 16 rows of h = silu(g) u for a warp's 32 outputs (one for each lane; they are one block): codes into `staging`, the first
+// term's 16 rows of 32 bytes and then the second's; returns the scale byte of row lane % 16, lanes 0 to 15 of the first term's.
+__device__ __forceinline__ uint32_t encode_h(const uint32_t (&g)[16], const uint32_t (&u)[16], uint8_t* staging, int lane) {
+  uint32_t byte = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const float v = silu(__uint_as_float(g[i])) * __uint_as_float(u[i]);
@@ -161,9 +163,18 @@ __device__ __forceinline__ void store_h(const mx4::Rows& h, const uint32_t (&g)[
     mx4::split2(v, 0.0f, mx4::inverse_scale(b1), mx4::scale_ratio(b1, b2), c1, c2);
     staging[i * 32 + lane] = (uint8_t)c1;
     staging[512 + i * 32 + lane] = (uint8_t)c2;
-    if ((lane & 15) == i) bytes = lane < 16 ? b1 : b2;
+    if ((lane & 15) == i) byte = lane < 16 ? b1 : b2;
   }
   __syncwarp();
+  return byte;
+}
+
+// They go to rows of `pitch` bytes; row: the first one's place there, in_tile: in its tile of `rows`; col0: the first lane's
+// column; scales: of the tile and its chunk; block: which of the chunk's four.
+template <int kRows>
+__device__ __forceinline__ void store_h(const mx4::Rows& h, const uint32_t (&g)[16], const uint32_t (&u)[16], uint8_t* staging,
+                                        int row, int in_tile, int rows, size_t pitch, int col0, uint8_t* scales, int block, int lane) {
+  const uint32_t byte = encode_h(g, u, staging, lane);
   const int r = lane >> 1;                             // two lanes for each row
   if (in_tile + r < rows) {
     const size_t at = (size_t)(row + r) * pitch + col0 + 16 * (lane & 1);
@@ -172,7 +183,24 @@ __device__ __forceinline__ void store_h(const mx4::Rows& h, const uint32_t (&g)[
       *reinterpret_cast<uint4*>(h.code[t] + at) = *reinterpret_cast<const uint4*>(staging + 512 * t + 16 * lane);
   }
   if (in_tile + (lane & 15) < rows)
-    scales[mx4::row_scale_at<kRows>(in_tile + (lane & 15), lane >> 4, rows) + block] = (uint8_t)bytes;
+    scales[mx4::row_scale_at<kRows>(in_tile + (lane & 15), lane >> 4, rows) + block] = (uint8_t)byte;
+  __syncwarp();
+}
+
+// ... or into the image of the tile's chunk.
+template <int kRows>
+__device__ __forceinline__ void store_h_image(uint8_t* image, const uint32_t (&g)[16], const uint32_t (&u)[16], uint8_t* staging,
+                                              int in_tile, int rows, int block, int lane) {
+  const uint32_t byte = encode_h(g, u, staging, lane);
+  const int r = in_tile + (lane >> 1);
+  if (r < rows) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      *reinterpret_cast<uint4*>(image + mx4::image_code_at(r, t, rows, 2 * block + (lane & 1))) =
+          *reinterpret_cast<const uint4*>(staging + 512 * t + 16 * lane);
+  }
+  if (in_tile + (lane & 15) < rows)
+    image[mx4::row_scale_at<kRows>(in_tile + (lane & 15), lane >> 4, rows) + block] = (uint8_t)byte;
   __syncwarp();
 }
 
@@ -192,29 +220,43 @@ __device__ __forceinline__ void store_y(__nv_bfloat16* __restrict__ y, const uin
   __syncwarp();
 }
 
-// ------------------------------------------------------------------------------------------- narrow
-template <int kRows_, bool kGateUp_, int kStages_>
-struct Narrow {
+// ------------------------------------------------------------------------------------------- short slots
+// The whole FFN in one launch, for slots of few rows: what there is to do is to read the weights, and three launches in a row
+// cost 35 us beside the 29 that two 4096 x 14336 experts take to read (each has to start, build its tables, fill its ring and join
+// its sums).  The blocks (one for each SM, a cooperative launch) wait for one another twice, when the rows are split and when
+// h is there; the weights of the next product are loaded meanwhile.
+//  - A tile is two weight tiles of 128 outputs (gate and up of the same outputs, or two neighbours of down) times the rows of a
+//    slot.  The K steps of all tiles are dealt evenly to the blocks, whatever their number; a tile that several blocks share is
+//    joined by the one that finishes last.
+//  - Both terms of a row are columns of one MMA (of few columns it takes 40 clocks whatever their number: it waits for its 128
+//    weight rows), side by side in the accumulator, and added up in the epilogue.
+//  - x and h lie in the workspace as the images that a chunk of a tile has in shared memory (512 bytes of scales, then 128-byte
+//    rows, swizzled): one bulk copy for each chunk.
+//  - What a step costs beside its bytes: a wait, an expected count and a TMA load take one thread 300 clocks, so a stage is two
+//    weight tiles, 16 KB of memory; the waits around four MMAs take 380 clocks in which the tensor core, which holds few of
+//    them, runs dry, so two warps issue, each for its tile of the two (one warp for both: 409 ns for a stage, memory takes 370).
+// Warps: 0 loads weights, 2 rows, 1 and 3 issue products, 4..7 split the rows and drain the accumulators.
+template <int kRows_, int kStages_>
+struct Short {
   static constexpr int kRows = kRows_;                 // of a tile at most
-  static constexpr bool kGateUp = kGateUp_;
   static constexpr int kStages = kStages_;
-  static constexpr int kMats = kGateUp ? 2 : 1;        // weight matrices that share the rows
-  static constexpr int kCols = 2 * kRows;              // accumulator columns of a matrix: both terms
-  static constexpr int kABytes = kTile * kChunk;       // of shared memory; half of them are loaded
-  static constexpr int kBBytes = kCols * kChunk;
-  static constexpr int kScaleOffset = kMats * kABytes + kBBytes;
-  static constexpr int kStageBytes = round_up(kScaleOffset + (kMats + 1) * kScaleTile, 1024);
-  static constexpr int kScaleCols = 4 * (kMats + 1);
-  static constexpr int kAccCols = kMats * kCols;
-  static constexpr int kColsUsed = 2 * kAccCols + kStages * kScaleCols;
-  static constexpr int kTmemCols = kColsUsed <= 128 ? 128 : kColsUsed <= 256 ? 256 : 512;
-  static constexpr int kThreads = 192;                 // loads, MMAs, four epilogue warps
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + sizeof(Tables) + 256 + 4 * kStaging;
+  static constexpr int kCols = 2 * kRows;              // accumulator columns of a weight tile: both terms
+  static constexpr int kABytes = kTile * kChunk;       // a weight tile in shared memory; half of them are loaded
+  static constexpr int kImage = mx4::kImageBytes<kRows>;
+  static constexpr int kScalesAt = 2 * kABytes;        // of a stage: the weights' scales, then the image, its rows from a multiple of 1024
+  static constexpr int kImageAt = kScalesAt + 3 * kScaleTile;
+  static constexpr int kStageBytes = round_up(kImageAt + kImage, 1024);
+  static constexpr int kStagingOffset = kStages * kStageBytes;
+  static constexpr int kTablesOffset = kStagingOffset + 4 * kStaging;
+  static constexpr int kBarsOffset = kTablesOffset + 2 * (int)sizeof(Tables);
+  static constexpr int kAccCols = 2 * kCols;
+  static constexpr int kColsUsed = 2 * kAccCols + 16 * kStages;      // each issuing warp has its own copies of the scales
+  static constexpr int kTmemCols = kColsUsed <= 256 ? 256 : 512;
+  static constexpr int kThreads = 256;
+  static constexpr size_t kSmem = 1024 + kBarsOffset + 256;
+  static_assert((kImageAt + kScaleTile) % 1024 == 0, "swizzled rows");
   static_assert(kRows % 16 == 0 && kCols <= 128 && kColsUsed <= 512 && kSmem <= 227 * 1024, "does not fit");
-};
-
-struct Weights {
-  const uint8_t* scale[2];          // gate, up; or down
+  static_assert(kSmem > 114 * 1024, "one block for each SM: the blocks wait for one another");
 };
 
 // What a block does of all K steps, [begin, end) of the tiles one after the other, and who shares a tile with it.
@@ -233,215 +275,324 @@ struct Share {
   __device__ int owner(int64_t p) const { return (int)(((p + 1) * blocks - 1) / steps); }
 };
 
+// The blocks' barrier: a count in the context's memory that only grows, by the number of blocks for each meeting.
+struct Meeting {
+  unsigned long long* count;
+  volatile unsigned long long* goal;               // [2], shared memory: what the count is when all have come; 0 = not here yet
+  // by one thread, after a barrier behind the others' writes
+  __device__ void arrive(int which) const {
+    __threadfence();
+    const unsigned long long n = gridDim.x, old = atomicAdd(count, 1ull);
+    goal[which] = (old / n + 1) * n;
+  }
+  __device__ bool wait(int which, volatile int* abort_flag) const {
+    const long long t0 = clock64();
+    while (true) {
+      const unsigned long long want = goal[which];
+      if (want) {
+        unsigned long long now;
+        asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(now) : "l"(count) : "memory");
+        if (now >= want) return true;
+      }
+      if (*abort_flag) return false;
+      if (clock64() - t0 > kWaitLimitCycles) {
+        *abort_flag = 1;
+        return false;
+      }
+    }
+  }
+};
+
+// this thread's writes to global memory before, and what it reads there after, an exchange with bulk copies
+__device__ __forceinline__ void fence_proxy_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
+
 template <class Cfg>
 __global__ void __launch_bounds__(Cfg::kThreads, 1)
-narrow_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ CUtensorMap tm_w1,
-              const __grid_constant__ CUtensorMap tm_r0, const __grid_constant__ CUtensorMap tm_r1, const Weights w,
-              const uint8_t* __restrict__ row_scale, const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert,
-              int S, int E, int n_dim, int k_dim, int rcap, const mx4::Rows h, __nv_bfloat16* __restrict__ y,
-              int32_t* __restrict__ arrived, float* __restrict__ partial, int32_t* __restrict__ status) {
-  constexpr int kStages = Cfg::kStages, kRows = Cfg::kRows, kMats = Cfg::kMats;
+short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant__ CUtensorMap tm_up,
+             const __grid_constant__ CUtensorMap tm_down, const uint8_t* __restrict__ gate_scale, const uint8_t* __restrict__ up_scale,
+             const uint8_t* __restrict__ down_scale, const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off,
+             const int32_t* __restrict__ slot_expert, int S, int E, int D, int F, int rcap, uint8_t* x_image, uint8_t* h_image,
+             __nv_bfloat16* __restrict__ y, int32_t* arrived, float* partial, unsigned long long* meetings,
+             int32_t* __restrict__ status) {
+  constexpr int kRows = Cfg::kRows, kStages = Cfg::kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  Tables& tb = *reinterpret_cast<Tables*>(smem + (size_t)kStages * Cfg::kStageBytes);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)kStages * Cfg::kStageBytes + sizeof(Tables));
-  uint64_t* full = bars;                     // [kStages]  loads -> MMA
-  uint64_t* empty = bars + kStages;          // [kStages]  MMA -> loads
-  uint64_t* acc_full = bars + 2 * kStages;   // [2]  MMA -> epilogue
-  uint64_t* acc_empty = acc_full + 2;        // [2]  epilogue -> MMA
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  Tables& tb = *reinterpret_cast<Tables*>(smem + Cfg::kTablesOffset);                      // row tiles
+  Tables& rows_before = *reinterpret_cast<Tables*>(smem + Cfg::kTablesOffset + sizeof(Tables));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::kBarsOffset);     // [kStages]  both loaders -> MMAs
+  uint64_t* empty = full + kStages;                  // [kStages]  both issuing warps -> loaders
+  uint64_t* acc_full = empty + kStages;              // [2]  both issuing warps -> epilogue
+  uint64_t* acc_empty = acc_full + 2;                // [2]
+  volatile unsigned long long* goal = reinterpret_cast<volatile unsigned long long*>(acc_empty + 2);      // [2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* is_last = abort_flag + 1;
-  static_assert((2 * kStages + 4) * 8 + 12 <= 256, "barriers fit their space");
+  static_assert((2 * kStages + 6) * 8 + 12 <= 256, "barriers fit their space");
 
   const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
-  const int m_tiles = mx4::tiles_of(n_dim), chunks = mx4::chunks_of(k_dim);
-
+  const int d_chunks = mx4::chunks_of(D), f_chunks = mx4::chunks_of(F);      // f_chunks also the tiles of gate + up
+  const int d_tiles = (d_chunks + 1) / 2;                                    // of down
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 2); mbar_init(&empty[i], 2); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 2); mbar_init(&acc_empty[i], 4); goal[i] = 0; }
     *abort_flag = 0;
     fence_mbar_init();
-    prefetch_tensormap(&tm_w0);
-    if (kMats == 2) prefetch_tensormap(&tm_w1);
-    prefetch_tensormap(&tm_r0);
-    prefetch_tensormap(&tm_r1);
+    prefetch_tensormap(&tm_gate);
+    prefetch_tensormap(&tm_up);
+    prefetch_tensormap(&tm_down);
   }
-  launch_dependents();
-  wait_for_predecessor();
   if (warp == 1) {
     tmem_alloc(tmem_slot, Cfg::kTmemCols);
     tmem_relinquish();
   }
   build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status);
+  build_tables<Cfg::kThreads, 1>(rows_before, slot_row_off, slot_expert, S, E, 1, rcap, status);
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  const Share share((int64_t)tb.tile_base[S] * m_tiles * chunks, gridDim.x, blockIdx.x);
+  const int64_t row_tiles = tb.tile_base[S];
+  const Share up_share(row_tiles * f_chunks * d_chunks, gridDim.x, blockIdx.x);
+  const Share down_share(row_tiles * d_tiles * f_chunks, gridDim.x, blockIdx.x);
+  const Meeting meeting = {meetings, goal};
+
+  // calls body(tile, its number, k0, k1) for each tile, or part of one, of this block
+  auto for_tiles = [&](const Share& share, int m_tiles, int chunks, auto&& body) {
+    for (int64_t p = share.begin; p < share.end;) {
+      const int64_t t = p / chunks;
+      const int k0 = (int)(p - t * chunks), k1 = (int)min((int64_t)chunks, k0 + share.end - p);
+      if (!body(tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles), t, k0, k1)) return false;
+      p += k1 - k0;
+    }
+    return true;
+  };
+  auto up_tiles = [&](auto&& body) { return for_tiles(up_share, f_chunks, d_chunks, body); };
+  auto down_tiles = [&](auto&& body) { return for_tiles(down_share, d_tiles, f_chunks, body); };
 
   if (warp == 0) {
     if (lane == 0) {
       int stage = 0;
       uint32_t phase = 0;
-      bool ok = true;
-      for (int64_t p = share.begin; ok && p < share.end;) {
-        const int64_t t = p / chunks;
-        const int k0 = (int)(p - t * chunks), k1 = (int)min((int64_t)chunks, k0 + share.end - p);
-        const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
-        const int padded = round_up(tc.rows, 16);
-        const uint32_t bytes = kMats * (Cfg::kABytes / 2 + kScaleTile) + 2 * padded * kChunk + kScaleTile;
-        const size_t scale_at = ((size_t)tc.expert * m_tiles + tc.m) * chunks * kScaleTile;
-        const uint8_t* rows_at = row_scale + (size_t)tc.row_tile * chunks * kScaleTile;
-        for (int c = k0; c < k1; ++c) {
-          if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag)) { ok = false; break; }
-          uint8_t* a = smem + (size_t)stage * Cfg::kStageBytes;
-          uint8_t* b = a + kMats * Cfg::kABytes;
-          uint8_t* sc = a + Cfg::kScaleOffset;
-          mbar_arrive_expect_tx(&full[stage], bytes);
-#pragma unroll
-          for (int m = 0; m < kMats; ++m) {
-            tma_load_3d(a + m * Cfg::kABytes, m ? &tm_w1 : &tm_w0, &full[stage], c * kChunk, tc.m * kTile, tc.expert);
-            bulk_load(sc + m * kScaleTile, w.scale[m] + scale_at + (size_t)c * kScaleTile, kScaleTile, &full[stage]);
+      // the two weight tiles of chunks k0 .. k1 - 1: rows m0, m1 of either matrix, their scales at s0, s1 (m1 < 0: there is one)
+      auto load = [&](const CUtensorMap* tm0, const CUtensorMap* tm1, int expert, int m0, int m1, const uint8_t* s0, const uint8_t* s1,
+                      int k0, int k1) {
+        for (int c = k0; c < k1; ++c, s0 += kScaleTile, s1 += kScaleTile) {
+          if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag)) return false;
+          uint8_t* a = smem + stage * Cfg::kStageBytes;
+          mbar_arrive_expect_tx(&full[stage], (m1 < 0 ? 1 : 2) * (Cfg::kABytes / 2 + kScaleTile));
+          tma_load_3d(a, tm0, &full[stage], c * kChunk, m0, expert);
+          bulk_load(a + Cfg::kScalesAt, s0, kScaleTile, &full[stage]);
+          if (m1 >= 0) {
+            tma_load_3d(a + Cfg::kABytes, tm1, &full[stage], c * kChunk, m1, expert);
+            bulk_load(a + Cfg::kScalesAt + kScaleTile, s1, kScaleTile, &full[stage]);
           }
-          for (int r = 0; r < padded; r += 16) {
-            tma_load_2d(b + r * kChunk, &tm_r0, &full[stage], c * kChunk, tc.row0 + r);
-            tma_load_2d(b + (padded + r) * kChunk, &tm_r1, &full[stage], c * kChunk, tc.row0 + r);
-          }
-          bulk_load(sc + kMats * kScaleTile, rows_at + (size_t)c * kScaleTile, kScaleTile, &full[stage]);
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
-        p += k1 - k0;
-      }
+        return true;
+      };
+      const bool ok = up_tiles([&](const Tile& tc, int64_t, int k0, int k1) {
+        const size_t at = (((size_t)tc.expert * f_chunks + tc.m) * d_chunks + k0) * kScaleTile;
+        return load(&tm_gate, &tm_up, tc.expert, tc.m * kTile, tc.m * kTile, gate_scale + at, up_scale + at, k0, k1);
+      }) && down_tiles([&](const Tile& tc, int64_t, int k0, int k1) {
+        const uint8_t* s0 = down_scale + (((size_t)tc.expert * d_chunks + 2 * tc.m) * f_chunks + k0) * kScaleTile;
+        return load(&tm_down, &tm_down, tc.expert, 2 * tc.m * kTile, 2 * tc.m + 1 < d_chunks ? (2 * tc.m + 1) * kTile : -1, s0,
+                    s0 + (size_t)f_chunks * kScaleTile, k0, k1);
+      });
       if (!ok) linger();
     }
-  } else if (warp == 1) {
-    const uint32_t ring = smem_u32(smem);
-    const uint32_t scale_cols = tmem_base + 2 * Cfg::kAccCols;
+  } else if (warp == 2) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      auto load = [&](const uint8_t* image, const Tile& tc, int chunks, int k0, int k1) {
+        const uint32_t bytes = kScaleTile + 2 * round_up(tc.rows, 16) * kChunk;
+        const uint8_t* from = image + ((size_t)tc.row_tile * chunks + k0) * Cfg::kImage;
+        for (int c = k0; c < k1; ++c, from += Cfg::kImage) {
+          if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag)) return false;
+          mbar_arrive_expect_tx(&full[stage], bytes);
+          bulk_load(smem + stage * Cfg::kStageBytes + Cfg::kImageAt, from, bytes, &full[stage]);
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+        return true;
+      };
+      bool ok = meeting.wait(0, abort_flag);
+      fence_proxy_async_global();
+      ok = ok && up_tiles([&](const Tile& tc, int64_t, int k0, int k1) { return load(x_image, tc, d_chunks, k0, k1); });
+      ok = ok && meeting.wait(1, abort_flag);
+      fence_proxy_async_global();
+      ok = ok && down_tiles([&](const Tile& tc, int64_t, int k0, int k1) { return load(h_image, tc, f_chunks, k0, k1); });
+      if (!ok) linger();
+    }
+  } else if (warp == 1 || warp == 3) {
+    const int which = warp >> 1;                       // of the two weight tiles
+    const uint32_t base = smem_u32(smem);
+    const uint32_t scale_cols = tmem_base + 2 * Cfg::kAccCols + 8 * which;
     int stage = 0, acc = 0;
     uint32_t phase = 0, acc_phase = 0;
-    bool ok = true;
-    for (int64_t p = share.begin; ok && p < share.end;) {
-      const int64_t t = p / chunks;
-      const int k0 = (int)(p - t * chunks), k1 = (int)min((int64_t)chunks, k0 + share.end - p);
-      const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+    auto multiply = [&](bool there, const Tile& tc, int k0, int k1) {
       const uint32_t idesc = idesc_mx_e2m1_e4m3(kTile, 2 * round_up(tc.rows, 16));
-      if (!warp_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag)) break;
+      if (!warp_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag)) return false;
       tc_fence_after_sync();
-      const uint32_t d = tmem_base + (uint32_t)acc * Cfg::kAccCols;
+      const uint32_t d = tmem_base + (uint32_t)acc * Cfg::kAccCols + which * Cfg::kCols;
       for (int c = k0; c < k1; ++c) {
-        if (!warp_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
+        if (!warp_wait(&full[stage], phase, abort_flag)) return false;
         tc_fence_after_sync();
-        const uint32_t a = ring + (uint32_t)stage * Cfg::kStageBytes;
-        const uint32_t sc = a + Cfg::kScaleOffset;
-        const uint64_t da = smem_desc_k_sw128(a), db = smem_desc_k_sw128(a + kMats * Cfg::kABytes);
-        const uint32_t ts = scale_cols + (uint32_t)stage * Cfg::kScaleCols;     // (the ring frees a stage's columns with it)
+        const uint32_t at = base + stage * Cfg::kStageBytes;
+        const uint64_t da = smem_desc_k_sw128(at + which * Cfg::kABytes), db = smem_desc_k_sw128(at + Cfg::kImageAt + kScaleTile);
+        const uint32_t ws = scale_cols + 16 * stage, rs = ws + 4;      // (the ring frees a stage's columns with it)
         if (elect_one()) {
-#pragma unroll
-          for (int i = 0; i < kMats + 1; ++i) copy_scales(ts + 4 * i, smem_desc_scales(sc + i * kScaleTile));
-#pragma unroll
-          for (int m = 0; m < kMats; ++m) {
+          if (there) {
+            copy_scales(rs, smem_desc_scales(at + Cfg::kImageAt));
+            copy_scales(ws, smem_desc_scales(at + Cfg::kScalesAt + which * kScaleTile));
 #pragma unroll
             for (int j = 0; j < kChunk / mx4::kBlock; ++j)
-              mma_mx(d + m * Cfg::kCols, da + (uint64_t)((m * Cfg::kABytes + j * mx4::kBlock) >> 4),
-                     db + (uint64_t)((j * mx4::kBlock) >> 4), idesc | idesc_mx_block(j), ts + 4 * m, ts + 4 * kMats,
-                     (c - k0) | j);
+              mma_mx(d, da + (uint64_t)((j * mx4::kBlock) >> 4), db + (uint64_t)((j * mx4::kBlock) >> 4), idesc | idesc_mx_block(j), ws,
+                     rs, (c - k0) | j);
           }
           mma_commit(&empty[stage]);
         }
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
-      if (!ok) break;
       if (elect_one()) mma_commit(&acc_full[acc]);
       acc ^= 1;
       if (acc == 0) acc_phase ^= 1u;
-      p += k1 - k0;
-    }
-    if (*abort_flag) linger();
+      return true;
+    };
+    const bool ok = up_tiles([&](const Tile& tc, int64_t, int k0, int k1) { return multiply(true, tc, k0, k1); }) &&
+                    down_tiles([&](const Tile& tc, int64_t, int k0, int k1) { return multiply(2 * tc.m + which < d_chunks, tc, k0, k1); });
+    if (!ok) linger();
   } else {
     const int quarter = warp & 3, thread = quarter * 32 + lane;
-    uint8_t* staging = smem + (size_t)kStages * Cfg::kStageBytes + sizeof(Tables) + 256 + quarter * kStaging;
-    const size_t h_pitch = (size_t)m_tiles * kChunk;
+    uint8_t* staging = smem + Cfg::kStagingOffset + quarter * kStaging;
+    // x in two terms: a warp does 1024 columns of a row
+    {
+      if (thread < 2) arrived[thread * mx4::kMaxCtas + blockIdx.x] = 0;
+      const int col_blocks = (d_chunks * kChunk + kSplitCols - 1) / kSplitCols;
+      const int64_t work = (int64_t)rows_before.tile_base[S] * col_blocks;
+      for (int64_t b = (int64_t)quarter * gridDim.x + blockIdx.x; b < work; b += 4 * (int64_t)gridDim.x) {
+        const int n = (int)(b / col_blocks), col0 = (int)(b - (int64_t)n * col_blocks) * kSplitCols;
+        int lo = 0, hi = S;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (rows_before.tile_base[mid] <= n) lo = mid; else hi = mid;
+        }
+        const int r = n - rows_before.tile_base[lo], in_tile = r % kRows;
+        const int rows_in_tile = min(kRows, rows_before.tile_base[lo + 1] - rows_before.tile_base[lo] - (r - in_tile));
+        uint8_t* image = x_image + (size_t)(tb.tile_base[lo] + r / kRows) * d_chunks * Cfg::kImage;
+        split_row(xp + (size_t)(__ldg(slot_row_off + lo) + r) * D, D, col0, lane, [&](int col, uint2 first, uint2 second) {
+          uint8_t* at = image + (size_t)(col / kChunk) * Cfg::kImage + (col & 8);
+          *reinterpret_cast<uint2*>(at + mx4::image_code_at(in_tile, 0, rows_in_tile, col % kChunk / 16)) = first;
+          *reinterpret_cast<uint2*>(at + mx4::image_code_at(in_tile, 1, rows_in_tile, col % kChunk / 16)) = second;
+        }, [&](int chunk, uint32_t first, uint32_t second) {
+          uint8_t* at = image + (size_t)chunk * Cfg::kImage;
+          *reinterpret_cast<uint32_t*>(at + mx4::row_scale_at<kRows>(in_tile, 0, rows_in_tile)) = first;
+          *reinterpret_cast<uint32_t*>(at + mx4::row_scale_at<kRows>(in_tile, 1, rows_in_tile)) = second;
+        });
+      }
+    }
+    fence_proxy_async_global();
+    named_sync(1, 128);
+    if (thread == 0) meeting.arrive(0);
+
     int acc = 0;
     uint32_t acc_phase = 0;
     bool ok = true;                  // a warp whose wait ran out still meets the others at every barrier below
-    for (int64_t p = share.begin; p < share.end;) {
-      const int64_t t = p / chunks;
-      const int k0 = (int)(p - t * chunks), k1 = (int)min((int64_t)chunks, k0 + share.end - p);
-      const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+    auto drain = [&](auto gate_up, const Share& share, int32_t* arrived_here, const Tile& tc, int64_t t, int k0, int k1, int chunks) {
       const int padded = round_up(tc.rows, 16);
       const bool whole = k1 - k0 == chunks;
       const int first = whole ? 0 : share.owner(t * chunks), last = whole ? 0 : share.owner((t + 1) * chunks - 1);
-      // a block's unfinished tiles: the one that it begins and does not end, and the one that another block began
-      auto part = [&](int block) { return partial + ((size_t)2 * block + (block == first)) * kMats * kRows * kTile; };
-      const int col0 = tc.m * kTile + quarter * 32;    // this warp's first output
-      uint8_t* scales = h.scale + ((size_t)tc.row_tile * m_tiles + tc.m) * kScaleTile;
-      ok = ok && __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, 64));
-      tc_fence_after_sync();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * Cfg::kAccCols;
-      for (int r = 0; ok && r < tc.rows; r += 16) {
-        uint32_t v[kMats][16], second[kMats][16];
+      // a block's unfinished tiles: the one that it begins and does not end, and the one that another block began
+      auto part = [&](int block) { return partial + ((size_t)2 * block + (block == first)) * 2 * kRows * kTile; };
+      auto read = [&](uint32_t (&v)[2][16], int r) {
+        uint32_t second[2][16];
 #pragma unroll
-        for (int m = 0; m < kMats; ++m) {
+        for (int m = 0; m < 2; ++m) {
           tmem_ld16(taddr + m * Cfg::kCols + r, v[m]);
           tmem_ld16(taddr + m * Cfg::kCols + padded + r, second[m]);
         }
         tmem_ld_wait();
 #pragma unroll
-        for (int m = 0; m < kMats; ++m)
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[m][i] = __float_as_uint(__uint_as_float(v[m][i]) + __uint_as_float(second[m][i]));
-        if (!whole) {
-          float* to = part(blockIdx.x);
+      };
+      auto finish = [&](uint32_t (&v)[2][16], int r) {
+        if constexpr (decltype(gate_up)::value) {
+          store_h_image<kRows>(h_image + ((size_t)tc.row_tile * f_chunks + tc.m) * Cfg::kImage, v[0], v[1], staging, r, tc.rows, quarter,
+                               lane);
+        } else {
 #pragma unroll
-          for (int m = 0; m < kMats; ++m)
+          for (int m = 0; m < 2; ++m) store_y(y, v[m], staging, tc.row0 + r, r, tc.rows, D, (2 * tc.m + m) * kTile + quarter * 32, lane);
+        }
+      };
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, 64));
+      tc_fence_after_sync();
+      bool join = false;
+      if (whole) {
+        for (int r = 0; ok && r < tc.rows; r += 16) {
+          uint32_t v[2][16];
+          read(v, r);
+          finish(v, r);
+        }
+      } else {
+        float* to = part(blockIdx.x);
+        for (int r = 0; ok && r < tc.rows; r += 16) {
+          uint32_t v[2][16];
+          read(v, r);
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               if (r + i < tc.rows) __stcg(to + (m * kRows + r + i) * kTile + thread, __uint_as_float(v[m][i]));
-        } else if constexpr (Cfg::kGateUp) {
-          store_h<kRows>(h, v[0], v[kMats - 1], staging, tc.row0 + r, r, tc.rows, h_pitch, col0, scales, quarter, lane);
-        } else {
-          store_y(y, v[0], staging, tc.row0 + r, r, tc.rows, n_dim, col0, lane);
         }
+        named_sync(1, 128);
+        if (thread == 0) {
+          __threadfence();
+          *is_last = !*abort_flag && atomicAdd(&arrived_here[first], 1) == last - first;
+          __threadfence();
+        }
+        named_sync(1, 128);
+        join = *is_last;
+        named_sync(1, 128);                            // is_last is read before it is written again
+      }
+      // the block that comes last adds the parts up, in the order of the blocks; its own it still has
+      for (int r = 0; join && r < tc.rows; r += 16) {
+        uint32_t own[2][16], v[2][16];
+        read(own, r);
+        for (int b = first; b <= last; ++b) {
+          const float* from = part(b);
+          const bool mine = b == (int)blockIdx.x;
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float add = __uint_as_float(own[m][i]);
+              if (!mine && r + i < tc.rows) add = __ldcg(from + (m * kRows + r + i) * kTile + thread);
+              v[m][i] = __float_as_uint(b == first ? add : __uint_as_float(v[m][i]) + add);
+            }
+        }
+        finish(v, r);
       }
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&acc_empty[acc]);
       acc ^= 1;
       if (acc == 0) acc_phase ^= 1u;
-      if (!whole) {
-        // the block that comes last adds the parts up, in the order of the blocks
-        __threadfence();
-        named_sync(1, 128);
-        if (thread == 0) *is_last = !*abort_flag && atomicAdd(&arrived[first], 1) == last - first;
-        named_sync(1, 128);
-        if (*is_last) {
-          __threadfence();
-          for (int r = 0; r < tc.rows; r += 16) {
-            uint32_t v[kMats][16];
-#pragma unroll
-            for (int m = 0; m < kMats; ++m)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) v[m][i] = 0;
-            for (int b = first; b <= last; ++b) {
-              const float* from = part(b);
-#pragma unroll
-              for (int m = 0; m < kMats; ++m)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                  if (r + i < tc.rows)
-                    v[m][i] = __float_as_uint(__uint_as_float(v[m][i]) + __ldcg(from + (m * kRows + r + i) * kTile + thread));
-            }
-            if constexpr (Cfg::kGateUp)
-              store_h<kRows>(h, v[0], v[kMats - 1], staging, tc.row0 + r, r, tc.rows, h_pitch, col0, scales, quarter, lane);
-            else
-              store_y(y, v[0], staging, tc.row0 + r, r, tc.rows, n_dim, col0, lane);
-          }
-        }
-        named_sync(1, 128);                            // is_last is read before it is written again
-      }
-      p += k1 - k0;
+      return true;
+    };
+    up_tiles([&](const Tile& tc, int64_t t, int k0, int k1) {
+      return drain(std::true_type(), up_share, arrived, tc, t, k0, k1, d_chunks);
+    });
+    fence_proxy_async_global();
+    named_sync(1, 128);
+    if (thread == 0) {
+      meeting.wait(0, abort_flag);                     // (a block without tiles comes here early)
+      meeting.arrive(1);
     }
+    down_tiles([&](const Tile& tc, int64_t t, int k0, int k1) {
+      return drain(std::false_type(), down_share, arrived + mx4::kMaxCtas, tc, t, k0, k1, f_chunks);
+    });
   }
 
   __syncwarp();
@@ -453,6 +604,10 @@ narrow_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__
     tmem_dealloc(tmem_base, Cfg::kTmemCols);
   }
 }
+
+struct Weights {
+  const uint8_t* scale[2];          // gate, up; or down
+};
 
 // ------------------------------------------------------------------------------------------- wide
 // A pair of CTAs works 256 weight rows x up to 224 rows of a slot; each CTA loads its 128 weight rows and half of the slot's
@@ -768,37 +923,41 @@ int tmap_failed(moegps_ctx* ctx) {
   return MOEGPS_ERR_CUDA;
 }
 
-template <int kRows>
 int launch_split(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   const moegps_shape_t& s = ctx->shape;
   const int64_t units = (c.l.rows / kSplitRows + s.S) * ((mx4::chunks_of(s.D) * kChunk + kSplitCols - 1) / kSplitCols);
   const int64_t resident = 8 * (int64_t)ctx->sm_count;
-  split_kernel<kRows><<<(unsigned)(units < resident ? units : resident), kSplitThreads, 0, st>>>(
-      static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert, s.S, s.E, s.D, (int)c.l.rows, c.x,
-      reinterpret_cast<int32_t*>(c.workspace + c.l.arrived), ctx->d_status);
-  MOEGPS_AFTER_LAUNCH(ctx, "rows=%d", kRows);
+  split_kernel<224><<<(unsigned)(units < resident ? units : resident), kSplitThreads, 0, st>>>(
+      static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert, s.S, s.E, s.D, (int)c.l.rows, c.x, ctx->d_status);
+  MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }
 
 template <class Cfg>
-int launch_narrow(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
+int launch_short(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   const moegps_shape_t& s = ctx->shape;
-  const int n_dim = Cfg::kGateUp ? s.F : s.D, k_dim = Cfg::kGateUp ? s.D : s.F;
-  const int cols = mx4::chunks_of(k_dim) * kChunk;
-  const mx4::Rows& in = Cfg::kGateUp ? c.x : c.h;
-  CUtensorMap w0, w1, r0, r1;
-  if (!moegps_make_tmap_codes4(&w0, Cfg::kGateUp ? c.gate4 : c.down4, s.E, n_dim, cols, kTile) ||
-      !moegps_make_tmap_codes4(&w1, Cfg::kGateUp ? c.up4 : c.down4, s.E, n_dim, cols, kTile) ||
-      !moegps_make_tmap_bytes(&r0, in.code[0], c.l.rows, cols, 16, true) ||
-      !moegps_make_tmap_bytes(&r1, in.code[1], c.l.rows, cols, 16, true))
+  const int dc = mx4::chunks_of(s.D) * kChunk, fc = mx4::chunks_of(s.F) * kChunk;
+  CUtensorMap gate, up, down;
+  if (!moegps_make_tmap_codes4(&gate, c.gate4, s.E, s.F, dc, kTile) || !moegps_make_tmap_codes4(&up, c.up4, s.E, s.F, dc, kTile) ||
+      !moegps_make_tmap_codes4(&down, c.down4, s.E, s.D, fc, kTile))
     return tmap_failed(ctx);
-  MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(narrow_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
-  const int grid = ctx->sm_count < mx4::kMaxCtas ? ctx->sm_count : mx4::kMaxCtas;
-  MOEGPS_CUDA_TRY(ctx, launch_after(narrow_kernel<Cfg>, dim3(grid), Cfg::kThreads, Cfg::kSmem, st, w0, w1, r0, r1,
-                                    Cfg::kGateUp ? c.up_scale : c.down_scale, in.scale, c.slot_row_off, c.slot_expert, s.S, s.E, n_dim,
-                                    k_dim, (int)c.l.rows, c.h, c.yp,
-                                    reinterpret_cast<int32_t*>(c.workspace + c.l.arrived) + (Cfg::kGateUp ? 0 : mx4::kMaxCtas),
-                                    reinterpret_cast<float*>(c.workspace + c.l.partial), ctx->d_status));
+  MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(short_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeCooperative;            // all blocks run at once: they wait for one another
+  attr.val.cooperative = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctx->sm_count < mx4::kMaxCtas ? ctx->sm_count : mx4::kMaxCtas);
+  cfg.blockDim = dim3(Cfg::kThreads);
+  cfg.dynamicSmemBytes = Cfg::kSmem;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  uint8_t* ws = c.workspace;
+  MOEGPS_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, short_kernel<Cfg>, gate, up, down, c.up_scale.scale[0], c.up_scale.scale[1],
+                                          c.down_scale.scale[0], static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert,
+                                          s.S, s.E, s.D, s.F, (int)c.l.rows, ws + c.l.x_code, ws + c.l.h_code, c.yp,
+                                          reinterpret_cast<int32_t*>(ws + c.l.arrived), reinterpret_cast<float*>(ws + c.l.partial),
+                                          ctx->d_meetings, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx, "rows=%d", Cfg::kRows);
   return MOEGPS_OK;
 }
@@ -843,23 +1002,10 @@ int moegps_launch_expert_ffn4(moegps_ctx* ctx, const void* xp, const int32_t* sl
   uint8_t* ws = c.workspace;
   c.x = {{ws + c.l.x_code, ws + c.l.x_code + c.l.x_code_bytes}, ws + c.l.x_scale};
   c.h = {{ws + c.l.h_code, ws + c.l.h_code + c.l.h_code_bytes}, ws + c.l.h_scale};
-  int rc = MOEGPS_OK;
-  switch (c.l.cut) {
-    case mx4::Cut::k16:
-      rc = launch_split<16>(ctx, c, st);
-      if (rc == MOEGPS_OK) rc = launch_narrow<Narrow<16, true, 5>>(ctx, c, st);
-      if (rc == MOEGPS_OK) rc = launch_narrow<Narrow<16, false, 10>>(ctx, c, st);
-      return rc;
-    case mx4::Cut::k48:
-      rc = launch_split<48>(ctx, c, st);
-      if (rc == MOEGPS_OK) rc = launch_narrow<Narrow<48, true, 4>>(ctx, c, st);
-      if (rc == MOEGPS_OK) rc = launch_narrow<Narrow<48, false, 7>>(ctx, c, st);
-      return rc;
-    case mx4::Cut::k224:
-      rc = launch_split<224>(ctx, c, st);
-      if (rc == MOEGPS_OK) rc = launch_wide<Wide<true>>(ctx, c, st);
-      if (rc == MOEGPS_OK) rc = launch_wide<Wide<false>>(ctx, c, st);
-      return rc;
-  }
-  return MOEGPS_ERR_UNSUPPORTED_SHAPE;
+  if (c.l.cut == mx4::Cut::k16) return launch_short<Short<16, 5>>(ctx, c, st);
+  if (c.l.cut == mx4::Cut::k48) return launch_short<Short<48, 4>>(ctx, c, st);
+  int rc = launch_split(ctx, c, st);
+  if (rc == MOEGPS_OK) rc = launch_wide<Wide<true>>(ctx, c, st);
+  if (rc == MOEGPS_OK) rc = launch_wide<Wide<false>>(ctx, c, st);
+  return rc;
 }

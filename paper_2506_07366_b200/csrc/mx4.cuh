@@ -93,11 +93,21 @@ __host__ __device__ constexpr int row_scale_at(int row, int term, int rows_in_ti
   return scale_byte_at(row + term * ((rows_in_tile + 15) / 16 * 16));
 }
 
-// Rows of activations in two terms: codes [rows][chunks * 128] for each, scales [row tile][chunk][kRowScaleBytes].
+// Tiles of 224 rows.  Rows of activations in two terms: codes [rows][chunks * 128] for each, scales [row tile][chunk]
+// [kRowScaleBytes].
 struct Rows {
   uint8_t* code[2];
   uint8_t* scale;
 };
+
+// Tiles of 16 or 48 rows: for each tile and chunk the image that the products want in shared memory, the scales and behind them
+// 128 bytes for each row, the first term's and then (from a multiple of 16 rows) the second's; the 16-byte pieces of a row are
+// swizzled by the row's number.
+template <int kRows>
+constexpr int kImageBytes = kScaleTile + 2 * kRows * kChunk;
+__host__ __device__ constexpr int image_code_at(int row, int term, int rows_in_tile, int piece) {
+  return kScaleTile + (row + term * ((rows_in_tile + 15) / 16 * 16)) * kChunk + ((piece ^ (row % 8)) * 16);
+}
 
 inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -106,30 +116,36 @@ constexpr int kMaxCtas = 148;      // blocks of a launch that joins partial sums
 struct Layout {
   Cut cut;
   int64_t rows, row_tiles;         // Rcap; tiles of rows at most
-  size_t x_code, x_scale, h_code, h_scale, arrived, partial, total;     // offsets (the second term's codes follow the first's)
+  // offsets: images, or codes (the second term's follow the first's) and scales; counts and parts of joined sums
+  size_t x_code, x_scale, h_code, h_scale, arrived, partial, total;
   size_t x_code_bytes, h_code_bytes;
-  size_t x_scale_bytes, h_scale_bytes;
 };
 
 inline Layout layout_of(const moegps_shape_t& s) {
   Layout l;
   l.cut = cut_of(s);
   const int n = rows_of(l.cut);
-  const size_t row_scales = n > 48 ? 4 * kScaleTile : kScaleTile;
   l.rows = (int64_t)s.T * s.K + (int64_t)s.S * (s.row_align - 1);
   l.row_tiles = l.rows / n + s.S;
-  l.x_code_bytes = align256((size_t)l.rows * chunks_of(s.D) * kChunk);
-  l.h_code_bytes = align256((size_t)l.rows * chunks_of(s.F) * kChunk);
-  l.x_scale_bytes = align256((size_t)l.row_tiles * chunks_of(s.D) * row_scales);
-  l.h_scale_bytes = align256((size_t)l.row_tiles * chunks_of(s.F) * row_scales);
+  const size_t dc = chunks_of(s.D), fc = chunks_of(s.F);
   l.x_code = 0;
-  l.x_scale = l.x_code + 2 * l.x_code_bytes;
-  l.h_code = l.x_scale + l.x_scale_bytes;
-  l.h_scale = l.h_code + 2 * l.h_code_bytes;
-  l.arrived = l.h_scale + l.h_scale_bytes;
+  if (l.cut == Cut::k224) {
+    const size_t scales = (size_t)l.row_tiles * kRowScaleBytes<224>;
+    l.x_code_bytes = align256((size_t)l.rows * dc * kChunk);
+    l.h_code_bytes = align256((size_t)l.rows * fc * kChunk);
+    l.x_scale = 2 * l.x_code_bytes;
+    l.h_code = l.x_scale + align256(scales * dc);
+    l.h_scale = l.h_code + 2 * l.h_code_bytes;
+    l.arrived = l.partial = l.total = l.h_scale + align256(scales * fc);
+    return l;
+  }
+  const size_t image = l.cut == Cut::k16 ? kImageBytes<16> : kImageBytes<48>;
+  l.x_code_bytes = align256(l.row_tiles * dc * image);
+  l.h_code_bytes = align256(l.row_tiles * fc * image);
+  l.h_code = l.x_code_bytes;
+  l.x_scale = l.h_scale = l.arrived = l.h_code + l.h_code_bytes;
   l.partial = l.arrived + align256(2 * kMaxCtas * sizeof(int32_t));
-  // each block leaves at most two unfinished tiles: 2 matrices x n rows x 128 fp32
-  l.total = l.partial + (n > 48 ? 0 : (size_t)kMaxCtas * 2 * 2 * n * kTile * sizeof(float));
+  l.total = l.partial + (size_t)kMaxCtas * 2 * 2 * n * kTile * sizeof(float);     // a block leaves at most two unfinished tiles
   return l;
 }
 
