@@ -152,11 +152,11 @@ constexpr int kStaging = 1024;
 
 // 16 rows of h = silu(g) u for a warp's 32 outputs (one for each lane; they are one block): codes into `staging`, the first
 // term's 16 rows of 32 bytes and then the second's; returns the scale byte of row lane % 16, lanes 0 to 15 of the first term's.
-__device__ __forceinline__ uint32_t encode_h(const uint32_t (&g)[16], const uint32_t (&u)[16], uint8_t* staging, int lane) {
+__device__ __forceinline__ uint32_t encode_h(const float (&g)[16], const float (&u)[16], uint8_t* staging, int lane) {
   uint32_t byte = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const float v = silu(__uint_as_float(g[i])) * __uint_as_float(u[i]);
+    const float v = silu(g[i]) * u[i];
     const uint32_t b1 = mx4::term_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
     const uint32_t b2 = mx4::second_scale(b1);
     uint32_t c1, c2;
@@ -172,7 +172,7 @@ __device__ __forceinline__ uint32_t encode_h(const uint32_t (&g)[16], const uint
 // They go to rows of `pitch` bytes; row: the first one's place there, in_tile: in its tile of `rows`; col0: the first lane's
 // column; scales: of the tile and its chunk; block: which of the chunk's four.
 template <int kRows>
-__device__ __forceinline__ void store_h(const mx4::Rows& h, const uint32_t (&g)[16], const uint32_t (&u)[16], uint8_t* staging,
+__device__ __forceinline__ void store_h(const mx4::Rows& h, const float (&g)[16], const float (&u)[16], uint8_t* staging,
                                         int row, int in_tile, int rows, size_t pitch, int col0, uint8_t* scales, int block, int lane) {
   const uint32_t byte = encode_h(g, u, staging, lane);
   const int r = lane >> 1;                             // two lanes for each row
@@ -189,7 +189,7 @@ __device__ __forceinline__ void store_h(const mx4::Rows& h, const uint32_t (&g)[
 
 // ... or into the image of the tile's chunk.
 template <int kRows>
-__device__ __forceinline__ void store_h_image(uint8_t* image, const uint32_t (&g)[16], const uint32_t (&u)[16], uint8_t* staging,
+__device__ __forceinline__ void store_h_image(uint8_t* image, const float (&g)[16], const float (&u)[16], uint8_t* staging,
                                               int in_tile, int rows, int block, int lane) {
   const uint32_t byte = encode_h(g, u, staging, lane);
   const int r = in_tile + (lane >> 1);
@@ -205,11 +205,11 @@ __device__ __forceinline__ void store_h_image(uint8_t* image, const uint32_t (&g
 }
 
 // 16 rows of y for a warp's 32 outputs, col0 the first
-__device__ __forceinline__ void store_y(__nv_bfloat16* __restrict__ y, const uint32_t (&v)[16], uint8_t* staging, int row, int in_tile,
+__device__ __forceinline__ void store_y(__nv_bfloat16* __restrict__ y, const float (&v)[16], uint8_t* staging, int row, int in_tile,
                                         int rows, int D, int col0, int lane) {
 #pragma unroll
   for (int i = 0; i < 16; ++i)
-    reinterpret_cast<__nv_bfloat16*>(staging)[i * 32 + lane] = __float2bfloat16_rn(__uint_as_float(v[i]));
+    reinterpret_cast<__nv_bfloat16*>(staging)[i * 32 + lane] = __float2bfloat16_rn(v[i]);
   __syncwarp();
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -223,11 +223,14 @@ __device__ __forceinline__ void store_y(__nv_bfloat16* __restrict__ y, const uin
 // ------------------------------------------------------------------------------------------- short slots
 // The whole FFN in one launch, for slots of few rows: what there is to do is to read the weights, and three launches in a row
 // cost 35 us beside the 29 that two 4096 x 14336 experts take to read (each has to start, build its tables, fill its ring and join
-// its sums).  The blocks (one for each SM, a cooperative launch) wait for one another twice, when the rows are split and when
-// h is there; the weights of the next product are loaded meanwhile.
+// its sums).  The blocks are one for each SM, a cooperative launch, and wait for one another: all for all when the rows are split,
+// then for the parts of h that they need; the weights of the next product are loaded meanwhile.
 //  - A tile is two weight tiles of 128 outputs (gate and up of the same outputs, or two neighbours of down) times the rows of a
-//    slot.  The K steps of all tiles are dealt evenly to the blocks, whatever their number; a tile that several blocks share is
-//    joined by the one that finishes last.
+//    slot.  The K steps of all tiles are dealt evenly to the blocks, whatever their number.  Sums that several blocks share are
+//    added up in the order of the blocks, by the one that begins the tile: it is the last tile of that block and the first of the
+//    other (there are mostly two), whose part is there by then.  A tile of down that three or more share is added up by all of
+//    them, some of the rows each, at the end.  (Joined by the block that came last, behind a fence and an atomic count, it took 5.5
+//    us at the end of each product; down by the first of five blocks 8, and two blocks that add up half of the rows each 6.6.)
 //  - Both terms of a row are columns of one MMA (of few columns it takes 40 clocks whatever their number: it waits for its 128
 //    weight rows), side by side in the accumulator, and added up in the epilogue.
 //  - x and h lie in the workspace as the images that a chunk of a tile has in shared memory (512 bytes of scales, then 128-byte
@@ -259,47 +262,81 @@ struct Short {
   static_assert(kSmem > 114 * 1024, "one block for each SM: the blocks wait for one another");
 };
 
-// What a block does of all K steps, [begin, end) of the tiles one after the other, and who shares a tile with it.
+// What a block does of all K steps, [begin, end) of the tiles one after the other, from step `chunk` of tile `tile`.  (A 64-bit
+// division takes half a microsecond: these are the only ones, and 32-bit ones where they can be.)
 struct Share {
-  int64_t steps;                    // of all tiles
-  int blocks;                       // that have any
-  int64_t begin, end;
-  __device__ Share(int64_t steps_, int grid, int block) : steps(steps_), blocks((int)min((int64_t)grid, steps_)) {
-    begin = end = 0;
-    if (block < blocks) {
-      begin = steps * block / blocks;
-      end = steps * (block + 1) / blocks;
+  int64_t each;                     // steps of a block, one more in the first `more`
+  int blocks, more;                 // blocks: that have any
+  int64_t begin, end, tile;
+  int chunk;
+  __device__ Share(int64_t steps, int chunks, int grid, int block) {
+    blocks = (int)min((int64_t)grid, steps);
+    each = begin = end = tile = more = chunk = 0;
+    if (block >= blocks) return;
+    if (steps >> 32) {
+      each = steps / blocks;
+      more = (int)(steps % blocks);
+    } else {
+      each = (uint32_t)steps / (uint32_t)blocks;
+      more = (uint32_t)steps % (uint32_t)blocks;
     }
+    begin = begin_of(block);
+    end = begin_of(block + 1);
+    tile = begin >> 32 ? begin / chunks : (uint32_t)begin / (uint32_t)chunks;
+    chunk = (int)(begin - tile * chunks);
   }
-  // the block that has step p: the last one that begins at or before it
-  __device__ int owner(int64_t p) const { return (int)(((p + 1) * blocks - 1) / steps); }
+  __device__ int64_t begin_of(int b) const { return b * each + min(b, more); }
+  // the blocks that share a tile of block b
+  __device__ int first_of(int64_t t, int chunks, int b) const {
+    while (begin_of(b) > t * chunks) --b;
+    return b;
+  }
+  __device__ int last_of(int64_t t, int chunks, int b) const {
+    while (begin_of(b + 1) < (t + 1) * chunks) ++b;
+    return b;
+  }
 };
 
-// The blocks' barrier: a count in the context's memory that only grows, by the number of blocks for each meeting.
+__device__ __forceinline__ unsigned long long load_acquire(const unsigned long long* p) {
+  unsigned long long v;
+  asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ int load_acquire(const int* p) {
+  int v;
+  asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add_release(int* p, int n) {
+  asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(p), "r"(n) : "memory");
+}
+
+// polls until ready() holds, for a limited time
+template <class Ready>
+__device__ __forceinline__ bool poll(volatile int* abort_flag, Ready&& ready) {
+  const long long t0 = clock64();
+  while (!ready()) {
+    if (*abort_flag) return false;
+    if (clock64() - t0 > kWaitLimitCycles) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+  return true;
+}
+
+// The blocks' barrier, once in a launch: a count in the context's memory that only grows, by the number of blocks each time.
 struct Meeting {
   unsigned long long* count;
-  volatile unsigned long long* goal;               // [2], shared memory: what the count is when all have come; 0 = not here yet
+  volatile unsigned long long* goal;               // shared memory: what the count is when all have come; 0 = not here yet
   // by one thread, after a barrier behind the others' writes
-  __device__ void arrive(int which) const {
+  __device__ void arrive() const {
     __threadfence();
     const unsigned long long n = gridDim.x, old = atomicAdd(count, 1ull);
-    goal[which] = (old / n + 1) * n;
+    *goal = (old / n + 1) * n;
   }
-  __device__ bool wait(int which, volatile int* abort_flag) const {
-    const long long t0 = clock64();
-    while (true) {
-      const unsigned long long want = goal[which];
-      if (want) {
-        unsigned long long now;
-        asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(now) : "l"(count) : "memory");
-        if (now >= want) return true;
-      }
-      if (*abort_flag) return false;
-      if (clock64() - t0 > kWaitLimitCycles) {
-        *abort_flag = 1;
-        return false;
-      }
-    }
+  __device__ bool wait(volatile int* abort_flag) const {
+    return poll(abort_flag, [&]() { const unsigned long long want = *goal; return want && load_acquire(count) >= want; });
   }
 };
 
@@ -312,7 +349,7 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
              const __grid_constant__ CUtensorMap tm_down, const uint8_t* __restrict__ gate_scale, const uint8_t* __restrict__ up_scale,
              const uint8_t* __restrict__ down_scale, const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off,
              const int32_t* __restrict__ slot_expert, int S, int E, int D, int F, int rcap, uint8_t* x_image, uint8_t* h_image,
-             __nv_bfloat16* __restrict__ y, int32_t* arrived, float* partial, unsigned long long* meetings,
+             __nv_bfloat16* __restrict__ y, int* part_there, int* h_there, float* partial, unsigned long long* meetings,
              int32_t* __restrict__ status) {
   constexpr int kRows = Cfg::kRows, kStages = Cfg::kStages;
   extern __shared__ uint8_t smem_raw[];
@@ -323,18 +360,18 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
   uint64_t* empty = full + kStages;                  // [kStages]  both issuing warps -> loaders
   uint64_t* acc_full = empty + kStages;              // [2]  both issuing warps -> epilogue
   uint64_t* acc_empty = acc_full + 2;                // [2]
-  volatile unsigned long long* goal = reinterpret_cast<volatile unsigned long long*>(acc_empty + 2);      // [2]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 4);
+  volatile unsigned long long* goal = reinterpret_cast<volatile unsigned long long*>(acc_empty + 2);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 3);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  volatile int* is_last = abort_flag + 1;
-  static_assert((2 * kStages + 6) * 8 + 12 <= 256, "barriers fit their space");
+  static_assert((2 * kStages + 5) * 8 + 8 <= 256, "barriers fit their space");
 
   const int warp = uniform_warp_index(), lane = threadIdx.x & 31;
   const int d_chunks = mx4::chunks_of(D), f_chunks = mx4::chunks_of(F);      // f_chunks also the tiles of gate + up
   const int d_tiles = (d_chunks + 1) / 2;                                    // of down
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 2); mbar_init(&empty[i], 2); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 2); mbar_init(&acc_empty[i], 4); goal[i] = 0; }
+    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 2); mbar_init(&acc_empty[i], 4); }
+    *goal = 0;
     *abort_flag = 0;
     fence_mbar_init();
     prefetch_tensormap(&tm_gate);
@@ -345,24 +382,23 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
     tmem_alloc(tmem_slot, Cfg::kTmemCols);
     tmem_relinquish();
   }
-  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status);
-  build_tables<Cfg::kThreads, 1>(rows_before, slot_row_off, slot_expert, S, E, 1, rcap, status);
+  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status, &rows_before);
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
   const int64_t row_tiles = tb.tile_base[S];
-  const Share up_share(row_tiles * f_chunks * d_chunks, gridDim.x, blockIdx.x);
-  const Share down_share(row_tiles * d_tiles * f_chunks, gridDim.x, blockIdx.x);
+  const Share up_share(row_tiles * f_chunks * d_chunks, d_chunks, gridDim.x, blockIdx.x);
+  const Share down_share(row_tiles * d_tiles * f_chunks, f_chunks, gridDim.x, blockIdx.x);
   const Meeting meeting = {meetings, goal};
 
   // calls body(tile, its number, k0, k1) for each tile, or part of one, of this block
   auto for_tiles = [&](const Share& share, int m_tiles, int chunks, auto&& body) {
-    for (int64_t p = share.begin; p < share.end;) {
-      const int64_t t = p / chunks;
-      const int k0 = (int)(p - t * chunks), k1 = (int)min((int64_t)chunks, k0 + share.end - p);
+    int64_t t = share.tile, left = share.end - share.begin;
+    for (int k0 = share.chunk; left > 0; k0 = 0, ++t) {
+      const int k1 = (int)min((int64_t)chunks, k0 + left);
       if (!body(tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles), t, k0, k1)) return false;
-      p += k1 - k0;
+      left -= k1 - k0;
     }
     return true;
   };
@@ -401,28 +437,42 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
       if (!ok) linger();
     }
   } else if (warp == 2) {
+    int stage = 0;
+    uint32_t phase = 0;
+    // by one lane
+    auto load = [&](const uint8_t* image, const Tile& tc, int chunks, int k0, int k1) {
+      const uint32_t bytes = kScaleTile + 2 * round_up(tc.rows, 16) * kChunk;
+      const uint8_t* from = image + ((size_t)tc.row_tile * chunks + k0) * Cfg::kImage;
+      for (int c = k0; c < k1; ++c, from += Cfg::kImage) {
+        if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag)) return false;
+        mbar_arrive_expect_tx(&full[stage], bytes);
+        bulk_load(smem + stage * Cfg::kStageBytes + Cfg::kImageAt, from, bytes, &full[stage]);
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      }
+      return true;
+    };
+    bool ok = true;
     if (lane == 0) {
-      int stage = 0;
-      uint32_t phase = 0;
-      auto load = [&](const uint8_t* image, const Tile& tc, int chunks, int k0, int k1) {
-        const uint32_t bytes = kScaleTile + 2 * round_up(tc.rows, 16) * kChunk;
-        const uint8_t* from = image + ((size_t)tc.row_tile * chunks + k0) * Cfg::kImage;
-        for (int c = k0; c < k1; ++c, from += Cfg::kImage) {
-          if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag)) return false;
-          mbar_arrive_expect_tx(&full[stage], bytes);
-          bulk_load(smem + stage * Cfg::kStageBytes + Cfg::kImageAt, from, bytes, &full[stage]);
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
-        }
-        return true;
-      };
-      bool ok = meeting.wait(0, abort_flag);
+      ok = meeting.wait(abort_flag);
       fence_proxy_async_global();
       ok = ok && up_tiles([&](const Tile& tc, int64_t, int k0, int k1) { return load(x_image, tc, d_chunks, k0, k1); });
-      ok = ok && meeting.wait(1, abort_flag);
-      fence_proxy_async_global();
-      ok = ok && down_tiles([&](const Tile& tc, int64_t, int k0, int k1) { return load(h_image, tc, f_chunks, k0, k1); });
-      if (!ok) linger();
     }
+    ok = __all_sync(0xffffffffu, ok);
+    // 32 chunks of h at a time, when the four warps that wrote each have reported
+    ok = ok && down_tiles([&](const Tile& tc, int64_t, int k0, int k1) {
+      for (int c = k0; c < k1; c += 32) {
+        const int* there = h_there + (size_t)tc.row_tile * f_chunks + min(c + lane, k1 - 1);
+        bool go = poll(abort_flag, [&]() { return load_acquire(there) == 4; });
+        go = __all_sync(0xffffffffu, go);
+        if (lane == 0 && go) {
+          fence_proxy_async_global();
+          go = load(h_image, tc, f_chunks, c, min(c + 32, k1));
+        }
+        if (!__all_sync(0xffffffffu, go)) return false;
+      }
+      return true;
+    });
+    if (!ok && lane == 0) linger();
   } else if (warp == 1 || warp == 3) {
     const int which = warp >> 1;                       // of the two weight tiles
     const uint32_t base = smem_u32(smem);
@@ -466,7 +516,8 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
     uint8_t* staging = smem + Cfg::kStagingOffset + quarter * kStaging;
     // x in two terms: a warp does 1024 columns of a row
     {
-      if (thread < 2) arrived[thread * mx4::kMaxCtas + blockIdx.x] = 0;
+      if (thread < 3) part_there[thread * mx4::kMaxCtas + blockIdx.x] = 0;
+      for (int64_t i = (int64_t)blockIdx.x * 128 + thread; i < row_tiles * f_chunks; i += 128 * (int64_t)gridDim.x) h_there[i] = 0;
       const int col_blocks = (d_chunks * kChunk + kSplitCols - 1) / kSplitCols;
       const int64_t work = (int64_t)rows_before.tile_base[S] * col_blocks;
       for (int64_t b = (int64_t)quarter * gridDim.x + blockIdx.x; b < work; b += 4 * (int64_t)gridDim.x) {
@@ -492,106 +543,136 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
     }
     fence_proxy_async_global();
     named_sync(1, 128);
-    if (thread == 0) meeting.arrive(0);
+    if (thread == 0) meeting.arrive();
 
     int acc = 0;
     uint32_t acc_phase = 0;
-    bool ok = true;                  // a warp whose wait ran out still meets the others at every barrier below
-    auto drain = [&](auto gate_up, const Share& share, int32_t* arrived_here, const Tile& tc, int64_t t, int k0, int k1, int chunks) {
+    bool ok = true;
+    // what a block leaves of a tile that it shares: 0 of gate + up, begun by another, of down 1 begun by another, 2 begun by itself;
+    // the four warps count when it is there
+    auto there_of = [&](int which, int block) { return part_there + which * mx4::kMaxCtas + block; };
+    auto part = [&](int which, int block) { return partial + ((size_t)which * mx4::kMaxCtas + block) * 2 * kRows * kTile + thread; };
+    auto drain = [&](auto gate_up, const Share& share, const Tile& tc, int64_t t, int k0, int k1, int chunks) {
+      constexpr bool kGateUp = decltype(gate_up)::value;
       const int padded = round_up(tc.rows, 16);
-      const bool whole = k1 - k0 == chunks;
-      const int first = whole ? 0 : share.owner(t * chunks), last = whole ? 0 : share.owner((t + 1) * chunks - 1);
+      const int first = share.first_of(t, chunks, blockIdx.x), last = share.last_of(t, chunks, blockIdx.x);
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * Cfg::kAccCols;
-      // a block's unfinished tiles: the one that it begins and does not end, and the one that another block began
-      auto part = [&](int block) { return partial + ((size_t)2 * block + (block == first)) * 2 * kRows * kTile; };
-      auto read = [&](uint32_t (&v)[2][16], int r) {
-        uint32_t second[2][16];
+      auto read = [&](float (&v)[2][16], int r) {
+        uint32_t term[2][2][16];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-          tmem_ld16(taddr + m * Cfg::kCols + r, v[m]);
-          tmem_ld16(taddr + m * Cfg::kCols + padded + r, second[m]);
+          tmem_ld16(taddr + m * Cfg::kCols + r, term[m][0]);
+          tmem_ld16(taddr + m * Cfg::kCols + padded + r, term[m][1]);
         }
         tmem_ld_wait();
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[m][i] = __float_as_uint(__uint_as_float(v[m][i]) + __uint_as_float(second[m][i]));
+          for (int i = 0; i < 16; ++i) v[m][i] = __uint_as_float(term[m][0][i]) + __uint_as_float(term[m][1][i]);
       };
-      auto finish = [&](uint32_t (&v)[2][16], int r) {
-        if constexpr (decltype(gate_up)::value) {
-          store_h_image<kRows>(h_image + ((size_t)tc.row_tile * f_chunks + tc.m) * Cfg::kImage, v[0], v[1], staging, r, tc.rows, quarter,
-                               lane);
-        } else {
+      // what the other blocks have of 16 rows
+      auto others = [&](float (&v)[2][16], int r) {
 #pragma unroll
-          for (int m = 0; m < 2; ++m) store_y(y, v[m], staging, tc.row0 + r, r, tc.rows, D, (2 * tc.m + m) * kTile + quarter * 32, lane);
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[m][i] = 0.0f;
+        for (int b = first + 1; b <= last; ++b) {
+          const float* from = part(kGateUp ? 0 : 1, b);
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (r + i < tc.rows) v[m][i] += __ldcg(from + (m * kRows + r + i) * kTile);
         }
       };
-      ok = ok && __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, 64));
-      tc_fence_after_sync();
-      bool join = false;
-      if (whole) {
+      if (first == (int)blockIdx.x && (kGateUp || last <= first + 1)) {
+        float rest[2][16];
+        if (last > first && lane == 0)
+          for (int b = first + 1; ok && b <= last; ++b) ok = poll(abort_flag, [&]() { return load_acquire(there_of(kGateUp ? 0 : 1, b)) == 4; });
+        ok = __all_sync(0xffffffffu, ok);
+        if (ok) others(rest, 0);                       // under way while its own part is still being added up
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, 64));
+        tc_fence_after_sync();
         for (int r = 0; ok && r < tc.rows; r += 16) {
-          uint32_t v[2][16];
+          float v[2][16];
+          if (r > 0) others(rest, r);
           read(v, r);
-          finish(v, r);
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[m][i] += rest[m][i];
+          if constexpr (kGateUp) {
+            store_h_image<kRows>(h_image + ((size_t)tc.row_tile * f_chunks + tc.m) * Cfg::kImage, v[0], v[1], staging, r, tc.rows,
+                                 quarter, lane);
+          } else {
+#pragma unroll
+            for (int m = 0; m < 2; ++m) store_y(y, v[m], staging, tc.row0 + r, r, tc.rows, D, (2 * tc.m + m) * kTile + quarter * 32, lane);
+          }
+        }
+        if (kGateUp) {
+          fence_proxy_async_global();
+          __syncwarp();
+          if (lane == 0 && ok) add_release(h_there + (size_t)tc.row_tile * f_chunks + tc.m, 1);
         }
       } else {
-        float* to = part(blockIdx.x);
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, 64));
+        tc_fence_after_sync();
+        const int which = kGateUp ? 0 : 1 + (first == (int)blockIdx.x);
+        float* to = part(which, blockIdx.x);
         for (int r = 0; ok && r < tc.rows; r += 16) {
-          uint32_t v[2][16];
+          float v[2][16];
           read(v, r);
 #pragma unroll
           for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (r + i < tc.rows) __stcg(to + (m * kRows + r + i) * kTile + thread, __uint_as_float(v[m][i]));
+              if (r + i < tc.rows) __stcg(to + (m * kRows + r + i) * kTile, v[m][i]);
         }
-        named_sync(1, 128);
-        if (thread == 0) {
-          __threadfence();
-          *is_last = !*abort_flag && atomicAdd(&arrived_here[first], 1) == last - first;
-          __threadfence();
-        }
-        named_sync(1, 128);
-        join = *is_last;
-        named_sync(1, 128);                            // is_last is read before it is written again
-      }
-      // the block that comes last adds the parts up, in the order of the blocks; its own it still has
-      for (int r = 0; join && r < tc.rows; r += 16) {
-        uint32_t own[2][16], v[2][16];
-        read(own, r);
-        for (int b = first; b <= last; ++b) {
-          const float* from = part(b);
-          const bool mine = b == (int)blockIdx.x;
-#pragma unroll
-          for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float add = __uint_as_float(own[m][i]);
-              if (!mine && r + i < tc.rows) add = __ldcg(from + (m * kRows + r + i) * kTile + thread);
-              v[m][i] = __float_as_uint(b == first ? add : __uint_as_float(v[m][i]) + add);
-            }
-        }
-        finish(v, r);
+        __syncwarp();
+        if (lane == 0 && ok) add_release(there_of(which, blockIdx.x), 1);
       }
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&acc_empty[acc]);
       acc ^= 1;
       if (acc == 0) acc_phase ^= 1u;
-      return true;
+      return ok;
     };
-    up_tiles([&](const Tile& tc, int64_t t, int k0, int k1) {
-      return drain(std::true_type(), up_share, arrived, tc, t, k0, k1, d_chunks);
+    if (lane == 0) ok = meeting.wait(abort_flag);      // the counts that are added to below have been set to zero
+    ok = __all_sync(0xffffffffu, ok);
+    ok = ok && up_tiles([&](const Tile& tc, int64_t t, int k0, int k1) {
+      return drain(std::true_type(), up_share, tc, t, k0, k1, d_chunks);
     });
-    fence_proxy_async_global();
-    named_sync(1, 128);
-    if (thread == 0) {
-      meeting.wait(0, abort_flag);                     // (a block without tiles comes here early)
-      meeting.arrive(1);
-    }
-    down_tiles([&](const Tile& tc, int64_t t, int k0, int k1) {
-      return drain(std::false_type(), down_share, arrived + mx4::kMaxCtas, tc, t, k0, k1, f_chunks);
+    ok = ok && down_tiles([&](const Tile& tc, int64_t t, int k0, int k1) {
+      return drain(std::false_type(), down_share, tc, t, k0, k1, f_chunks);
+    });
+    ok = ok && down_tiles([&](const Tile& tc, int64_t t, int k0, int k1) {
+      const int first = down_share.first_of(t, f_chunks, blockIdx.x), last = down_share.last_of(t, f_chunks, blockIdx.x);
+      const int n = last - first + 1, i = (int)blockIdx.x - first, end = tc.rows * (i + 1) / n;
+      if (n <= 2) return true;
+      for (int b = first + lane; ok && b <= last; b += 32)
+        ok = poll(abort_flag, [&]() { return load_acquire(there_of(1 + (b == first), b)) == 4; });
+      ok = __all_sync(0xffffffffu, ok);
+      for (int r = tc.rows * i / n; ok && r < end; r += 4) {
+        float v[2][4] = {};
+#pragma unroll 4
+        for (int b = first; b <= last; ++b) {
+          const float* from = part(1 + (b == first), b);
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (r + j < end) v[m][j] += __ldcg(from + (m * kRows + r + j) * kTile);
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const int col = (2 * tc.m + m) * kTile + thread;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (r + j < end && col < D) y[(size_t)(tc.row0 + r + j) * D + col] = __float2bfloat16_rn(v[m][j]);
+        }
+      }
+      return ok;
     });
   }
 
@@ -860,18 +941,22 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
         for (int i = 0; i < half; i += 16) {
           // the gate's warps finish the first half of the rows, the up's the second
           const int mine = up ? half + i : i, other = up ? i : half + i;
-          uint32_t v[16], give[16], get[16];
+          uint32_t give[16], keep[16];
           if (ok) {
             tmem_ld16(taddr + other, give);
-            tmem_ld16(taddr + mine, v);
+            tmem_ld16(taddr + mine, keep);
             tmem_ld_wait();
           }
           float* buffer = exchange + turn * 16 * 32 + lane;            // of warp 0; a warp has 2 * 16 * 32
 #pragma unroll
           for (int j = 0; j < 16; ++j) buffer[quarter * 1024 + j * 32] = __uint_as_float(give[j]);
+          float v[16], get[16];
           named_sync(1 + (quarter & 1), 64);           // (before a buffer is written again both have met here once more)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) get[j] = __float_as_uint(buffer[(quarter ^ 2) * 1024 + j * 32]);
+          for (int j = 0; j < 16; ++j) {
+            get[j] = buffer[(quarter ^ 2) * 1024 + j * 32];
+            v[j] = __uint_as_float(keep[j]);
+          }
           turn ^= 1;
           if (!ok) continue;
           if (up)
@@ -882,9 +967,12 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
       } else {
         const int col0 = tc.m * Cfg::kOutputs + rank * kTile + quarter * 32;
         for (int r = 0; ok && r < tc.rows; r += 16) {
-          uint32_t v[16];
-          tmem_ld16(taddr + r, v);
+          uint32_t bits[16];
+          float v[16];
+          tmem_ld16(taddr + r, bits);
           tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(bits[i]);
           store_y(y, v, staging, tc.row0 + r, r, tc.rows, n_dim, col0, lane);
         }
       }
@@ -956,7 +1044,8 @@ int launch_short(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   MOEGPS_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, short_kernel<Cfg>, gate, up, down, c.up_scale.scale[0], c.up_scale.scale[1],
                                           c.down_scale.scale[0], static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert,
                                           s.S, s.E, s.D, s.F, (int)c.l.rows, ws + c.l.x_code, ws + c.l.h_code, c.yp,
-                                          reinterpret_cast<int32_t*>(ws + c.l.arrived), reinterpret_cast<float*>(ws + c.l.partial),
+                                          reinterpret_cast<int*>(ws + c.l.part_there), reinterpret_cast<int*>(ws + c.l.h_there),
+                                          reinterpret_cast<float*>(ws + c.l.partial),
                                           ctx->d_meetings, ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx, "rows=%d", Cfg::kRows);
   return MOEGPS_OK;

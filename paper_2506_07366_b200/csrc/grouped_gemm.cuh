@@ -106,10 +106,11 @@ __device__ __forceinline__ void store_chunk(const uint32_t (&o)[16], uint8_t* st
 // all 1024 this took over 2 us of a 12 us launch on an 8-slot layer.
 // A slot whose extent is not inside [0, rcap] (offsets negative, decreasing or past the buffers) gets no
 // tiles: nothing is read or written for it, and the caller is told.
+// rows_before (optional): the same for the rows of the slots that have tiles.
 template <int kThreads, int kRows = BM>       // kRows: rows of a tile
 __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restrict__ slot_row_off,
                                              const int32_t* __restrict__ slot_expert, int S, int E, int n_tiles, int rcap,
-                                             int32_t* __restrict__ status) {
+                                             int32_t* __restrict__ status, Tables* rows_before = nullptr) {
   for (int s = threadIdx.x; s < S; s += kThreads) {
     int cnt = 0;
     const int lo = slot_row_off[s], hi = slot_row_off[s + 1];
@@ -122,13 +123,15 @@ __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restri
       if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
     }
     tb.tile_base[s] = cnt;
+    if (rows_before) rows_before->tile_base[s] = cnt ? hi - lo : 0;
   }
   __syncthreads();
-  // exclusive prefix sum of the counts (warp 0: lane l owns `per` consecutive entries)
-  if (threadIdx.x < 32) {
-    const int lane = threadIdx.x, per = (S + 31) / 32, first = min(lane * per, S), last = min(first + per, S);
+  // exclusive prefix sums of the counts, a warp for each table (lane l owns `per` consecutive entries)
+  if (threadIdx.x < (rows_before ? 64 : 32)) {
+    int32_t* base = threadIdx.x < 32 ? tb.tile_base : rows_before->tile_base;
+    const int lane = threadIdx.x & 31, per = (S + 31) / 32, first = min(lane * per, S), last = min(first + per, S);
     int sum = 0;
-    for (int s = first; s < last; ++s) sum += tb.tile_base[s];
+    for (int s = first; s < last; ++s) sum += base[s];
     int incl = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -137,11 +140,11 @@ __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restri
     }
     int run = incl - sum;
     for (int s = first; s < last; ++s) {
-      const int v = tb.tile_base[s];
-      tb.tile_base[s] = run;
+      const int v = base[s];
+      base[s] = run;
       run += v;
     }
-    if (lane == 31) tb.tile_base[S] = incl;
+    if (lane == 31) base[S] = incl;
   }
 }
 

@@ -116,8 +116,8 @@ constexpr int kMaxCtas = 148;      // blocks of a launch that joins partial sums
 struct Layout {
   Cut cut;
   int64_t rows, row_tiles;         // Rcap; tiles of rows at most
-  // offsets: images, or codes (the second term's follow the first's) and scales; counts and parts of joined sums
-  size_t x_code, x_scale, h_code, h_scale, arrived, partial, total;
+  // offsets: images, or codes (the second term's follow the first's) and scales; what of h and of shared sums is there, their parts
+  size_t x_code, x_scale, h_code, h_scale, part_there, h_there, partial, total;
   size_t x_code_bytes, h_code_bytes;
 };
 
@@ -136,16 +136,18 @@ inline Layout layout_of(const moegps_shape_t& s) {
     l.x_scale = 2 * l.x_code_bytes;
     l.h_code = l.x_scale + align256(scales * dc);
     l.h_scale = l.h_code + 2 * l.h_code_bytes;
-    l.arrived = l.partial = l.total = l.h_scale + align256(scales * fc);
+    l.part_there = l.h_there = l.partial = l.total = l.h_scale + align256(scales * fc);
     return l;
   }
   const size_t image = l.cut == Cut::k16 ? kImageBytes<16> : kImageBytes<48>;
   l.x_code_bytes = align256(l.row_tiles * dc * image);
   l.h_code_bytes = align256(l.row_tiles * fc * image);
   l.h_code = l.x_code_bytes;
-  l.x_scale = l.h_scale = l.arrived = l.h_code + l.h_code_bytes;
-  l.partial = l.arrived + align256(2 * kMaxCtas * sizeof(int32_t));
-  l.total = l.partial + (size_t)kMaxCtas * 2 * 2 * n * kTile * sizeof(float);     // a block leaves at most two unfinished tiles
+  l.x_scale = l.h_scale = l.part_there = l.h_code + l.h_code_bytes;
+  l.h_there = l.part_there + align256(3 * kMaxCtas * sizeof(int32_t));
+  l.partial = l.h_there + align256(l.row_tiles * fc * sizeof(int32_t));
+  // a block leaves at most one unfinished tile of gate + up behind and two of down
+  l.total = l.partial + (size_t)kMaxCtas * 3 * 2 * n * kTile * sizeof(float);
   return l;
 }
 
