@@ -8,8 +8,8 @@
 // groups by the TMA load that brings it (8 bytes of codes, 8 unused): 8 KB of memory traffic for 16 KB of shared memory,
 // and no thread touches a weight.  The scales of the rows lie in the workspace as tensor memory wants them, tile by tile.
 //
-// Two ways, by rows for each slot (mx4::cut_of): up to 48 one launch that is bound by reading weights (short_kernel), beyond
-// that three that are bound by products (split_kernel, wide_kernel twice).  Every wait is bounded.
+// Two ways, side by side in a call or one for all slots (mx4::cut_of): for slots of few rows one launch that is bound by reading
+// weights (short_kernel), for long ones three that are bound by products (split_kernel, wide_kernel twice).  Every wait is bounded.
 #include <type_traits>
 
 #include "common.cuh"
@@ -61,8 +61,7 @@ __device__ __forceinline__ void linger() {
 
 // ------------------------------------------------------------------------------------------- split
 constexpr int kSplitThreads = 256;
-constexpr int kSplitRows = 8;      // rows of a block's unit: one for each warp
-constexpr int kSplitCols = 1024;   // its columns
+constexpr int kSplitCols = 1024;   // columns of a row that a warp does at a time
 
 // Columns col0 .. col0 + 1023 of a row by a warp: codes(column, first term's eight codes, second term's) for each lane's
 // eight columns, scales(chunk, word of the first term's four scale bytes, of the second's) once for each chunk.
@@ -89,7 +88,7 @@ __device__ __forceinline__ void split_row(const __nv_bfloat16* __restrict__ x, i
     uint32_t c1[4], c2[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      mx4::split2(__uint_as_float(words[j] << 16), __uint_as_float(words[j] & 0xffff0000u), inv, ratio, c1[j], c2[j]);
+      mx4::split2(__uint_as_float(words[j] << 16), __uint_as_float(words[j] & 0xffff0000u), {inv, inv}, {ratio, ratio}, c1[j], c2[j]);
     // the four scale bytes of a chunk, from lanes 0, 4, 8, 12 of its half-warp
     uint32_t w1 = b1 << (8 * ((lane >> 2) & 3)), w2 = b2 << (8 * ((lane >> 2) & 3));
     w1 |= __shfl_xor_sync(0xffffffffu, w1, 4);
@@ -103,33 +102,44 @@ __device__ __forceinline__ void split_row(const __nv_bfloat16* __restrict__ x, i
   }
 }
 
+// The rows of all slots, and of each its columns in blocks of kSplitCols, dealt to `workers` warps one after the other:
+// body(slot, row of the slot, first column).  rows_before: rows of the slots before each.  (Without a division for each unit:
+// a 64-bit one takes as long as a unit's arithmetic.)
+template <class Body>
+__device__ __forceinline__ void for_rows(const Tables& rows_before, int S, int D, int worker, int workers, Body&& body) {
+  const int rows = rows_before.tile_base[S], col_blocks = (D + kSplitCols - 1) / kSplitCols;
+  const int row_step = workers / col_blocks, col_step = workers - row_step * col_blocks;
+  int n = worker / col_blocks, block = worker - n * col_blocks, slot = 0;
+  while (n < rows) {
+    if (rows_before.tile_base[slot + 1] <= n) {
+      int hi = S;                                      // the last slot that begins at or before row n
+      while (hi - slot > 1) {
+        const int mid = (slot + hi) >> 1;
+        if (rows_before.tile_base[mid] <= n) slot = mid; else hi = mid;
+      }
+    }
+    body(slot, n - rows_before.tile_base[slot], block * kSplitCols);
+    n = n > INT32_MAX - row_step - 1 ? INT32_MAX : n + row_step;
+    block += col_step;
+    if (block >= col_blocks) { block -= col_blocks; ++n; }
+  }
+}
+
 template <int kRows>
 __global__ void __launch_bounds__(kSplitThreads)
 split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert,
-             int S, int E, int D, int rcap, const mx4::Rows out, int32_t* __restrict__ status) {
-  static_assert(kRows % kSplitRows == 0, "a unit's rows belong to one tile");
-  __shared__ Tables units, tiles;                     // groups of kSplitRows rows, tiles of rows
+             int S, int E, int D, int rcap, int min_rows, const mx4::Rows out, int32_t* __restrict__ status) {
+  __shared__ Tables tiles, rows_before;
   launch_dependents();
   wait_for_predecessor();
-  build_tables<kSplitThreads, kSplitRows>(units, slot_row_off, slot_expert, S, E, 1, rcap, status);
-  build_tables<kSplitThreads, kRows>(tiles, slot_row_off, slot_expert, S, E, 1, rcap, status);
+  build_tables<kSplitThreads, kRows>(tiles, slot_row_off, slot_expert, S, E, 1, rcap, status, &rows_before, min_rows);
   __syncthreads();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int chunks = mx4::chunks_of(D);
-  const int col_blocks = (chunks * kChunk + kSplitCols - 1) / kSplitCols;
-  const int64_t work = (int64_t)units.tile_base[S] * col_blocks;
-  for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
-    const int group = (int)(b / col_blocks), col0 = (int)(b - (int64_t)group * col_blocks) * kSplitCols;
-    int lo = 0, hi = S;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (units.tile_base[mid] <= group) lo = mid; else hi = mid;
-    }
-    const int first = __ldg(slot_row_off + lo), slot_rows = __ldg(slot_row_off + lo + 1) - first;
-    const int r = (group - units.tile_base[lo]) * kSplitRows + warp;      // row of the slot
-    if (r >= slot_rows) continue;
-    const int row = first + r, in_tile = r % kRows, tile = tiles.tile_base[lo] + r / kRows;
-    const int rows_in_tile = min(kRows, slot_rows - (r - in_tile));
+  constexpr int kWarps = kSplitThreads / 32;
+  for_rows(rows_before, S, D, blockIdx.x * kWarps + warp, gridDim.x * kWarps, [&](int slot, int r, int col0) {
+    const int row = __ldg(slot_row_off + slot) + r, in_tile = r % kRows, tile = tiles.tile_base[slot] + r / kRows;
+    const int rows_in_tile = min(kRows, rows_before.tile_base[slot + 1] - rows_before.tile_base[slot] - (r - in_tile));
     split_row(xp + (size_t)row * D, D, col0, lane, [&](int col, uint2 c1, uint2 c2) {
       const size_t at = (size_t)row * (chunks * kChunk) + col;
       *reinterpret_cast<uint2*>(out.code[0] + at) = c1;
@@ -139,7 +149,7 @@ split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ s
       *reinterpret_cast<uint32_t*>(scales + mx4::row_scale_at<kRows>(in_tile, 0, rows_in_tile)) = w1;
       *reinterpret_cast<uint32_t*>(scales + mx4::row_scale_at<kRows>(in_tile, 1, rows_in_tile)) = w2;
     });
-  }
+  });
 }
 
 // ------------------------------------------------------------------------------------------- epilogues
@@ -152,18 +162,33 @@ constexpr int kStaging = 1024;
 
 // 16 rows of h = silu(g) u for a warp's 32 outputs (one for each lane; they are one block): codes into `staging`, the first
 // term's 16 rows of 32 bytes and then the second's; returns the scale byte of row lane % 16, lanes 0 to 15 of the first term's.
+// Step by step over all rows, and two rows in a conversion: row by row it took 150 clocks a row, one latency after the other.
 __device__ __forceinline__ uint32_t encode_h(const float (&g)[16], const float (&u)[16], uint8_t* staging, int lane) {
+  float v[16];
+  uint32_t top[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = silu(g[i]) * u[i];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top[i] = __reduce_max_sync(0xffffffffu, __float_as_uint(v[i]) & 0x7fffffffu);
   uint32_t byte = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float v = silu(g[i]) * u[i];
-    const uint32_t b1 = mx4::term_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
-    const uint32_t b2 = mx4::second_scale(b1);
+  for (int i = 0; i < 16; i += 2) {
+    uint32_t b1[2], b2[2];
+    float inv[2], ratio[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      b1[j] = mx4::term_scale(top[i + j]);
+      b2[j] = mx4::second_scale(b1[j]);
+      inv[j] = mx4::inverse_scale(b1[j]);
+      ratio[j] = mx4::scale_ratio(b1[j], b2[j]);
+      if ((lane & 15) == i + j) byte = lane < 16 ? b1[j] : b2[j];
+    }
     uint32_t c1, c2;
-    mx4::split2(v, 0.0f, mx4::inverse_scale(b1), mx4::scale_ratio(b1, b2), c1, c2);
+    mx4::split2(v[i], v[i + 1], inv, ratio, c1, c2);
     staging[i * 32 + lane] = (uint8_t)c1;
+    staging[(i + 1) * 32 + lane] = (uint8_t)(c1 >> 8);
     staging[512 + i * 32 + lane] = (uint8_t)c2;
-    if ((lane & 15) == i) byte = lane < 16 ? b1 : b2;
+    staging[512 + (i + 1) * 32 + lane] = (uint8_t)(c2 >> 8);
   }
   __syncwarp();
   return byte;
@@ -348,7 +373,7 @@ __global__ void __launch_bounds__(Cfg::kThreads, 1)
 short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant__ CUtensorMap tm_up,
              const __grid_constant__ CUtensorMap tm_down, const uint8_t* __restrict__ gate_scale, const uint8_t* __restrict__ up_scale,
              const uint8_t* __restrict__ down_scale, const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off,
-             const int32_t* __restrict__ slot_expert, int S, int E, int D, int F, int rcap, uint8_t* x_image, uint8_t* h_image,
+             const int32_t* __restrict__ slot_expert, int S, int E, int D, int F, int rcap, int max_rows, uint8_t* x_image, uint8_t* h_image,
              __nv_bfloat16* __restrict__ y, int* part_there, int* h_there, float* partial, unsigned long long* meetings,
              int32_t* __restrict__ status) {
   constexpr int kRows = Cfg::kRows, kStages = Cfg::kStages;
@@ -382,7 +407,7 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
     tmem_alloc(tmem_slot, Cfg::kTmemCols);
     tmem_relinquish();
   }
-  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status, &rows_before);
+  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status, &rows_before, 1, max_rows);
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
@@ -518,19 +543,11 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
     {
       if (thread < 3) part_there[thread * mx4::kMaxCtas + blockIdx.x] = 0;
       for (int64_t i = (int64_t)blockIdx.x * 128 + thread; i < row_tiles * f_chunks; i += 128 * (int64_t)gridDim.x) h_there[i] = 0;
-      const int col_blocks = (d_chunks * kChunk + kSplitCols - 1) / kSplitCols;
-      const int64_t work = (int64_t)rows_before.tile_base[S] * col_blocks;
-      for (int64_t b = (int64_t)quarter * gridDim.x + blockIdx.x; b < work; b += 4 * (int64_t)gridDim.x) {
-        const int n = (int)(b / col_blocks), col0 = (int)(b - (int64_t)n * col_blocks) * kSplitCols;
-        int lo = 0, hi = S;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (rows_before.tile_base[mid] <= n) lo = mid; else hi = mid;
-        }
-        const int r = n - rows_before.tile_base[lo], in_tile = r % kRows;
-        const int rows_in_tile = min(kRows, rows_before.tile_base[lo + 1] - rows_before.tile_base[lo] - (r - in_tile));
-        uint8_t* image = x_image + (size_t)(tb.tile_base[lo] + r / kRows) * d_chunks * Cfg::kImage;
-        split_row(xp + (size_t)(__ldg(slot_row_off + lo) + r) * D, D, col0, lane, [&](int col, uint2 first, uint2 second) {
+      for_rows(rows_before, S, D, quarter * gridDim.x + blockIdx.x, 4 * gridDim.x, [&](int slot, int r, int col0) {
+        const int in_tile = r % kRows;
+        const int rows_in_tile = min(kRows, rows_before.tile_base[slot + 1] - rows_before.tile_base[slot] - (r - in_tile));
+        uint8_t* image = x_image + (size_t)(tb.tile_base[slot] + r / kRows) * d_chunks * Cfg::kImage;
+        split_row(xp + (size_t)(__ldg(slot_row_off + slot) + r) * D, D, col0, lane, [&](int col, uint2 first, uint2 second) {
           uint8_t* at = image + (size_t)(col / kChunk) * Cfg::kImage + (col & 8);
           *reinterpret_cast<uint2*>(at + mx4::image_code_at(in_tile, 0, rows_in_tile, col % kChunk / 16)) = first;
           *reinterpret_cast<uint2*>(at + mx4::image_code_at(in_tile, 1, rows_in_tile, col % kChunk / 16)) = second;
@@ -539,7 +556,7 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
           *reinterpret_cast<uint32_t*>(at + mx4::row_scale_at<kRows>(in_tile, 0, rows_in_tile)) = first;
           *reinterpret_cast<uint32_t*>(at + mx4::row_scale_at<kRows>(in_tile, 1, rows_in_tile)) = second;
         });
-      }
+      });
     }
     fence_proxy_async_global();
     named_sync(1, 128);
@@ -702,7 +719,7 @@ struct Weights {
 template <bool kGateUp_>
 struct Wide {
   static constexpr bool kGateUp = kGateUp_;
-  static constexpr int kRows = 224, kStages = 4;
+  static constexpr int kRows = mx4::kLongRows, kStages = 4;
   static constexpr int kABytes = kTile * kChunk;       // half of them are loaded
   static constexpr int kBBytes = kRows / 2 * kChunk;   // of a term
   static constexpr int kRowScales = mx4::kRowScaleBytes<kRows>;
@@ -718,7 +735,10 @@ struct Wide {
   static constexpr int kThreads = 256;
   static constexpr size_t kSmem =
       1024 + (size_t)kStages * kStageBytes + kGroups * kGroupBytes + kExchange + sizeof(Tables) + 256 + 4 * kStaging;
-  static constexpr int kBigBox = kRows / 2;            // rows of a TMA box where a CTA has more than half as many, else 16
+  // Rows come in one TMA box of 112 or in boxes of 32: a box takes its warp some 60 clocks, and 14 boxes of 16 for a chunk,
+  // with the weights' two, held the products up (down on 16384 tokens 3.5 ms, 2.8 with one box).
+  static constexpr int kBigBox = kRows / 2, kSmallBox = 32;
+  __device__ static constexpr int loaded_rows(int half) { return half > kBigBox / 2 ? kBigBox : round_up(half, kSmallBox); }
   static_assert(2 * kRows + kScaleBufs * kScaleCols <= 512 && kSmem <= 227 * 1024, "does not fit");
 };
 
@@ -729,7 +749,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
             const __grid_constant__ CUtensorMap tm_big0, const __grid_constant__ CUtensorMap tm_big1,
             const __grid_constant__ CUtensorMap tm_ws, const __grid_constant__ CUtensorMap tm_rs, const Weights w,
             const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert, int S, int E, int n_dim, int k_dim,
-            int rcap, const mx4::Rows h, __nv_bfloat16* __restrict__ y, int32_t* __restrict__ status) {
+            int rcap, int min_rows, const mx4::Rows h, __nv_bfloat16* __restrict__ y, int32_t* __restrict__ status) {
   constexpr int kStages = Cfg::kStages, kRows = Cfg::kRows;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -770,7 +790,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
     tmem_alloc_pair(tmem_slot, 512);
     tmem_relinquish_pair();
   }
-  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status);
+  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status, nullptr, min_rows);
   __syncwarp();
   tc_fence_before_sync();
   cluster_sync_all();
@@ -786,36 +806,51 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
       const uint32_t leader_full = map_to_cta(smem_u32(full), 0);
       for (int64_t t = pair; ok && t < total; t += pairs) {
         const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
-        const int half = round_up(tc.rows, 32) / 2, row0 = tc.row0 + rank * half;
-        const bool big = half > Cfg::kBigBox / 2;
-        const uint32_t bytes = 2 * (Cfg::kABytes / 2 + 2 * (big ? Cfg::kBigBox : half) * kChunk + Cfg::kRowScales + (Cfg::kGateUp ? 0 : kScaleTile));
+        const uint32_t bytes =
+            2 * (Cfg::kABytes / 2 + 2 * Cfg::loaded_rows(round_up(tc.rows, 32) / 2) * kChunk + Cfg::kRowScales +
+                 (Cfg::kGateUp ? 0 : kScaleTile));
         const int out0 = tc.m * Cfg::kOutputs + rank * (Cfg::kOutputs / 2);
         // (down) rows of 128 bytes of the weights' scales; outputs behind the last tile meet zero weights, whatever their scales
         const int ws0 = ((tc.expert * mx4::tiles_of(n_dim) + out0 / kTile) * chunks) * (kScaleTile / 128);
-        const int rs0 = tc.row_tile * chunks * (Cfg::kRowScales / 128);
         for (int c = 0; c < chunks; ++c) {
           if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag)) { ok = false; break; }
           uint8_t* a = smem + (size_t)stage * Cfg::kStageBytes;
-          uint8_t* b = a + Cfg::kABytes;
-          uint8_t* sc = a + Cfg::kScaleOffset;
           if (rank == 0) mbar_arrive_expect_tx(&full[stage], bytes);
           const uint32_t to = leader_full + stage * 8;
-          if constexpr (Cfg::kGateUp) {
-            tma_load_3d_pair(a, &tm_w0, to, c * kChunk, out0, tc.expert);
+          tma_load_3d_pair(a, &tm_w0, to, c * kChunk, out0, tc.expert);
+          if constexpr (Cfg::kGateUp)
             tma_load_3d_pair(a + Cfg::kABytes / 2, &tm_w1, to, c * kChunk, out0, tc.expert);
-          } else {
-            tma_load_3d_pair(a, &tm_w0, to, c * kChunk, out0, tc.expert);
-            tma_load_2d_pair(sc + Cfg::kRowScales, &tm_ws, to, 0, ws0 + c * (kScaleTile / 128));
-          }
-          if (big) {
+          else
+            tma_load_2d_pair(a + Cfg::kScaleOffset + Cfg::kRowScales, &tm_ws, to, 0, ws0 + c * (kScaleTile / 128));
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (!ok) linger();
+    }
+  } else if (warp == 3) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      const uint32_t leader_full = map_to_cta(smem_u32(full), 0);
+      for (int64_t t = pair; ok && t < total; t += pairs) {
+        const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+        const int half = round_up(tc.rows, 32) / 2, row0 = tc.row0 + rank * half;
+        const int rs0 = tc.row_tile * chunks * (Cfg::kRowScales / 128);
+        for (int c = 0; c < chunks; ++c) {
+          if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag)) { ok = false; break; }
+          uint8_t* b = smem + (size_t)stage * Cfg::kStageBytes + Cfg::kABytes;
+          const uint32_t to = leader_full + stage * 8;
+          tma_load_2d_pair(b + 2 * Cfg::kBBytes, &tm_rs, to, 0, rs0 + c * (Cfg::kRowScales / 128));
+          if (half > Cfg::kBigBox / 2) {
             tma_load_2d_pair(b, &tm_big0, to, c * kChunk, row0);
             tma_load_2d_pair(b + Cfg::kBBytes, &tm_big1, to, c * kChunk, row0);
+          } else {
+            for (int r = 0; r < half; r += Cfg::kSmallBox) {
+              tma_load_2d_pair(b + r * kChunk, &tm_r0, to, c * kChunk, row0 + r);
+              tma_load_2d_pair(b + Cfg::kBBytes + r * kChunk, &tm_r1, to, c * kChunk, row0 + r);
+            }
           }
-          for (int r = big ? half : 0; r < half; r += 16) {
-            tma_load_2d_pair(b + r * kChunk, &tm_r0, to, c * kChunk, row0 + r);
-            tma_load_2d_pair(b + Cfg::kBBytes + r * kChunk, &tm_r1, to, c * kChunk, row0 + r);
-          }
-          tma_load_2d_pair(sc, &tm_rs, to, 0, rs0 + c * (Cfg::kRowScales / 128));
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -1013,10 +1048,11 @@ int tmap_failed(moegps_ctx* ctx) {
 
 int launch_split(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   const moegps_shape_t& s = ctx->shape;
-  const int64_t units = (c.l.rows / kSplitRows + s.S) * ((mx4::chunks_of(s.D) * kChunk + kSplitCols - 1) / kSplitCols);
+  const int64_t units = (c.l.rows * ((s.D + kSplitCols - 1) / kSplitCols) + kSplitThreads / 32 - 1) / (kSplitThreads / 32);
   const int64_t resident = 8 * (int64_t)ctx->sm_count;
-  split_kernel<224><<<(unsigned)(units < resident ? units : resident), kSplitThreads, 0, st>>>(
-      static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert, s.S, s.E, s.D, (int)c.l.rows, c.x, ctx->d_status);
+  split_kernel<mx4::kLongRows><<<(unsigned)(units < resident ? units : resident), kSplitThreads, 0, st>>>(
+      static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert, s.S, s.E, s.D, (int)c.l.rows,
+      c.l.cut.short_rows + 1, c.x, ctx->d_status);
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }
@@ -1043,7 +1079,7 @@ int launch_short(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   uint8_t* ws = c.workspace;
   MOEGPS_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, short_kernel<Cfg>, gate, up, down, c.up_scale.scale[0], c.up_scale.scale[1],
                                           c.down_scale.scale[0], static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert,
-                                          s.S, s.E, s.D, s.F, (int)c.l.rows, ws + c.l.x_code, ws + c.l.h_code, c.yp,
+                                          s.S, s.E, s.D, s.F, (int)c.l.rows, c.l.cut.short_rows, ws + c.l.x_image, ws + c.l.h_image, c.yp,
                                           reinterpret_cast<int*>(ws + c.l.part_there), reinterpret_cast<int*>(ws + c.l.h_there),
                                           reinterpret_cast<float*>(ws + c.l.partial),
                                           ctx->d_meetings, ctx->d_status));
@@ -1062,18 +1098,19 @@ int launch_wide(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   const int box = Cfg::kGateUp ? 64 : kTile;
   if (!moegps_make_tmap_codes4(&w0, Cfg::kGateUp ? c.gate4 : c.down4, s.E, n_dim, cols, box) ||
       !moegps_make_tmap_codes4(&w1, Cfg::kGateUp ? c.up4 : c.down4, s.E, n_dim, cols, box) ||
-      !moegps_make_tmap_bytes(&r0, in.code[0], c.l.rows, cols, 16, true) ||
-      !moegps_make_tmap_bytes(&r1, in.code[1], c.l.rows, cols, 16, true) ||
+      !moegps_make_tmap_bytes(&r0, in.code[0], c.l.rows, cols, Cfg::kSmallBox, true) ||
+      !moegps_make_tmap_bytes(&r1, in.code[1], c.l.rows, cols, Cfg::kSmallBox, true) ||
       !moegps_make_tmap_bytes(&big0, in.code[0], c.l.rows, cols, Cfg::kBigBox, true) ||
       !moegps_make_tmap_bytes(&big1, in.code[1], c.l.rows, cols, Cfg::kBigBox, true) ||
       !moegps_make_tmap_bytes(&wsm, ws.scale[0], (uint64_t)s.E * mx4::tiles_of(n_dim) * chunks * (kScaleTile / 128), 128,
                               kScaleTile / 128, false) ||
-      !moegps_make_tmap_bytes(&rsm, in.scale, (uint64_t)c.l.row_tiles * chunks * (Cfg::kRowScales / 128), 128,
+      !moegps_make_tmap_bytes(&rsm, in.scale, (uint64_t)c.l.long_tiles * chunks * (Cfg::kRowScales / 128), 128,
                               Cfg::kRowScales / 128, false))
     return tmap_failed(ctx);
   MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(wide_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
   MOEGPS_CUDA_TRY(ctx, launch_after(wide_kernel<Cfg>, dim3(ctx->sm_count / 2 * 2), Cfg::kThreads, Cfg::kSmem, st, w0, w1, r0, r1,
-                                    big0, big1, wsm, rsm, ws, c.slot_row_off, c.slot_expert, s.S, s.E, n_dim, k_dim, (int)c.l.rows, c.h, c.yp,
+                                    big0, big1, wsm, rsm, ws, c.slot_row_off, c.slot_expert, s.S, s.E, n_dim, k_dim, (int)c.l.rows, c.l.cut.short_rows + 1, c.h,
+                                    c.yp,
                                     ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx, "rows=%d", Cfg::kRows);
   return MOEGPS_OK;
@@ -1091,10 +1128,13 @@ int moegps_launch_expert_ffn4(moegps_ctx* ctx, const void* xp, const int32_t* sl
   uint8_t* ws = c.workspace;
   c.x = {{ws + c.l.x_code, ws + c.l.x_code + c.l.x_code_bytes}, ws + c.l.x_scale};
   c.h = {{ws + c.l.h_code, ws + c.l.h_code + c.l.h_code_bytes}, ws + c.l.h_scale};
-  if (c.l.cut == mx4::Cut::k16) return launch_short<Short<16, 5>>(ctx, c, st);
-  if (c.l.cut == mx4::Cut::k48) return launch_short<Short<48, 4>>(ctx, c, st);
-  int rc = launch_split(ctx, c, st);
-  if (rc == MOEGPS_OK) rc = launch_wide<Wide<true>>(ctx, c, st);
-  if (rc == MOEGPS_OK) rc = launch_wide<Wide<false>>(ctx, c, st);
+  int rc = MOEGPS_OK;
+  if (!c.l.cut.all_short()) {
+    rc = launch_split(ctx, c, st);
+    if (rc == MOEGPS_OK) rc = launch_wide<Wide<true>>(ctx, c, st);
+    if (rc == MOEGPS_OK) rc = launch_wide<Wide<false>>(ctx, c, st);
+  }
+  if (rc == MOEGPS_OK && c.l.cut.short_rows > 0)
+    rc = c.l.cut.tile_rows == 16 ? launch_short<Short<16, 5>>(ctx, c, st) : launch_short<Short<48, 4>>(ctx, c, st);
   return rc;
 }

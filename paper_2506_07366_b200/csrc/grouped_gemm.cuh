@@ -106,11 +106,13 @@ __device__ __forceinline__ void store_chunk(const uint32_t (&o)[16], uint8_t* st
 // all 1024 this took over 2 us of a 12 us launch on an 8-slot layer.
 // A slot whose extent is not inside [0, rcap] (offsets negative, decreasing or past the buffers) gets no
 // tiles: nothing is read or written for it, and the caller is told.
-// rows_before (optional): the same for the rows of the slots that have tiles.
+// rows_before (optional): the same for the rows of the slots that have tiles.  Slots of fewer than min_rows or more than
+// max_rows rows are left to another launch.
 template <int kThreads, int kRows = BM>       // kRows: rows of a tile
 __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restrict__ slot_row_off,
                                              const int32_t* __restrict__ slot_expert, int S, int E, int n_tiles, int rcap,
-                                             int32_t* __restrict__ status, Tables* rows_before = nullptr) {
+                                             int32_t* __restrict__ status, Tables* rows_before = nullptr, int min_rows = 1,
+                                             int max_rows = INT32_MAX) {
   for (int s = threadIdx.x; s < S; s += kThreads) {
     int cnt = 0;
     const int lo = slot_row_off[s], hi = slot_row_off[s + 1];
@@ -118,7 +120,7 @@ __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restri
     if (lo < 0 || hi < lo || hi > rcap) {
       if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
     } else if (hi > lo && e >= 0 && e < E) {
-      cnt = ((hi - lo + kRows - 1) / kRows) * n_tiles;
+      if (hi - lo >= min_rows && hi - lo <= max_rows) cnt = ((hi - lo + kRows - 1) / kRows) * n_tiles;
     } else if (hi > lo && e >= E) {
       if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
     }

@@ -62,25 +62,43 @@ __device__ __forceinline__ float scale_ratio(uint32_t first, uint32_t second) {
   return __uint_as_float((127u + first - second) << 23);
 }
 
-// two values -> the codes of their two terms; inv = 2^-k, ratio = 2^(k1 - k2)
-__device__ __forceinline__ void split2(float a, float b, float inv, float ratio, uint32_t& first, uint32_t& second) {
-  const float2 y = make_float2(a * inv, b * inv);
+// two values -> the codes of their two terms; inv = 2^-k, ratio = 2^(k1 - k2) of each
+__device__ __forceinline__ void split2(float a, float b, const float (&inv)[2], const float (&ratio)[2], uint32_t& first,
+                                       uint32_t& second) {
+  const float2 y = make_float2(a * inv[0], b * inv[1]);
   const __nv_fp8x2_storage_t c = __nv_cvt_float2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3);
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(c, __NV_E4M3);
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
   first = c;
-  second = __nv_cvt_float2_to_fp8x2(make_float2((y.x - f.x) * ratio, (y.y - f.y) * ratio), __NV_SATFINITE, __NV_E4M3);
+  second = __nv_cvt_float2_to_fp8x2(make_float2((y.x - f.x) * ratio[0], (y.y - f.y) * ratio[1]), __NV_SATFINITE, __NV_E4M3);
 }
 
 // ------------------------------------------------------------------------------------------- workspace of expert_ffn4
-// How the rows of a slot are cut into tiles (chosen by shape alone, it decides the layout of the workspace).
-enum class Cut { k16, k48, k224 };
+// How the rows are worked (chosen by shape alone, it decides the layout of the workspace): slots of up to short_rows rows in
+// tiles of tile_rows by the launch for short slots, longer ones in tiles of 224 by those for long slots; either may be all.
+struct Cut {
+  int tile_rows, short_rows;
+  bool all_short() const { return short_rows == INT32_MAX; }
+};
+// By the rows that a slot has on average (the actual loads are only known on the device; where popular experts have many times
+// that, short slots in one launch and long ones in the others are best) and the time that reading every slot's weights once takes,
+// 2.5 ns for 16 KB.  Measured (us; layers A: 256 experts 7168 x 2048, 970 us of weights, zipf 1; B: 64 experts 2048 x 1408, 53; C: 8
+// experts 4096 x 14336, 107; D: 8 experts 1024 x 2048, 4):
+//   tiles of 16 or 48 rows: A 1.8 rows a slot 389 / 417, 3.6 604 / 560; B 3.6 62 / 66, 9.6 88 / 86; C 8 144 / 151, 16 177 / 164
+//   short or both: A 7 rows a slot 749 / 766, 14 1107 / 1058, 28 1658 / 1277
+//   short or long: B 38 157 / 182, 58 189 / 195, 77 229 / 213; C 64 268 / 326, 96 366 / 361; D 128 52 / 60, 256 66 / 71, 512 100 / 103
+//   long or both, where neither is better by more than 3 %: B from 77, C from 96, D from 256 rows a slot
 inline Cut cut_of(const moegps_shape_t& s) {
   const int64_t R = (int64_t)s.T * s.K, slots = R < s.S ? R : s.S;
   const int64_t per_slot = slots > 0 ? (R + slots - 1) / slots : 0;
-  return per_slot <= 16 ? Cut::k16 : per_slot <= 48 ? Cut::k48 : Cut::k224;
+  const int64_t d = chunks_of(s.D), f = chunks_of(s.F);
+  const double weights_us = 0.0025 * s.S * (double)(f * d + (d + 1) / 2 * f);
+  const bool heavy = weights_us > 300.0;
+  if (per_slot <= (heavy ? 3 : 8)) return {16, INT32_MAX};
+  if (per_slot <= (heavy ? 10 : weights_us > 20.0 ? 64 : 256)) return {48, INT32_MAX};
+  return {48, heavy ? 48 : 0};
 }
-inline int rows_of(Cut c) { return c == Cut::k16 ? 16 : c == Cut::k48 ? 48 : 224; }
+constexpr int kLongRows = 224;
 
 // Scale bytes of a tile's rows for one chunk, in the order of tensor memory (scale_byte_at).
 // Tiles of 16 or 48 rows: both terms stacked in one group of 512 bytes, the second term's rows behind the first's, which are
@@ -115,39 +133,41 @@ constexpr int kMaxCtas = 148;      // blocks of a launch that joins partial sums
 
 struct Layout {
   Cut cut;
-  int64_t rows, row_tiles;         // Rcap; tiles of rows at most
-  // offsets: images, or codes (the second term's follow the first's) and scales; what of h and of shared sums is there, their parts
-  size_t x_code, x_scale, h_code, h_scale, part_there, h_there, partial, total;
+  int64_t rows, short_tiles, long_tiles;       // Rcap; tiles of rows at most
+  // offsets: images of x and h; what of h and of shared sums is there, their parts; codes (the second term's follow the first's) and
+  // scales of x and h
+  size_t x_image, h_image, part_there, h_there, partial, x_code, x_scale, h_code, h_scale, total;
   size_t x_code_bytes, h_code_bytes;
 };
 
 inline Layout layout_of(const moegps_shape_t& s) {
   Layout l;
   l.cut = cut_of(s);
-  const int n = rows_of(l.cut);
+  const int n = l.cut.tile_rows;
   l.rows = (int64_t)s.T * s.K + (int64_t)s.S * (s.row_align - 1);
-  l.row_tiles = l.rows / n + s.S;
-  const size_t dc = chunks_of(s.D), fc = chunks_of(s.F);
-  l.x_code = 0;
-  if (l.cut == Cut::k224) {
-    const size_t scales = (size_t)l.row_tiles * kRowScaleBytes<224>;
-    l.x_code_bytes = align256((size_t)l.rows * dc * kChunk);
-    l.h_code_bytes = align256((size_t)l.rows * fc * kChunk);
-    l.x_scale = 2 * l.x_code_bytes;
-    l.h_code = l.x_scale + align256(scales * dc);
-    l.h_scale = l.h_code + 2 * l.h_code_bytes;
-    l.part_there = l.h_there = l.partial = l.total = l.h_scale + align256(scales * fc);
-    return l;
-  }
-  const size_t image = l.cut == Cut::k16 ? kImageBytes<16> : kImageBytes<48>;
-  l.x_code_bytes = align256(l.row_tiles * dc * image);
-  l.h_code_bytes = align256(l.row_tiles * fc * image);
-  l.h_code = l.x_code_bytes;
-  l.x_scale = l.h_scale = l.part_there = l.h_code + l.h_code_bytes;
-  l.h_there = l.part_there + align256(3 * kMaxCtas * sizeof(int32_t));
-  l.partial = l.h_there + align256(l.row_tiles * fc * sizeof(int32_t));
+  l.short_tiles = l.cut.all_short() ? l.rows / n + s.S : s.S * ((l.cut.short_rows + n - 1) / n);
+  l.long_tiles = l.cut.all_short() ? 0 : l.rows / kLongRows + s.S;
+  const size_t dc = chunks_of(s.D), fc = chunks_of(s.F), image = n == 16 ? kImageBytes<16> : kImageBytes<48>;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += align256(bytes);
+    return here;
+  };
+  l.x_image = take(l.short_tiles * dc * image);
+  l.h_image = take(l.short_tiles * fc * image);
+  l.part_there = take(3 * kMaxCtas * sizeof(int32_t));
+  l.h_there = take(l.short_tiles * fc * sizeof(int32_t));
   // a block leaves at most one unfinished tile of gate + up behind and two of down
-  l.total = l.partial + (size_t)kMaxCtas * 3 * 2 * n * kTile * sizeof(float);
+  l.partial = take((size_t)kMaxCtas * 3 * 2 * n * kTile * sizeof(float));
+  const size_t long_rows = l.cut.all_short() ? 0 : l.rows;
+  l.x_code_bytes = align256(long_rows * dc * kChunk);
+  l.h_code_bytes = align256(long_rows * fc * kChunk);
+  l.x_code = take(2 * l.x_code_bytes);
+  l.x_scale = take(l.long_tiles * dc * kRowScaleBytes<kLongRows>);
+  l.h_code = take(2 * l.h_code_bytes);
+  l.h_scale = take(l.long_tiles * fc * kRowScaleBytes<kLongRows>);
+  l.total = at;
   return l;
 }
 

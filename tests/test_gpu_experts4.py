@@ -201,6 +201,27 @@ def test_ffn_against_64_bits(c):
         again.nan_to_num(5.0), yp.nan_to_num(5.0))       # the same bits (rows of the padding may be any NaN)
 
 
+@pytest.mark.parametrize("align", [1, 16])
+def test_short_and_long_slots_in_one_call(align, monkeypatch, capfd):
+    """Many slots of one expert, some with more rows than the launch for short slots takes: both kinds of launches run."""
+    monkeypatch.setenv("MOEGPS_TRACE", "1")
+    rng = np.random.default_rng(4)
+    rows = [int(v) for v in rng.choice([0, 1, 5, 16, 17, 47, 48], 1016)] + [49, 64, 112, 223, 224, 225, 500, 900]
+    rng.shuffle(rows)
+    shape = binding.Shape(sum(rows), 1280, 1000, 1, 1, 1024, 0, align)
+    ctx, g, packed, dense, ws = make(shape, 31)
+    off, expert = slots(rows, [0] * 1024, align)
+    xp = normal(g, shape.Rcap, shape.D)
+    yp = torch.full((shape.Rcap, shape.D), 13.0, dtype=torch.bfloat16, device=DEV)
+    capfd.readouterr()
+    call(ctx, xp, off, expert, packed, yp, ws)
+    ctx.check_status()
+    launched = capfd.readouterr().err
+    for kernel in ("launch_split", "launch_wide", "launch_short"):
+        assert kernel in launched
+    check(xp, off, expert, dense, yp, 13.0)
+
+
 def test_values_over_a_wide_range():
     """Rows with magnitudes from 2^-60 to 2^30 beside each other, zero rows, single large values, weights with scales from 2^-40 up."""
     shape = binding.Shape(40, 256, 160, 2, 1, 2, 0, 1)
