@@ -61,53 +61,60 @@ __device__ __forceinline__ void linger() {
 
 // ------------------------------------------------------------------------------------------- split
 constexpr int kSplitThreads = 256;
-constexpr int kSplitCols = 1024;   // columns of a row that a warp does at a time
 
-// Columns col0 .. col0 + 1023 of a row by a warp: codes(column, first term's eight codes, second term's) for each lane's
-// eight columns, scales(chunk, word of the first term's four scale bytes, of the second's) once for each chunk.
-template <class Codes, class Scales>
-__device__ __forceinline__ void split_row(const __nv_bfloat16* __restrict__ x, int D, int col0, int lane, Codes&& codes, Scales&& scales) {
-  uint4 v[kSplitCols / 256];
+// Sixteen columns of a row from `x` on (zeros behind column D).
+struct Cols16 {
+  uint4 v[2];
+};
+__device__ __forceinline__ Cols16 load16(const __nv_bfloat16* __restrict__ x, int col, int D) {
+  Cols16 c;
 #pragma unroll
-  for (int i = 0; i < kSplitCols / 256; ++i) {
-    const int col = col0 + 256 * i + 8 * lane;
-    v[i] = make_uint4(0, 0, 0, 0);
-    if (col < D) v[i] = *reinterpret_cast<const uint4*>(x + col);
+  for (int i = 0; i < 2; ++i) {
+    c.v[i] = make_uint4(0, 0, 0, 0);
+    if (col + 8 * i < D) c.v[i] = *reinterpret_cast<const uint4*>(x + col + 8 * i);
   }
+  return c;
+}
+// Sixteen columns for each lane -> its codes of both terms; word: the four scale bytes of the chunk that its 8 lanes hold.
+// (Two lanes to a block of 32, and two values in each step behind the scaling: x 2^-k has no more bits than an fp16.  With 8
+// columns for each lane and single values this arithmetic took longer than memory.)
+__device__ __forceinline__ void split16(const Cols16& c, int lane, uint4 (&code)[2], uint32_t (&word)[2]) {
+  const uint32_t w[8] = {c.v[0].x, c.v[0].y, c.v[0].z, c.v[0].w, c.v[1].x, c.v[1].y, c.v[1].z, c.v[1].w};
+  uint32_t m2 = 0;
 #pragma unroll
-  for (int i = 0; i < kSplitCols / 256; ++i) {
-    const int col = col0 + 256 * i + 8 * lane;        // a warp's 256 columns are two chunks: whole half-warps are inside or not
-    const uint32_t words[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-    const uint32_t m2 = __vmaxu2(__vmaxu2(words[0] & 0x7fff7fffu, words[1] & 0x7fff7fffu),
-                                 __vmaxu2(words[2] & 0x7fff7fffu, words[3] & 0x7fff7fffu));
-    uint32_t m = max(m2 & 0xffffu, m2 >> 16);         // as integers, NaN and infinity are the largest
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));   // over the four lanes of a block
-    const uint32_t b1 = mx4::term_scale(m << 16), b2 = mx4::second_scale(b1);
-    const float inv = mx4::inverse_scale(b1), ratio = mx4::scale_ratio(b1, b2);
-    uint32_t c1[4], c2[4];
+  for (int j = 0; j < 8; ++j) m2 = __vmaxu2(m2, w[j] & 0x7fff7fffu);
+  uint32_t m = max(m2 & 0xffffu, m2 >> 16);           // as integers, NaN and infinity are the largest
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  const uint32_t b1 = mx4::term_scale(m << 16), b2 = mx4::second_scale(b1);
+  const float inv = mx4::inverse_scale(b1);
+  const __half2 ratio = __float2half2_rn(mx4::scale_ratio(b1, b2));
+  uint32_t out[2][4] = {};
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      mx4::split2(__uint_as_float(words[j] << 16), __uint_as_float(words[j] & 0xffff0000u), {inv, inv}, {ratio, ratio}, c1[j], c2[j]);
-    // the four scale bytes of a chunk, from lanes 0, 4, 8, 12 of its half-warp
-    uint32_t w1 = b1 << (8 * ((lane >> 2) & 3)), w2 = b2 << (8 * ((lane >> 2) & 3));
-    w1 |= __shfl_xor_sync(0xffffffffu, w1, 4);
-    w2 |= __shfl_xor_sync(0xffffffffu, w2, 4);
-    w1 |= __shfl_xor_sync(0xffffffffu, w1, 8);
-    w2 |= __shfl_xor_sync(0xffffffffu, w2, 8);
-    if (col < (D + kChunk - 1) / kChunk * kChunk) {
-      codes(col, make_uint2(c1[0] | c1[1] << 16, c1[2] | c1[3] << 16), make_uint2(c2[0] | c2[1] << 16, c2[2] | c2[3] << 16));
-      if ((lane & 15) == 0) scales(col / kChunk, w1, w2);
-    }
+  for (int j = 0; j < 8; ++j) {
+    const __half2 y = __floats2half2_rn(__uint_as_float(w[j] << 16) * inv, __uint_as_float(w[j] & 0xffff0000u) * inv);
+    const __nv_fp8x2_storage_t c1 = __nv_cvt_halfraw2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3);
+    const __half2 f = __nv_cvt_fp8x2_to_halfraw2(c1, __NV_E4M3);
+    const __nv_fp8x2_storage_t c2 = __nv_cvt_halfraw2_to_fp8x2(__hmul2(__hsub2(y, f), ratio), __NV_SATFINITE, __NV_E4M3);
+    out[0][j >> 1] |= (uint32_t)c1 << (16 * (j & 1));
+    out[1][j >> 1] |= (uint32_t)c2 << (16 * (j & 1));
+  }
+  // the scale bytes, from lanes 0, 2, 4, 6 of the eight
+  word[0] = b1 << (8 * ((lane >> 1) & 3));
+  word[1] = b2 << (8 * ((lane >> 1) & 3));
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    code[t] = make_uint4(out[t][0], out[t][1], out[t][2], out[t][3]);
+    word[t] |= __shfl_xor_sync(0xffffffffu, word[t], 2);
+    word[t] |= __shfl_xor_sync(0xffffffffu, word[t], 4);
   }
 }
 
-// The rows of all slots, and of each its columns in blocks of kSplitCols, dealt to `workers` warps one after the other:
+// The rows of all slots, and of each its columns in blocks of kCols, dealt to `workers` warps one after the other:
 // body(slot, row of the slot, first column).  rows_before: rows of the slots before each.  (Without a division for each unit:
 // a 64-bit one takes as long as a unit's arithmetic.)
-template <class Body>
+template <int kCols, class Body>
 __device__ __forceinline__ void for_rows(const Tables& rows_before, int S, int D, int worker, int workers, Body&& body) {
-  const int rows = rows_before.tile_base[S], col_blocks = (D + kSplitCols - 1) / kSplitCols;
+  const int rows = rows_before.tile_base[S], col_blocks = (D + kCols - 1) / kCols;
   const int row_step = workers / col_blocks, col_step = workers - row_step * col_blocks;
   int n = worker / col_blocks, block = worker - n * col_blocks, slot = 0;
   while (n < rows) {
@@ -118,37 +125,59 @@ __device__ __forceinline__ void for_rows(const Tables& rows_before, int S, int D
         if (rows_before.tile_base[mid] <= n) slot = mid; else hi = mid;
       }
     }
-    body(slot, n - rows_before.tile_base[slot], block * kSplitCols);
+    body(slot, n - rows_before.tile_base[slot], block * kCols);
     n = n > INT32_MAX - row_step - 1 ? INT32_MAX : n + row_step;
     block += col_step;
     if (block >= col_blocks) { block -= col_blocks; ++n; }
   }
 }
 
-template <int kRows>
+// For long slots.  A warp does 512 columns of rows b, b + 32, b + 64, b + 96 of 128 rows of a tile, whose scales lie side by
+// side: 16 bytes at a time (4 at a time, a row for itself, these writes took 28 of 100 us on 49152 rows x 2048).
 __global__ void __launch_bounds__(kSplitThreads)
 split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert,
              int S, int E, int D, int rcap, int min_rows, const mx4::Rows out, int32_t* __restrict__ status) {
-  __shared__ Tables tiles, rows_before;
+  constexpr int kRows = mx4::kLongRows, kUnits = 64;  // of a tile: 2 x 128 rows at most
+  __shared__ Tables units, tiles;
   launch_dependents();
   wait_for_predecessor();
-  build_tables<kSplitThreads, kRows>(tiles, slot_row_off, slot_expert, S, E, 1, rcap, status, &rows_before, min_rows);
+  build_tables<kSplitThreads, kRows>(units, slot_row_off, slot_expert, S, E, kUnits, rcap, status, nullptr, min_rows);
+  __syncthreads();
+  build_tables<kSplitThreads, kRows>(tiles, slot_row_off, slot_expert, S, E, 1, rcap, status, nullptr, min_rows);
   __syncthreads();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int chunks = mx4::chunks_of(D);
   constexpr int kWarps = kSplitThreads / 32;
-  for_rows(rows_before, S, D, blockIdx.x * kWarps + warp, gridDim.x * kWarps, [&](int slot, int r, int col0) {
-    const int row = __ldg(slot_row_off + slot) + r, in_tile = r % kRows, tile = tiles.tile_base[slot] + r / kRows;
-    const int rows_in_tile = min(kRows, rows_before.tile_base[slot + 1] - rows_before.tile_base[slot] - (r - in_tile));
-    split_row(xp + (size_t)row * D, D, col0, lane, [&](int col, uint2 c1, uint2 c2) {
-      const size_t at = (size_t)row * (chunks * kChunk) + col;
-      *reinterpret_cast<uint2*>(out.code[0] + at) = c1;
-      *reinterpret_cast<uint2*>(out.code[1] + at) = c2;
-    }, [&](int chunk, uint32_t w1, uint32_t w2) {
-      uint8_t* scales = out.scale + ((size_t)tile * chunks + chunk) * mx4::kRowScaleBytes<kRows>;
-      *reinterpret_cast<uint32_t*>(scales + mx4::row_scale_at<kRows>(in_tile, 0, rows_in_tile)) = w1;
-      *reinterpret_cast<uint32_t*>(scales + mx4::row_scale_at<kRows>(in_tile, 1, rows_in_tile)) = w2;
-    });
+  for_rows<512>(units, S, D, blockIdx.x * kWarps + warp, gridDim.x * kWarps, [&](int slot, int unit, int col0) {
+    const int first = __ldg(slot_row_off + slot), j = unit / kUnits, half = unit / 32 % 2, b = unit % 32;
+    const int rows = min(kRows, __ldg(slot_row_off + slot + 1) - first - j * kRows), in_tile = half * 128 + b;
+    if (in_tile >= rows) return;
+    const size_t row = (size_t)first + j * kRows + in_tile;
+    const int col = col0 + 16 * lane;
+    Cols16 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = load16(xp + (row + 32 * q) * D, col, in_tile + 32 * q < rows ? D : 0);
+    uint32_t words[2][4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint4 code[2];
+      uint32_t word[2];
+      split16(v[q], lane, code, word);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        words[t][q] = word[t];
+        if (in_tile + 32 * q < rows && col < chunks * kChunk)
+          *reinterpret_cast<uint4*>(out.code[t] + (row + 32 * q) * (size_t)(chunks * kChunk) + col) = code[t];
+      }
+    }
+    if ((lane & 7) == 0 && col < chunks * kChunk) {
+      uint8_t* scales =
+          out.scale + ((size_t)(tiles.tile_base[slot] + j) * chunks + col / kChunk) * mx4::kRowScaleBytes<kRows>;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        *reinterpret_cast<uint4*>(scales + mx4::row_scale_at<kRows>(in_tile, t, rows)) =
+            make_uint4(words[t][0], words[t][1], words[t][2], words[t][3]);
+    }
   });
 }
 
@@ -539,23 +568,27 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
   } else {
     const int quarter = warp & 3, thread = quarter * 32 + lane;
     uint8_t* staging = smem + Cfg::kStagingOffset + quarter * kStaging;
-    // x in two terms: a warp does 1024 columns of a row
+    // x in two terms: a warp does 512 columns of a row
     {
       if (thread < 3) part_there[thread * mx4::kMaxCtas + blockIdx.x] = 0;
       for (int64_t i = (int64_t)blockIdx.x * 128 + thread; i < row_tiles * f_chunks; i += 128 * (int64_t)gridDim.x) h_there[i] = 0;
-      for_rows(rows_before, S, D, quarter * gridDim.x + blockIdx.x, 4 * gridDim.x, [&](int slot, int r, int col0) {
+      for_rows<512>(rows_before, S, D, quarter * gridDim.x + blockIdx.x, 4 * gridDim.x, [&](int slot, int r, int col0) {
         const int in_tile = r % kRows;
         const int rows_in_tile = min(kRows, rows_before.tile_base[slot + 1] - rows_before.tile_base[slot] - (r - in_tile));
         uint8_t* image = x_image + (size_t)(tb.tile_base[slot] + r / kRows) * d_chunks * Cfg::kImage;
-        split_row(xp + (size_t)(__ldg(slot_row_off + slot) + r) * D, D, col0, lane, [&](int col, uint2 first, uint2 second) {
-          uint8_t* at = image + (size_t)(col / kChunk) * Cfg::kImage + (col & 8);
-          *reinterpret_cast<uint2*>(at + mx4::image_code_at(in_tile, 0, rows_in_tile, col % kChunk / 16)) = first;
-          *reinterpret_cast<uint2*>(at + mx4::image_code_at(in_tile, 1, rows_in_tile, col % kChunk / 16)) = second;
-        }, [&](int chunk, uint32_t first, uint32_t second) {
-          uint8_t* at = image + (size_t)chunk * Cfg::kImage;
-          *reinterpret_cast<uint32_t*>(at + mx4::row_scale_at<kRows>(in_tile, 0, rows_in_tile)) = first;
-          *reinterpret_cast<uint32_t*>(at + mx4::row_scale_at<kRows>(in_tile, 1, rows_in_tile)) = second;
-        });
+        const __nv_bfloat16* x = xp + (size_t)(__ldg(slot_row_off + slot) + r) * D;
+        const int col = col0 + 16 * lane;
+        uint4 code[2];
+        uint32_t word[2];
+        split16(load16(x, col, D), lane, code, word);
+        if (col < d_chunks * kChunk) {
+          uint8_t* at = image + (size_t)(col / kChunk) * Cfg::kImage;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            *reinterpret_cast<uint4*>(at + mx4::image_code_at(in_tile, t, rows_in_tile, col % kChunk / 16)) = code[t];
+            if ((lane & 7) == 0) *reinterpret_cast<uint32_t*>(at + mx4::row_scale_at<kRows>(in_tile, t, rows_in_tile)) = word[t];
+          }
+        }
       });
     }
     fence_proxy_async_global();
@@ -1048,9 +1081,9 @@ int tmap_failed(moegps_ctx* ctx) {
 
 int launch_split(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   const moegps_shape_t& s = ctx->shape;
-  const int64_t units = (c.l.rows * ((s.D + kSplitCols - 1) / kSplitCols) + kSplitThreads / 32 - 1) / (kSplitThreads / 32);
+  const int64_t units = c.l.long_tiles * 64 * ((s.D + 511) / 512) / (kSplitThreads / 32);
   const int64_t resident = 8 * (int64_t)ctx->sm_count;
-  split_kernel<mx4::kLongRows><<<(unsigned)(units < resident ? units : resident), kSplitThreads, 0, st>>>(
+  split_kernel<<<(unsigned)(units < resident ? units : resident), kSplitThreads, 0, st>>>(
       static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert, s.S, s.E, s.D, (int)c.l.rows,
       c.l.cut.short_rows + 1, c.x, ctx->d_status);
   MOEGPS_AFTER_LAUNCH(ctx);
