@@ -764,10 +764,11 @@ struct Wide {
   static constexpr int kScaleCols = 4 + 4 * kRowScales / kScaleTile;
   static constexpr int kScaleBufs = 3;                 // tensor memory has no room for four
   static constexpr int kOutputs = kGateUp ? 128 : 256; // of a pair's tile
-  static constexpr int kExchange = kGateUp ? 4 * 2 * 16 * 32 * 4 : 0;     // two buffers of 16 x 32 fp32 for each epilogue warp
-  static constexpr int kThreads = 256;
+  static constexpr int kEpilogueWarps = 8;
+  static constexpr int kExchange = kGateUp ? kEpilogueWarps * 16 * 32 * 4 : 0;      // 16 x 32 fp32 for each epilogue warp
+  static constexpr int kThreads = 128 + 32 * kEpilogueWarps;
   static constexpr size_t kSmem =
-      1024 + (size_t)kStages * kStageBytes + kGroups * kGroupBytes + kExchange + sizeof(Tables) + 256 + 4 * kStaging;
+      1024 + (size_t)kStages * kStageBytes + kGroups * kGroupBytes + kExchange + sizeof(Tables) + 256 + kEpilogueWarps * kStaging;
   // Rows come in one TMA box of 112 or in boxes of 32: a box takes its warp some 60 clocks, and 14 boxes of 16 for a chunk,
   // with the weights' two, held the products up (down on 16384 tokens 3.5 ms, 2.8 with one box).
   static constexpr int kBigBox = kRows / 2, kSmallBox = 32;
@@ -807,7 +808,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
     for (int i = 0; i < Cfg::kGroups; ++i) { mbar_init(&scales_full[i], 2); mbar_init(&scales_empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 8); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 2 * Cfg::kEpilogueWarps); }
     *abort_flag = 0;
     fence_mbar_init();
     prefetch_tensormap(&tm_w0);
@@ -988,10 +989,12 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
       if (!ok) linger();
     }
   } else if (warp >= 4) {
-    const int quarter = warp & 3;
-    uint8_t* staging = reinterpret_cast<uint8_t*>(bars) + 256 + quarter * kStaging;
+    // two warps for each quarter of the lanes: with one, the epilogue of a gate + up tile took 14000 clocks, as long as the products
+    // of 2048 columns
+    const int quarter = warp & 3, turn = (warp - 4) >> 2;
+    uint8_t* staging = reinterpret_cast<uint8_t*>(bars) + 256 + (warp - 4) * kStaging;
     const uint32_t leader_empty = map_to_cta(smem_u32(acc_empty), 0);
-    int acc = 0, turn = 0;
+    int acc = 0;
     uint32_t acc_phase = 0;
     bool ok = true;                  // a warp whose wait ran out still meets its partner at every barrier below
     for (int64_t t = pair; t < total; t += pairs) {
@@ -1006,7 +1009,9 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
         const int col0 = tc.m * kChunk + block * 32;
         uint8_t* scales = h.scale + ((size_t)tc.row_tile * m_tiles + tc.m) * Cfg::kRowScales;
         const int half = padded / 2;
-        for (int i = 0; i < half; i += 16) {
+        float* own_buffer = exchange + (warp - 4) * 16 * 32 + lane;
+        const float* partners = exchange + ((warp - 4) ^ 2) * 16 * 32 + lane;
+        for (int i = 16 * turn; i < half; i += 32) {
           // the gate's warps finish the first half of the rows, the up's the second
           const int mine = up ? half + i : i, other = up ? i : half + i;
           uint32_t give[16], keep[16];
@@ -1015,26 +1020,23 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
             tmem_ld16(taddr + mine, keep);
             tmem_ld_wait();
           }
-          float* buffer = exchange + turn * 16 * 32 + lane;            // of warp 0; a warp has 2 * 16 * 32
 #pragma unroll
-          for (int j = 0; j < 16; ++j) buffer[quarter * 1024 + j * 32] = __uint_as_float(give[j]);
-          float v[16], get[16];
-          named_sync(1 + (quarter & 1), 64);           // (before a buffer is written again both have met here once more)
+          for (int j = 0; j < 16; ++j) own_buffer[j * 32] = __uint_as_float(give[j]);
+          named_sync(1 + 2 * turn + (quarter & 1), 64);
+          float gate[16], value[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            get[j] = buffer[(quarter ^ 2) * 1024 + j * 32];
-            v[j] = __uint_as_float(keep[j]);
+            const float get = partners[j * 32], kept = __uint_as_float(keep[j]);
+            gate[j] = up ? get : kept;
+            value[j] = up ? kept : get;
           }
-          turn ^= 1;
-          if (!ok) continue;
-          if (up)
-            store_h<kRows>(h, get, v, staging, tc.row0 + mine, mine, tc.rows, (size_t)m_tiles * kChunk, col0, scales, block, lane);
-          else
-            store_h<kRows>(h, v, get, staging, tc.row0 + mine, mine, tc.rows, (size_t)m_tiles * kChunk, col0, scales, block, lane);
+          named_sync(1 + 2 * turn + (quarter & 1), 64);                // the buffers have been read
+          if (ok)
+            store_h<kRows>(h, gate, value, staging, tc.row0 + mine, mine, tc.rows, (size_t)m_tiles * kChunk, col0, scales, block, lane);
         }
       } else {
         const int col0 = tc.m * Cfg::kOutputs + rank * kTile + quarter * 32;
-        for (int r = 0; ok && r < tc.rows; r += 16) {
+        for (int r = 16 * turn; ok && r < tc.rows; r += 32) {
           uint32_t bits[16];
           float v[16];
           tmem_ld16(taddr + r, bits);
