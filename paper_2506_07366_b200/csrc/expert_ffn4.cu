@@ -1170,6 +1170,8 @@ int moegps_launch_expert_ffn4(moegps_ctx* ctx, const void* xp, const int32_t* sl
     if (rc == MOEGPS_OK) rc = launch_wide<Wide<false>>(ctx, c, st);
   }
   if (rc == MOEGPS_OK && c.l.cut.short_rows > 0)
-    rc = c.l.cut.tile_rows == 16 ? launch_short<Short<16, 5>>(ctx, c, st) : launch_short<Short<48, 4>>(ctx, c, st);
+    rc = c.l.cut.tile_rows == 16   ? launch_short<Short<16, 5>>(ctx, c, st)
+         : c.l.cut.tile_rows == 32 ? launch_short<Short<32, 5>>(ctx, c, st)
+                                   : launch_short<Short<48, 4>>(ctx, c, st);
   return rc;
 }
