@@ -280,10 +280,10 @@ __device__ __forceinline__ void store_y(__nv_bfloat16* __restrict__ y, const flo
 // its sums).  The blocks are one for each SM, a cooperative launch, and wait for one another: all for all when the rows are split,
 // then for the parts of h that they need; the weights of the next product are loaded meanwhile.
 //  - A tile is two weight tiles of 128 outputs (gate and up of the same outputs, or two neighbours of down) times the rows of a
-//    slot.  The K steps of all tiles are dealt evenly to the blocks, whatever their number.  Sums that several blocks share are
-//    added up in the order of the blocks, by the one that begins the tile: it is the last tile of that block and the first of the
-//    other (there are mostly two), whose part is there by then.  A tile of down that three or more share is added up by all of
-//    them, some of the rows each, at the end.  (Joined by the block that came last, behind a fence and an atomic count, it took 5.5
+//    slot.  The K steps of all tiles are dealt to the blocks (Share).  Sums that several blocks share are added up in the order of
+//    the blocks, by the one that begins the tile: it is the last tile of that block and the first of the other (there are mostly
+//    two), whose part is there by then.  A tile of down that three or more share is added up by all of them, some of the rows
+//    each, at the end.  (Joined by the block that came last, behind a fence and an atomic count, it took 5.5
 //    us at the end of each product; down by the first of five blocks 8, and two blocks that add up half of the rows each 6.6.)
 //  - Both terms of a row are columns of one MMA (of few columns it takes 40 clocks whatever their number: it waits for its 128
 //    weight rows), side by side in the accumulator, and added up in the epilogue.
@@ -316,30 +316,38 @@ struct Short {
   static_assert(kSmem > 114 * 1024, "one block for each SM: the blocks wait for one another");
 };
 
-// What a block does of all K steps, [begin, end) of the tiles one after the other, from step `chunk` of tile `tile`.  (A 64-bit
-// division takes half a microsecond: these are the only ones, and 32-bit ones where they can be.)
+// What a block does: `left` K steps of the tiles one after the other, from step `chunk` of tile `tile` on.  The steps are dealt
+// evenly, but whole tiles where that makes no block's share longer by more than kWorth steps: a step takes some 0.4 us, and parts of
+// a tile cost 4 to 6 to join (256 tokens of 8 experts 512 x 1024: 27.0 us in parts, 20.8 whole; one token of two 4096 x 14336
+// experts, where whole tiles of gate + up are 16 steps more: 51.3 and 53.7).  (32-bit divisions where they can be: a 64-bit one
+// takes half a microsecond.)
 struct Share {
-  int64_t each;                     // steps of a block, one more in the first `more`
-  int blocks, more;                 // blocks: that have any
-  int64_t begin, end, tile;
+  static constexpr int kWorth = 14;
+  int64_t each;                     // units of a block, one more in the first `more`
+  int more, unit;                   // unit: steps that are dealt together
+  int64_t left, tile;
   int chunk;
-  __device__ Share(int64_t steps, int chunks, int grid, int block) {
-    blocks = (int)min((int64_t)grid, steps);
-    each = begin = end = tile = more = chunk = 0;
-    if (block >= blocks) return;
-    if (steps >> 32) {
-      each = steps / blocks;
-      more = (int)(steps % blocks);
+  __device__ Share(int64_t tiles, int chunks, int grid, int block) {
+    each = left = tile = more = chunk = 0;
+    unit = 1;
+    if (tiles <= 0) return;
+    const int64_t rounds = tiles >> 31 ? (tiles + grid - 1) / grid : ((uint32_t)tiles + grid - 1) / (uint32_t)grid;
+    // rounds * chunks - steps / grid <= kWorth
+    if ((rounds * grid - tiles) * chunks <= (int64_t)kWorth * grid) unit = chunks;
+    const int64_t units = unit == 1 ? tiles * chunks : tiles;
+    if (units >> 32) {
+      each = units / grid;
+      more = (int)(units % grid);
     } else {
-      each = (uint32_t)steps / (uint32_t)blocks;
-      more = (uint32_t)steps % (uint32_t)blocks;
+      each = (uint32_t)units / (uint32_t)grid;
+      more = (uint32_t)units % (uint32_t)grid;
     }
-    begin = begin_of(block);
-    end = begin_of(block + 1);
+    const int64_t begin = begin_of(block);
+    left = begin_of(block + 1) - begin;
     tile = begin >> 32 ? begin / chunks : (uint32_t)begin / (uint32_t)chunks;
     chunk = (int)(begin - tile * chunks);
   }
-  __device__ int64_t begin_of(int b) const { return b * each + min(b, more); }
+  __device__ int64_t begin_of(int b) const { return (b * each + min(b, more)) * unit; }
   // the blocks that share a tile of block b
   __device__ int first_of(int64_t t, int chunks, int b) const {
     while (begin_of(b) > t * chunks) --b;
@@ -442,13 +450,13 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
   const int64_t row_tiles = tb.tile_base[S];
-  const Share up_share(row_tiles * f_chunks * d_chunks, d_chunks, gridDim.x, blockIdx.x);
-  const Share down_share(row_tiles * d_tiles * f_chunks, f_chunks, gridDim.x, blockIdx.x);
+  const Share up_share(row_tiles * f_chunks, d_chunks, gridDim.x, blockIdx.x);
+  const Share down_share(row_tiles * d_tiles, f_chunks, gridDim.x, blockIdx.x);
   const Meeting meeting = {meetings, goal};
 
   // calls body(tile, its number, k0, k1) for each tile, or part of one, of this block
   auto for_tiles = [&](const Share& share, int m_tiles, int chunks, auto&& body) {
-    int64_t t = share.tile, left = share.end - share.begin;
+    int64_t t = share.tile, left = share.left;
     for (int k0 = share.chunk; left > 0; k0 = 0, ++t) {
       const int k1 = (int)min((int64_t)chunks, k0 + left);
       if (!body(tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles), t, k0, k1)) return false;
@@ -568,25 +576,31 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
   } else {
     const int quarter = warp & 3, thread = quarter * 32 + lane;
     uint8_t* staging = smem + Cfg::kStagingOffset + quarter * kStaging;
-    // x in two terms: a warp does 512 columns of a row
+    // x in two terms: a warp does 1024 columns of a row
     {
       if (thread < 3) part_there[thread * mx4::kMaxCtas + blockIdx.x] = 0;
       for (int64_t i = (int64_t)blockIdx.x * 128 + thread; i < row_tiles * f_chunks; i += 128 * (int64_t)gridDim.x) h_there[i] = 0;
-      for_rows<512>(rows_before, S, D, quarter * gridDim.x + blockIdx.x, 4 * gridDim.x, [&](int slot, int r, int col0) {
+      for_rows<1024>(rows_before, S, D, quarter * gridDim.x + blockIdx.x, 4 * gridDim.x, [&](int slot, int r, int col0) {
         const int in_tile = r % kRows;
         const int rows_in_tile = min(kRows, rows_before.tile_base[slot + 1] - rows_before.tile_base[slot] - (r - in_tile));
         uint8_t* image = x_image + (size_t)(tb.tile_base[slot] + r / kRows) * d_chunks * Cfg::kImage;
         const __nv_bfloat16* x = xp + (size_t)(__ldg(slot_row_off + slot) + r) * D;
-        const int col = col0 + 16 * lane;
-        uint4 code[2];
-        uint32_t word[2];
-        split16(load16(x, col, D), lane, code, word);
-        if (col < d_chunks * kChunk) {
-          uint8_t* at = image + (size_t)(col / kChunk) * Cfg::kImage;
+        Cols16 v[2];
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            *reinterpret_cast<uint4*>(at + mx4::image_code_at(in_tile, t, rows_in_tile, col % kChunk / 16)) = code[t];
-            if ((lane & 7) == 0) *reinterpret_cast<uint32_t*>(at + mx4::row_scale_at<kRows>(in_tile, t, rows_in_tile)) = word[t];
+        for (int i = 0; i < 2; ++i) v[i] = load16(x, col0 + 512 * i + 16 * lane, D);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int col = col0 + 512 * i + 16 * lane;
+          uint4 code[2];
+          uint32_t word[2];
+          split16(v[i], lane, code, word);
+          if (col < d_chunks * kChunk) {
+            uint8_t* at = image + (size_t)(col / kChunk) * Cfg::kImage;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              *reinterpret_cast<uint4*>(at + mx4::image_code_at(in_tile, t, rows_in_tile, col % kChunk / 16)) = code[t];
+              if ((lane & 7) == 0) *reinterpret_cast<uint32_t*>(at + mx4::row_scale_at<kRows>(in_tile, t, rows_in_tile)) = word[t];
+            }
           }
         }
       });
