@@ -61,6 +61,7 @@ int moegps_create(moegps_ctx_t** out, const moegps_shape_t* shape, int device) {
   for (bool& b : ctx->ffn_attr_done) b = false;
   for (auto& v : ctx->data_gradient_attr_done)
     for (bool& b : v) b = false;
+  for (bool& b : ctx->ffn4_attr_done) b = false;
   ctx->weight_gradient_attr_done = ctx->router_weight_attr_done = false;
   ctx->rt_valid = false;
   ctx->route_attr_done = false;

@@ -136,14 +136,15 @@ __device__ __forceinline__ void for_rows(const Tables& rows_before, int S, int D
 // side: 16 bytes at a time (4 at a time, a row for itself, these writes took 28 of 100 us on 49152 rows x 2048).
 __global__ void __launch_bounds__(kSplitThreads)
 split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert,
-             int S, int E, int D, int rcap, int min_rows, const mx4::Rows out, int32_t* __restrict__ status) {
+             int S, int E, int D, int rcap, int min_rows, int max_tiles, const mx4::Rows out, int32_t* __restrict__ status) {
   constexpr int kRows = mx4::kLongRows, kUnits = 64;  // of a tile: 2 x 128 rows at most
   __shared__ Tables units, tiles;
   launch_dependents();
   wait_for_predecessor();
-  build_tables<kSplitThreads, kRows>(units, slot_row_off, slot_expert, S, E, kUnits, rcap, status, nullptr, min_rows);
+  build_tables<kSplitThreads, kRows>(units, slot_row_off, slot_expert, S, E, kUnits, rcap, status, nullptr, min_rows, INT32_MAX,
+                                     max_tiles * kUnits);
   __syncthreads();
-  build_tables<kSplitThreads, kRows>(tiles, slot_row_off, slot_expert, S, E, 1, rcap, status, nullptr, min_rows);
+  build_tables<kSplitThreads, kRows>(tiles, slot_row_off, slot_expert, S, E, 1, rcap, status, nullptr, min_rows, INT32_MAX, max_tiles);
   __syncthreads();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int chunks = mx4::chunks_of(D);
@@ -410,7 +411,7 @@ __global__ void __launch_bounds__(Cfg::kThreads, 1)
 short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant__ CUtensorMap tm_up,
              const __grid_constant__ CUtensorMap tm_down, const uint8_t* __restrict__ gate_scale, const uint8_t* __restrict__ up_scale,
              const uint8_t* __restrict__ down_scale, const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off,
-             const int32_t* __restrict__ slot_expert, int S, int E, int D, int F, int rcap, int max_rows, uint8_t* x_image, uint8_t* h_image,
+             const int32_t* __restrict__ slot_expert, int S, int E, int D, int F, int rcap, int max_rows, int max_tiles, uint8_t* x_image, uint8_t* h_image,
              __nv_bfloat16* __restrict__ y, int* part_there, int* h_there, float* partial, unsigned long long* meetings,
              int32_t* __restrict__ status) {
   constexpr int kRows = Cfg::kRows, kStages = Cfg::kStages;
@@ -444,7 +445,7 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
     tmem_alloc(tmem_slot, Cfg::kTmemCols);
     tmem_relinquish();
   }
-  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status, &rows_before, 1, max_rows);
+  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status, &rows_before, 1, max_rows, max_tiles);
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
@@ -583,7 +584,9 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
       for_rows<1024>(rows_before, S, D, quarter * gridDim.x + blockIdx.x, 4 * gridDim.x, [&](int slot, int r, int col0) {
         const int in_tile = r % kRows;
         const int rows_in_tile = min(kRows, rows_before.tile_base[slot + 1] - rows_before.tile_base[slot] - (r - in_tile));
-        uint8_t* image = x_image + (size_t)(tb.tile_base[slot] + r / kRows) * d_chunks * Cfg::kImage;
+        const int tile = tb.tile_base[slot] + r / kRows;
+        if (tile >= tb.tile_base[slot + 1]) return;    // left out
+        uint8_t* image = x_image + (size_t)tile * d_chunks * Cfg::kImage;
         const __nv_bfloat16* x = xp + (size_t)(__ldg(slot_row_off + slot) + r) * D;
         Cols16 v[2];
 #pragma unroll
@@ -797,7 +800,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
             const __grid_constant__ CUtensorMap tm_big0, const __grid_constant__ CUtensorMap tm_big1,
             const __grid_constant__ CUtensorMap tm_ws, const __grid_constant__ CUtensorMap tm_rs, const Weights w,
             const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert, int S, int E, int n_dim, int k_dim,
-            int rcap, int min_rows, const mx4::Rows h, __nv_bfloat16* __restrict__ y, int32_t* __restrict__ status) {
+            int rcap, int min_rows, int max_tiles, const mx4::Rows h, __nv_bfloat16* __restrict__ y, int32_t* __restrict__ status) {
   constexpr int kStages = Cfg::kStages, kRows = Cfg::kRows;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -838,7 +841,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
     tmem_alloc_pair(tmem_slot, 512);
     tmem_relinquish_pair();
   }
-  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status, nullptr, min_rows);
+  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status, nullptr, min_rows, INT32_MAX, max_tiles);
   __syncwarp();
   tc_fence_before_sync();
   cluster_sync_all();
@@ -1101,7 +1104,7 @@ int launch_split(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   const int64_t resident = 8 * (int64_t)ctx->sm_count;
   split_kernel<<<(unsigned)(units < resident ? units : resident), kSplitThreads, 0, st>>>(
       static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert, s.S, s.E, s.D, (int)c.l.rows,
-      c.l.cut.short_rows + 1, c.x, ctx->d_status);
+      c.l.cut.short_rows + 1, (int)c.l.long_tiles, c.x, ctx->d_status);
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }
@@ -1114,7 +1117,11 @@ int launch_short(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   if (!moegps_make_tmap_codes4(&gate, c.gate4, s.E, s.F, dc, kTile) || !moegps_make_tmap_codes4(&up, c.up4, s.E, s.F, dc, kTile) ||
       !moegps_make_tmap_codes4(&down, c.down4, s.E, s.D, fc, kTile))
     return tmap_failed(ctx);
-  MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(short_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
+  bool& attr_done = ctx->ffn4_attr_done[Cfg::kRows / 16];
+  if (!attr_done) {
+    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(short_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
+    attr_done = true;
+  }
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeCooperative;            // all blocks run at once: they wait for one another
   attr.val.cooperative = 1;
@@ -1128,7 +1135,7 @@ int launch_short(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   uint8_t* ws = c.workspace;
   MOEGPS_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, short_kernel<Cfg>, gate, up, down, c.up_scale.scale[0], c.up_scale.scale[1],
                                           c.down_scale.scale[0], static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert,
-                                          s.S, s.E, s.D, s.F, (int)c.l.rows, c.l.cut.short_rows, ws + c.l.x_image, ws + c.l.h_image, c.yp,
+                                          s.S, s.E, s.D, s.F, (int)c.l.rows, c.l.cut.short_rows, (int)c.l.short_tiles, ws + c.l.x_image, ws + c.l.h_image, c.yp,
                                           reinterpret_cast<int*>(ws + c.l.part_there), reinterpret_cast<int*>(ws + c.l.h_there),
                                           reinterpret_cast<float*>(ws + c.l.partial),
                                           ctx->d_meetings, ctx->d_status));
@@ -1156,9 +1163,13 @@ int launch_wide(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
       !moegps_make_tmap_bytes(&rsm, in.scale, (uint64_t)c.l.long_tiles * chunks * (Cfg::kRowScales / 128), 128,
                               Cfg::kRowScales / 128, false))
     return tmap_failed(ctx);
-  MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(wide_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
+  bool& attr_done = ctx->ffn4_attr_done[Cfg::kGateUp ? 0 : 4];
+  if (!attr_done) {
+    MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(wide_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
+    attr_done = true;
+  }
   MOEGPS_CUDA_TRY(ctx, launch_after(wide_kernel<Cfg>, dim3(ctx->sm_count / 2 * 2), Cfg::kThreads, Cfg::kSmem, st, w0, w1, r0, r1,
-                                    big0, big1, wsm, rsm, ws, c.slot_row_off, c.slot_expert, s.S, s.E, n_dim, k_dim, (int)c.l.rows, c.l.cut.short_rows + 1, c.h,
+                                    big0, big1, wsm, rsm, ws, c.slot_row_off, c.slot_expert, s.S, s.E, n_dim, k_dim, (int)c.l.rows, c.l.cut.short_rows + 1, (int)c.l.long_tiles, c.h,
                                     c.yp,
                                     ctx->d_status));
   MOEGPS_AFTER_LAUNCH(ctx, "rows=%d", Cfg::kRows);

@@ -107,12 +107,13 @@ __device__ __forceinline__ void store_chunk(const uint32_t (&o)[16], uint8_t* st
 // A slot whose extent is not inside [0, rcap] (offsets negative, decreasing or past the buffers) gets no
 // tiles: nothing is read or written for it, and the caller is told.
 // rows_before (optional): the same for the rows of the slots that have tiles.  Slots of fewer than min_rows or more than
-// max_rows rows are left to another launch.
+// max_rows rows are left to another launch.  Tiles from number max_tiles on (there are so many only where slots overlap) are left
+// out, and the caller is told.
 template <int kThreads, int kRows = BM>       // kRows: rows of a tile
 __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restrict__ slot_row_off,
                                              const int32_t* __restrict__ slot_expert, int S, int E, int n_tiles, int rcap,
                                              int32_t* __restrict__ status, Tables* rows_before = nullptr, int min_rows = 1,
-                                             int max_rows = INT32_MAX) {
+                                             int max_rows = INT32_MAX, int max_tiles = INT32_MAX) {
   for (int s = threadIdx.x; s < S; s += kThreads) {
     int cnt = 0;
     const int lo = slot_row_off[s], hi = slot_row_off[s + 1];
@@ -131,6 +132,7 @@ __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restri
   // exclusive prefix sums of the counts, a warp for each table (lane l owns `per` consecutive entries)
   if (threadIdx.x < (rows_before ? 64 : 32)) {
     int32_t* base = threadIdx.x < 32 ? tb.tile_base : rows_before->tile_base;
+    const int most = threadIdx.x < 32 ? max_tiles : INT32_MAX;
     const int lane = threadIdx.x & 31, per = (S + 31) / 32, first = min(lane * per, S), last = min(first + per, S);
     int sum = 0;
     for (int s = first; s < last; ++s) sum += base[s];
@@ -143,10 +145,13 @@ __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restri
     int run = incl - sum;
     for (int s = first; s < last; ++s) {
       const int v = base[s];
-      base[s] = run;
+      base[s] = min(run, most);
       run += v;
     }
-    if (lane == 31) base[S] = incl;
+    if (lane == 31) {
+      base[S] = min(incl, most);
+      if (incl > most && blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, S);
+    }
   }
 }
 

@@ -173,6 +173,9 @@ CASES = [
     dict(D=256, F=384, E=4, K=2, rows=[300, 1, 129, 210], align=1),
     dict(D=1000, F=1416, E=3, K=3, rows=[777, 0, 113], align=16),
     dict(D=128, F=128, E=2, K=1, rows=[2000, 48], align=128),
+    # long slots over odd numbers of tiles, chunks and blocks
+    dict(D=264, F=392, E=2, K=1, rows=[700, 31], align=1),
+    dict(D=392, F=40, E=1, K=1, rows=[449], align=8),
     # long sums, few rows
     dict(D=4096, F=2048, E=2, K=1, rows=[1, 15], align=1),
     dict(D=24, F=7168, E=2, K=1, rows=[20, 4], align=8),
@@ -307,6 +310,25 @@ def test_slots_without_expert_and_bad_tables():
                 assert ((yp[lo:hi].to(F64) - y).abs() <= most).all(), (bad_off, s)
                 yp[lo:hi] = 13.0
         assert torch.equal(yp, want)
+
+
+@pytest.mark.parametrize("T,rows", [(64, 60), (3000, 2900), (12000, 11900)])
+def test_overlapping_slots_stay_inside_the_workspace(T, rows):
+    """Tables that no plan makes: every other slot is the same rows.  More tiles than there is room for are left out and
+    reported; the first slots are right, and nothing behind the workspace or the result is touched."""
+    S = 40
+    shape = binding.Shape(T, 128, 128, 1, 1, S, 0, 1)
+    ctx, g, packed, dense, ws = make(shape, 8)
+    xp = normal(g, shape.Rcap, 128)
+    off = torch.tensor([0, rows] * (S // 2) + [0], dtype=torch.int32, device=DEV)
+    expert = torch.zeros(S, dtype=torch.int32, device=DEV)
+    room = torch.full((ws.numel() + (1 << 20),), 0x5A, dtype=torch.uint8, device=DEV)
+    out = torch.full((shape.Rcap + 500, 128), 13.0, dtype=torch.bfloat16, device=DEV)
+    call(ctx, xp, off, expert, packed, out[:shape.Rcap], room[:ws.numel()])
+    assert ctx.status() == binding.ERR_BAD_INDEX
+    assert (room[ws.numel():] == 0x5A).all() and (out[rows:] == 13.0).all()
+    y, most = bound(xp[:rows], *(w[0] for w in dense))
+    assert ((out[:rows].to(F64) - y).abs() <= most).all()
 
 
 def test_refusals_of_the_ffn():
