@@ -293,7 +293,8 @@ __device__ __forceinline__ void store_y(__nv_bfloat16* __restrict__ y, const flo
 //  - What a step costs beside its bytes: a wait, an expected count and a TMA load take one thread 300 clocks, so a stage is two
 //    weight tiles, 16 KB of memory; the waits around four MMAs take 380 clocks in which the tensor core, which holds few of
 //    them, runs dry, so two warps issue, each for its tile of the two (one warp for both: 409 ns for a stage, memory takes 370).
-// Warps: 0 loads weights, 2 rows, 1 and 3 issue products, 4..7 split the rows and drain the accumulators.
+// Warps: 0 loads weights; 1..7 split the rows first (eight rows of 7168 columns 5.1 us after the start, 8.1 with four warps), then 2 loads
+//    rows, 1 and 3 issue products, 4..7 drain the accumulators.
 template <int kRows_, int kStages_>
 struct Short {
   static constexpr int kRows = kRows_;                 // of a tile at most
@@ -468,6 +469,44 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
   auto up_tiles = [&](auto&& body) { return for_tiles(up_share, f_chunks, d_chunks, body); };
   auto down_tiles = [&](auto&& body) { return for_tiles(down_share, d_tiles, f_chunks, body); };
 
+  // x in two terms, by all warps but the one that loads weights: a warp does 1024 columns of a row
+  constexpr int kSplitters = Cfg::kThreads - 32;
+  if (warp > 0) {
+    const int worker = warp - 1, thread = worker * 32 + lane;
+    // nothing of h or of shared sums is there yet
+    if (thread < 3) part_there[thread * mx4::kMaxCtas + blockIdx.x] = 0;
+    for (int64_t i = (int64_t)blockIdx.x * kSplitters + thread; i < row_tiles * f_chunks; i += (int64_t)kSplitters * gridDim.x) h_there[i] = 0;
+    for_rows<1024>(rows_before, S, D, worker * gridDim.x + blockIdx.x, kSplitters / 32 * gridDim.x, [&](int slot, int r, int col0) {
+      const int in_tile = r % kRows;
+      const int rows_in_tile = min(kRows, rows_before.tile_base[slot + 1] - rows_before.tile_base[slot] - (r - in_tile));
+      const int tile = tb.tile_base[slot] + r / kRows;
+      if (tile >= tb.tile_base[slot + 1]) return;    // left out
+      uint8_t* image = x_image + (size_t)tile * d_chunks * Cfg::kImage;
+      const __nv_bfloat16* x = xp + (size_t)(__ldg(slot_row_off + slot) + r) * D;
+      Cols16 v[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) v[i] = load16(x, col0 + 512 * i + 16 * lane, D);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int col = col0 + 512 * i + 16 * lane;
+        uint4 code[2];
+        uint32_t word[2];
+        split16(v[i], lane, code, word);
+        if (col < d_chunks * kChunk) {
+          uint8_t* at = image + (size_t)(col / kChunk) * Cfg::kImage;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            *reinterpret_cast<uint4*>(at + mx4::image_code_at(in_tile, t, rows_in_tile, col % kChunk / 16)) = code[t];
+            if ((lane & 7) == 0) *reinterpret_cast<uint32_t*>(at + mx4::row_scale_at<kRows>(in_tile, t, rows_in_tile)) = word[t];
+          }
+        }
+      }
+    });
+    fence_proxy_async_global();
+    named_sync(1, kSplitters);
+    if (thread == 0) meeting.arrive();
+  }
+
   if (warp == 0) {
     if (lane == 0) {
       int stage = 0;
@@ -577,40 +616,6 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
   } else {
     const int quarter = warp & 3, thread = quarter * 32 + lane;
     uint8_t* staging = smem + Cfg::kStagingOffset + quarter * kStaging;
-    // x in two terms: a warp does 1024 columns of a row
-    {
-      if (thread < 3) part_there[thread * mx4::kMaxCtas + blockIdx.x] = 0;
-      for (int64_t i = (int64_t)blockIdx.x * 128 + thread; i < row_tiles * f_chunks; i += 128 * (int64_t)gridDim.x) h_there[i] = 0;
-      for_rows<1024>(rows_before, S, D, quarter * gridDim.x + blockIdx.x, 4 * gridDim.x, [&](int slot, int r, int col0) {
-        const int in_tile = r % kRows;
-        const int rows_in_tile = min(kRows, rows_before.tile_base[slot + 1] - rows_before.tile_base[slot] - (r - in_tile));
-        const int tile = tb.tile_base[slot] + r / kRows;
-        if (tile >= tb.tile_base[slot + 1]) return;    // left out
-        uint8_t* image = x_image + (size_t)tile * d_chunks * Cfg::kImage;
-        const __nv_bfloat16* x = xp + (size_t)(__ldg(slot_row_off + slot) + r) * D;
-        Cols16 v[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) v[i] = load16(x, col0 + 512 * i + 16 * lane, D);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int col = col0 + 512 * i + 16 * lane;
-          uint4 code[2];
-          uint32_t word[2];
-          split16(v[i], lane, code, word);
-          if (col < d_chunks * kChunk) {
-            uint8_t* at = image + (size_t)(col / kChunk) * Cfg::kImage;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              *reinterpret_cast<uint4*>(at + mx4::image_code_at(in_tile, t, rows_in_tile, col % kChunk / 16)) = code[t];
-              if ((lane & 7) == 0) *reinterpret_cast<uint32_t*>(at + mx4::row_scale_at<kRows>(in_tile, t, rows_in_tile)) = word[t];
-            }
-          }
-        }
-      });
-    }
-    fence_proxy_async_global();
-    named_sync(1, 128);
-    if (thread == 0) meeting.arrive();
 
     int acc = 0;
     uint32_t acc_phase = 0;
