@@ -80,8 +80,8 @@ typedef struct moegps_shape {
 typedef struct moegps_ctx moegps_ctx_t;   /* opaque: shape, device id, device status word, cached TMA descriptors */
 
 /* Create / destroy a context on CUDA device `device`.  Allocates one small block of device memory
- * (about 1 KiB: the status word and the router's histogram accumulators); this is the only device
- * allocation the library ever makes. */
+ * (about 2 KiB: the status word, the router's histogram accumulators and the count by which the blocks
+ * of expert_ffn4 meet); this is the only device allocation the library ever makes. */
 MOEGPS_API int moegps_create(moegps_ctx_t** out, const moegps_shape_t* shape, int device);
 MOEGPS_API int moegps_destroy(moegps_ctx_t* ctx);
 
@@ -388,7 +388,8 @@ MOEGPS_API int moegps_weights_dequantize4(moegps_ctx_t* ctx, const void* w4, con
  * once to bf16.  A row that holds an infinity or a NaN gives NaN.
  * xp, slot_row_off, slot_expert, yp as in moegps_expert_ffn: padding rows of a slot yield unspecified values, rows outside every
  * slot and slots with slot_expert < 0 are not written, a slot with an extent outside [0, Rcap] is skipped and
- * MOEGPS_ERR_BAD_INDEX recorded.
+ * MOEGPS_ERR_BAD_INDEX recorded.  Of slots that overlap (no plan makes such) those that exceed the workspace are left out, and the
+ * same is recorded.  yp may be xp.
  * workspace: moegps_expert_ffn4_workspace_bytes(shape) bytes, 16-byte aligned, contents irrelevant; its size cannot be checked
  * here.  Calls that may overlap on the GPU need a workspace each. */
 MOEGPS_API size_t moegps_expert_ffn4_workspace_bytes(const moegps_shape_t* shape);

@@ -110,7 +110,7 @@ __device__ __forceinline__ void split16(const Cols16& c, int lane, uint4 (&code)
 }
 
 // The rows of all slots, and of each its columns in blocks of kCols, dealt to `workers` warps one after the other:
-// body(slot, row of the slot, first column).  rows_before: rows of the slots before each.  (Without a division for each unit:
+// body(slot, row of the slot, first column), until it says false.  rows_before: rows of the slots before each.  (Without a division for each unit:
 // a 64-bit one takes as long as a unit's arithmetic.)
 template <int kCols, class Body>
 __device__ __forceinline__ void for_rows(const Tables& rows_before, int S, int D, int worker, int workers, Body&& body) {
@@ -125,7 +125,7 @@ __device__ __forceinline__ void for_rows(const Tables& rows_before, int S, int D
         if (rows_before.tile_base[mid] <= n) slot = mid; else hi = mid;
       }
     }
-    body(slot, n - rows_before.tile_base[slot], block * kCols);
+    if (!body(slot, n - rows_before.tile_base[slot], block * kCols)) return;
     n = n > INT32_MAX - row_step - 1 ? INT32_MAX : n + row_step;
     block += col_step;
     if (block >= col_blocks) { block -= col_blocks; ++n; }
@@ -152,7 +152,7 @@ split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ s
   for_rows<512>(units, S, D, blockIdx.x * kWarps + warp, gridDim.x * kWarps, [&](int slot, int unit, int col0) {
     const int first = __ldg(slot_row_off + slot), j = unit / kUnits, half = unit / 32 % 2, b = unit % 32;
     const int rows = min(kRows, __ldg(slot_row_off + slot + 1) - first - j * kRows), in_tile = half * 128 + b;
-    if (in_tile >= rows) return;
+    if (in_tile >= rows) return true;
     const size_t row = (size_t)first + j * kRows + in_tile;
     const int col = col0 + 16 * lane;
     Cols16 v[4];
@@ -179,6 +179,7 @@ split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ s
         *reinterpret_cast<uint4*>(scales + mx4::row_scale_at<kRows>(in_tile, t, rows)) =
             make_uint4(words[t][0], words[t][1], words[t][2], words[t][3]);
     }
+    return true;
   });
 }
 
@@ -480,7 +481,7 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
       const int in_tile = r % kRows;
       const int rows_in_tile = min(kRows, rows_before.tile_base[slot + 1] - rows_before.tile_base[slot] - (r - in_tile));
       const int tile = tb.tile_base[slot] + r / kRows;
-      if (tile >= tb.tile_base[slot + 1]) return;    // left out
+      if (tile >= tb.tile_base[slot + 1]) return false;      // left out, like all behind it
       uint8_t* image = x_image + (size_t)tile * d_chunks * Cfg::kImage;
       const __nv_bfloat16* x = xp + (size_t)(__ldg(slot_row_off + slot) + r) * D;
       Cols16 v[2];
@@ -501,6 +502,7 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
           }
         }
       }
+      return true;
     });
     fence_proxy_async_global();
     named_sync(1, kSplitters);

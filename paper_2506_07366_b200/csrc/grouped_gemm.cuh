@@ -134,22 +134,22 @@ __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restri
     int32_t* base = threadIdx.x < 32 ? tb.tile_base : rows_before->tile_base;
     const int most = threadIdx.x < 32 ? max_tiles : INT32_MAX;
     const int lane = threadIdx.x & 31, per = (S + 31) / 32, first = min(lane * per, S), last = min(first + per, S);
-    int sum = 0;
+    int64_t sum = 0;                                  // (slots that overlap can have more rows than an int32 holds)
     for (int s = first; s < last; ++s) sum += base[s];
-    int incl = sum;
+    int64_t incl = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, incl, d);
+      const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
       if (lane >= d) incl += o;
     }
-    int run = incl - sum;
+    int64_t run = incl - sum;
     for (int s = first; s < last; ++s) {
       const int v = base[s];
-      base[s] = min(run, most);
+      base[s] = (int)min(run, (int64_t)most);
       run += v;
     }
     if (lane == 31) {
-      base[S] = min(incl, most);
+      base[S] = (int)min(incl, (int64_t)most);
       if (incl > most && blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, S);
     }
   }

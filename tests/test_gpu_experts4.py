@@ -267,6 +267,27 @@ def test_rows_that_are_not_finite_stay_apart():
     assert torch.equal(got[keep], yp[keep])
 
 
+@pytest.mark.parametrize("T", [50, 700])                 # short and long slots
+def test_the_result_over_its_rows(T):
+    """yp = xp gives the same; in long slots too, rows that are not finite stay apart."""
+    shape = binding.Shape(T, 200, 136, 2, 1, 2, 0, 1)
+    ctx, g, packed, dense, ws = make(shape, 15)
+    xp = normal(g, T, 200)
+    xp[7, 150], xp[T - 1, 0] = float("inf"), float("nan")
+    off, expert = slots([T - 17, 17], [0, 1], 1)
+    yp = torch.zeros_like(xp)
+    call(ctx, xp, off, expert, packed, yp, ws)
+    keep = torch.ones(T, dtype=torch.bool, device=DEV)
+    keep[[7, T - 1]] = False
+    y, most = bound(xp[:T - 17], *(w[0] for w in dense))
+    ok = keep[:T - 17]
+    assert ((yp[:T - 17].to(F64) - y).abs() <= most)[ok].all()
+    assert torch.isnan(yp[~keep]).all() and torch.isfinite(yp[keep]).all()
+    call(ctx, xp, off, expert, packed, xp, ws)
+    ctx.check_status()
+    assert torch.equal(xp[keep], yp[keep]) and torch.isnan(xp[~keep]).all()
+
+
 def test_weights_that_are_not_finite():
     """A NaN block makes its output NaN for that expert's rows, and no other output."""
     shape = binding.Shape(8, 64, 64, 2, 1, 2, 0, 1)
@@ -329,6 +350,25 @@ def test_overlapping_slots_stay_inside_the_workspace(T, rows):
     assert (room[ws.numel():] == 0x5A).all() and (out[rows:] == 13.0).all()
     y, most = bound(xp[:rows], *(w[0] for w in dense))
     assert ((out[:rows].to(F64) - y).abs() <= most).all()
+
+
+def test_overlapping_slots_whose_sum_passes_32_bits():
+    """Half of 1024 slots are the same 16.7 million rows each: in the units of 64 to a tile in which they are dealt their sum is above 2^31."""
+    T, S = 1 << 21, 1024
+    shape = binding.Shape(T, 8, 8, 8, 8, S, 0, 1)
+    ctx, g, packed, dense, ws = make(shape, 9)
+    rows = shape.Rcap - 100
+    assert S // 2 * (-(-rows // 224) * 64) > 2 ** 31
+    xp = normal(g, shape.Rcap, 8)
+    off = torch.tensor([0, rows] * (S // 2) + [0], dtype=torch.int32, device=DEV)
+    expert = torch.zeros(S, dtype=torch.int32, device=DEV)
+    out = torch.full((shape.Rcap, 8), 13.0, dtype=torch.bfloat16, device=DEV)
+    call(ctx, xp, off, expert, packed, out, ws)
+    assert ctx.status() == binding.ERR_BAD_INDEX
+    assert (out[rows:] == 13.0).all()
+    for lo in (0, rows // 2, rows - 500):
+        y, most = bound(xp[lo:lo + 500], *(w[0] for w in dense))
+        assert ((out[lo:lo + 500].to(F64) - y).abs() <= most).all()
 
 
 def test_refusals_of_the_ffn():
