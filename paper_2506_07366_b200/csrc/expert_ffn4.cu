@@ -292,7 +292,8 @@ __device__ __forceinline__ void store_y(__nv_bfloat16* __restrict__ y, const flo
 //  - x and h lie in the workspace as the images that a chunk of a tile has in shared memory (512 bytes of scales, then 128-byte
 //    rows, swizzled): one bulk copy for each chunk.
 //  - What a step costs beside its bytes: a wait, an expected count and a TMA load take one thread 300 clocks, so a stage is two
-//    weight tiles, 16 KB of memory; the waits around four MMAs take 380 clocks in which the tensor core, which holds few of
+//    weight tiles, 16 KB of memory, and the warp that loads rows also states the bytes and brings the second tile's scales (with
+//    weights that lie in L2, 4096 rows of an expert 4096 x 4096 in tiles of 16: 835 us, 745 so); the waits around four MMAs take 380 clocks in which the tensor core, which holds few of
 //    them, runs dry, so two warps issue, each for its tile of the two (one warp for both: 409 ns for a stage, memory takes 370).
 // Warps: 0 loads weights; 1..7 split the rows first (eight rows of 7168 columns 5.1 us after the start, 8.1 with four warps), then 2 loads
 //    rows, 1 and 3 issue products, 4..7 drain the accumulators.
@@ -421,7 +422,7 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   Tables& tb = *reinterpret_cast<Tables*>(smem + Cfg::kTablesOffset);                      // row tiles
   Tables& rows_before = *reinterpret_cast<Tables*>(smem + Cfg::kTablesOffset + sizeof(Tables));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::kBarsOffset);     // [kStages]  both loaders -> MMAs
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::kBarsOffset);     // [kStages]  loads -> MMAs; the one that loads rows says how many bytes
   uint64_t* empty = full + kStages;                  // [kStages]  both issuing warps -> loaders
   uint64_t* acc_full = empty + kStages;              // [2]  both issuing warps -> epilogue
   uint64_t* acc_empty = acc_full + 2;                // [2]
@@ -434,7 +435,7 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
   const int d_chunks = mx4::chunks_of(D), f_chunks = mx4::chunks_of(F);      // f_chunks also the tiles of gate + up
   const int d_tiles = (d_chunks + 1) / 2;                                    // of down
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 2); mbar_init(&empty[i], 2); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 2); }
     for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 2); mbar_init(&acc_empty[i], 4); }
     *goal = 0;
     *abort_flag = 0;
@@ -513,44 +514,41 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
     if (lane == 0) {
       int stage = 0;
       uint32_t phase = 0;
-      // the two weight tiles of chunks k0 .. k1 - 1: rows m0, m1 of either matrix, their scales at s0, s1 (m1 < 0: there is one)
-      auto load = [&](const CUtensorMap* tm0, const CUtensorMap* tm1, int expert, int m0, int m1, const uint8_t* s0, const uint8_t* s1,
-                      int k0, int k1) {
-        for (int c = k0; c < k1; ++c, s0 += kScaleTile, s1 += kScaleTile) {
+      // the two weight tiles of chunks k0 .. k1 - 1: rows m0, m1 of either matrix (m1 < 0: there is one), the first's scales at s0
+      auto load = [&](const CUtensorMap* tm0, const CUtensorMap* tm1, int expert, int m0, int m1, const uint8_t* s0, int k0, int k1) {
+        for (int c = k0; c < k1; ++c, s0 += kScaleTile) {
           if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag)) return false;
           uint8_t* a = smem + stage * Cfg::kStageBytes;
-          mbar_arrive_expect_tx(&full[stage], (m1 < 0 ? 1 : 2) * (Cfg::kABytes / 2 + kScaleTile));
           tma_load_3d(a, tm0, &full[stage], c * kChunk, m0, expert);
+          if (m1 >= 0) tma_load_3d(a + Cfg::kABytes, tm1, &full[stage], c * kChunk, m1, expert);
           bulk_load(a + Cfg::kScalesAt, s0, kScaleTile, &full[stage]);
-          if (m1 >= 0) {
-            tma_load_3d(a + Cfg::kABytes, tm1, &full[stage], c * kChunk, m1, expert);
-            bulk_load(a + Cfg::kScalesAt + kScaleTile, s1, kScaleTile, &full[stage]);
-          }
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
         return true;
       };
       const bool ok = up_tiles([&](const Tile& tc, int64_t, int k0, int k1) {
         const size_t at = (((size_t)tc.expert * f_chunks + tc.m) * d_chunks + k0) * kScaleTile;
-        return load(&tm_gate, &tm_up, tc.expert, tc.m * kTile, tc.m * kTile, gate_scale + at, up_scale + at, k0, k1);
+        return load(&tm_gate, &tm_up, tc.expert, tc.m * kTile, tc.m * kTile, gate_scale + at, k0, k1);
       }) && down_tiles([&](const Tile& tc, int64_t, int k0, int k1) {
         const uint8_t* s0 = down_scale + (((size_t)tc.expert * d_chunks + 2 * tc.m) * f_chunks + k0) * kScaleTile;
-        return load(&tm_down, &tm_down, tc.expert, 2 * tc.m * kTile, 2 * tc.m + 1 < d_chunks ? (2 * tc.m + 1) * kTile : -1, s0,
-                    s0 + (size_t)f_chunks * kScaleTile, k0, k1);
+        return load(&tm_down, &tm_down, tc.expert, 2 * tc.m * kTile, 2 * tc.m + 1 < d_chunks ? (2 * tc.m + 1) * kTile : -1, s0, k0, k1);
       });
       if (!ok) linger();
     }
   } else if (warp == 2) {
     int stage = 0;
     uint32_t phase = 0;
-    // by one lane
-    auto load = [&](const uint8_t* image, const Tile& tc, int chunks, int k0, int k1) {
-      const uint32_t bytes = kScaleTile + 2 * round_up(tc.rows, 16) * kChunk;
+    // by one lane: the rows, and the second weight tile's scales at s1 (if there is one)
+    auto load = [&](const uint8_t* image, const uint8_t* s1, const Tile& tc, int chunks, int k0, int k1) {
+      const uint32_t image_bytes = kScaleTile + 2 * round_up(tc.rows, 16) * kChunk;
+      const uint32_t bytes = image_bytes + (s1 ? 2 : 1) * (Cfg::kABytes / 2 + kScaleTile);
       const uint8_t* from = image + ((size_t)tc.row_tile * chunks + k0) * Cfg::kImage;
       for (int c = k0; c < k1; ++c, from += Cfg::kImage) {
         if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag)) return false;
+        uint8_t* a = smem + stage * Cfg::kStageBytes;
         mbar_arrive_expect_tx(&full[stage], bytes);
-        bulk_load(smem + stage * Cfg::kStageBytes + Cfg::kImageAt, from, bytes, &full[stage]);
+        bulk_load(a + Cfg::kImageAt, from, image_bytes, &full[stage]);
+        if (s1) bulk_load(a + Cfg::kScalesAt + kScaleTile, s1 + (size_t)(c - k0) * kScaleTile, kScaleTile, &full[stage]);
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
       return true;
@@ -559,18 +557,21 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
     if (lane == 0) {
       ok = meeting.wait(abort_flag);
       fence_proxy_async_global();
-      ok = ok && up_tiles([&](const Tile& tc, int64_t, int k0, int k1) { return load(x_image, tc, d_chunks, k0, k1); });
+      ok = ok && up_tiles([&](const Tile& tc, int64_t, int k0, int k1) {
+        return load(x_image, up_scale + (((size_t)tc.expert * f_chunks + tc.m) * d_chunks + k0) * kScaleTile, tc, d_chunks, k0, k1);
+      });
     }
     ok = __all_sync(0xffffffffu, ok);
     // 32 chunks of h at a time, when the four warps that wrote each have reported
     ok = ok && down_tiles([&](const Tile& tc, int64_t, int k0, int k1) {
+      const uint8_t* s1 = down_scale + ((size_t)tc.expert * d_chunks + 2 * tc.m + 1) * f_chunks * kScaleTile;
       for (int c = k0; c < k1; c += 32) {
         const int* there = h_there + (size_t)tc.row_tile * f_chunks + min(c + lane, k1 - 1);
         bool go = poll(abort_flag, [&]() { return load_acquire(there) == 4; });
         go = __all_sync(0xffffffffu, go);
         if (lane == 0 && go) {
           fence_proxy_async_global();
-          go = load(h_image, tc, f_chunks, c, min(c + 32, k1));
+          go = load(h_image, 2 * tc.m + 1 < d_chunks ? s1 + (size_t)c * kScaleTile : nullptr, tc, f_chunks, c, min(c + 32, k1));
         }
         if (!__all_sync(0xffffffffu, go)) return false;
       }
