@@ -3,7 +3,8 @@
 // Both are bound by memory: 2 + 17/32 bytes a weight.  A block of 256 threads owns one tile of 128 outputs and one chunk of
 // 128 inputs, so the tile's 512 scale bytes are one run of memory; eight threads share an output's 128 inputs (two to a block of
 // 32: with one 16-byte load each and four to a block, the maximum and the scale took as long as memory), four outputs per thread
-// are in flight at once.
+// are in flight at once.  One matrix quantized and read back: 8 x 14336 x 4096 385 us (2.13 GB, 5.5 TB/s), 13 x 1000 x 1416 17.5 us
+// (21 without the early launch of the second).
 #include "bf16x8.cuh"
 #include "common.cuh"
 #include "mx4.cuh"
@@ -23,6 +24,8 @@ __global__ void __launch_bounds__(kThreads) quantize4_kernel(const __nv_bfloat16
   const int piece = threadIdx.x % kPieces, row = threadIdx.x / kPieces;
   const int col = chunk * mx4::kChunk + 16 * piece;
   const size_t row0 = (size_t)e * N;
+  launch_dependents();
+  wait_for_predecessor();
   uint4 v[kSteps][2];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
@@ -74,6 +77,8 @@ __global__ void __launch_bounds__(kThreads) dequantize4_kernel(const uint8_t* __
   const int piece = threadIdx.x % 16, row = threadIdx.x / 16;
   const int col = chunk * mx4::kChunk + 8 * piece;
   const size_t row0 = (size_t)e * N;
+  launch_dependents();
+  wait_for_predecessor();
   if (threadIdx.x < mx4::kScaleTile / 16)
     reinterpret_cast<uint4*>(scales)[threadIdx.x] =
         __ldcs(reinterpret_cast<const uint4*>(w4_scale + (size_t)blockIdx.x * mx4::kScaleTile) + threadIdx.x);
@@ -116,8 +121,8 @@ int moegps_launch_weights_quantize4(moegps_ctx* ctx, const void* w, bool down, v
   int N, C;
   unsigned blocks;
   dims(ctx->shape, down, N, C, blocks);
-  quantize4_kernel<<<blocks, kThreads, 0, st>>>(static_cast<const __nv_bfloat16*>(w), static_cast<uint8_t*>(w4),
-                                                static_cast<uint8_t*>(w4_scale), N, C);
+  MOEGPS_CUDA_TRY(ctx, launch_after(quantize4_kernel, dim3(blocks), kThreads, 0, st, static_cast<const __nv_bfloat16*>(w),
+                                    static_cast<uint8_t*>(w4), static_cast<uint8_t*>(w4_scale), N, C));
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }
@@ -126,8 +131,8 @@ int moegps_launch_weights_dequantize4(moegps_ctx* ctx, const void* w4, const voi
   int N, C;
   unsigned blocks;
   dims(ctx->shape, down, N, C, blocks);
-  dequantize4_kernel<<<blocks, kThreads, 0, st>>>(static_cast<const uint8_t*>(w4), static_cast<const uint8_t*>(w4_scale),
-                                                  static_cast<__nv_bfloat16*>(w), N, C);
+  MOEGPS_CUDA_TRY(ctx, launch_after(dequantize4_kernel, dim3(blocks), kThreads, 0, st, static_cast<const uint8_t*>(w4),
+                                    static_cast<const uint8_t*>(w4_scale), static_cast<__nv_bfloat16*>(w), N, C));
   MOEGPS_AFTER_LAUNCH(ctx);
   return MOEGPS_OK;
 }
