@@ -1109,7 +1109,7 @@ int tmap_failed(moegps_ctx* ctx) {
 int launch_split(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   const moegps_shape_t& s = ctx->shape;
   const int64_t units = c.l.long_tiles * 64 * ((s.D + 511) / 512) / (kSplitThreads / 32);
-  const int64_t resident = 8 * (int64_t)ctx->sm_count;
+  const int64_t resident = 4 * (int64_t)ctx->sm_count;         // what runs at once by registers (8 for each SM: 100 and 94 us, 49152 x 2048)
   split_kernel<<<(unsigned)(units < resident ? units : resident), kSplitThreads, 0, st>>>(
       static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert, s.S, s.E, s.D, (int)c.l.rows,
       c.l.cut.short_rows + 1, (int)c.l.long_tiles, c.x, ctx->d_status);
