@@ -478,6 +478,8 @@ class Context:
                                     t("workspace", u8))
         self._route_backward_bytes = route_backward_workspace_bytes(s)
         (up_codes, up_scales), (down_codes, down_scales) = s.w4_shapes(), s.w4_shapes(down=True)
+        # of a matrix, its codes and its scales; [1]: down
+        self._w4_shapes = ((s.E, s.F, s.D), up_codes, up_scales), ((s.E, s.D, s.F), down_codes, down_scales)
         self._expert_ffn4 = call("expert_ffn4", *xp, row_off, expert, t("gate4", u8, *up_codes), t("up4", u8, *up_codes),
                                  t("down4", u8, *down_codes), t("gate4_scale", u8, *up_scales), t("up4_scale", u8, *up_scales),
                                  t("down4_scale", u8, *down_scales), *yp, t("workspace", u8))
@@ -541,21 +543,19 @@ class Context:
     # -- experts in 4 bits --------------------------------------------------------------------
     def weights_quantize4(self, w, w4, w4_scale, down=False, stream=None):
         """w: bf16 [E, F, D] (down: [E, D, F]) -> codes and scales of Shape.w4_shapes(down)."""
-        s = self.shape
-        codes, scales = s.w4_shapes(down)
+        down = bool(down)
+        dense, codes, scales = self._w4_shapes[down]
         self._check(_lib().moegps_weights_quantize4(
-            self._h, _ptr(w, torch.bfloat16, (s.E, s.D, s.F) if down else (s.E, s.F, s.D), "w"), int(bool(down)),
-            _ptr(w4, torch.uint8, codes, "w4"), _ptr(w4_scale, torch.uint8, scales, "w4_scale"), _stream(stream)),
-            "moegps_weights_quantize4")
+            self._h, _ptr(w, torch.bfloat16, dense, "w"), down, _ptr(w4, torch.uint8, codes, "w4"),
+            _ptr(w4_scale, torch.uint8, scales, "w4_scale"), _stream(stream)), "moegps_weights_quantize4")
 
     def weights_dequantize4(self, w4, w4_scale, w, down=False, stream=None):
         """What the codes stand for, exactly, into w: bf16 [E, F, D] (down: [E, D, F])."""
-        s = self.shape
-        codes, scales = s.w4_shapes(down)
+        down = bool(down)
+        dense, codes, scales = self._w4_shapes[down]
         self._check(_lib().moegps_weights_dequantize4(
-            self._h, _ptr(w4, torch.uint8, codes, "w4"), _ptr(w4_scale, torch.uint8, scales, "w4_scale"), int(bool(down)),
-            _ptr(w, torch.bfloat16, (s.E, s.D, s.F) if down else (s.E, s.F, s.D), "w"), _stream(stream)),
-            "moegps_weights_dequantize4")
+            self._h, _ptr(w4, torch.uint8, codes, "w4"), _ptr(w4_scale, torch.uint8, scales, "w4_scale"), down,
+            _ptr(w, torch.bfloat16, dense, "w"), _stream(stream)), "moegps_weights_dequantize4")
 
     def expert_ffn4(self, xp, slot_row_off, slot_expert, gate4, up4, down4, gate4_scale, up4_scale, down4_scale, yp, workspace,
                     stream=None):
