@@ -85,7 +85,8 @@ struct Cut {
 // 2.5 ns for 16 KB.  Measured (us; layers A: 256 experts 7168 x 2048, 970 us of weights, zipf 1; B: 64 experts 2048 x 1408, 53; C: 8
 // experts 4096 x 14336, 107; D: 8 experts 1024 x 2048, 4):
 //   tiles of 16 or 48 rows: A 1.8 rows a slot 389 / 417, 3.6 604 / 560; B 3.6 62 / 66, 9.6 88 / 86; C 8 144 / 151, 16 177 / 164
-//   32 or 48: A 3.6 541 / 577, 14 1040 / 1097; B 9.6 84 / 87, 19 110 / 125; C 16 156 / 164; D 32 34 / 35, 64 29 / 27
+//   32 or 48: A 3.6 541 / 577, 14 1040 / 1097; B 9.6 84 / 87, 19 93 / 98, 38 134 / 131; C 16 145 / 161, 32 197 / 191 (in long runs,
+//     at the power limit, 161 / 178 and 224 / 215), 48 243 / 229; D 32 34 / 35, 64 29 / 27
 //   short or both: A 7 rows a slot 749 / 766, 14 1107 / 1058, 28 1658 / 1277
 //   short or long: B 38 157 / 182, 58 189 / 195, 77 229 / 213; C 64 268 / 326, 96 366 / 361; D 128 52 / 60, 256 66 / 71, 512 100 / 103
 //   long or both, where neither is better by more than 3 %: B from 77, C from 96, D from 256 rows a slot
@@ -96,7 +97,7 @@ inline Cut cut_of(const moegps_shape_t& s) {
   const double weights_us = 0.0025 * s.S * (double)(f * d + (d + 1) / 2 * f);
   const bool heavy = weights_us > 300.0;
   if (per_slot <= (heavy ? 3 : 8)) return {16, INT32_MAX};
-  if (per_slot <= (heavy ? 10 : weights_us > 20.0 ? 64 : 256)) return {per_slot <= 32 ? 32 : 48, INT32_MAX};
+  if (per_slot <= (heavy ? 10 : weights_us > 20.0 ? 64 : 256)) return {per_slot <= 24 ? 32 : 48, INT32_MAX};
   return {32, heavy ? 32 : 0};
 }
 constexpr int kLongRows = 224;
