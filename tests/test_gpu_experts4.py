@@ -433,6 +433,43 @@ def test_two_streams_and_a_graph():
         check(xa, off, expert, dense, ya, 13.0)
 
 
+@pytest.mark.parametrize("rows", [[50, 3, 0, 43], [700, 1, 0, 500]])          # short and long slots
+def test_one_context_on_two_streams_and_in_two_branches_of_a_graph(rows):
+    """Calls that overlap, each with its workspace; the context's first call is a captured one."""
+    T = sum(rows)
+    shape = binding.Shape(T, 256, 384, 4, 1, 4, 0, 1)
+    ctx, g, packed, dense, ws = make(shape, 22)
+    ctx = binding.Context(shape)
+    off, expert = slots(rows, [0, 1, 2, 3], 1)
+    x = [normal(g, T, 256) for _ in range(2)]
+    y = [torch.full((T, 256), 13.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    w = [ws, torch.empty_like(ws)]
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        for i, stream in enumerate((here, side)):
+            call(ctx, x[i], off, expert, packed, y[i], w[i], stream=stream)
+        here.wait_stream(side)
+    for _ in range(10):
+        graph.replay()
+    torch.cuda.synchronize()
+    ctx.check_status()
+    captured = [v.clone() for v in y]
+    for i in range(2):
+        check(x[i], off, expert, dense, y[i], 13.0)
+        y[i].fill_(13.0)
+    streams = [torch.cuda.Stream(), side]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            call(ctx, x[i], off, expert, packed, y[i], w[i], stream=streams[i])
+    torch.cuda.synchronize()
+    ctx.check_status()
+    assert all(torch.equal(a, b) for a, b in zip(y, captured))
+
+
 # ------------------------------------------------------------------------------------------- layer
 LAYERS = [
     (wl.WORKLOADS["tiny"].scaled(sigma_x=1.0, S=11), 16),
