@@ -29,7 +29,7 @@ struct moegps_ctx {
   bool tm2_valid;
   bool ffn_attr_done[3]; // dynamic shared-memory limit raised: gate+up, down, gate+up with kept activations
   bool data_gradient_attr_done[2][4];   // the same for the gradient's kernels: (act, input) x tile shapes
-  bool ffn4_attr_done[5];   // on 4-bit weights: gate+up of long slots; short slots in tiles of 16, 32, 48; down of long slots
+  bool ffn4_attr_done[4];   // on 4-bit weights: short runs of slots in tiles of up to 48, 32 rows; gate+up of long ones, their down
   bool weight_gradient_attr_done, router_weight_attr_done;
   // cached TMA descriptors of the router
   const void* rt_key[2];

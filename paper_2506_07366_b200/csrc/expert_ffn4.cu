@@ -8,7 +8,7 @@
 // groups by the TMA load that brings it (8 bytes of codes, 8 unused): 8 KB of memory traffic for 16 KB of shared memory,
 // and no thread touches a weight.  The scales of the rows lie in the workspace as tensor memory wants them, tile by tile.
 //
-// Two ways, side by side in a call or one for all slots (mx4::cut_of): for slots of few rows one launch that is bound by reading
+// Two ways, side by side in a call or one for all (mx4::cut_of): for runs of few rows one launch that is bound by reading
 // weights (short_kernel), for long ones three that are bound by products (split_kernel, wide_kernel twice).  Every wait is bounded.
 #include <type_traits>
 
@@ -20,36 +20,117 @@
 namespace {
 
 using namespace sm100;
-using grouped_gemm::build_tables;
 using grouped_gemm::kMaxS;
-using grouped_gemm::Tables;
 using mx4::kChunk;
 using mx4::kScaleTile;
 using mx4::kTile;
 
 __host__ __device__ constexpr int round_up(int n, int to) { return (n + to - 1) / to * to; }
 
-// A tile: rows row0 .. row0 + rows - 1 of one slot, times tile m of its expert's outputs.
+// Slots that follow one another and hold copies of one expert are one run of rows (a plan puts copies side by side): their weights
+// are read once, and tiles are cut from all their rows (48 tokens over 64 experts in 80 slots 55 -> 49 us).  Tiles and rows before
+// each slot; a run counts as its first slot.
+struct alignas(16) Runs {
+  int32_t tiles[kMaxS + 1], rows[kMaxS + 1];
+  uint32_t begins[kMaxS / 32];        // a bit for each slot that is not of the run before it
+};
+
+// All kThreads threads of the block call it; the sums are there after the next __syncthreads().  A slot whose extent is not inside
+// [0, rcap] gets no tiles, and the caller is told.  Runs of fewer than min_rows or more than max_rows rows are left to another
+// launch.  Tiles from number max_tiles on (there are so many only where slots overlap) are left out, and the caller is told.
+template <int kThreads, int kRows>
+__device__ __forceinline__ void build_runs(Runs& runs, const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert,
+                                           int S, int E, int rcap, int min_rows, int max_rows, int max_tiles,
+                                           int32_t* __restrict__ status) {
+  constexpr int kTurns = (kMaxS + kThreads - 1) / kThreads;
+  const int lane = threadIdx.x & 31;
+  // an expert, or a negative number where there is no copy or none that is in order
+  auto key_of = [&](int s, bool report) {
+    const int lo = slot_row_off[s], hi = slot_row_off[s + 1], e = slot_expert[s];
+    const bool good = lo >= 0 && hi >= lo && hi <= rcap;
+    if (report && (!good || (hi > lo && e >= E)) && blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
+    return good && e < E ? e : -1;
+  };
+  int key[kTurns];
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    const int s = i * kThreads + threadIdx.x;
+    if (s - lane >= S) break;                                    // (a whole warp)
+    key[i] = s < S ? key_of(s, true) : -1;
+    int before = __shfl_up_sync(0xffffffffu, key[i], 1);
+    if (lane == 0 && s > 0) before = key_of(s - 1, false);
+    const uint32_t begins = __ballot_sync(0xffffffffu, s < S && (s == 0 || key[i] != before));
+    if (lane == 0) runs.begins[s / 32] = begins;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    const int s = i * kThreads + threadIdx.x;
+    if (s >= S) break;
+    int word = s / 32, rows = 0;
+    if (key[i] >= 0 && (runs.begins[word] >> lane & 1)) {
+      uint32_t next = runs.begins[word] & ~((2u << lane) - 1);
+      while (!next && ++word < (S + 31) / 32) next = runs.begins[word];
+      rows = slot_row_off[next ? 32 * word + __ffs(next) - 1 : S] - slot_row_off[s];
+      if (rows < min_rows || rows > max_rows) rows = 0;
+    }
+    runs.tiles[s] = rows / kRows + (rows % kRows != 0);
+    runs.rows[s] = rows;
+  }
+  __syncthreads();
+  // exclusive sums of both, a warp for each, lane l has `per` consecutive slots
+  if (threadIdx.x < 64) {
+    int32_t* base = threadIdx.x < 32 ? runs.tiles : runs.rows;
+    const int per = (S + 31) / 32, first = min(lane * per, S), last = min(first + per, S);
+    int64_t sum = 0;                                             // (slots that overlap can have more rows than an int32 holds)
+    for (int s = first; s < last; ++s) sum += base[s];
+    int64_t incl = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += o;
+    }
+    const int64_t most = threadIdx.x < 32 ? max_tiles : INT32_MAX;
+    int64_t run = incl - sum;
+    for (int s = first; s < last; ++s) {
+      const int v = base[s];
+      base[s] = (int)min(run, most);
+      run += v;
+    }
+    if (lane == 31) {
+      base[S] = (int)min(incl, most);
+      if (incl > most && blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, S);
+    }
+  }
+}
+
+// A tile: rows row0 .. row0 + rows - 1 of one run, times tile m of its expert's outputs.
 struct Tile {
   int row0, rows, m, expert, row_tile;
 };
 
-// tb: first row tile of each slot.  Tiles are ordered by slot, then outputs, then rows, so that neighbours share weights.
+// Tiles are ordered by run, in it by groups of up to `group` row tiles, then by outputs, then by rows, so that neighbours share weights
+// and the rows of a group stay in L2.
 template <int kRows>
-__device__ __forceinline__ Tile tile_at(const Tables& tb, const int32_t* __restrict__ slot_row_off,
-                                        const int32_t* __restrict__ slot_expert, int S, int64_t t, int m_tiles) {
-  int lo = 0, hi = S;                 // find s with base[s] * m_tiles <= t < base[s + 1] * m_tiles
+__device__ __forceinline__ Tile tile_at(const Runs& runs, const int32_t* __restrict__ slot_row_off,
+                                        const int32_t* __restrict__ slot_expert, int S, int64_t t, int m_tiles, int group) {
+  int lo = 0, hi = S;                 // the last s with tiles[s] * m_tiles <= t
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if ((int64_t)tb.tile_base[mid] * m_tiles <= t) lo = mid; else hi = mid;
+    if ((int64_t)runs.tiles[mid] * m_tiles <= t) lo = mid; else hi = mid;
   }
-  const int base = tb.tile_base[lo], n = tb.tile_base[lo + 1] - base;
-  const int local = (int)(t - (int64_t)base * m_tiles);       // below n * m_tiles of one slot
+  const int base = runs.tiles[lo];
+  int n = runs.tiles[lo + 1] - base, local = (int)(t - (int64_t)base * m_tiles), j = 0;       // below n * m_tiles of one run
+  if (n > group) {
+    j = local / (group * m_tiles) * group;
+    local -= j * m_tiles;
+    n = min(group, n - j);
+  }
   Tile c;
   c.m = local / n;
-  const int j = local - c.m * n;
+  j += local - c.m * n;
   c.row0 = __ldg(slot_row_off + lo) + j * kRows;
-  c.rows = min(kRows, __ldg(slot_row_off + lo + 1) - c.row0);
+  c.rows = max(1, min(kRows, runs.rows[lo + 1] - runs.rows[lo] - j * kRows));    // (1: sums of rows that were cut off)
   c.expert = __ldg(slot_expert + lo);
   c.row_tile = base + j;
   return c;
@@ -109,49 +190,46 @@ __device__ __forceinline__ void split16(const Cols16& c, int lane, uint4 (&code)
   }
 }
 
-// The rows of all slots, and of each its columns in blocks of kCols, dealt to `workers` warps one after the other:
-// body(slot, row of the slot, first column), until it says false.  rows_before: rows of the slots before each.  (Without a division for each unit:
+// The rows of all runs (kUnits for each count of `before`), and of each its columns in blocks of kCols, dealt to `workers` warps one
+// after the other: body(first slot, row of the run, first column), until it says false.  (Without a division for each unit:
 // a 64-bit one takes as long as a unit's arithmetic.)
-template <int kCols, class Body>
-__device__ __forceinline__ void for_rows(const Tables& rows_before, int S, int D, int worker, int workers, Body&& body) {
-  const int rows = rows_before.tile_base[S], col_blocks = (D + kCols - 1) / kCols;
+template <int kCols, int kUnits, class Body>
+__device__ __forceinline__ void for_rows(const int32_t* before, int S, int D, int worker, int workers, Body&& body) {
+  const int rows = before[S] * kUnits, col_blocks = (D + kCols - 1) / kCols;
   const int row_step = workers / col_blocks, col_step = workers - row_step * col_blocks;
   int n = worker / col_blocks, block = worker - n * col_blocks, slot = 0;
   while (n < rows) {
-    if (rows_before.tile_base[slot + 1] <= n) {
+    if (before[slot + 1] * kUnits <= n) {
       int hi = S;                                      // the last slot that begins at or before row n
       while (hi - slot > 1) {
         const int mid = (slot + hi) >> 1;
-        if (rows_before.tile_base[mid] <= n) slot = mid; else hi = mid;
+        if (before[mid] * kUnits <= n) slot = mid; else hi = mid;
       }
     }
-    if (!body(slot, n - rows_before.tile_base[slot], block * kCols)) return;
+    if (!body(slot, n - before[slot] * kUnits, block * kCols)) return;
     n = n > INT32_MAX - row_step - 1 ? INT32_MAX : n + row_step;
     block += col_step;
     if (block >= col_blocks) { block -= col_blocks; ++n; }
   }
 }
 
-// For long slots.  A warp does 512 columns of rows b, b + 32, b + 64, b + 96 of 128 rows of a tile, whose scales lie side by
+// For long runs.  A warp does 512 columns of rows b, b + 32, b + 64, b + 96 of 128 rows of a tile, whose scales lie side by
 // side: 16 bytes at a time (4 at a time, a row for itself, these writes took 28 of 100 us on 49152 rows x 2048).
 __global__ void __launch_bounds__(kSplitThreads)
 split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert,
              int S, int E, int D, int rcap, int min_rows, int max_tiles, const mx4::Rows out, int32_t* __restrict__ status) {
   constexpr int kRows = mx4::kLongRows, kUnits = 64;  // of a tile: 2 x 128 rows at most
-  __shared__ Tables units, tiles;
+  __shared__ Runs runs;
   launch_dependents();
   wait_for_predecessor();
-  build_tables<kSplitThreads, kRows>(units, slot_row_off, slot_expert, S, E, kUnits, rcap, status, nullptr, min_rows, INT32_MAX,
-                                     max_tiles * kUnits);
-  __syncthreads();
-  build_tables<kSplitThreads, kRows>(tiles, slot_row_off, slot_expert, S, E, 1, rcap, status, nullptr, min_rows, INT32_MAX, max_tiles);
+  build_runs<kSplitThreads, kRows>(runs, slot_row_off, slot_expert, S, E, rcap, min_rows, INT32_MAX, max_tiles, status);
   __syncthreads();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int chunks = mx4::chunks_of(D);
   constexpr int kWarps = kSplitThreads / 32;
-  for_rows<512>(units, S, D, blockIdx.x * kWarps + warp, gridDim.x * kWarps, [&](int slot, int unit, int col0) {
+  for_rows<512, kUnits>(runs.tiles, S, D, blockIdx.x * kWarps + warp, gridDim.x * kWarps, [&](int slot, int unit, int col0) {
     const int first = __ldg(slot_row_off + slot), j = unit / kUnits, half = unit / 32 % 2, b = unit % 32;
-    const int rows = min(kRows, __ldg(slot_row_off + slot + 1) - first - j * kRows), in_tile = half * 128 + b;
+    const int rows = min(kRows, runs.rows[slot + 1] - runs.rows[slot] - j * kRows), in_tile = half * 128 + b;
     if (in_tile >= rows) return true;
     const size_t row = (size_t)first + j * kRows + in_tile;
     const int col = col0 + 16 * lane;
@@ -173,7 +251,7 @@ split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ s
     }
     if ((lane & 7) == 0 && col < chunks * kChunk) {
       uint8_t* scales =
-          out.scale + ((size_t)(tiles.tile_base[slot] + j) * chunks + col / kChunk) * mx4::kRowScaleBytes<kRows>;
+          out.scale + ((size_t)(runs.tiles[slot] + j) * chunks + col / kChunk) * mx4::kRowScaleBytes<kRows>;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
         *reinterpret_cast<uint4*>(scales + mx4::row_scale_at<kRows>(in_tile, t, rows)) =
@@ -276,8 +354,8 @@ __device__ __forceinline__ void store_y(__nv_bfloat16* __restrict__ y, const flo
   __syncwarp();
 }
 
-// ------------------------------------------------------------------------------------------- short slots
-// The whole FFN in one launch, for slots of few rows: what there is to do is to read the weights, and three launches in a row
+// ------------------------------------------------------------------------------------------- short runs
+// The whole FFN in one launch, for runs of few rows: what there is to do is to read the weights, and three launches in a row
 // cost 35 us beside the 29 that two 4096 x 14336 experts take to read (each has to start, build its tables, fill its ring and join
 // its sums).  The blocks are one for each SM, a cooperative launch, and wait for one another: all for all when the rows are split,
 // then for the parts of h that they need; the weights of the next product are loaded meanwhile.
@@ -293,7 +371,7 @@ __device__ __forceinline__ void store_y(__nv_bfloat16* __restrict__ y, const flo
 //    rows, swizzled): one bulk copy for each chunk.
 //  - What a step costs beside its bytes: a wait, an expected count and a TMA load take one thread 300 clocks, so a stage is two
 //    weight tiles, 16 KB of memory, and the warp that loads rows also states the bytes and brings the second tile's scales (with
-//    weights that lie in L2, 4096 rows of an expert 4096 x 4096 in tiles of 16: 835 us, 745 so); the waits around four MMAs take 380 clocks in which the tensor core, which holds few of
+//    weights that lie in L2, 4096 rows of an expert 4096 x 4096 in tiles of 32: 451 us, 432 so); the waits around four MMAs take 380 clocks in which the tensor core, which holds few of
 //    them, runs dry, so two warps issue, each for its tile of the two (one warp for both: 409 ns for a stage, memory takes 370).
 // Warps: 0 loads weights; 1..7 split the rows first (eight rows of 7168 columns 5.1 us after the start, 8.1 with four warps), then 2 loads
 //    rows, 1 and 3 issue products, 4..7 drain the accumulators.
@@ -309,7 +387,7 @@ struct Short {
   static constexpr int kStageBytes = round_up(kImageAt + kImage, 1024);
   static constexpr int kStagingOffset = kStages * kStageBytes;
   static constexpr int kTablesOffset = kStagingOffset + 4 * kStaging;
-  static constexpr int kBarsOffset = kTablesOffset + 2 * (int)sizeof(Tables);
+  static constexpr int kBarsOffset = kTablesOffset + (int)sizeof(Runs);
   static constexpr int kAccCols = 2 * kCols;
   static constexpr int kColsUsed = 2 * kAccCols + 16 * kStages;      // each issuing warp has its own copies of the scales
   static constexpr int kTmemCols = kColsUsed <= 256 ? 256 : 512;
@@ -420,8 +498,7 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
   constexpr int kRows = Cfg::kRows, kStages = Cfg::kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  Tables& tb = *reinterpret_cast<Tables*>(smem + Cfg::kTablesOffset);                      // row tiles
-  Tables& rows_before = *reinterpret_cast<Tables*>(smem + Cfg::kTablesOffset + sizeof(Tables));
+  Runs& runs = *reinterpret_cast<Runs*>(smem + Cfg::kTablesOffset);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::kBarsOffset);     // [kStages]  loads -> MMAs; the one that loads rows says how many bytes
   uint64_t* empty = full + kStages;                  // [kStages]  both issuing warps -> loaders
   uint64_t* acc_full = empty + kStages;              // [2]  both issuing warps -> epilogue
@@ -448,12 +525,12 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
     tmem_alloc(tmem_slot, Cfg::kTmemCols);
     tmem_relinquish();
   }
-  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status, &rows_before, 1, max_rows, max_tiles);
+  build_runs<Cfg::kThreads, kRows>(runs, slot_row_off, slot_expert, S, E, rcap, 1, max_rows, max_tiles, status);
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  const int64_t row_tiles = tb.tile_base[S];
+  const int64_t row_tiles = runs.tiles[S];
   const Share up_share(row_tiles * f_chunks, d_chunks, gridDim.x, blockIdx.x);
   const Share down_share(row_tiles * d_tiles, f_chunks, gridDim.x, blockIdx.x);
   const Meeting meeting = {meetings, goal};
@@ -463,7 +540,7 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
     int64_t t = share.tile, left = share.left;
     for (int k0 = share.chunk; left > 0; k0 = 0, ++t) {
       const int k1 = (int)min((int64_t)chunks, k0 + left);
-      if (!body(tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles), t, k0, k1)) return false;
+      if (!body(tile_at<kRows>(runs, slot_row_off, slot_expert, S, t, m_tiles, INT32_MAX), t, k0, k1)) return false;
       left -= k1 - k0;
     }
     return true;
@@ -478,11 +555,11 @@ short_kernel(const __grid_constant__ CUtensorMap tm_gate, const __grid_constant_
     // nothing of h or of shared sums is there yet
     if (thread < 3) part_there[thread * mx4::kMaxCtas + blockIdx.x] = 0;
     for (int64_t i = (int64_t)blockIdx.x * kSplitters + thread; i < row_tiles * f_chunks; i += (int64_t)kSplitters * gridDim.x) h_there[i] = 0;
-    for_rows<1024>(rows_before, S, D, worker * gridDim.x + blockIdx.x, kSplitters / 32 * gridDim.x, [&](int slot, int r, int col0) {
+    for_rows<1024, 1>(runs.rows, S, D, worker * gridDim.x + blockIdx.x, kSplitters / 32 * gridDim.x, [&](int slot, int r, int col0) {
       const int in_tile = r % kRows;
-      const int rows_in_tile = min(kRows, rows_before.tile_base[slot + 1] - rows_before.tile_base[slot] - (r - in_tile));
-      const int tile = tb.tile_base[slot] + r / kRows;
-      if (tile >= tb.tile_base[slot + 1]) return false;      // left out, like all behind it
+      const int rows_in_tile = min(kRows, runs.rows[slot + 1] - runs.rows[slot] - (r - in_tile));
+      const int tile = runs.tiles[slot] + r / kRows;
+      if (tile >= runs.tiles[slot + 1]) return false;      // left out, like all behind it
       uint8_t* image = x_image + (size_t)tile * d_chunks * Cfg::kImage;
       const __nv_bfloat16* x = xp + (size_t)(__ldg(slot_row_off + slot) + r) * D;
       Cols16 v[2];
@@ -766,7 +843,7 @@ struct Weights {
 };
 
 // ------------------------------------------------------------------------------------------- wide
-// A pair of CTAs works 256 weight rows x up to 224 rows of a slot; each CTA loads its 128 weight rows and half of the slot's
+// A pair of CTAs works 256 weight rows x up to 224 rows of a run; each CTA loads its 128 weight rows and half of those
 // rows.  Gate + up: a CTA's 128 weight rows are 64 gate rows and the 64 up rows of the same outputs, so that a tile needs
 // 224 accumulator columns and not twice that, and two tiles fit tensor memory; in the epilogue the warps of the gate's
 // lanes and of the up's exchange half of their values through shared memory.
@@ -789,11 +866,14 @@ struct Wide {
   static constexpr int kScaleCols = 4 + 4 * kRowScales / kScaleTile;
   static constexpr int kScaleBufs = 3;                 // tensor memory has no room for four
   static constexpr int kOutputs = kGateUp ? 128 : 256; // of a pair's tile
+  // Bytes of both terms of the rows of a group, which are read once for each tile of outputs: runs of 14400 rows x 4096, 118 MB, in
+  // one group pushed each other out of L2 (16384 tokens 8.8 ms, 10.3 so).  4 to 48 MB take the same.
+  static constexpr int kGroupL2 = 24 << 20;
   static constexpr int kEpilogueWarps = 8;
   static constexpr int kExchange = kGateUp ? kEpilogueWarps * 16 * 32 * 4 : 0;      // 16 x 32 fp32 for each epilogue warp
   static constexpr int kThreads = 128 + 32 * kEpilogueWarps;
   static constexpr size_t kSmem =
-      1024 + (size_t)kStages * kStageBytes + kGroups * kGroupBytes + kExchange + sizeof(Tables) + 256 + kEpilogueWarps * kStaging;
+      1024 + (size_t)kStages * kStageBytes + kGroups * kGroupBytes + kExchange + sizeof(Runs) + 256 + kEpilogueWarps * kStaging;
   // Rows come in one TMA box of 112 or in boxes of 32: a box takes its warp some 60 clocks, and 14 boxes of 16 for a chunk,
   // with the weights' two, held the products up (down on 16384 tokens 3.5 ms, 2.8 with one box).
   static constexpr int kBigBox = kRows / 2, kSmallBox = 32;
@@ -814,8 +894,8 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* w_scales = smem + (size_t)kStages * Cfg::kStageBytes;
   float* exchange = reinterpret_cast<float*>(w_scales + Cfg::kGroups * Cfg::kGroupBytes);
-  Tables& tb = *reinterpret_cast<Tables*>(reinterpret_cast<uint8_t*>(exchange) + Cfg::kExchange);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(&tb) + sizeof(Tables));
+  Runs& runs = *reinterpret_cast<Runs*>(reinterpret_cast<uint8_t*>(exchange) + Cfg::kExchange);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(&runs) + sizeof(Runs));
   uint64_t* full = bars;                     // [kStages]  both CTAs' loads -> MMA, on the leader
   uint64_t* empty = bars + kStages;          // [kStages]  MMA -> loads, in both
   uint64_t* acc_full = bars + 2 * kStages;   // [2]  MMA -> epilogue, in both
@@ -849,13 +929,14 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
     tmem_alloc_pair(tmem_slot, 512);
     tmem_relinquish_pair();
   }
-  build_tables<Cfg::kThreads, kRows>(tb, slot_row_off, slot_expert, S, E, 1, rcap, status, nullptr, min_rows, INT32_MAX, max_tiles);
+  build_runs<Cfg::kThreads, kRows>(runs, slot_row_off, slot_expert, S, E, rcap, min_rows, INT32_MAX, max_tiles, status);
   __syncwarp();
   tc_fence_before_sync();
   cluster_sync_all();
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  const int64_t total = (int64_t)tb.tile_base[S] * m_tiles;
+  const int64_t total = (int64_t)runs.tiles[S] * m_tiles;
+  const int rows_together = max(1, Cfg::kGroupL2 / (2 * kRows * kChunk * chunks));
 
   if (warp == 0) {
     if (lane == 0) {
@@ -864,7 +945,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
       bool ok = true;
       const uint32_t leader_full = map_to_cta(smem_u32(full), 0);
       for (int64_t t = pair; ok && t < total; t += pairs) {
-        const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+        const Tile tc = tile_at<kRows>(runs, slot_row_off, slot_expert, S, t, m_tiles, rows_together);
         const uint32_t bytes =
             2 * (Cfg::kABytes / 2 + 2 * Cfg::loaded_rows(round_up(tc.rows, 32) / 2) * kChunk + Cfg::kRowScales +
                  (Cfg::kGateUp ? 0 : kScaleTile));
@@ -893,7 +974,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
       bool ok = true;
       const uint32_t leader_full = map_to_cta(smem_u32(full), 0);
       for (int64_t t = pair; ok && t < total; t += pairs) {
-        const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+        const Tile tc = tile_at<kRows>(runs, slot_row_off, slot_expert, S, t, m_tiles, rows_together);
         const int half = round_up(tc.rows, 32) / 2, row0 = tc.row0 + rank * half;
         const int rs0 = tc.row_tile * chunks * (Cfg::kRowScales / 128);
         for (int c = 0; c < chunks; ++c) {
@@ -932,7 +1013,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
       --pending;
     };
     for (int64_t t = pair; ok && t < total; t += pairs) {
-      const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+      const Tile tc = tile_at<kRows>(runs, slot_row_off, slot_expert, S, t, m_tiles, rows_together);
       const size_t at = ((size_t)tc.expert * m_tiles + tc.m) * chunks * kScaleTile + 16 * lane + 8 * rank;
       for (int c = 0; c < chunks; c += Cfg::kGroup) {
         if (!__all_sync(0xffffffffu, mbar_wait(&scales_empty[group], phase ^ 1u, abort_flag))) { ok = false; break; }
@@ -963,7 +1044,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
       int64_t step = 0;
       bool ok = true;
       for (int64_t t = pair; ok && t < total; t += pairs) {
-        const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+        const Tile tc = tile_at<kRows>(runs, slot_row_off, slot_expert, S, t, m_tiles, rows_together);
         const uint32_t idesc = idesc_mx_e2m1_e4m3(2 * kTile, round_up(tc.rows, 32));
         if (!warp_wait_cluster(&acc_empty[acc], acc_phase ^ 1u, abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
@@ -1023,7 +1104,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
     uint32_t acc_phase = 0;
     bool ok = true;                  // a warp whose wait ran out still meets its partner at every barrier below
     for (int64_t t = pair; t < total; t += pairs) {
-      const Tile tc = tile_at<kRows>(tb, slot_row_off, slot_expert, S, t, m_tiles);
+      const Tile tc = tile_at<kRows>(runs, slot_row_off, slot_expert, S, t, m_tiles, rows_together);
       const int padded = round_up(tc.rows, 32);
       ok = ok && __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, 64));
       tc_fence_after_sync();
@@ -1125,7 +1206,7 @@ int launch_short(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   if (!moegps_make_tmap_codes4(&gate, c.gate4, s.E, s.F, dc, kTile) || !moegps_make_tmap_codes4(&up, c.up4, s.E, s.F, dc, kTile) ||
       !moegps_make_tmap_codes4(&down, c.down4, s.E, s.D, fc, kTile))
     return tmap_failed(ctx);
-  bool& attr_done = ctx->ffn4_attr_done[Cfg::kRows / 16];
+  bool& attr_done = ctx->ffn4_attr_done[Cfg::kRows / 32];
   if (!attr_done) {
     MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(short_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
     attr_done = true;
@@ -1171,7 +1252,7 @@ int launch_wide(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
       !moegps_make_tmap_bytes(&rsm, in.scale, (uint64_t)c.l.long_tiles * chunks * (Cfg::kRowScales / 128), 128,
                               Cfg::kRowScales / 128, false))
     return tmap_failed(ctx);
-  bool& attr_done = ctx->ffn4_attr_done[Cfg::kGateUp ? 0 : 4];
+  bool& attr_done = ctx->ffn4_attr_done[Cfg::kGateUp ? 2 : 3];
   if (!attr_done) {
     MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(wide_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
     attr_done = true;
@@ -1203,8 +1284,6 @@ int moegps_launch_expert_ffn4(moegps_ctx* ctx, const void* xp, const int32_t* sl
     if (rc == MOEGPS_OK) rc = launch_wide<Wide<false>>(ctx, c, st);
   }
   if (rc == MOEGPS_OK && c.l.cut.short_rows > 0)
-    rc = c.l.cut.tile_rows == 16   ? launch_short<Short<16, 5>>(ctx, c, st)
-         : c.l.cut.tile_rows == 32 ? launch_short<Short<32, 5>>(ctx, c, st)
-                                   : launch_short<Short<48, 4>>(ctx, c, st);
+    rc = c.l.cut.tile_rows == 32 ? launch_short<Short<32, 5>>(ctx, c, st) : launch_short<Short<48, 4>>(ctx, c, st);
   return rc;
 }

@@ -106,14 +106,10 @@ __device__ __forceinline__ void store_chunk(const uint32_t (&o)[16], uint8_t* st
 // all 1024 this took over 2 us of a 12 us launch on an 8-slot layer.
 // A slot whose extent is not inside [0, rcap] (offsets negative, decreasing or past the buffers) gets no
 // tiles: nothing is read or written for it, and the caller is told.
-// rows_before (optional): the same for the rows of the slots that have tiles.  Slots of fewer than min_rows or more than
-// max_rows rows are left to another launch.  Tiles from number max_tiles on (there are so many only where slots overlap) are left
-// out, and the caller is told.
 template <int kThreads, int kRows = BM>       // kRows: rows of a tile
 __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restrict__ slot_row_off,
                                              const int32_t* __restrict__ slot_expert, int S, int E, int n_tiles, int rcap,
-                                             int32_t* __restrict__ status, Tables* rows_before = nullptr, int min_rows = 1,
-                                             int max_rows = INT32_MAX, int max_tiles = INT32_MAX) {
+                                             int32_t* __restrict__ status) {
   for (int s = threadIdx.x; s < S; s += kThreads) {
     int cnt = 0;
     const int lo = slot_row_off[s], hi = slot_row_off[s + 1];
@@ -121,37 +117,31 @@ __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restri
     if (lo < 0 || hi < lo || hi > rcap) {
       if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
     } else if (hi > lo && e >= 0 && e < E) {
-      if (hi - lo >= min_rows && hi - lo <= max_rows) cnt = ((hi - lo + kRows - 1) / kRows) * n_tiles;
+      cnt = ((hi - lo + kRows - 1) / kRows) * n_tiles;
     } else if (hi > lo && e >= E) {
       if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
     }
     tb.tile_base[s] = cnt;
-    if (rows_before) rows_before->tile_base[s] = cnt ? hi - lo : 0;
   }
   __syncthreads();
-  // exclusive prefix sums of the counts, a warp for each table (lane l owns `per` consecutive entries)
-  if (threadIdx.x < (rows_before ? 64 : 32)) {
-    int32_t* base = threadIdx.x < 32 ? tb.tile_base : rows_before->tile_base;
-    const int most = threadIdx.x < 32 ? max_tiles : INT32_MAX;
-    const int lane = threadIdx.x & 31, per = (S + 31) / 32, first = min(lane * per, S), last = min(first + per, S);
-    int64_t sum = 0;                                  // (slots that overlap can have more rows than an int32 holds)
-    for (int s = first; s < last; ++s) sum += base[s];
-    int64_t incl = sum;
+  // exclusive prefix sum of the counts (warp 0: lane l owns `per` consecutive entries)
+  if (threadIdx.x < 32) {
+    const int lane = threadIdx.x, per = (S + 31) / 32, first = min(lane * per, S), last = min(first + per, S);
+    int sum = 0;
+    for (int s = first; s < last; ++s) sum += tb.tile_base[s];
+    int incl = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
+      const int o = __shfl_up_sync(0xffffffffu, incl, d);
       if (lane >= d) incl += o;
     }
-    int64_t run = incl - sum;
+    int run = incl - sum;
     for (int s = first; s < last; ++s) {
-      const int v = base[s];
-      base[s] = (int)min(run, (int64_t)most);
+      const int v = tb.tile_base[s];
+      tb.tile_base[s] = run;
       run += v;
     }
-    if (lane == 31) {
-      base[S] = (int)min(incl, (int64_t)most);
-      if (incl > most && blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, S);
-    }
+    if (lane == 31) tb.tile_base[S] = incl;
   }
 }
 

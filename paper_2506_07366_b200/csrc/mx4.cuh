@@ -74,30 +74,31 @@ __device__ __forceinline__ void split2(float a, float b, const float (&inv)[2], 
 }
 
 // ------------------------------------------------------------------------------------------- workspace of expert_ffn4
-// How the rows are worked (chosen by shape alone, it decides the layout of the workspace): slots of up to short_rows rows in
-// tiles of tile_rows by the launch for short slots, longer ones in tiles of 224 by those for long slots; either may be all.
+// How the rows are worked (chosen by shape alone, it decides the layout of the workspace).  Copies of an expert side by side are
+// one run of rows.  Runs of up to short_rows rows are worked in tiles of tile_rows by the launch for short runs, longer ones in
+// tiles of 224 by those for long runs; either may be all.
 struct Cut {
   int tile_rows, short_rows;
   bool all_short() const { return short_rows == INT32_MAX; }
 };
-// By the rows that a slot has on average (the actual loads are only known on the device; where popular experts have many times
-// that, short slots in one launch and long ones in the others are best) and the time that reading every slot's weights once takes,
-// 2.5 ns for 16 KB.  Measured (us; layers A: 256 experts 7168 x 2048, 970 us of weights, zipf 1; B: 64 experts 2048 x 1408, 53; C: 8
+// By the rows that an expert has on average (the actual loads are only known on the device; where popular experts have many times
+// that, short runs in one launch and long ones in the others are best) and the time that reading all weights once takes, 2.5 ns for
+// 16 KB.  Measured (us; layers A: 256 experts 7168 x 2048, 860 us of weights, zipf 1; B: 64 experts 2048 x 1408, 42; C: 8
 // experts 4096 x 14336, 107; D: 8 experts 1024 x 2048, 4):
-//   tiles of 16 or 48 rows: A 1.8 rows a slot 389 / 417, 3.6 604 / 560; B 3.6 62 / 66, 9.6 88 / 86; C 8 144 / 151, 16 177 / 164
-//   32 or 48: A 3.6 541 / 577, 14 1040 / 1097; B 9.6 84 / 87, 19 93 / 98, 38 134 / 131; C 16 145 / 161, 32 197 / 191 (in long runs,
-//     at the power limit, 161 / 178 and 224 / 215), 48 243 / 229; D 32 34 / 35, 64 29 / 27
-//   short or both: A 7 rows a slot 749 / 766, 14 1107 / 1058, 28 1658 / 1277
-//   short or long: B 38 157 / 182, 58 189 / 195, 77 229 / 213; C 64 268 / 326, 96 366 / 361; D 128 52 / 60, 256 66 / 71, 512 100 / 103
-//   long or both, where neither is better by more than 3 %: B from 77, C from 96, D from 256 rows a slot
+//   tiles of 32 or 48 rows: A 2 rows an expert 326 / 332; B 4.5 47 / 54, 12 68 / 68, 24 91 / 87, 48 133 / 122; C 16 145 / 161, 32 197 / 191
+//     (in long runs, at the power limit, 161 / 178 and 224 / 215), 48 243 / 229; D 32 34 / 35, 64 29 / 27.  (Tiles of 16: as 32 up to
+//     16 rows a run, behind that more, B 4.5 54.)
+//   short or both: A 2 326 / 346, 4 477 / 449, 8 665 / 592, 16 1008 / 840, 32 1695 / 1216
+//   short or long: B 48 122 / 150, 96 185 / 190; C 64 268 / 326, 96 366 / 361; D 128 52 / 60, 256 66 / 71, 512 100 / 103
+//   long or both, where neither is better by more than 3 %: B and C from 96, D from 256 rows an expert
 inline Cut cut_of(const moegps_shape_t& s) {
-  const int64_t R = (int64_t)s.T * s.K, slots = R < s.S ? R : s.S;
-  const int64_t per_slot = slots > 0 ? (R + slots - 1) / slots : 0;
+  const int64_t R = (int64_t)s.T * s.K, experts = R < s.E ? R : s.E;
+  const int64_t per = experts > 0 ? (R + experts - 1) / experts : 0;
   const int64_t d = chunks_of(s.D), f = chunks_of(s.F);
-  const double weights_us = 0.0025 * s.S * (double)(f * d + (d + 1) / 2 * f);
+  const double weights_us = 0.0025 * s.E * (double)(f * d + (d + 1) / 2 * f);
   const bool heavy = weights_us > 300.0;
-  if (per_slot <= (heavy ? 3 : 8)) return {16, INT32_MAX};
-  if (per_slot <= (heavy ? 10 : weights_us > 20.0 ? 64 : 256)) return {per_slot <= 24 ? 32 : 48, INT32_MAX};
+  if (per <= (heavy ? 3 : 24)) return {32, INT32_MAX};
+  if (!heavy && per <= (weights_us > 20.0 ? 96 : 256)) return {48, INT32_MAX};
   return {32, heavy ? 32 : 0};
 }
 constexpr int kLongRows = 224;
@@ -149,7 +150,7 @@ inline Layout layout_of(const moegps_shape_t& s) {
   l.rows = (int64_t)s.T * s.K + (int64_t)s.S * (s.row_align - 1);
   l.short_tiles = l.cut.all_short() ? l.rows / n + s.S : s.S * ((l.cut.short_rows + n - 1) / n);
   l.long_tiles = l.cut.all_short() ? 0 : l.rows / kLongRows + s.S;
-  const size_t dc = chunks_of(s.D), fc = chunks_of(s.F), image = n == 16 ? kImageBytes<16> : n == 32 ? kImageBytes<32> : kImageBytes<48>;
+  const size_t dc = chunks_of(s.D), fc = chunks_of(s.F), image = n == 32 ? kImageBytes<32> : kImageBytes<48>;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;

@@ -206,14 +206,19 @@ def test_ffn_against_64_bits(c):
 
 @pytest.mark.parametrize("align", [1, 16])
 def test_short_and_long_slots_in_one_call(align, monkeypatch, capfd):
-    """Many slots of one expert, some with more rows than the launch for short slots takes: both kinds of launches run."""
+    """Heavy weights, and some slots with more rows than the launch for short slots takes: both kinds of launches run.  Copies of an
+    expert side by side, some short by themselves and long together, and apart."""
     monkeypatch.setenv("MOEGPS_TRACE", "1")
     rng = np.random.default_rng(4)
-    rows = [int(v) for v in rng.choice([0, 1, 5, 16, 17, 47, 48], 1016)] + [49, 64, 112, 223, 224, 225, 500, 900]
+    E, S = 128, 160
+    rows = [int(v) for v in rng.choice([0, 1, 5, 16, 17, 31, 32, 33, 47], S - 8)] + [49, 64, 112, 223, 224, 225, 500, 900]
     rng.shuffle(rows)
-    shape = binding.Shape(sum(rows), 1280, 1000, 1, 1, 1024, 0, align)
+    experts = sorted(list(range(E)) + [int(v) for v in rng.integers(0, E, S - E)])
+    experts[3], experts[150] = experts[150], experts[3]
+    experts[20:40] = [7] * 20
+    shape = binding.Shape(sum(rows), 2560, 4000, E, 1, S, 0, align)
     ctx, g, packed, dense, ws = make(shape, 31)
-    off, expert = slots(rows, [0] * 1024, align)
+    off, expert = slots(rows, experts, align)
     xp = normal(g, shape.Rcap, shape.D)
     yp = torch.full((shape.Rcap, shape.D), 13.0, dtype=torch.bfloat16, device=DEV)
     capfd.readouterr()
@@ -222,6 +227,24 @@ def test_short_and_long_slots_in_one_call(align, monkeypatch, capfd):
     launched = capfd.readouterr().err
     for kernel in ("launch_split", "launch_wide", "launch_short"):
         assert kernel in launched
+    check(xp, off, expert, dense, yp, 13.0)
+
+
+@pytest.mark.parametrize("align", [1, 4])
+@pytest.mark.parametrize("rows,experts", [
+    ([5, 9, 0, 30, 2, 40, 1, 3, 3, 0], [1, 1, 1, 1, 0, 2, 2, 1, 1, 1]),             # copies side by side, with empty ones, and apart
+    ([20, 7, 0, 9, 11, 0, 6], [0, 0, -1, 0, 0, 2, 0]),                              # a slot without expert, another expert's empty one
+    ([300, 500, 100, 1, 224, 224, 223], [2, 2, 0, 0, 1, 1, 1]),                     # long ones
+    ([1] * 70 + [9, 8, 7, 0], [0] * 35 + [1] * 35 + [2, 2, 2, 2]),                  # more slots than a warp has lanes
+])
+def test_copies_side_by_side(rows, experts, align):
+    shape = binding.Shape(sum(rows), 264, 392, 3, 1, len(rows), 0, align)
+    ctx, g, packed, dense, ws = make(shape, 17)
+    off, expert = slots(rows, experts, align)
+    xp = normal(g, shape.Rcap, 264)
+    yp = torch.full((shape.Rcap, 264), 13.0, dtype=torch.bfloat16, device=DEV)
+    call(ctx, xp, off, expert, packed, yp, ws)
+    ctx.check_status()
     check(xp, off, expert, dense, yp, 13.0)
 
 
