@@ -28,7 +28,7 @@ using mx4::kTile;
 __host__ __device__ constexpr int round_up(int n, int to) { return (n + to - 1) / to * to; }
 
 // Slots that follow one another and hold copies of one expert are one run of rows (a plan puts copies side by side): their weights
-// are read once, and tiles are cut from all their rows (48 tokens over 64 experts in 80 slots 55 -> 49 us).  Tiles and rows before
+// are read once, and tiles are cut from all their rows (48 tokens over 64 experts in 80 slots 55 -> 48 us).  Tiles and rows before
 // each slot; a run counts as its first slot.
 struct alignas(16) Runs {
   int32_t tiles[kMaxS + 1], rows[kMaxS + 1];

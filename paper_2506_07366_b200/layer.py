@@ -233,7 +233,8 @@ class MoeLayer4(MoeLayer):
 
     Each of w_gate, w_up [E, F, D] and w_down [E, D, F] is a bf16 tensor, rounded to 4 bits here, or the pair (codes, scales)
     of one that is in 4 bits already (Shape.w4_shapes; binding.w4_scale_tiles brings a checkpoint's scale bytes into that order).
-    The layer keeps the pairs.  dense_experts() gives the weights back as bf16, for instance to train on what was rounded.
+    The rounding is on the current stream, like any torch operation here.  The layer keeps the pairs.  dense_experts() gives the
+    weights back as bf16, for instance to train on what was rounded.
     """
 
     def _set_experts(self, w_gate, w_up, w_down):
