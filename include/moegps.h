@@ -254,7 +254,8 @@ MOEGPS_API int moegps_dispatch_static(moegps_ctx_t* ctx, const void* x, const in
  * All rows of a slot's extent are computed (padding rows yield unspecified values); rows outside
  * every slot and slots with slot_expert < 0 are not written.  A slot whose extent in slot_row_off
  * is not inside [0, Rcap] (negative, decreasing, or past the buffers) is skipped entirely and
- * MOEGPS_ERR_BAD_INDEX is recorded. */
+ * MOEGPS_ERR_BAD_INDEX is recorded.  So are the last of slots that overlap (no plan makes such) where all
+ * tiles together exceed 2^30. */
 MOEGPS_API int moegps_expert_ffn(moegps_ctx_t* ctx, const void* xp, const int32_t* slot_row_off,
                       const int32_t* slot_expert, const void* w_gate, const void* w_up,
                       const void* w_down, void* h_ws, void* yp, void* stream);

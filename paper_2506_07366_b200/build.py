@@ -18,7 +18,7 @@ SOURCES = ["api.cu", "route.cu", "histogram.cu", "plan.cu", "pack.cu", "dispatch
            "predictor.cu", "selftest.cu", "expert_ffn_backward.cu", "shuffle_backward.cu", "route_backward.cu",
            "experts4.cu", "expert_ffn4.cu"]
 HEADERS = ["common.cuh", "sm100.cuh", "route_epilogue.cuh", "slot_offsets.cuh", "grouped_gemm.cuh", "act8.cuh", "bf16x8.cuh",
-           "route_backward.cuh", "mx4.cuh"]
+           "route_backward.cuh", "mx4.cuh", "tile_sums.cuh"]
 
 
 def _nvcc() -> str:

@@ -4,6 +4,7 @@
 
 #include "common.cuh"
 #include "sm100.cuh"
+#include "tile_sums.cuh"
 
 namespace grouped_gemm {
 
@@ -105,7 +106,8 @@ __device__ __forceinline__ void store_chunk(const uint32_t (&o)[16], uint8_t* st
 // caller's next __syncthreads().  All kThreads threads of the block call it.  Only the S entries in use are walked: with
 // all 1024 this took over 2 us of a 12 us launch on an 8-slot layer.
 // A slot whose extent is not inside [0, rcap] (offsets negative, decreasing or past the buffers) gets no
-// tiles: nothing is read or written for it, and the caller is told.
+// tiles: nothing is read or written for it, and the caller is told.  So is it where slots overlap so often that their tiles
+// pass tile_sums::kMost: the slots from there on get none.
 template <int kThreads, int kRows = BM>       // kRows: rows of a tile
 __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restrict__ slot_row_off,
                                              const int32_t* __restrict__ slot_expert, int S, int E, int n_tiles, int rcap,
@@ -117,31 +119,32 @@ __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restri
     if (lo < 0 || hi < lo || hi > rcap) {
       if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
     } else if (hi > lo && e >= 0 && e < E) {
-      cnt = ((hi - lo + kRows - 1) / kRows) * n_tiles;
+      cnt = tile_sums::tiles_of(hi - lo, kRows, n_tiles);
     } else if (hi > lo && e >= E) {
       if (blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, s);
     }
     tb.tile_base[s] = cnt;
   }
   __syncthreads();
-  // exclusive prefix sum of the counts (warp 0: lane l owns `per` consecutive entries)
+  // exclusive prefix sum of the counts, by warp 0
   if (threadIdx.x < 32) {
-    const int lane = threadIdx.x, per = (S + 31) / 32, first = min(lane * per, S), last = min(first + per, S);
-    int sum = 0;
-    for (int s = first; s < last; ++s) sum += tb.tile_base[s];
-    int incl = sum;
+    const int lane = threadIdx.x;
+    const tile_sums::Lane own(lane, S);
+    const int64_t sum = own.sum(tb.tile_base);
+    int64_t incl = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, incl, d);
+      const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
       if (lane >= d) incl += o;
     }
-    int run = incl - sum;
-    for (int s = first; s < last; ++s) {
-      const int v = tb.tile_base[s];
-      tb.tile_base[s] = run;
-      run += v;
+    const int64_t total = __shfl_sync(0xffffffffu, incl, 31);
+    int32_t kept = (int32_t)total;
+    if (total > tile_sums::kMost) {
+      kept = __reduce_max_sync(0xffffffffu, own.kept(tb.tile_base, incl - sum, tile_sums::kMost));
+      if (threadIdx.x == 0 && blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, S);
     }
-    if (lane == 31) tb.tile_base[S] = incl;
+    own.write(tb.tile_base, incl - sum, kept);
+    if (lane == 31) tb.tile_base[S] = kept;
   }
 }
 
