@@ -69,7 +69,7 @@ typedef enum moegps_error {
 
 /* Problem shape, fixed for the life of a context.
  * Limits: 1 <= K <= min(E, 8); E <= 256; E <= S <= 1024; D and F multiples of 8;
- * T*K + S*(row_align-1) < 2^31; row_align a power of two in [1, 256]. */
+ * T*K + S*(row_align-1) <= 2^31 - 256; row_align a power of two in [1, 256]. */
 typedef struct moegps_shape {
   int32_t T, D, F, E, K, S;
   int32_t gate_mode;   /* 0: softmax over the K selected logits; 1: sigmoid, then renormalise over the K */

@@ -19,7 +19,7 @@ int check_shape(const moegps_shape_t* s) {
   if (a < 1 || a > 256 || (a & (a - 1)) != 0) return MOEGPS_ERR_UNSUPPORTED_SHAPE;
   if (s->gate_mode != 0 && s->gate_mode != 1) return MOEGPS_ERR_INVALID_ARG;
   if (s->c_max < 0) return MOEGPS_ERR_INVALID_ARG;
-  if (moegps_rcap_of(*s) >= (int64_t)INT32_MAX) return MOEGPS_ERR_UNSUPPORTED_SHAPE;
+  if (moegps_rcap_of(*s) > (int64_t)INT32_MAX - 255) return MOEGPS_ERR_UNSUPPORTED_SHAPE;   // a tile of 256 rows from the last row on
   return MOEGPS_OK;
 }
 

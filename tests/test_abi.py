@@ -60,6 +60,15 @@ def test_invalid_shapes_are_rejected(lib, bad):
     assert binding.workspace_bytes(s) == 0
 
 
+@pytest.mark.parametrize("S,align,most", [(8, 1, 2 ** 31 - 256), (1024, 256, 2 ** 31 - 256)])
+def test_most_rows(lib, S, align, most):
+    """The number of any row of a tile of 256 that begins at one of them is an int32."""
+    T = most - S * (align - 1)
+    last = binding.Shape(T, 8, 8, 8, 1, S, 0, align)
+    assert binding.rcap(last) == most and most - 1 + 255 < 2 ** 31
+    assert binding.rcap(binding.Shape(T + 1, 8, 8, 8, 1, S, 0, align)) == -1
+
+
 def test_error_strings(lib):
     seen = set()
     for code in range(0, -9, -1):
