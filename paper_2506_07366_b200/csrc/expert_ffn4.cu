@@ -379,6 +379,7 @@ template <int kRows_, int kStages_>
 struct Short {
   static constexpr int kRows = kRows_;                 // of a tile at most
   static constexpr int kStages = kStages_;
+  static constexpr int kFlag = kRows == 48 ? 0 : 1;    // of ffn4_attr_done
   static constexpr int kCols = 2 * kRows;              // accumulator columns of a weight tile: both terms
   static constexpr int kABytes = kTile * kChunk;       // a weight tile in shared memory; half of them are loaded
   static constexpr int kImage = mx4::kImageBytes<kRows>;
@@ -854,6 +855,7 @@ struct Weights {
 template <bool kGateUp_>
 struct Wide {
   static constexpr bool kGateUp = kGateUp_;
+  static constexpr int kFlag = kGateUp ? 2 : 3;        // of ffn4_attr_done
   static constexpr int kRows = mx4::kLongRows, kStages = 4;
   static constexpr int kABytes = kTile * kChunk;       // half of them are loaded
   static constexpr int kBBytes = kRows / 2 * kChunk;   // of a term
@@ -1171,6 +1173,13 @@ wide_kernel(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ C
 }
 
 // ------------------------------------------------------------------------------------------- host
+using Short48 = Short<48, 4>;
+using Short32 = Short<32, 5>;
+constexpr int kFlags[] = {Short48::kFlag, Short32::kFlag, Wide<true>::kFlag, Wide<false>::kFlag};
+static_assert(kFlags[0] == 0 && kFlags[1] == 1 && kFlags[2] == 2 && kFlags[3] == 3 &&
+                  sizeof(moegps_ctx::ffn4_attr_done) / sizeof(bool) == 4,
+              "each kernel has a flag of its own for its raised shared-memory limit");
+
 struct Call {
   const void* xp;
   const int32_t *slot_row_off, *slot_expert;
@@ -1206,7 +1215,7 @@ int launch_short(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   if (!moegps_make_tmap_codes4(&gate, c.gate4, s.E, s.F, dc, kTile) || !moegps_make_tmap_codes4(&up, c.up4, s.E, s.F, dc, kTile) ||
       !moegps_make_tmap_codes4(&down, c.down4, s.E, s.D, fc, kTile))
     return tmap_failed(ctx);
-  bool& attr_done = ctx->ffn4_attr_done[Cfg::kRows / 32];
+  bool& attr_done = ctx->ffn4_attr_done[Cfg::kFlag];
   if (!attr_done) {
     MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(short_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
     attr_done = true;
@@ -1252,7 +1261,7 @@ int launch_wide(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
       !moegps_make_tmap_bytes(&rsm, in.scale, (uint64_t)c.l.long_tiles * chunks * (Cfg::kRowScales / 128), 128,
                               Cfg::kRowScales / 128, false))
     return tmap_failed(ctx);
-  bool& attr_done = ctx->ffn4_attr_done[Cfg::kGateUp ? 2 : 3];
+  bool& attr_done = ctx->ffn4_attr_done[Cfg::kFlag];
   if (!attr_done) {
     MOEGPS_CUDA_TRY(ctx, cudaFuncSetAttribute(wide_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::kSmem));
     attr_done = true;
@@ -1284,6 +1293,6 @@ int moegps_launch_expert_ffn4(moegps_ctx* ctx, const void* xp, const int32_t* sl
     if (rc == MOEGPS_OK) rc = launch_wide<Wide<false>>(ctx, c, st);
   }
   if (rc == MOEGPS_OK && c.l.cut.short_rows > 0)
-    rc = c.l.cut.tile_rows == 32 ? launch_short<Short<32, 5>>(ctx, c, st) : launch_short<Short<48, 4>>(ctx, c, st);
+    rc = c.l.cut.tile_rows == 32 ? launch_short<Short32>(ctx, c, st) : launch_short<Short48>(ctx, c, st);
   return rc;
 }
