@@ -392,7 +392,8 @@ MOEGPS_API int moegps_weights_dequantize4(moegps_ctx_t* ctx, const void* w4, con
  * MOEGPS_ERR_BAD_INDEX recorded.  Of slots that overlap (no plan makes such) those that exceed the workspace are left out, and the
  * same is recorded.  yp may be xp.
  * workspace: moegps_expert_ffn4_workspace_bytes(shape) bytes, 16-byte aligned, contents irrelevant; its size cannot be checked
- * here.  Calls that may overlap on the GPU need a workspace each; one context may serve them. */
+ * here.  Calls that may overlap on the GPU need a workspace each; one context may serve them.  A device with more than 160 SMs:
+ * MOEGPS_ERR_UNIMPLEMENTED. */
 MOEGPS_API size_t moegps_expert_ffn4_workspace_bytes(const moegps_shape_t* shape);
 MOEGPS_API int moegps_expert_ffn4(moegps_ctx_t* ctx, const void* xp, const int32_t* slot_row_off, const int32_t* slot_expert,
                                   const void* gate4, const void* up4, const void* down4, const void* gate4_scale,

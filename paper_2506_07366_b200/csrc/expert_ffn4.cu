@@ -471,6 +471,11 @@ __device__ __forceinline__ bool poll(volatile int* abort_flag, Ready&& ready) {
 }
 
 // The blocks' barrier, once in a launch: a count in the context's memory that only grows, by the number of blocks each time.
+// It serves all launches of a context, on whatever streams: no block of another one arrives before all of a launch's have.  For there
+// are as many blocks as SMs, all resident at once (the launch is cooperative), and each takes more than half of an SM's shared
+// memory, so a block of the other launch finds room where one has retired; and every block waits here before it retires.  (Fewer blocks
+// than SMs, or a block that does not wait, and the counts of two launches mix.  A block that retires because a wait ran out does so
+// too, but then MOEGPS_ERR_TIMEOUT is recorded in the same context.)
 struct Meeting {
   unsigned long long* count;
   volatile unsigned long long* goal;               // shared memory: what the count is when all have come; 0 = not here yet
@@ -1224,7 +1229,7 @@ int launch_short(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   attr.id = cudaLaunchAttributeCooperative;            // all blocks run at once: they wait for one another
   attr.val.cooperative = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctx->sm_count < mx4::kMaxCtas ? ctx->sm_count : mx4::kMaxCtas);
+  cfg.gridDim = dim3(mx4::short_blocks(ctx->sm_count));
   cfg.blockDim = dim3(Cfg::kThreads);
   cfg.dynamicSmemBytes = Cfg::kSmem;
   cfg.stream = st;
@@ -1286,6 +1291,7 @@ int moegps_launch_expert_ffn4(moegps_ctx* ctx, const void* xp, const int32_t* sl
   uint8_t* ws = c.workspace;
   c.x = {{ws + c.l.x_code, ws + c.l.x_code + c.l.x_code_bytes}, ws + c.l.x_scale};
   c.h = {{ws + c.l.h_code, ws + c.l.h_code + c.l.h_code_bytes}, ws + c.l.h_scale};
+  if (mx4::short_blocks(ctx->sm_count) == 0) return MOEGPS_ERR_UNIMPLEMENTED;
   int rc = MOEGPS_OK;
   if (!c.l.cut.all_short()) {
     rc = launch_split(ctx, c, st);

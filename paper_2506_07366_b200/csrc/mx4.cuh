@@ -132,7 +132,10 @@ __host__ __device__ constexpr int image_code_at(int row, int term, int rows_in_t
 
 inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-constexpr int kMaxCtas = 148;      // blocks of a launch that joins partial sums; what they leave for each other is sized by it
+// Blocks of the launch for short runs: one for each SM, and not fewer (see Meeting in expert_ffn4.cu).  What they leave for each other
+// in the workspace is sized by the most that are known, before a device is; more are refused (0).
+constexpr int kMaxCtas = 160;
+inline int short_blocks(int sm_count) { return sm_count <= kMaxCtas ? sm_count : 0; }
 
 struct Layout {
   Cut cut;
