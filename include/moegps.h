@@ -384,9 +384,10 @@ MOEGPS_API int moegps_weights_dequantize4(moegps_ctx_t* ctx, const void* w4, con
 
 /* expert_ffn4 - moegps_expert_ffn on 4-bit weights: for every row rho of slot s with e = slot_expert[s], W4 what the codes
  * stand for:  h = silu(gate4[e] xp[rho]) * (up4[e] xp[rho]);   yp[rho] = down4[e] h.
- * The products are exact (a row is split into two e4m3 terms that add up to it, see csrc/mx4.cuh; values below 2^-15 of the
- * largest of their 32 neighbours are off by at most 2^-21 of that), sums are fp32, h is kept to 2^-9 relative and yp is rounded
- * once to bf16.  A row that holds an infinity or a NaN gives NaN.
+ * The products are exact (a row is split into two e4m3 terms that add up to it, see csrc/mx4.cuh; values below 2^-13 of the
+ * largest of their 32 neighbours may be off, by at most 2^-21 of that), sums are fp32, h is kept to 2^-9 relative or to 2^-21 of
+ * the largest of its 32 neighbours, whichever is more, and yp is rounded once to bf16.  A row that holds an infinity or a NaN, or
+ * whose h is beyond fp32, gives NaN.
  * xp, slot_row_off, slot_expert, yp as in moegps_expert_ffn: padding rows of a slot yield unspecified values, rows outside every
  * slot and slots with slot_expert < 0 are not written, a slot with an extent outside [0, Rcap] is skipped and
  * MOEGPS_ERR_BAD_INDEX recorded.  Of slots that overlap (no plan makes such) those that exceed the workspace are left out, and the

@@ -16,11 +16,12 @@
 // 2^k for 32 values of a row on either side, fp32 accumulation).  A bf16 has 8 significant bits and an e4m3 has 4, so x is
 // written as two e4m3 terms: x = 2^k (c1 + 2^-4 c2) with c1 = x 2^-k rounded to nearest and c2 the rest.  k is the smallest
 // integer with max|x| <= 448 * 2^k over 32 values.  The rest is at most half a step of c1, i.e. at most 8 steps of bf16, so
-// it fits c2 exactly: nothing is lost above 2^-6 * 2^k, and below that the error is at most 2^-14 * 2^k, which is 2^-21 of the
-// block's maximum.  Two products at twice the rate cost what one bf16 product costs, and the weights go to the tensor core as
-// they are in memory.
-// For values with more bits than bf16 (the hidden activations, straight from the accumulator) the same two terms are off by
-// at most 2^-9 relative, half of what a rounding to bf16 is.
+// it fits c2 exactly: nothing is lost above 2^-6 * 2^k, and below that the error is at most 2^-14 * 2^k.  The block's maximum is above
+// 224 * 2^k: what may be off is below 2^-13 of it, by at most 2^-21 of it.  Two products at twice the rate cost what one bf16
+// product costs, and the weights go to the tensor core as they are in memory.
+// For values with more bits than bf16 (the hidden activations, straight from the accumulator) the same two terms are off by at
+// most 2^-9 relative, half of what a rounding to bf16 is, or by the 2^-14 * 2^k of the second term's last step where that is more
+// (below 2^-12 of the block's maximum; 2^-137 for k < -123).
 #pragma once
 
 #include <cuda_fp16.h>

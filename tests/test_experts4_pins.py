@@ -85,3 +85,47 @@ def test_null_context(lib):
     assert lib.moegps_weights_quantize4(None, p, 0, p, p, None) == binding.ERR_INVALID_ARG
     assert lib.moegps_weights_dequantize4(None, p, p, 0, p, None) == binding.ERR_INVALID_ARG
     assert lib.moegps_expert_ffn4(None, *[p] * 11, None) == binding.ERR_INVALID_ARG
+
+
+# ------------------------------------------------------------------------------------------- rows in two terms
+def two_terms(v, top):
+    """fp64 v, |v| <= top, as the products take them: two e4m3 terms with a power of two each, by the largest of the block."""
+    mantissa, e = np.frexp(top)
+    k = max(int(e) - 9 + int(mantissa > 0.875), -127)    # smallest with top <= 448 * 2^k
+    k2 = max(k - 4, -127)
+    e4m3 = lambda a: torch.from_numpy(a).float().to(torch.float8_e4m3fn).double().numpy()  # noqa: E731
+    first = e4m3(v * 2.0 ** -k) * 2.0 ** k
+    return first + e4m3((v - first) * 2.0 ** -k2) * 2.0 ** k2
+
+
+ALL_BF16 = (torch.arange(0, 0x7f80, dtype=torch.int32) << 16).view(torch.float32).double().numpy()       # 0 and up
+
+
+@pytest.mark.parametrize("unit", [1.0, 2.0 ** -100, 2.0 ** 110])
+def test_bf16_in_two_terms(unit):
+    """Every bf16 beside every largest value that has the same scale: exact from 2^-13 of it on, 2^-21 of it off at most below."""
+    largest_off = 0.0
+    for top in ALL_BF16[(ALL_BF16 > 224 * unit) & (ALL_BF16 <= 448 * unit)]:
+        v = ALL_BF16[ALL_BF16 <= top]
+        off = np.abs(two_terms(v, top) - v)
+        assert (off[v >= 2.0 ** -13 * top] == 0).all() and off.max() <= 2.0 ** -21 * top
+        largest_off = max(largest_off, v[off > 0].max() / top)
+    assert largest_off > 2.0 ** -14                      # 2^-14 would be too much to promise
+
+
+def test_smallest_bf16_in_two_terms():
+    for top in (2.0 ** -116, 2.0 ** -118, 1.5 * 2.0 ** -120, 2.0 ** -126, 2.0 ** -133):
+        v = ALL_BF16[ALL_BF16 <= top]
+        assert np.array_equal(two_terms(v, top), v)
+
+
+@pytest.mark.parametrize("top", [224.0 + 2.0 ** -16, 300.0, 448.0])
+@pytest.mark.parametrize("unit", [1.0, 2.0 ** 100])
+def test_fp32_in_two_terms(top, unit):
+    """2^-9 relative or 2^-21 of the largest; the first alone does not hold."""
+    rng = np.random.default_rng(int(top))
+    v = rng.uniform(0.5, 1.0, 400000) * 2.0 ** -rng.integers(0, 26, 400000) * top
+    v = v.astype(np.float32).astype(np.float64) * unit
+    off = np.abs(two_terms(v, top * unit) - v)
+    assert (off <= np.maximum(2.0 ** -9 * v, 2.0 ** -21 * top * unit)).all()
+    assert (off <= 2.0 ** -9 * v)[v >= 2.0 ** -12 * top * unit].all() and (off > 2.0 ** -9 * v).any()
