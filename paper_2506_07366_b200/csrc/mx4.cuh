@@ -92,15 +92,19 @@ struct Cut {
 //   short or both: A 2 326 / 346, 4 477 / 449, 8 665 / 592, 16 1008 / 840, 32 1695 / 1216
 //   short or long: B 48 122 / 150, 96 185 / 190; C 64 268 / 326, 96 366 / 361; D 128 52 / 60, 256 66 / 71, 512 100 / 103
 //   long or both, where neither is better by more than 3 %: B and C from 96, D from 256 rows an expert
+// Padding is worked like other rows: where slots are aligned to more rows than a tile of 32 has, a run has that many at least (all short /
+// all long, aligned to 128: A 8 tokens 1235 / 536, C 8 tokens 363 / 296, B 48 tokens 146 / 123).
 inline Cut cut_of(const moegps_shape_t& s) {
   const int64_t R = (int64_t)s.T * s.K, experts = R < s.E ? R : s.E;
   const int64_t per = experts > 0 ? (R + experts - 1) / experts : 0;
+  const bool padded = s.row_align > 32;
+  const int64_t rows = padded && per < s.row_align ? s.row_align : per;
   const int64_t d = chunks_of(s.D), f = chunks_of(s.F);
   const double weights_us = 0.0025 * s.E * (double)(f * d + (d + 1) / 2 * f);
   const bool heavy = weights_us > 300.0;
-  if (per <= (heavy ? 3 : 24)) return {32, INT32_MAX};
-  if (!heavy && per <= (weights_us > 20.0 ? 96 : 256)) return {48, INT32_MAX};
-  return {32, heavy ? 32 : 0};
+  if (rows <= (heavy ? 3 : 24)) return {32, INT32_MAX};
+  if (!heavy && rows <= (weights_us > 20.0 ? 96 : 256)) return {48, INT32_MAX};
+  return {32, heavy && !padded ? 32 : 0};              // (padded: no run is short)
 }
 constexpr int kLongRows = 224;
 

@@ -43,3 +43,29 @@ def test_blocks_that_wait_for_one_another(lib):
         lib.cut(ctypes.byref(s.c_struct()), out)
         # three parts, two weight tiles of 128 outputs each, for the rows of a tile, fp32
         assert lib.partial_bytes(ctypes.byref(s.c_struct())) == most * 3 * 2 * out[0] * 128 * 4
+
+
+def cut(lib, E, D, F, K, T, align=16):
+    """'short' (with the rows of a tile), 'long' or 'both'."""
+    out = (ctypes.c_int * 2)()
+    lib.cut(ctypes.byref(binding.Shape(T, D, F, E, K, E, 0, align).c_struct()), out)
+    if out[1] == 2 ** 31 - 1:
+        return f"short {out[0]}"
+    return "both" if out[1] else "long"
+
+
+LAYERS = dict(fine=(256, 7168, 2048, 8), mixtral=(8, 4096, 14336, 2), many=(64, 2048, 1408, 6), light=(8, 1024, 2048, 2))
+
+
+@pytest.mark.parametrize("align", [64, 128, 256])
+def test_padding_is_rows_like_others(lib, align):
+    """Few tokens whose slots are aligned to more rows than a tile has: as many rows an expert as the alignment."""
+    for name, (E, D, F, K) in LAYERS.items():
+        for T in (1, 2, 8, 32):
+            whole = max(1, align * min(E, T * K) // K)   # tokens that fill as many rows
+            few, full = cut(lib, E, D, F, K, T, align), cut(lib, E, D, F, K, align * E // K, align)
+            assert few == full, (name, T, whole)
+    assert cut(lib, *LAYERS["fine"], 1, align) == "long"
+    if align > 96:
+        assert cut(lib, *LAYERS["mixtral"], 1, align) == cut(lib, *LAYERS["many"], 8, align) == "long"
+    assert cut(lib, *LAYERS["light"], 1, align) == "short 48"

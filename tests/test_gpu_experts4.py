@@ -555,3 +555,36 @@ def test_large_layer_by_slots():
     call(ctx, xp, off, expert, packed, yp, ws)
     ctx.check_status()
     check(xp, off, expert, dense, yp, 13.0)
+
+
+@pytest.mark.parametrize("D,F", [(4096, 264), (520, 4096)])
+def test_runs_worked_in_groups_of_rows(D, F):
+    """Runs whose rows do not stay in L2 together, over several tiles of outputs: 4096 inputs in groups of 13 row tiles, the last
+    group not full, its last tile neither.  The first size meets it in gate + up, the second in down."""
+    rows = [7000, 0, 2912, 13]
+    shape = binding.Shape(sum(rows), D, F, 2, 1, 4, 0, 1)
+    ctx, g, packed, dense, ws = make(shape, 41, std=0.02)
+    off, expert = slots(rows, [0, 1, 1, 0], 1)
+    xp = normal(g, shape.Rcap, D)
+    yp = torch.full((shape.Rcap, D), 13.0, dtype=torch.bfloat16, device=DEV)
+    call(ctx, xp, off, expert, packed, yp, ws)
+    ctx.check_status()
+    check(xp, off, expert, dense, yp, 13.0)
+
+
+@pytest.mark.parametrize("align", [1, 16, 32, 64, 128, 256])
+@pytest.mark.parametrize("T", [1, 40])
+def test_few_tokens_at_any_alignment(align, T):
+    """Slots that hold a row or two each, of weights that are read in 40 us: all ways that the alignment leads to."""
+    shape = binding.Shape(T, 1024, 2560, 64, 4, 70, 0, align)
+    ctx, g, packed, dense, ws = make(shape, 51, std=0.03)
+    counts = torch.bincount(torch.randint(0, 70, (4 * T,), generator=g, device=DEV), minlength=70).tolist()
+    experts = sorted(list(range(64)) + [3, 3, 3, 10, 10, 63])
+    off, expert = slots(counts, experts, align)
+    xp = torch.zeros(shape.Rcap, 1024, dtype=torch.bfloat16, device=DEV)
+    for s, n in enumerate(counts):
+        xp[int(off[s]):int(off[s]) + n] = normal(g, n, 1024)
+    yp = torch.full((shape.Rcap, 1024), 13.0, dtype=torch.bfloat16, device=DEV)
+    call(ctx, xp, off, expert, packed, yp, ws)
+    ctx.check_status()
+    check(xp, off, expert, dense, yp, 13.0, used=counts)
