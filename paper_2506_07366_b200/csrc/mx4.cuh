@@ -82,29 +82,41 @@ struct Cut {
   int tile_rows, short_rows;
   bool all_short() const { return short_rows == INT32_MAX; }
 };
-// By the rows that an expert has on average (the actual loads are only known on the device; where popular experts have many times
-// that, short runs in one launch and long ones in the others are best) and the time that reading all weights once takes, 2.5 ns for
-// 16 KB.  Measured (us; layers A: 256 experts 7168 x 2048, 860 us of weights, zipf 1; B: 64 experts 2048 x 1408, 42; C: 8
-// experts 4096 x 14336, 107; D: 8 experts 1024 x 2048, 4):
-//   tiles of 32 or 48 rows: A 2 rows an expert 326 / 332; B 4.5 47 / 54, 12 68 / 68, 24 91 / 87, 48 133 / 122; C 16 145 / 161, 32 197 / 191
-//     (in long runs, at the power limit, 161 / 178 and 224 / 215), 48 243 / 229; D 32 34 / 35, 64 29 / 27.  (Tiles of 16: as 32 up to
-//     16 rows a run, behind that more, B 4.5 54.)
-//   short or both: A 2 326 / 346, 4 477 / 449, 8 665 / 592, 16 1008 / 840, 32 1695 / 1216
-//   short or long: B 48 122 / 150, 96 185 / 190; C 64 268 / 326, 96 366 / 361; D 128 52 / 60, 256 66 / 71, 512 100 / 103
-//   long or both, where neither is better by more than 3 %: B and C from 96, D from 256 rows an expert
-// Padding is worked like other rows: where slots are aligned to more rows than a tile of 32 has, a run has that many at least (all short /
-// all long, aligned to 128: A 8 tokens 1235 / 536, C 8 tokens 363 / 296, B 48 tokens 146 / 123).
+// By the rows that an expert has on average (the actual loads are only known on the device), the experts, and the time that reading
+// all weights once takes, 2.5 ns for 16 KB.  Padding is worked like other rows: where slots are aligned to more rows than a tile of
+// 32 has, a run has that many at least (256 experts 7168 x 2048, 8 tokens aligned to 128: 1235 us all short, 536 all long; 8 experts
+// 4096 x 14336 363 / 296, 64 experts 2048 x 1408 and 48 tokens 146 / 123).
+// Short runs in one launch and long ones in the others cost 20 to 60 us for the launches and save passes over the weights of popular
+// experts: the more rows an expert has, the more weights there are, and, where loads differ like 1 / rank, the more experts.  Measured
+// (us, all short / both; experts x time of weights in 1000 us beside the layer, rows an expert behind it):
+//   256 experts 7168 x 2048 (220)   2: 319 / 337, 4: 486 / 476, 8: 709 / 652, 32: 1650 / 1262
+//   64 of 4096 x 14336 (55)         8: 687 / 755, 12: 808 / 814, 16: 985 / 933, 64: 2717 / 2170
+//   160 of 4096 x 2048 (49)         8: 283 / 295, 12: 328 / 331, 24: 540 / 465, 96: 1535 / 1046
+//   160 of 4096 x 1536 (37)         8: 200 / 215, 12: 273 / 284, 16: 344 / 333, 64: 866 / 636
+//   128 of 4096 x 1280 (20)         16: 261 / 266, 24: 312 / 307, 32: 378 / 345, 96: 787 / 555
+//   48 of 4096 x 5632 (12)          16: 363 / 396, 32: 538 / 535, 64: 834 / 694
+//   32 of 4096 x 8192 (8)           32: 490 / 532, 48: 618 / 609, 64: 750 / 692
+//   16 of 4096 x 10752 (3), 64 of 2048 x 1408 (3)     64: 474 / 492 and 139 / 169, 96: 624 / 620 and 189 / 193
+// so they part at 480 by rows x experts x time.  (Where all experts are about as popular, rank^-0.3, later: 64 of 4096 x 4096 (16) 32:
+// 476 / 509, 64: 770 / 819, 96: 1122 / 1016.)
+// Few experts or light weights, which do not come to that before, turn from all short to all long at 96 rows (8 of 4096 x 14336 64:
+// 321 / 345, 96: 398 / 421; 64 of 2048 x 1408 64: 139 / 169, 96: 189 / 202), the lightest later, at 3000 by rows x us (32 of 2048 x 1408,
+// 21 us, 128: 120 / 129, 192: 160 / 152; 64 of 1024 x 1024, 15 us, 128: 114 / 119, 192: 156 / 148), but at 256 (8 of 1024 x 2048, 4 us,
+// 128: 35 / 47, 256: 53 / 56, 512: 84 / 80).  Beyond, both take 3 to 6 % less than all long on 64 of 2048 x 1408, as much on 16 of
+// 4096 x 10752, 2 to 12 % more on the others.
+// Tiles of 32 or 48 rows, by rows an expert: 64 of 2048 x 1408 4: 47 / 51, 24: 92 / 91, 64: 156 / 139; 8 of 4096 x 14336 16: 146 / 160, 32:
+// 219 / 215, 96: 423 / 398; 32 of 4096 x 8192 24: 413 / 465, 32: 490 / 535, 96: 1082 / 954; 16 of 4096 x 10752 16: 227 / 235, 32: 306 / 300.
 inline Cut cut_of(const moegps_shape_t& s) {
   const int64_t R = (int64_t)s.T * s.K, experts = R < s.E ? R : s.E;
   const int64_t per = experts > 0 ? (R + experts - 1) / experts : 0;
   const bool padded = s.row_align > 32;
-  const int64_t rows = padded && per < s.row_align ? s.row_align : per;
+  const double rows = (double)(padded && per < s.row_align ? s.row_align : per);
   const int64_t d = chunks_of(s.D), f = chunks_of(s.F);
   const double weights_us = 0.0025 * s.E * (double)(f * d + (d + 1) / 2 * f);
-  const bool heavy = weights_us > 300.0;
-  if (rows <= (heavy ? 3 : 24)) return {32, INT32_MAX};
-  if (!heavy && rows <= (weights_us > 20.0 ? 96 : 256)) return {48, INT32_MAX};
-  return {32, heavy && !padded ? 32 : 0};              // (padded: no run is short)
+  const double by_weights = 3e3 / weights_us, part = 480e3 / (s.E * weights_us);
+  const double most = by_weights < 96.0 ? 96.0 : by_weights < 256.0 ? by_weights : 256.0;
+  if (rows <= (part < most ? part : most)) return {rows <= 24.0 ? 32 : 48, INT32_MAX};
+  return {32, part < most && !padded ? 32 : 0};        // (padded: no run is short)
 }
 constexpr int kLongRows = 224;
 

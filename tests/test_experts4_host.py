@@ -69,3 +69,25 @@ def test_padding_is_rows_like_others(lib, align):
     if align > 96:
         assert cut(lib, *LAYERS["mixtral"], 1, align) == cut(lib, *LAYERS["many"], 8, align) == "long"
     assert cut(lib, *LAYERS["light"], 1, align) == "short 48"
+
+
+@pytest.mark.parametrize("align", [1, 16, 32])
+def test_cut_of_layers(lib, align):
+    for name, T, want in (("fine", 1, "short 32"), ("fine", 64, "short 32"), ("fine", 128, "both"), ("fine", 4096, "both"),
+                          ("mixtral", 1, "short 32"), ("mixtral", 96, "short 32"), ("mixtral", 128, "short 48"),
+                          ("mixtral", 384, "short 48"), ("mixtral", 400, "long"), ("mixtral", 16384, "long"),
+                          ("many", 48, "short 32"), ("many", 512, "short 48"), ("many", 8192, "long"),
+                          ("light", 1, "short 32"), ("light", 256, "short 48"), ("light", 2048, "long")):
+        assert cut(lib, *LAYERS[name], T, align) == want, (name, T)
+    # few experts, whatever their weights, are not worked in both ways before they have dozens of rows each; many are
+    assert cut(lib, 24, 4096, 14336, 2, 288) == "short 32" and cut(lib, 24, 4096, 14336, 2, 576) == "short 48"
+    assert cut(lib, 160, 4096, 1536, 8, 960) == "both" and cut(lib, 128, 4096, 1280, 8, 768) == "both"
+
+
+@pytest.mark.parametrize("E", [8, 32, 64, 160, 256])
+def test_cut_does_not_jump_with_the_weights(lib, E):
+    """A few columns more change the rows an expert from which both ways are taken by as little."""
+    first = []
+    for F in range(1024, 16385, 256):
+        first.append(next((per for per in range(1, 600) if not cut(lib, E, 4096, F, 1, per * E).startswith("short")), 600))
+    assert all(b <= a and a - b <= 1 + a * 0.25 for a, b in zip(first, first[1:])), first

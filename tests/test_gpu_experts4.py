@@ -588,3 +588,19 @@ def test_few_tokens_at_any_alignment(align, T):
     call(ctx, xp, off, expert, packed, yp, ws)
     ctx.check_status()
     check(xp, off, expert, dense, yp, 13.0, used=counts)
+
+
+@pytest.mark.parametrize("most", [3, 40])                # below and above what heavy weights turn to launches of both kinds at
+def test_many_experts_of_heavy_weights(most):
+    shape_of = lambda T: binding.Shape(T, 2560, 4000, 128, 1, 128, 0, 1)  # noqa: E731
+    rng = np.random.default_rng(most)
+    rows = [int(v) for v in rng.integers(0, most + 1, 126)] + [50, 130]
+    shape = shape_of(sum(rows))
+    ctx, g, packed, dense, ws = make(shape, 52)
+    off, expert = slots(rows, [int(v) for v in rng.permutation(128)], 1)
+    xp = normal(g, shape.Rcap, shape.D)
+    yp = torch.full((shape.Rcap, shape.D), 13.0, dtype=torch.bfloat16, device=DEV)
+    call(ctx, xp, off, expert, packed, yp, ws)
+    ctx.check_status()
+    assert ctx.launch_count() - 6 == (1 if sum(rows) <= 128 * 12 else 4)
+    check(xp, off, expert, dense, yp, 13.0)
