@@ -130,21 +130,21 @@ __device__ __forceinline__ void build_tables(Tables& tb, const int32_t* __restri
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x;
     const tile_sums::Lane own(lane, S);
-    const int64_t sum = own.sum(tb.tile_base);
-    int64_t incl = sum;
+    uint32_t incl = own.sum(tb.tile_base);
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane >= d) incl += o;
+      const uint32_t o = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl = tile_sums::add(incl, o);
     }
-    const int64_t total = __shfl_sync(0xffffffffu, incl, 31);
-    int32_t kept = (int32_t)total;
-    if (total > tile_sums::kMost) {
-      kept = __reduce_max_sync(0xffffffffu, own.kept(tb.tile_base, incl - sum, tile_sums::kMost));
+    uint32_t before = __shfl_up_sync(0xffffffffu, incl, 1);
+    if (lane == 0) before = 0;
+    uint32_t kept = __shfl_sync(0xffffffffu, incl, 31);
+    if (kept > tile_sums::kMost) {
+      kept = __reduce_max_sync(0xffffffffu, own.kept(tb.tile_base, before, tile_sums::kMost));
       if (threadIdx.x == 0 && blockIdx.x == 0) moegps_report(status, MOEGPS_ERR_BAD_INDEX, S);
     }
-    own.write(tb.tile_base, incl - sum, kept);
-    if (lane == 31) tb.tile_base[S] = kept;
+    own.write(tb.tile_base, before, kept);
+    if (lane == 31) tb.tile_base[S] = (int)kept;
   }
 }
 
