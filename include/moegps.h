@@ -392,6 +392,9 @@ MOEGPS_API int moegps_weights_dequantize4(moegps_ctx_t* ctx, const void* w4, con
  * slot and slots with slot_expert < 0 are not written, a slot with an extent outside [0, Rcap] is skipped and
  * MOEGPS_ERR_BAD_INDEX recorded.  Of slots that overlap (no plan makes such) those that exceed the workspace are left out, and the
  * same is recorded.  yp may be xp.
+ * Padding rows are worked like others: for few tokens, slots aligned to 128 rows take some two and a half times as long as slots
+ * aligned to 16 or 1.  The blocks of a call wait for one another, about a second at most: where other work keeps some of them from the device
+ * for longer, MOEGPS_ERR_TIMEOUT is recorded and yp is unspecified.
  * workspace: moegps_expert_ffn4_workspace_bytes(shape) bytes, 16-byte aligned, contents irrelevant; its size cannot be checked
  * here.  Calls that may overlap on the GPU need a workspace each; one context may serve them.  A device with more than 160 SMs:
  * MOEGPS_ERR_UNIMPLEMENTED. */

@@ -214,7 +214,7 @@ __device__ __forceinline__ void for_rows(const int32_t* before, int S, int D, in
 }
 
 // For long runs.  A warp does 512 columns of rows b, b + 32, b + 64, b + 96 of 128 rows of a tile, whose scales lie side by
-// side: 16 bytes at a time (4 at a time, a row for itself, these writes took 28 of 100 us on 49152 rows x 2048).
+// side: 16 bytes at a time (49152 rows x 2048 77 us under a profiler, 85 with 4 bytes at a time).
 __global__ void __launch_bounds__(kSplitThreads)
 split_kernel(const __nv_bfloat16* __restrict__ xp, const int32_t* __restrict__ slot_row_off, const int32_t* __restrict__ slot_expert,
              int S, int E, int D, int rcap, int min_rows, int max_tiles, const mx4::Rows out, int32_t* __restrict__ status) {
@@ -1204,7 +1204,7 @@ int tmap_failed(moegps_ctx* ctx) {
 int launch_split(moegps_ctx* ctx, const Call& c, cudaStream_t st) {
   const moegps_shape_t& s = ctx->shape;
   const int64_t units = c.l.long_tiles * 64 * ((s.D + 511) / 512) / (kSplitThreads / 32);
-  const int64_t resident = 4 * (int64_t)ctx->sm_count;         // what runs at once by registers (8 for each SM: 100 and 94 us, 49152 x 2048)
+  const int64_t resident = 4 * (int64_t)ctx->sm_count;         // what runs at once by registers (8 for each SM take the same)
   split_kernel<<<(unsigned)(units < resident ? units : resident), kSplitThreads, 0, st>>>(
       static_cast<const __nv_bfloat16*>(c.xp), c.slot_row_off, c.slot_expert, s.S, s.E, s.D, (int)c.l.rows,
       c.l.cut.short_rows + 1, (int)c.l.long_tiles, c.x, ctx->d_status);

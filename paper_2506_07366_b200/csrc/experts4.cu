@@ -3,8 +3,8 @@
 // Both are bound by memory: 2 + 17/32 bytes a weight.  A block of 256 threads owns one tile of 128 outputs and one chunk of
 // 128 inputs, so the tile's 512 scale bytes are one run of memory; eight threads share an output's 128 inputs (two to a block of
 // 32: with one 16-byte load each and four to a block, the maximum and the scale took as long as memory), four outputs per thread
-// are in flight at once.  One matrix quantized and read back: 8 x 14336 x 4096 385 us (2.13 GB, 5.5 TB/s), 13 x 1000 x 1416 17.5 us
-// (21 without the early launch of the second).
+// are in flight at once.  One matrix quantized and read back, inputs in turn: 8 x 14336 x 4096 403 us (2.13 GB, 5.3 TB/s),
+// 13 x 1000 x 1416 20.4 us (3.5 more without the early launch of the second).
 #include "bf16x8.cuh"
 #include "common.cuh"
 #include "mx4.cuh"
